@@ -187,7 +187,7 @@ def _recur(s):
 def _recur_train(s):
     a, keep, b = _gates(s)
     h = _scan(keep.clone(), b)
-    lam = s["dh"].float()
+    lam = s["dh"].float().clone()  # (a tensor of 32 bits is its own float(), and the inputs stay as they are)
     lam[:, -1] += s["dlast"]
     after = torch.zeros_like(keep)
     after[:, :-1] = keep[:, 1:]
