@@ -262,6 +262,127 @@ ceca_status_t dsgd_logreg_grad_static(const float *A, const float *labels, const
 /* Host function.  Size in bytes of the buffer dsgd_logreg_grad_static works in. */
 size_t dsgd_logreg_grad_static_capacity(void);
 
+/* Element types of the calls below (arithmetic, sums and carried states are fp32 whatever the storage;
+ * a bf16 output is rounded to nearest even once, on the store). */
+typedef enum { DSGD_F32 = 0, DSGD_BF16 = 1 } dsgd_type_t;
+typedef enum { DSGD_I32 = 0, DSGD_I64 = 1 } dsgd_index_t;
+
+/*
+ * Token embedding of n agents that train language models (not in the paper, which leaves f_i generic;
+ * the table E_i is a block of columns of agent i's row of X or Y, its gradient one of G):
+ *   out[i, s, :] = scale * E_i[tokens[i, s], :]
+ * E: device, table_type; row v of agent i's table starts at E + i*agent_stride + v*row_stride.
+ * agent_stride may be 0: one table that all agents read.  tokens: device, tokens_type, agent i's start at
+ * tokens + i*tokens_stride, contiguous.  A token outside [0, v) marks an empty position: its output
+ * row is zero.  out: device, out_type; position s of agent i starts at out + i*out_agent_stride +
+ * s*out_row_stride.  Strides count elements; rows themselves are contiguous, and neither the rows of
+ * out nor those of E may overlap.  t = 0 is allowed and does nothing.
+ * Errors: CECA_ERR_INVALID_ARG (NULL where data is needed, n, v or d < 1, t < 0, v or t >= 2^31, a row
+ * stride below d, a negative stride, a bad type).
+ * Speed: 128-bit accesses need every row to start on a 16-byte boundary; other layouts run a narrower
+ * form.
+ */
+ceca_status_t dsgd_embed_lookup(const void *E, const void *tokens, void *out, int32_t n, int64_t t, int64_t v,
+                                int64_t d, int64_t agent_stride, int64_t row_stride, int64_t tokens_stride,
+                                int64_t out_agent_stride, int64_t out_row_stride, int32_t table_type,
+                                int32_t tokens_type, int32_t out_type, float scale, void *stream);
+
+/*
+ * The gradient of dsgd_embed_lookup with respect to the tables, given `dout`, the gradient with respect
+ * to `out` (same layout and type rules as out; out_agent_stride and out_row_stride may be 0 here):
+ *   dE_i[w, :] = scale * sum over { s : tokens[i, s] = w } of dout[i, s, :]
+ * Every row of every dE_i is written, with zeros where no position holds the token; with accumulate != 0
+ * the sum is added to what the row holds instead, and rows without a token are not touched.
+ * The positions of each token are listed in ascending order first, and the sums run over that list in an
+ * order that depends on the arguments alone: results are identical from run to run.
+ * workspace: device, 16-byte aligned, at least dsgd_embed_workspace_bytes(n, t, v, d) bytes.
+ * Errors: as above, and CECA_ERR_WORKSPACE; agent_stride must keep the agents' tables apart (n > 1).
+ */
+ceca_status_t dsgd_embed_grad(const void *dout, const void *tokens, void *dE, int32_t n, int64_t t, int64_t v,
+                              int64_t d, int64_t agent_stride, int64_t row_stride, int64_t tokens_stride,
+                              int64_t out_agent_stride, int64_t out_row_stride, int32_t table_type,
+                              int32_t tokens_type, int32_t out_type, float scale, int32_t accumulate,
+                              void *workspace, size_t workspace_bytes, void *stream);
+
+/* Host function.  Minimum workspace size of dsgd_embed_grad in bytes (0 for sizes it refuses). */
+size_t dsgd_embed_workspace_bytes(int32_t n, int64_t t, int64_t v, int64_t d);
+
+/*
+ * Gated linear recurrence over the steps of b sequences, channel by channel (not in the paper; the
+ * sequence mixer of the language-model workload):
+ *   a = sigmoid(f[i, s, c]),   h[i, s, c] = keep * h[i, s-1, c] + (1 - a) * x[i, s, c]
+ * with keep = a, except keep = 0 at a step that begins a document (starts[i, s] != 0): whatever the state
+ * was, an infinity or NaN included, does not reach past it.  h[i, -1, c] = h0[i, c], or 0 when h0 is NULL.
+ * x, f, h: device, `type`; step s of sequence i starts at p + i*p_seq_stride + s*p_step_stride, its d
+ * channels contiguous (so x and f may be halves of one projection).  h0, h_last: device fp32, b x d
+ * dense; starts: device, one byte per step, b x t dense, may be NULL.  h_last receives the fp32 state
+ * after step t-1 (the initial state when t = 0) and may be NULL; it may be h0 itself.
+ * marks: device fp32, b x dsgd_recurrence_marks(t) x d dense, receives the states the gradient starts
+ * from; NULL when no gradient is wanted.
+ * h may be x or f when the strides are the same (each element is read before it is written).
+ * Errors: CECA_ERR_INVALID_ARG (NULL where data is needed, b or d < 1, t < 0, t >= 2^31, a step stride
+ * below d, a negative stride, a bad type).
+ * Speed: 128-bit accesses need every step of every tensor to start on a 16-byte boundary and d to be a
+ * multiple of 16 bytes; other layouts run a narrower form.
+ */
+ceca_status_t dsgd_recurrence(const void *x, const void *f, const float *h0, const uint8_t *starts, void *h,
+                              float *h_last, float *marks, int64_t b, int64_t t, int64_t d, int64_t x_seq_stride,
+                              int64_t x_step_stride, int64_t f_seq_stride, int64_t f_step_stride,
+                              int64_t h_seq_stride, int64_t h_step_stride, int32_t type, void *stream);
+
+/* Host function.  How many states per sequence and channel `marks` holds for sequences of t steps. */
+int64_t dsgd_recurrence_marks(int64_t t);
+
+/*
+ * The gradient of dsgd_recurrence.  dh: the gradient with respect to h (type of h; its strides may be 0);
+ * dh_last: with respect to h_last, device fp32 b x d, may be NULL.  marks: as the forward call wrote
+ * them for the same x, f, h0, starts.  With l[s] = dh[s] + keep[s+1] l[s+1], l[t-1] = dh[t-1] + dh_last:
+ *   dx[s] = (1 - a) l[s],   df[s] = a (1 - a) l[s] (p - x[s]),   dh0 = keep[0] l[0]
+ * where p is the state before step s (0 where a document begins).  The states are computed again from
+ * the marks in fp32; h itself is not read.  dx, df: `type`; dh0: device fp32, b x d, may be NULL; it is
+ * dh_last for t = 0.  dx may be x or dh, df may be f (same strides).  Errors: as dsgd_recurrence.
+ */
+ceca_status_t dsgd_recurrence_grad(const void *x, const void *f, const void *dh, const float *marks,
+                                   const uint8_t *starts, const float *dh_last, void *dx, void *df, float *dh0,
+                                   int64_t b, int64_t t, int64_t d, int64_t x_seq_stride, int64_t x_step_stride,
+                                   int64_t f_seq_stride, int64_t f_step_stride, int64_t dh_seq_stride,
+                                   int64_t dh_step_stride, int64_t dx_seq_stride, int64_t dx_step_stride,
+                                   int64_t df_seq_stride, int64_t df_step_stride, int32_t type, void *stream);
+
+/*
+ * Distillation from a teacher's top logits (not in the paper; the loss of the language-model workload).
+ * Row i (a position of some agent) has the student's logits z[i, 0..v) and up to k teacher logits t[i, j]
+ * at the vocabulary entries idx[i, j].  An idx outside [0, v), or a t / T of -infinity, means that the
+ * teacher sent fewer entries.  With the temperature T, q = softmax(z[i] / T) and
+ *   teacher_lse == NULL:  p_j = exp(t_j / T - N), N = log sum_j exp(t_j / T): the teacher renormalised over
+ *     what it sent;                 loss[i] = w_i * sum_j p_j (log p_j - log q[idx_j])
+ *   teacher_lse != NULL:  N = teacher_lse[i], the teacher's own log-sum-exp of its logits / T over the whole
+ *     vocabulary, so that p0 = max(0, 1 - sum_j p_j) is its mass outside its top; it is compared with the
+ *     student's there, q0 = sum of q outside the top:
+ *                                   loss[i] = w_i * (sum_j p_j (log p_j - log q[idx_j]) + p0 log(p0 / q0))
+ * w_i = weight[i] (1 when weight is NULL).  A row with w_i = 0, or without any teacher entry, has loss 0
+ * and a zero gradient, and its logits are not read.  The gradient is
+ *   dz[i, c] = (w_i / T) * (q_c - sum of p_j over { j : idx_j = c })        at the top's entries,
+ *   dz[i, c] = (w_i / T) * (q_c, less p0 q_c / q0 with a teacher_lse)       elsewhere
+ * (no factor T^2: fold it into the weight).  An entry that a row lists twice counts with both p_j.  Logits of
+ * -infinity have q = 0; a row of nothing else has q = 0 throughout.
+ * z, dz: device, logits_type, r x v with row strides ldz, lddz >= v; idx: device, index_type, r x k with
+ * row stride ldi >= k; t: device, teacher_type, r x k with row stride ldt >= k; teacher_lse, weight, loss:
+ * device fp32, r elements.  dz may be z with the same row stride (another one: CECA_ERR_UNSUPPORTED).
+ * Errors: CECA_ERR_INVALID_ARG (NULL where data is needed, r < 0, v < 1, k < 0, v >= 2^31, k > 4096, a row
+ * stride below the row, temperature not positive and finite, a bad type).
+ */
+ceca_status_t dsgd_distill_loss(const void *z, const void *idx, const void *t, const float *teacher_lse,
+                                const float *weight, float *loss, int64_t r, int64_t v, int64_t k, int64_t ldz,
+                                int64_t ldi, int64_t ldt, int32_t logits_type, int32_t index_type,
+                                int32_t teacher_type, float temperature, void *stream);
+
+/* The loss and its gradient in one pass over the logits. */
+ceca_status_t dsgd_distill_grad(const void *z, const void *idx, const void *t, const float *teacher_lse,
+                                const float *weight, float *loss, void *dz, int64_t r, int64_t v, int64_t k,
+                                int64_t ldz, int64_t ldi, int64_t ldt, int64_t lddz, int32_t logits_type,
+                                int32_t index_type, int32_t teacher_type, float temperature, void *stream);
+
 typedef enum {
   CECA_WS_CONSENSUS_FUSED = 1,    /* ceca_consensus_rounds, fused = 1                      */
   CECA_WS_CONSENSUS_UNFUSED = 2,  /* ceca_consensus_rounds, fused = 0 with Y_out == NULL   */

@@ -18,7 +18,8 @@ EXPORTS = ["ceca_schedule", "ceca_gossip_sgd_step", "ceca_consensus_rounds", "ds
            "ceca_workspace_bytes", "ceca_read_status", "ceca_gossip_sgd_step_host", "ceca_status_string",
            "dsgd_logreg_grad_static", "dsgd_logreg_grad_static_capacity", "dsgd_lsq_grad",
            "ceca_fused_wait_selftest", "ceca_gossip_sgd_step_bf16", "dsgd_grad_shard_dots", "dsgd_grad_shard_sum",
-           "dsgd_grad_shard_apply"]
+           "dsgd_grad_shard_apply", "dsgd_embed_lookup", "dsgd_embed_grad", "dsgd_embed_workspace_bytes", "dsgd_recurrence",
+           "dsgd_recurrence_marks", "dsgd_recurrence_grad", "dsgd_distill_loss", "dsgd_distill_grad"]
 
 
 class Round(ctypes.Structure):
@@ -83,6 +84,23 @@ def library():
     lib.ceca_read_status.restype = ctypes.c_int
     lib.ceca_gossip_sgd_step_host.argtypes = [vp, vp, vp, i32, i64, i64, f32, i32, i64, vp, ctypes.c_size_t]
     lib.ceca_gossip_sgd_step_host.restype = ctypes.c_int
+    sz = ctypes.c_size_t
+    lib.dsgd_embed_lookup.argtypes = [vp, vp, vp, i32] + [i64] * 8 + [i32] * 3 + [f32, vp]
+    lib.dsgd_embed_lookup.restype = ctypes.c_int
+    lib.dsgd_embed_grad.argtypes = [vp, vp, vp, i32] + [i64] * 8 + [i32] * 3 + [f32, i32, vp, sz, vp]
+    lib.dsgd_embed_grad.restype = ctypes.c_int
+    lib.dsgd_embed_workspace_bytes.argtypes = [i32, i64, i64, i64]
+    lib.dsgd_embed_workspace_bytes.restype = sz
+    lib.dsgd_recurrence.argtypes = [vp] * 7 + [i64] * 9 + [i32, vp]
+    lib.dsgd_recurrence.restype = ctypes.c_int
+    lib.dsgd_recurrence_marks.argtypes = [i64]
+    lib.dsgd_recurrence_marks.restype = i64
+    lib.dsgd_recurrence_grad.argtypes = [vp] * 9 + [i64] * 13 + [i32, vp]
+    lib.dsgd_recurrence_grad.restype = ctypes.c_int
+    lib.dsgd_distill_loss.argtypes = [vp] * 6 + [i64] * 6 + [i32] * 3 + [f32, vp]
+    lib.dsgd_distill_loss.restype = ctypes.c_int
+    lib.dsgd_distill_grad.argtypes = [vp] * 7 + [i64] * 7 + [i32] * 3 + [f32, vp]
+    lib.dsgd_distill_grad.restype = ctypes.c_int
     lib.ceca_status_string.argtypes = [ctypes.c_int]
     lib.ceca_status_string.restype = ctypes.c_char_p
     _lib = lib
