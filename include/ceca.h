@@ -320,15 +320,20 @@ size_t dsgd_embed_workspace_bytes(int32_t n, int64_t t, int64_t v, int64_t d);
  * marks: device fp32, b x dsgd_recurrence_marks(t) x d dense, receives the states the gradient starts
  * from; NULL when no gradient is wanted.
  * h may be x or f when the strides are the same (each element is read before it is written).
+ * workspace: device, 16-byte aligned, at least dsgd_recurrence_workspace_bytes(b, t, d) bytes (0, and then
+ * NULL will do, where b and d alone make enough work for the GPU).
  * Errors: CECA_ERR_INVALID_ARG (NULL where data is needed, b or d < 1, t < 0, t >= 2^31, a step stride
- * below d, a negative stride, a bad type).
- * Speed: 128-bit accesses need every step of every tensor to start on a 16-byte boundary and d to be a
- * multiple of 16 bytes; other layouts run a narrower form.
+ * below d, a negative stride, a bad type), CECA_ERR_WORKSPACE.
+ * Speed: best where every step of every tensor starts on a 16-byte boundary, then on a 4-byte one.
  */
 ceca_status_t dsgd_recurrence(const void *x, const void *f, const float *h0, const uint8_t *starts, void *h,
                               float *h_last, float *marks, int64_t b, int64_t t, int64_t d, int64_t x_seq_stride,
                               int64_t x_step_stride, int64_t f_seq_stride, int64_t f_step_stride,
-                              int64_t h_seq_stride, int64_t h_step_stride, int32_t type, void *stream);
+                              int64_t h_seq_stride, int64_t h_step_stride, int32_t type, void *workspace,
+                              size_t workspace_bytes, void *stream);
+
+/* Host function.  Minimum workspace size of dsgd_recurrence and dsgd_recurrence_grad in bytes. */
+size_t dsgd_recurrence_workspace_bytes(int64_t b, int64_t t, int64_t d);
 
 /* Host function.  How many states per sequence and channel `marks` holds for sequences of t steps. */
 int64_t dsgd_recurrence_marks(int64_t t);
@@ -347,7 +352,8 @@ ceca_status_t dsgd_recurrence_grad(const void *x, const void *f, const void *dh,
                                    int64_t b, int64_t t, int64_t d, int64_t x_seq_stride, int64_t x_step_stride,
                                    int64_t f_seq_stride, int64_t f_step_stride, int64_t dh_seq_stride,
                                    int64_t dh_step_stride, int64_t dx_seq_stride, int64_t dx_step_stride,
-                                   int64_t df_seq_stride, int64_t df_step_stride, int32_t type, void *stream);
+                                   int64_t df_seq_stride, int64_t df_step_stride, int32_t type, void *workspace,
+                                   size_t workspace_bytes, void *stream);
 
 /*
  * Distillation from a teacher's top logits (not in the paper; the loss of the language-model workload).

@@ -19,7 +19,7 @@ EXPORTS = ["ceca_schedule", "ceca_gossip_sgd_step", "ceca_consensus_rounds", "ds
            "dsgd_logreg_grad_static", "dsgd_logreg_grad_static_capacity", "dsgd_lsq_grad",
            "ceca_fused_wait_selftest", "ceca_gossip_sgd_step_bf16", "dsgd_grad_shard_dots", "dsgd_grad_shard_sum",
            "dsgd_grad_shard_apply", "dsgd_embed_lookup", "dsgd_embed_grad", "dsgd_embed_workspace_bytes", "dsgd_recurrence",
-           "dsgd_recurrence_marks", "dsgd_recurrence_grad", "dsgd_distill_loss", "dsgd_distill_grad"]
+           "dsgd_recurrence_marks", "dsgd_recurrence_grad", "dsgd_recurrence_workspace_bytes", "dsgd_distill_loss", "dsgd_distill_grad"]
 
 
 class Round(ctypes.Structure):
@@ -91,11 +91,13 @@ def library():
     lib.dsgd_embed_grad.restype = ctypes.c_int
     lib.dsgd_embed_workspace_bytes.argtypes = [i32, i64, i64, i64]
     lib.dsgd_embed_workspace_bytes.restype = sz
-    lib.dsgd_recurrence.argtypes = [vp] * 7 + [i64] * 9 + [i32, vp]
+    lib.dsgd_recurrence.argtypes = [vp] * 7 + [i64] * 9 + [i32, vp, sz, vp]
     lib.dsgd_recurrence.restype = ctypes.c_int
+    lib.dsgd_recurrence_workspace_bytes.argtypes = [i64] * 3
+    lib.dsgd_recurrence_workspace_bytes.restype = sz
     lib.dsgd_recurrence_marks.argtypes = [i64]
     lib.dsgd_recurrence_marks.restype = i64
-    lib.dsgd_recurrence_grad.argtypes = [vp] * 9 + [i64] * 13 + [i32, vp]
+    lib.dsgd_recurrence_grad.argtypes = [vp] * 9 + [i64] * 13 + [i32, vp, sz, vp]
     lib.dsgd_recurrence_grad.restype = ctypes.c_int
     lib.dsgd_distill_loss.argtypes = [vp] * 6 + [i64] * 6 + [i32] * 3 + [f32, vp]
     lib.dsgd_distill_loss.restype = ctypes.c_int

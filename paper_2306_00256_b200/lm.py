@@ -112,11 +112,24 @@ def dsgd_recurrence_marks(t):
     return int(library().dsgd_recurrence_marks(t))
 
 
-def dsgd_recurrence(x, f, h0=None, starts=None, h=None, h_last=None, save=False, stream=None):
+def dsgd_recurrence_workspace_bytes(b, t, d):
+    return int(library().dsgd_recurrence_workspace_bytes(b, t, d))
+
+
+def _recurrence_workspace(workspace, x, stream):
+    """(tensor or None, bytes): the caller's workspace, or one allocated here where the sizes need it."""
+    if workspace is None:
+        size = library().dsgd_recurrence_workspace_bytes(*x.shape)
+        workspace = _empty((size,), torch.uint8, x, stream) if size else None
+    return workspace, 0 if workspace is None else workspace.numel() * workspace.element_size()
+
+
+def dsgd_recurrence(x, f, h0=None, starts=None, h=None, h_last=None, save=False, workspace=None, stream=None):
     """h[:, s] = keep * h[:, s-1] + (1 - sigmoid(f[:, s])) * x[:, s], keep = sigmoid(f[:, s]) or 0 where starts is set,
     for x, f [b, t, d] of one type (float32 or bfloat16).  h0: float32 [b, d]; starts: uint8 or bool [b, t].
     Returns (h, h_last, marks): h like x, h_last the float32 state after the last step, marks what
-    dsgd_recurrence_grad starts from (None unless save).  One new token is t = 1 with h0 = h_last = the kept state."""
+    dsgd_recurrence_grad starts from (None unless save).  One new token is t = 1 with h0 = h_last = the kept state.
+    workspace: device memory of dsgd_recurrence_workspace_bytes(b, t, d) bytes, allocated here when it is None."""
     _need(x.dim() == 3 and f.shape == x.shape and f.dtype == x.dtype, "x and f must be [b, t, d] of one type")
     b, t, d = x.shape
     code = _rows(x, "x")
@@ -125,7 +138,7 @@ def dsgd_recurrence(x, f, h0=None, starts=None, h=None, h_last=None, save=False,
     if starts is not None and starts.dtype == torch.bool:
         starts = starts.view(torch.uint8)
     _dense(starts, "starts", (b, t), torch.uint8)
-    _device(x, f, h0, starts, h, h_last)
+    _device(x, f, h0, starts, h, h_last, workspace)
     if h is None:
         h = _empty((b, t, d), x.dtype, x, stream)
     _need(h.shape == x.shape and h.dtype == x.dtype, "h must have the shape and type of x")
@@ -134,14 +147,15 @@ def dsgd_recurrence(x, f, h0=None, starts=None, h=None, h_last=None, save=False,
         h_last = _empty((b, d), torch.float32, x, stream)
     _dense(h_last, "h_last", (b, d))
     marks = _empty((b, dsgd_recurrence_marks(t), d), torch.float32, x, stream) if save else None
+    workspace, size = _recurrence_workspace(workspace, x, stream)
     st = library().dsgd_recurrence(_p(x), _p(f), _p(h0), _p(starts), _p(h), _p(h_last), _p(marks), b, t, d,
                                    _seq(x), _step(x, 1), _seq(f), _step(f, 1), _seq(h), _step(h, 1), code,
-                                   _stream(stream))
+                                   _p(workspace), size, _stream(stream))
     _check(st, "dsgd_recurrence")
     return h, h_last, marks
 
 
-def dsgd_recurrence_grad(x, f, dh, marks, h0=None, starts=None, dh_last=None, dx=None, df=None, dh0=None, stream=None):
+def dsgd_recurrence_grad(x, f, dh, marks, h0=None, starts=None, dh_last=None, dx=None, df=None, dh0=None, workspace=None, stream=None):
     """The gradient of dsgd_recurrence at the same x, f, h0, starts, from the marks that it saved: returns
     (dx, df, dh0), dh0 float32 [b, d] with respect to the initial state, given or zero (h0 itself lies in the marks)."""
     _need(x.dim() == 3 and f.shape == x.shape == dh.shape and f.dtype == x.dtype == dh.dtype, "x, f and dh must be [b, t, d] of one type")
@@ -154,7 +168,7 @@ def dsgd_recurrence_grad(x, f, dh, marks, h0=None, starts=None, dh_last=None, dx
     if starts is not None and starts.dtype == torch.bool:
         starts = starts.view(torch.uint8)
     _dense(starts, "starts", (b, t), torch.uint8)
-    _device(x, f, dh, marks, starts, dh_last, dx, df, dh0)
+    _device(x, f, dh, marks, starts, dh_last, dx, df, dh0, workspace)
     dx = _empty((b, t, d), x.dtype, x, stream) if dx is None else dx
     df = _empty((b, t, d), x.dtype, x, stream) if df is None else df
     dh0 = _empty((b, d), torch.float32, x, stream) if dh0 is None else dh0
@@ -163,9 +177,11 @@ def dsgd_recurrence_grad(x, f, dh, marks, h0=None, starts=None, dh_last=None, dx
     for g, name in ((dx, "dx"), (df, "df")):
         _need(g.shape == x.shape and g.dtype == x.dtype, "%s must have the shape and type of x" % name)
         _rows(g, name)
+    workspace, size = _recurrence_workspace(workspace, x, stream)
     st = library().dsgd_recurrence_grad(_p(x), _p(f), _p(dh), _p(marks), _p(starts), _p(dh_last), _p(dx), _p(df), _p(dh0),
                                         b, t, d, _seq(x), _step(x, 1), _seq(f), _step(f, 1), _seq(dh), _step(dh, 1),
-                                        _seq(dx), _step(dx, 1), _seq(df), _step(df, 1), code, _stream(stream))
+                                        _seq(dx), _step(dx, 1), _seq(df), _step(df, 1), code, _p(workspace),
+                                        size, _stream(stream))
     _check(st, "dsgd_recurrence_grad")
     return dx, df, dh0
 

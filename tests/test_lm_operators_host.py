@@ -72,9 +72,9 @@ def _call(name, args, **change):
 LOOKUP = dict(E=P, tokens=P, out=P, n=2, t=4, v=8, d=16, agent=128, row=16, tok=4, o_agent=64, o_row=16, te=0, ti=0, to=0, scale=1.0, stream=None)
 GRAD = dict(dout=P, tokens=P, dE=P, n=2, t=4, v=8, d=16, agent=128, row=16, tok=4, o_agent=64, o_row=16, te=0, ti=0, to=0, scale=1.0,
             acc=0, ws=P, size=1 << 20, stream=None)
-RECUR = dict(x=P, f=P, h0=None, starts=None, h=P, last=P, marks=None, b=2, t=4, d=16, xs=64, xt=16, fs=64, ft=16, hs=64, ht=16, type=0, stream=None)
+RECUR = dict(x=P, f=P, h0=None, starts=None, h=P, last=P, marks=None, b=2, t=4, d=16, xs=64, xt=16, fs=64, ft=16, hs=64, ht=16, type=0, ws=None, size=0, stream=None)
 RGRAD = dict(x=P, f=P, dh=P, marks=P, starts=None, dlast=None, dx=P, df=P, dh0=None, b=2, t=4, d=16, xs=64, xt=16, fs=64, ft=16, dhs=64, dht=16,
-             dxs=64, dxt=16, dfs=64, dft=16, type=0, stream=None)
+             dxs=64, dxt=16, dfs=64, dft=16, type=0, ws=None, size=0, stream=None)
 LOSS = dict(z=P, idx=P, t=P, lse=None, w=None, loss=P, r=2, v=8, k=3, ldz=8, ldi=3, ldt=3, tz=0, ti=0, tt=0, temp=1.0, stream=None)
 DGRAD = dict(z=P, idx=P, t=P, lse=None, w=None, loss=P, dz=P, r=2, v=8, k=3, ldz=8, ldi=3, ldt=3, lddz=8, tz=0, ti=0, tt=0, temp=1.0, stream=None)
 BIG = 1 << 31
@@ -124,6 +124,14 @@ def test_distillation_refuses_outputs_that_are_missing_or_crossed():
     assert _call("dsgd_distill_grad", DGRAD, ldz=9, lddz=8) == UNSUPPORTED   # P is both z and dz
 
 
+def test_recurrence_refuses_a_workspace_that_does_not_do():
+    t, size = 5000, ceca.dsgd_recurrence_workspace_bytes(2, 5000, 16)
+    assert size > 0 and size % 4 == 0
+    for ws, have in ((None, 0), (P, size - 1), (ctypes.c_void_p(4104), size)):
+        assert _call("dsgd_recurrence", RECUR, t=t, ws=ws, size=have) == WORKSPACE
+        assert _call("dsgd_recurrence_grad", RGRAD, t=t, ws=ws, size=have) == WORKSPACE
+
+
 def test_calls_without_work_succeed_without_a_device():
     assert _call("dsgd_embed_lookup", LOOKUP, t=0, out=None) == 0
     assert _call("dsgd_distill_loss", LOSS, r=0, z=None, loss=None) == 0
@@ -132,6 +140,8 @@ def test_calls_without_work_succeed_without_a_device():
 def test_sizes():
     assert [ceca.dsgd_recurrence_marks(t) for t in (-1, 0, 1)] == [0, 0, 1]
     assert ceca.dsgd_recurrence_marks(100000) > ceca.dsgd_recurrence_marks(1000) >= 1
+    assert ceca.dsgd_recurrence_workspace_bytes(64, 1000, 2048) == 0 and ceca.dsgd_recurrence_workspace_bytes(1, 1, 64) == 0
+    assert ceca.dsgd_recurrence_workspace_bytes(0, 100, 64) == 0
     assert ceca.dsgd_embed_workspace_bytes(2, 100, 1000, 64) >= 4 * (2 * 100 + 2 * 1001)
     for bad in ((0, 1, 1, 1), (1, -1, 1, 1), (1, 1, 0, 1), (1, 1, 1, 0), (1, BIG, 1, 1)):
         assert ceca.dsgd_embed_workspace_bytes(*bad) == 0
