@@ -367,7 +367,7 @@ ceca_status_t dsgd_recurrence_grad(const void *x, const void *f, const void *dh,
  *     student's there, q0 = sum of q outside the top:
  *                                   loss[i] = w_i * (sum_j p_j (log p_j - log q[idx_j]) + p0 log(p0 / q0))
  * w_i = weight[i] (1 when weight is NULL).  A row with w_i = 0, or without any teacher entry, has loss 0
- * and a zero gradient, and its logits are not read.  The gradient is
+ * and a zero gradient, whatever its logits hold.  The gradient is
  *   dz[i, c] = (w_i / T) * (q_c - sum of p_j over { j : idx_j = c })        at the top's entries,
  *   dz[i, c] = (w_i / T) * (q_c, less p0 q_c / q0 with a teacher_lse)       elsewhere
  * (no factor T^2: fold it into the weight).  An entry that a row lists twice counts with both p_j.  Logits of

@@ -3,13 +3,15 @@
 //   q = softmax(z / T),  p_j = exp(t_j / T - N),  loss = w (sum_j p_j (log p_j - log q_j) [+ p0 log(p0 / q0)])
 //   dz = (w / T) (q - p) at the top's entries, (w / T) (q [- p0 q / q0]) elsewhere
 //
-// One CTA takes a row (a cluster of them where there are few rows) in two passes over it.  The first keeps a running
-// maximum and a running sum of exponentials per thread, over the entries outside the top: q0 must not come from a
+// A CTA takes a row, or a cluster of up to 8 takes a part of it each: as many as it takes to hold the row in shared
+// memory, 32 KB a CTA, six CTAs an SM whose phases overlap; more where there are few rows.  Every thread copies the
+// vectors that it will work on, asynchronously, while the teacher's entries are gathered, so a row is read once.  (Rows
+// above 512 KB are read twice, the second time mostly from L2.)  A first pass keeps a running maximum and a running sum
+// of exponentials per thread, with a teacher_lse over the entries outside the top alone: q0 must not come from a
 // difference of sums that may be nearly equal.  A bitmap in shared memory says which entries are in the top; the few of
-// them are gathered and summed apart.  The second pass writes w / T (1 / S [- p0 / S0]) exp(z / T - M) everywhere and
-// the top's entries are then written over.  The second read of a row comes from L2: all rows in work together fill less
-// than half of it.  Exponents are (z - M) log2(e) / T, the difference first: the sums stay right for logits of any size,
-// masks of the type's lowest value among them.
+// them are gathered and summed apart.  The second pass writes w / T (1 / S [- p0 / S0]) exp((z - M) / T) everywhere,
+// and the top's entries are then written over.  Exponents are taken to base 2, z c - M c with
+// c = log2(e) / T in one fma.
 #include <cooperative_groups.h>
 #include <cuda_runtime.h>
 
@@ -28,10 +30,15 @@ namespace {
 namespace cg = cooperative_groups;
 
 constexpr int kMaxTop = 4096;
-constexpr int kMaxThreads = 512, kMaxWarps = kMaxThreads / 32;
 constexpr int kMaxCluster = 8;
-constexpr int64_t kMaxBits = 1 << 20;   // of the bitmap; longer rows wrap around in it
-constexpr int kDeep = 4;                // vectors a thread loads before it uses the first
+// Bytes of a row that a CTA holds, and what it may hold where kMaxCluster CTAs are not enough for that.
+constexpr int64_t kHeld = 32 << 10, kMostHeld = 64 << 10;
+constexpr int64_t kMaxBits = 1 << 20;   // of the bitmap; longer parts wrap around in it
+constexpr int kDeep = 4;                // vectors a thread works on at a time
+constexpr float kLn2 = 0.6931471805599453f;
+// Beyond this the rounding of M c (2^-24 of it) could itself overflow an exponential.  Logits of this size are masks of
+// the type's lowest value; a row that has no other gets its own, slower sums of 2^((z - M) c).
+constexpr float kFar = 1e8f;
 
 struct DistillArgs {
   const void *z, *idx, *t;
@@ -39,10 +46,12 @@ struct DistillArgs {
   float *loss;
   void *dz;
   int64_t v, k, ldz, ldi, ldt, lddz;
-  float scale;        // log2(e) / T
+  float scale;        // c = log2(e) / T
   float temperature;
+  int32_t idx64, t16; // the types of idx and t
   int32_t cluster;    // CTAs per row
-  int32_t words;      // of the bitmap
+  int32_t per;        // vectors of each CTA
+  int32_t words;      // of the bitmap, a multiple of 4
 };
 
 // 16 bytes of logits.
@@ -78,222 +87,308 @@ template <typename T> __device__ __forceinline__ void strike(Vec<T> &v, uint32_t
       else word(v.w, e / 2) = e % 2 ? (word(v.w, e / 2) & 0xffffu) | 0xff800000u : (word(v.w, e / 2) & 0xffff0000u) | 0xff80u;
     }
 }
-__device__ __forceinline__ float top_of(const Vec<float> &v) {
-  return fmaxf(fmaxf(__uint_as_float(v.w.x), __uint_as_float(v.w.y)), fmaxf(__uint_as_float(v.w.z), __uint_as_float(v.w.w)));
+// The largest element of D vectors.
+template <int D> __device__ __forceinline__ float top_of(const Vec<float> *v) {
+  float m = -INFINITY;
+#pragma unroll
+  for (int u = 0; u < D; ++u)
+    m = fmaxf(m, fmaxf(fmaxf(__uint_as_float(v[u].w.x), __uint_as_float(v[u].w.y)), fmaxf(__uint_as_float(v[u].w.z), __uint_as_float(v[u].w.w))));
+  return m;
 }
-__device__ __forceinline__ float top_of(const Vec<bf16> &v) {
+template <int D> __device__ __forceinline__ float top_of(const Vec<bf16> *v) {
   const auto h = [](uint32_t x) { return *reinterpret_cast<const __nv_bfloat162 *>(&x); };
-  const __nv_bfloat162 m = __hmax2(__hmax2(h(v.w.x), h(v.w.y)), __hmax2(h(v.w.z), h(v.w.w)));
+  __nv_bfloat162 m = h(v[0].w.x);
+#pragma unroll
+  for (int u = 0; u < D; ++u) m = __hmax2(m, __hmax2(__hmax2(h(v[u].w.x), h(v[u].w.y)), __hmax2(h(v[u].w.z), h(v[u].w.w))));
   return fmaxf(__low2float(m), __high2float(m));
 }
 
-// A row as whole vectors on 16-byte boundaries: vector 0 begins `pad` elements before the row, and the last may end after
-// it.  Slot s is element s - pad.
-template <typename T> struct Row {
-  const T *at0;   // where vector 0 begins
-  int pad;
-  int64_t slots, vectors;
-  __device__ __forceinline__ Row(const T *row, int64_t v) {
-    pad = (int)((reinterpret_cast<uintptr_t>(row) & 15) / sizeof(T));
-    at0 = row - pad;
-    slots = v + pad;
-    vectors = (slots + Vec<T>::N - 1) / Vec<T>::N;
-  }
-  __device__ __forceinline__ bool whole(int64_t j) const { return (j > 0 || pad == 0) && (j + 1) * Vec<T>::N <= slots; }
-  // vector j, with -infinity for what is not of the row
-  __device__ __forceinline__ Vec<T> load(int64_t j, bool last_use) const {
-    Vec<T> v = all_least<T>();
-    if (whole(j)) {
-      const uint4 *p = reinterpret_cast<const uint4 *>(at0) + j;
-      v.w = last_use ? __ldcs(p) : *p;
-    } else if (j < vectors) {
-      T *e = reinterpret_cast<T *>(&v.w);
-      for (int i = 0; i < Vec<T>::N; ++i) {
-        const int64_t s = j * Vec<T>::N + i;
-        if (s >= pad && s < slots) e[i] = at0[s];
-      }
-    }
-    return v;
-  }
-};
-
-// Sums or maxima over the CTA of up to N values at once, each in one fixed order.
-template <int N, bool MAX> __device__ __forceinline__ void over_block(float *x, float *red) {
-  const int warps = blockDim.x >> 5;
-#pragma unroll
-  for (int i = 0; i < N; ++i) {
-#pragma unroll
-    for (int o = 16; o; o >>= 1) {
-      const float y = __shfl_xor_sync(0xffffffffu, x[i], o);
-      x[i] = MAX ? fmaxf(x[i], y) : x[i] + y;
-    }
-    if ((threadIdx.x & 31) == 0) red[i * kMaxWarps + (threadIdx.x >> 5)] = x[i];
-  }
-  __syncthreads();
-#pragma unroll
-  for (int i = 0; i < N; ++i) {
-    x[i] = red[i * kMaxWarps];
-    for (int w = 1; w < warps; ++w) x[i] = MAX ? fmaxf(x[i], red[i * kMaxWarps + w]) : x[i] + red[i * kMaxWarps + w];
-  }
-}
-
-// Shared memory behind the bitmap: k entries of each.
-struct Entries {
-  int32_t *at;    // the vocabulary entry, or -1
-  float *t, *z;   // the teacher's logit / T, the student's logit
-};
-
-template <typename TZ, typename TT, typename TI, bool CLUSTER>
-__global__ void __launch_bounds__(kMaxThreads, 2) distill_kernel(const DistillArgs p) {
-  constexpr int N = Vec<TZ>::N, P = Vec<TZ>::P;
-  extern __shared__ uint32_t bitmap[];
-  __shared__ float red[4][4 * kMaxWarps];
-  __shared__ float share[2];
-  Entries en;
-  en.at = reinterpret_cast<int32_t *>(bitmap + p.words);
-  en.t = reinterpret_cast<float *>(en.at + p.k);
-  en.z = en.t + p.k;
-  const int ranks = CLUSTER ? p.cluster : 1;
-  const int64_t row = CLUSTER ? blockIdx.x / ranks : blockIdx.x;
-  const int rank = CLUSTER ? (int)(blockIdx.x - row * ranks) : 0;
-  const TZ *z = static_cast<const TZ *>(p.z) + row * p.ldz;
-  TZ *dz = p.dz ? static_cast<TZ *>(p.dz) + row * p.lddz : nullptr;
-  const TI *idx = static_cast<const TI *>(p.idx) + row * p.ldi;
-  const TT *t = static_cast<const TT *>(p.t) + row * p.ldt;
-  const float w = p.weight ? p.weight[row] : 1.f;
-  const bool tail = p.teacher_lse != nullptr;
-  const Row<TZ> rz(z, p.v);
-  const bool together = ((reinterpret_cast<uintptr_t>(z) ^ reinterpret_cast<uintptr_t>(dz)) & 15) == 0;
-  // this CTA's vectors and slots
-  const int64_t per = (rz.vectors + ranks - 1) / ranks;
-  const int64_t v0 = rank * per, v1 = min(rz.vectors, v0 + per);
-  const int64_t slot0 = v0 * N, slot1 = v1 * N;
-  const bool wraps = slot1 - slot0 > kMaxBits;   // then a set bit only says that an entry may be there
-
-  for (int c = threadIdx.x; c < p.words; c += blockDim.x) bitmap[c] = 0;
-  __syncthreads();
-  // the top: its entries, which of them are there, the bitmap
-  int some = 0, twice = 0;
-  float x[4] = {-INFINITY, -INFINITY, 0.f, 0.f};   // maxima of z and of t over the top
-  for (int j = threadIdx.x; j < p.k; j += blockDim.x) {
-    const int64_t at = idx[j];
-    const float tj = widen(t[j]) / p.temperature;
-    const bool there = w != 0.f && at >= 0 && at < p.v && !(tj == -INFINITY);
-    en.at[j] = there ? (int32_t)at : -1;
-    en.t[j] = tj;
-    if (!there) continue;
-    some = 1;
-    const float zj = widen(z[at]);
-    en.z[j] = zj;
-    x[0] = fmaxf(x[0], zj);
-    x[1] = fmaxf(x[1], tj);
-    const int64_t slot = at + rz.pad;
-    if (slot >= slot0 && slot < slot1) {
-      const uint32_t b = (uint32_t)((slot - slot0) & (kMaxBits - 1));
-      twice |= atomicOr(bitmap + (b >> 5), 1u << (b & 31)) >> (b & 31) & 1;
-    }
-  }
-  some = __syncthreads_or(some);
-  if (!some) {   // nothing to learn here, and nothing read
-    if (threadIdx.x == 0 && rank == 0 && p.loss) p.loss[row] = 0.f;
-    if (dz) {
-      for (int64_t j = v0 + threadIdx.x; j < v1; j += blockDim.x) {
-        if (together && rz.whole(j)) __stcs(reinterpret_cast<uint4 *>(dz - rz.pad) + j, make_uint4(0, 0, 0, 0));
-        else
-          for (int i = 0; i < N; ++i) {
-            const int64_t s = j * N + i;
-            if (s >= rz.pad && s < rz.slots) narrow(dz + s - rz.pad, 0.f);
-          }
-      }
-    }
-    return;
-  }
-  twice = __syncthreads_or(twice);
-
-  // which of vector j's elements are in the top
-  const auto in_top = [&](int64_t j) -> uint32_t {
-    const uint32_t b = (uint32_t)((j * N - slot0) & (kMaxBits - 1));
-    uint32_t m = bitmap[b >> 5] >> (b & 31) & ((1u << N) - 1);
-    if (m && wraps) {
-      uint32_t sure = 0;
-      for (int e = 0; e < p.k; ++e) {
-        const int64_t s = (int64_t)en.at[e] + rz.pad - j * N;
-        if (en.at[e] >= 0 && s >= 0 && s < N) sure |= 1u << s;
-      }
-      m = sure;
-    }
-    return m;
-  };
-
-  // pass 1: maximum and sum over the entries outside the top
-  float m = -INFINITY;
+// What one thread has seen: sum counts 2^(z c - k), k = m c.
+struct Seen {
+  float m = -kFar, k;
   Val<2> sum{0.f, 0.f};
-  for (int64_t base = v0; base < v1; base += (int64_t)kDeep * blockDim.x) {
-    Vec<TZ> a[kDeep];
-    float top = -INFINITY;
-#pragma unroll
-    for (int u = 0; u < kDeep; ++u) {
-      const int64_t j = base + (int64_t)u * blockDim.x + threadIdx.x;
-      a[u] = j < v1 ? rz.load(j, !dz) : all_least<TZ>();
-    }
-#pragma unroll
-    for (int u = 0; u < kDeep; ++u) {
-      const int64_t j = base + (int64_t)u * blockDim.x + threadIdx.x;
-      const uint32_t mask = j < v1 ? in_top(j) : 0;
-      if (mask) strike(a[u], mask);
-      top = fmaxf(top, top_of(a[u]));
-    }
+  __device__ __forceinline__ explicit Seen(float scale) { k = m * scale; }
+  template <int D, typename T> __device__ __forceinline__ void take(const Vec<T> *a, float scale) {
+    const float top = top_of<D>(a);
     if (top > m) {
-      sum = mul(sum, all<2>(ex2((m - top) * p.scale)));
+      const float was = k;
       m = top;
+      k = m * scale;
+      sum = mul(sum, all<2>(ex2(was - k)));
     }
-    const Val<2> from = all<2>(m == -INFINITY ? 0.f : m), by = all<2>(p.scale);
+    const Val<2> shift = all<2>(-k), by = all<2>(scale);
 #pragma unroll
-    for (int u = 0; u < kDeep; ++u)
+    for (int u = 0; u < D; ++u)
 #pragma unroll
-      for (int i = 0; i < P; ++i) {
-        Val<2> y = mul(sub(pair(a[u], i), from), by);
+      for (int i = 0; i < Vec<T>::P; ++i) {
+        Val<2> y = fma(pair(a[u], i), by, shift);
         y.x = ex2(y.x);
         y.y = ex2(y.y);
         sum = add(sum, y);
       }
   }
-  cg::cluster_group cl = cg::this_cluster();
-  x[0] = fmaxf(x[0], m);
-  over_block<2, true>(x, red[0]);
-  if (CLUSTER) {
-    if (threadIdx.x == 0) share[0] = x[0];
-    cl.sync();
-    for (int r = 0; r < ranks; ++r) x[0] = fmaxf(x[0], *cl.map_shared_rank(share, r));
+};
+
+// The part of a row that a CTA takes, in slots: slot s is element s - pad, so that vectors of N slots lie on 16-byte
+// boundaries.  Whole vectors are [w0, w1); what the row has before and after them in this part, fewer than N elements
+// each, goes one to a thread (`edge`, a slot, or -1).
+template <typename T> struct Part {
+  static constexpr int N = Vec<T>::N;
+  int pad;
+  int64_t slot0, slot1, w0, w1, edge;
+  __device__ __forceinline__ Part(const T *row, int64_t v, int rank, int64_t per) {
+    pad = (int)((reinterpret_cast<uintptr_t>(row) & 15) / sizeof(T));
+    const int64_t slots = v + pad, vectors = (slots + N - 1) / N;
+    const int64_t v0 = min(vectors, rank * per), v1 = min(vectors, v0 + per);
+    slot0 = v0 * N;
+    slot1 = v1 * N;
+    w0 = v0 + (v0 == 0 && pad > 0);
+    w1 = max(w0, min(v1, slots / N));
+    edge = -1;
+    const int i = threadIdx.x;
+    if (i < N) {
+      if (v0 == 0 && pad > 0 && i >= pad && i < slots && v1 > 0) edge = i;
+    } else if (i < 2 * N) {
+      const int64_t s = w1 * N + i - N;
+      if (v1 == vectors && v1 > v0 && s < slots && s >= slot0 && w1 >= w0 && !(w1 == 0 && pad > 0)) edge = s;
+    }
   }
-  const float M = x[0] == -INFINITY ? 0.f : x[0], tmax = x[1];
-  // sums: outside the top; of the top's exp(z / T), each entry once; of the teacher's weights and of their terms of the loss
-  x[0] = m == -INFINITY ? 0.f : (sum.x + sum.y) * ex2((m - M) * p.scale);
+};
+
+__device__ __forceinline__ float warp_max(float x) {
+  asm("redux.sync.max.f32 %0, %0, 0xffffffff;" : "+f"(x));
+  return x;
+}
+__device__ __forceinline__ float warp_sum(float x) {
+#pragma unroll
+  for (int o = 16; o; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
+  return x;
+}
+// Sums or maxima of up to four values over a CTA of W warps, and over its cluster, each in one fixed order.  `red` (W
+// of them) and `share` (one per CTA of the cluster) are this call's own.
+template <int N, bool MAX, int W, bool CLUSTER> __device__ __forceinline__ void over_row(float *x, float4 *red, float4 *share, int rank, int ranks) {
+  const auto both = [](float a, float b) { return MAX ? fmaxf(a, b) : a + b; };
+  const auto gather = [&](const float4 *v, int n) {
+    float4 q = v[0];
+#pragma unroll
+    for (int i = 0; i < N; ++i) x[i] = (&q.x)[i];
+    for (int k = 1; k < n; ++k) {
+      q = v[k];
+#pragma unroll
+      for (int i = 0; i < N; ++i) x[i] = both(x[i], (&q.x)[i]);
+    }
+  };
+  float4 q;
+#pragma unroll
+  for (int i = 0; i < N; ++i) (&q.x)[i] = x[i] = MAX ? warp_max(x[i]) : warp_sum(x[i]);
+  if (W > 1) {
+    if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = q;
+    __syncthreads();
+    gather(red, W);
+  }
+  if (CLUSTER) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) (&q.x)[i] = x[i];
+    if (threadIdx.x < 32) {
+      if (threadIdx.x < ranks) *cg::this_cluster().map_shared_rank(share + rank, threadIdx.x) = q;
+      asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+    } else {   // has published nothing
+      asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
+    }
+    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+    gather(share, ranks);
+  }
+}
+
+// Shared memory behind the bitmap: k entries of each.
+struct Entries {
+  int32_t *at;    // the vocabulary entry where it lies in this part, or -1
+  float *t, *z;   // the teacher's logit / T, the student's logit
+};
+
+// HELD: the part fits in shared memory.
+template <typename TZ, int THREADS, bool CLUSTER, bool HELD>
+__global__ void __launch_bounds__(THREADS, 768 / THREADS) distill_kernel(const DistillArgs p) {
+  constexpr int N = Vec<TZ>::N, P = Vec<TZ>::P, W = THREADS / 32, hop = kDeep * THREADS;
+  extern __shared__ uint4 memory[];   // the part's whole vectors, the bitmap, the entries
+  __shared__ float4 red[3][W], share[3][kMaxCluster];
+  uint32_t *bitmap = reinterpret_cast<uint32_t *>(memory + (HELD ? p.per : 0));
+  Entries en;
+  en.at = reinterpret_cast<int32_t *>(bitmap + p.words);
+  en.t = reinterpret_cast<float *>(en.at + p.k);
+  en.z = en.t + p.k;
+  const int tid = threadIdx.x, ranks = CLUSTER ? p.cluster : 1;
+  const uint32_t row = CLUSTER ? blockIdx.x / ranks : blockIdx.x;
+  const int rank = CLUSTER ? (int)(blockIdx.x - row * ranks) : 0;
+  const TZ *z = static_cast<const TZ *>(p.z) + row * p.ldz;
+  TZ *dz = p.dz ? static_cast<TZ *>(p.dz) + row * p.lddz : nullptr;
+  const auto listed = [&](int j) -> int64_t {
+    const int64_t i = row * p.ldi + j;
+    return p.idx64 ? static_cast<const int64_t *>(p.idx)[i] : static_cast<const int32_t *>(p.idx)[i];
+  };
+  const auto teacher = [&](int j) -> float {
+    const int64_t i = row * p.ldt + j;
+    return p.t16 ? widen(static_cast<const bf16 *>(p.t)[i]) : static_cast<const float *>(p.t)[i];
+  };
+  const float w = p.weight ? p.weight[row] : 1.f;
+  const bool tail = p.teacher_lse != nullptr;
+  const float lse = tail ? p.teacher_lse[row] : 0.f;
+  int64_t at = -1;   // the thread's first entry is on its way before the row is
+  float tj = 0.f;
+  if (tid < p.k) {
+    at = listed(tid);
+    tj = teacher(tid);
+  }
+  const Part<TZ> part(z, p.v, rank, p.per);
+  const int64_t slot0 = part.slot0, slot1 = part.slot1;
+  const bool together = ((reinterpret_cast<uintptr_t>(z) ^ reinterpret_cast<uintptr_t>(dz)) & 15) == 0;
+  const int count = (int)(part.w1 - part.w0);
+  const uint4 *from = reinterpret_cast<const uint4 *>(z - part.pad) + part.w0 + tid;
+  uint4 *dst = reinterpret_cast<uint4 *>(dz - part.pad) + part.w0 + tid;   // used when z and dz lie together
+  const uint4 *src = HELD ? memory + tid : from;
+
+  // every CTA of the cluster runs before anybody writes into its shared memory
+  if (CLUSTER) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
+  const auto nothing = [&]() {   // no loss, a zero gradient
+    if (tid == 0 && rank == 0 && p.loss) p.loss[row] = 0.f;
+    if (dz) {
+      if (together)
+        for (int j = 0; j < count - tid; j += THREADS) __stcs(dst + j, make_uint4(0, 0, 0, 0));
+      else
+        for (int64_t e = part.w0 * N + tid; e < part.w1 * N; e += THREADS) narrow(dz + e - part.pad, 0.f);
+      if (part.edge >= 0) narrow(dz + part.edge - part.pad, 0.f);
+    }
+  };
+  for (int c = tid; c < p.words / 4; c += THREADS) reinterpret_cast<uint4 *>(bitmap)[c] = make_uint4(0, 0, 0, 0);
+  if (w == 0.f) {
+    if (CLUSTER) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+    nothing();
+    return;
+  }
+  const float edge = part.edge >= 0 ? widen(z[part.edge - part.pad]) : 0.f;
+  if (HELD) {
+    const uint32_t to = smem_u32(memory + tid);
+    for (int j = 0; j < count - tid; j += THREADS)
+      asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to + j * 16), "l"(from + j) : "memory");
+  }
+  __syncthreads();
+  // the top: its entries, which of them lie in this part, the bitmap
+  float x[4] = {-kFar, -INFINITY, 0.f, 0.f};   // maxima of z and of t over the top; whether an entry is listed twice
+  for (int j = tid; j < p.k; j += THREADS) {
+    if (j != tid) {
+      at = listed(j);
+      tj = teacher(j);
+    }
+    tj /= p.temperature;
+    const bool there = at >= 0 && at < p.v && !(tj == -INFINITY);
+    const int64_t slot = at + part.pad;
+    const bool here = there && slot >= slot0 && slot < slot1;
+    en.at[j] = here ? (int32_t)at : -1;
+    en.t[j] = tj;
+    if (there) x[1] = fmaxf(x[1], tj == tj ? tj : INFINITY);   // (a NaN is there as well)
+    if (here) {
+      const uint32_t b = (uint32_t)((slot - slot0) & (kMaxBits - 1));
+      if (atomicOr(bitmap + (b >> 5), 1u << (b & 31)) >> (b & 31) & 1) x[2] = 1.f;
+      const float zj = widen(z[at]);
+      en.z[j] = zj;
+      x[0] = fmaxf(x[0], zj);
+    }
+  }
+  __syncthreads();
+  if (HELD) asm volatile("cp.async.wait_all;" ::: "memory");   // a thread uses what it has copied itself
+  if (CLUSTER) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+
+  // which of the N slots from s on (a multiple of N) are in the top
+  const uint8_t *bytes = reinterpret_cast<const uint8_t *>(bitmap);
+  const auto in_top = [&](int64_t s) -> uint32_t {
+    const uint32_t b = (uint32_t)((s - slot0) & (kMaxBits - 1));
+    uint32_t m = N == 8 ? bytes[b >> 3] : bytes[b >> 3] >> (b & 4) & 15u;
+    if (!HELD && m && slot1 - slot0 > kMaxBits) {   // the bitmap wraps around: the bit may be another slot's
+      m = 0;
+      for (int e = 0; e < p.k; ++e) {
+        const int64_t d = (int64_t)en.at[e] + part.pad - s;
+        if (en.at[e] >= 0 && d >= 0 && d < N) m |= 1u << d;
+      }
+    }
+    return m;
+  };
+  const auto counts = [&](int64_t s) { return !tail || !(in_top(s / N * N) >> (s % N) & 1); };   // in pass 1's sum
+
+  // pass 1: maximum and sum, in tail mode over the entries outside the top
+  Seen seen(p.scale);
+  if (part.edge >= 0 && counts(part.edge)) {
+    seen.m = fmaxf(seen.m, edge);
+    seen.k = seen.m * p.scale;
+    seen.sum.x = ex2(fmaf(edge, p.scale, -seen.k));
+  }
+  const int64_t s0 = (part.w0 + tid) * N;
+  int base = 0;
+  for (; base + hop <= count; base += hop) {
+    Vec<TZ> a[kDeep];
+#pragma unroll
+    for (int u = 0; u < kDeep; ++u) a[u].w = src[base + u * THREADS];
+    if (tail) {
+      uint32_t mask[kDeep], any = 0;
+#pragma unroll
+      for (int u = 0; u < kDeep; ++u) any |= mask[u] = in_top(s0 + (int64_t)(base + u * THREADS) * N);
+      if (any)
+#pragma unroll
+        for (int u = 0; u < kDeep; ++u) strike(a[u], mask[u]);
+    }
+    seen.take<kDeep>(a, p.scale);
+  }
+  for (int j = base; j < count - tid; j += THREADS) {
+    Vec<TZ> a;
+    a.w = src[j];
+    if (tail) {
+      const uint32_t mask = in_top(s0 + (int64_t)j * N);
+      if (mask) strike(a, mask);
+    }
+    seen.take<1>(&a, p.scale);
+  }
+  x[0] = fmaxf(x[0], seen.m);
+  over_row<3, true, W, CLUSTER>(x, red[0], share[0], rank, ranks);
+  if (x[1] == -INFINITY) {   // no teacher entry
+    nothing();
+    return;
+  }
+  float M = x[0];
+  const bool twice = x[2] != 0.f;
+  const float norm = tail ? lse : x[1];
+  float sum = seen.sum.x + seen.sum.y;
+  const bool far = !(fabsf(M) < kFar);
+  if (far) {   // logits beyond +-kFar only (or infinite, or NaN): once more, element by element
+    float top[1] = {-INFINITY};
+    const int64_t s1 = min(slot1, p.v + part.pad);
+    for (int64_t s = max(slot0, (int64_t)part.pad) + tid; s < s1; s += THREADS) top[0] = fmaxf(top[0], widen(z[s - part.pad]));
+    over_row<1, true, W, CLUSTER>(top, red[1], share[1], rank, ranks);
+    M = top[0] == -INFINITY ? 0.f : top[0];
+    sum = 0.f;
+    for (int64_t s = max(slot0, (int64_t)part.pad) + tid; s < s1; s += THREADS)
+      if (counts(s)) sum += ex2((widen(z[s - part.pad]) - M) * p.scale);
+  }
+  const float K = M * p.scale;
+  const auto exponent = [&](float v) { return far ? (v - M) * p.scale : fmaf(v, p.scale, -K); };
+  // sums: of 2^(z c - K) by pass 1 and over the top, each entry once; of the teacher's weights and of their terms of the
+  // loss
+  x[0] = far ? sum : sum * ex2(seen.k - K);
   x[1] = x[2] = x[3] = 0.f;
-  const float norm = tail ? p.teacher_lse[row] : tmax;
-  for (int j = threadIdx.x; j < p.k; j += blockDim.x) {
+  for (int j = tid; j < p.k; j += THREADS) {
     if (en.at[j] < 0) continue;
     bool first = true;
-    if (twice || wraps || CLUSTER)   // (a CTA of a cluster has seen the bits of its own slots only)
+    if (twice)
       for (int e = 0; e < j; ++e) first &= en.at[e] != en.at[j];
-    const float y = en.z[j] - M;
-    if (first) x[1] += ex2(y * p.scale);
+    const float y = exponent(en.z[j]);
+    if (tail && first) x[1] += ex2(y);
     const float lp = en.t[j] - norm, pj = expf(lp);
     x[2] += pj;
-    if (pj > 0.f) x[3] += pj * (lp - y / p.temperature);
+    if (pj > 0.f) x[3] += pj * (lp - kLn2 * y);
   }
-  over_block<4, false>(x, red[1]);
-  float out = x[0];
-  if (CLUSTER) {
-    if (threadIdx.x == 0) share[1] = out;
-    cl.sync();
-    out = 0.f;
-    for (int r = 0; r < ranks; ++r) out += *cl.map_shared_rank(share + 1, r);
-  }
-  const float total = out + x[1];
+  over_row<4, false, W, CLUSTER>(x, red[2], share[2], rank, ranks);
+  const float out = x[0], total = x[0] + x[1];
   const float mass = tail ? 1.f : x[2];   // what the teacher's weights are divided by
   const float rest = tail ? fmaxf(0.f, 1.f - x[2]) : 0.f;
-  if (threadIdx.x == 0 && rank == 0 && p.loss) {
+  if (tid == 0 && rank == 0 && p.loss) {
     float l = tail ? x[3] + x[2] * logf(total) : x[3] / mass - logf(mass) + logf(total);
     if (rest > 0.f) l += rest * logf(rest / (out / total));
     if (total == 0.f) l = INFINITY;
@@ -304,43 +399,42 @@ __global__ void __launch_bounds__(kMaxThreads, 2) distill_kernel(const DistillAr
     const float scale = w / p.temperature;
     const float inside = total == 0.f ? 0.f : scale / total;
     const float outside = rest > 0.f && out > 0.f ? inside - scale * (rest / out) : inside;
-    const Val<2> from = all<2>(M), by = all<2>(p.scale), factor = all<2>(outside);
-    for (int64_t base = v0; base < v1; base += (int64_t)kDeep * blockDim.x) {
-      Vec<TZ> a[kDeep];
-#pragma unroll
-      for (int u = 0; u < kDeep; ++u) {
-        const int64_t j = base + (int64_t)u * blockDim.x + threadIdx.x;
-        if (j < v1) a[u] = rz.load(j, true);
-      }
-#pragma unroll
-      for (int u = 0; u < kDeep; ++u) {
-        const int64_t j = base + (int64_t)u * blockDim.x + threadIdx.x;
-        if (j >= v1) continue;
+    if (together && !far) {
+      const Val<2> shift = all<2>(-K), by = all<2>(p.scale), factor = all<2>(outside);
+      const auto turn = [&](Vec<TZ> v) {
 #pragma unroll
         for (int i = 0; i < P; ++i) {
-          Val<2> y = mul(sub(pair(a[u], i), from), by);
+          Val<2> y = fma(pair(v, i), by, shift);
           y.x = ex2(y.x);
           y.y = ex2(y.y);
-          set_pair(a[u], i, mul(y, factor));
+          set_pair(v, i, mul(y, factor));
         }
-        if (together && rz.whole(j)) {
-          __stcs(reinterpret_cast<uint4 *>(dz - rz.pad) + j, a[u].w);
-        } else {
-          const TZ *e = reinterpret_cast<const TZ *>(&a[u].w);
-          for (int i = 0; i < N; ++i) {
-            const int64_t s = j * N + i;
-            if (s >= rz.pad && s < rz.slots) dz[s - rz.pad] = e[i];
-          }
-        }
+        return v.w;
+      };
+      for (base = 0; base + hop <= count; base += hop) {
+        Vec<TZ> a[kDeep];
+#pragma unroll
+        for (int u = 0; u < kDeep; ++u) a[u].w = src[base + u * THREADS];
+#pragma unroll
+        for (int u = 0; u < kDeep; ++u) __stcs(dst + base + u * THREADS, turn(a[u]));
       }
+      for (int j = base; j < count - tid; j += THREADS) {
+        Vec<TZ> a;
+        a.w = src[j];
+        __stcs(dst + j, turn(a));
+      }
+      if (part.edge >= 0) narrow(dz + part.edge - part.pad, ex2(exponent(edge)) * outside);
+    } else {   // element by element, from memory (where dz is z, each thread reads what it writes over)
+      const int64_t s1 = min(slot1, p.v + part.pad);
+      for (int64_t s = max(slot0, (int64_t)part.pad) + tid; s < s1; s += THREADS)
+        narrow(dz + s - part.pad, ex2(exponent(widen(z[s - part.pad]))) * outside);
     }
     __syncthreads();
-    for (int j = threadIdx.x; j < p.k; j += blockDim.x) {
-      const int64_t slot = (int64_t)en.at[j] + rz.pad;
-      if (en.at[j] < 0 || slot < slot0 || slot >= slot1) continue;
+    for (int j = tid; j < p.k; j += THREADS) {
+      if (en.at[j] < 0) continue;
       float pc = expf(en.t[j] - norm);
       bool first = true;
-      if (twice || wraps) {   // an entry listed twice counts with both weights, in the order of the list
+      if (twice) {   // an entry listed twice counts with both weights, in the order of the list
         pc = 0.f;
         for (int e = 0; e < p.k; ++e)
           if (en.at[e] == en.at[j]) {
@@ -348,22 +442,21 @@ __global__ void __launch_bounds__(kMaxThreads, 2) distill_kernel(const DistillAr
             pc += expf(en.t[e] - norm);
           }
       }
-      if (first) narrow(dz + en.at[j], ex2((en.z[j] - M) * p.scale) * inside - scale * (pc / mass));
+      if (first) narrow(dz + en.at[j], ex2(exponent(en.z[j])) * inside - scale * (pc / mass));
     }
   }
-  if (CLUSTER) cl.sync();   // nobody leaves while another CTA may still read its share
 }
 
-template <typename TZ, typename TT, typename TI, bool CLUSTER>
-cudaError_t launch(const DistillArgs &p, int64_t r, int threads, cudaStream_t s) {
+template <typename TZ, int THREADS, bool CLUSTER, bool HELD> cudaError_t launch(const DistillArgs &p, int64_t r, cudaStream_t s) {
   static std::atomic<uint64_t> done{0};
-  auto kernel = distill_kernel<TZ, TT, TI, CLUSTER>;
-  const size_t most = kMaxBits / 8 + 12 * (size_t)kMaxTop, bytes = 4 * (size_t)p.words + 12 * (size_t)p.k;
+  auto kernel = distill_kernel<TZ, THREADS, CLUSTER, HELD>;
+  const size_t fixed = 12 * (size_t)kMaxTop, most = fixed + (HELD ? kMostHeld + kMostHeld / sizeof(TZ) / 8 + 16 : kMaxBits / 8);
+  const size_t bytes = (HELD ? 16 * (size_t)p.per : 0) + 4 * (size_t)p.words + 12 * (size_t)p.k;
   cudaError_t e = set_max_shared_once(reinterpret_cast<const void *>(kernel), most, &done);
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3((unsigned)(r * p.cluster));
-  cfg.blockDim = dim3(threads);
+  cfg.blockDim = dim3(THREADS);
   cfg.dynamicSmemBytes = bytes;
   cfg.stream = s;
   cudaLaunchAttribute at{};
@@ -373,20 +466,23 @@ cudaError_t launch(const DistillArgs &p, int64_t r, int threads, cudaStream_t s)
   return cudaLaunchKernelEx(&cfg, kernel, p);
 }
 
-template <typename TZ, typename TT, typename TI> cudaError_t launch_rows(DistillArgs p, int64_t r, cudaStream_t s) {
+template <typename TZ> cudaError_t launch_rows(DistillArgs p, int64_t r, cudaStream_t s) {
   constexpr int N = Vec<TZ>::N;
   const int64_t vectors = ceil_div(p.v + N - 1, N);   // of the row on the least fortunate boundary
-  // CTAs per row: one, unless the rows leave SMs empty and there are at least kDeep vectors for each thread of a CTA
+  // CTAs per row: what holds the row, and more where the rows leave SMs empty and a part is still 16 vectors a thread
   p.cluster = 1;
-  while (p.cluster < kMaxCluster && r * p.cluster * 2 <= sm_count() && vectors / (p.cluster * 2) >= kDeep * kMaxThreads) p.cluster *= 2;
+  while (p.cluster < kMaxCluster && (16 * ceil_div(vectors, p.cluster) > kHeld ||
+                                     (r * p.cluster * 2 <= 4 * sm_count() && vectors >= 2 * 16 * 128 * p.cluster)))
+    p.cluster *= 2;
   const int64_t per = ceil_div(vectors, p.cluster);
-  p.words = (int32_t)(std::min(kMaxBits, ceil_div(per * N, 32) * 32) / 32);
-  const int threads = (int)std::min<int64_t>(kMaxThreads, std::max<int64_t>(128, ceil_div(per, 32) * 32));
-  return p.cluster > 1 ? launch<TZ, TT, TI, true>(p, r, threads, s) : launch<TZ, TT, TI, false>(p, r, threads, s);
-}
-
-template <typename TZ, typename TT> cudaError_t launch_i(const DistillArgs &p, int32_t it, int64_t r, cudaStream_t s) {
-  return it == DSGD_I64 ? launch_rows<TZ, TT, int64_t>(p, r, s) : launch_rows<TZ, TT, int32_t>(p, r, s);
+  p.per = (int32_t)per;
+  p.words = (int32_t)(std::min(kMaxBits, ceil_div(per * N, 128) * 128) / 32);
+  if (16 * per > kMostHeld) return launch<TZ, 256, true, false>(p, r, s);
+  if (16 * per > kHeld) return launch<TZ, 256, true, true>(p, r, s);
+  if (p.cluster > 1) return launch<TZ, 128, true, true>(p, r, s);
+  // few vectors a thread for short rows, so that many of them are at work on an SM
+  if (per <= 8 * 32) return launch<TZ, 32, false, true>(p, r, s);
+  return per <= 8 * 64 ? launch<TZ, 64, false, true>(p, r, s) : launch<TZ, 128, false, true>(p, r, s);
 }
 
 ceca_status_t distill(const void *z, const void *idx, const void *t, const float *teacher_lse, const float *weight,
@@ -405,12 +501,10 @@ ceca_status_t distill(const void *z, const void *idx, const void *t, const float
   p.v = v; p.k = k; p.ldz = ldz; p.ldi = ldi; p.ldt = ldt; p.lddz = lddz;
   p.scale = (float)(1.4426950408889634 / (double)temperature);
   p.temperature = temperature;
+  p.idx64 = index_type == DSGD_I64;
+  p.t16 = teacher_type == DSGD_BF16;
   const cudaStream_t s = static_cast<cudaStream_t>(stream);
-  cudaError_t e;
-  if (logits_type == DSGD_F32)
-    e = teacher_type == DSGD_F32 ? launch_i<float, float>(p, index_type, r, s) : launch_i<float, bf16>(p, index_type, r, s);
-  else
-    e = teacher_type == DSGD_F32 ? launch_i<bf16, float>(p, index_type, r, s) : launch_i<bf16, bf16>(p, index_type, r, s);
+  const cudaError_t e = logits_type == DSGD_F32 ? launch_rows<float>(p, r, s) : launch_rows<bf16>(p, r, s);
   return e == cudaSuccess ? CECA_OK : CECA_ERR_CUDA;
 }
 
