@@ -134,23 +134,25 @@ struct Seen {
 // each, goes one to a thread (`edge`, a slot, or -1).
 template <typename T> struct Part {
   static constexpr int N = Vec<T>::N;
-  int pad;
-  int64_t slot0, slot1, w0, w1, edge;
-  __device__ __forceinline__ Part(const T *row, int64_t v, int rank, int64_t per) {
+  int pad, w0, w1;
+  uint32_t slot0, slot1;
+  int64_t edge;
+  __device__ __forceinline__ Part(const T *row, int64_t v, int rank, int per) {
     pad = (int)((reinterpret_cast<uintptr_t>(row) & 15) / sizeof(T));
-    const int64_t slots = v + pad, vectors = (slots + N - 1) / N;
-    const int64_t v0 = min(vectors, rank * per), v1 = min(vectors, v0 + per);
-    slot0 = v0 * N;
-    slot1 = v1 * N;
+    const uint32_t slots = (uint32_t)v + pad;
+    const int vectors = (int)((slots + N - 1) / N);
+    const int v0 = min(vectors, rank * per), v1 = min(vectors, v0 + per);
+    slot0 = (uint32_t)v0 * N;
+    slot1 = (uint32_t)v1 * N;
     w0 = v0 + (v0 == 0 && pad > 0);
-    w1 = max(w0, min(v1, slots / N));
+    w1 = max(w0, min(v1, (int)(slots / N)));
     edge = -1;
     const int i = threadIdx.x;
     if (i < N) {
-      if (v0 == 0 && pad > 0 && i >= pad && i < slots && v1 > 0) edge = i;
+      if (v0 == 0 && pad > 0 && i >= pad && i < slots) edge = i;
     } else if (i < 2 * N) {
-      const int64_t s = w1 * N + i - N;
-      if (v1 == vectors && v1 > v0 && s < slots && s >= slot0 && w1 >= w0 && !(w1 == 0 && pad > 0)) edge = s;
+      const uint32_t s = (uint32_t)w1 * N + i - N;
+      if (v1 == vectors && v1 > v0 && s < slots && s < slot1) edge = s;
     }
   }
 };
@@ -164,40 +166,37 @@ __device__ __forceinline__ float warp_sum(float x) {
   for (int o = 16; o; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
   return x;
 }
-// Sums or maxima of up to four values over a CTA of W warps, and over its cluster, each in one fixed order.  `red` (W
-// of them) and `share` (one per CTA of the cluster) are this call's own.
-template <int N, bool MAX, int W, bool CLUSTER> __device__ __forceinline__ void over_row(float *x, float4 *red, float4 *share, int rank, int ranks) {
-  const auto both = [](float a, float b) { return MAX ? fmaxf(a, b) : a + b; };
-  const auto gather = [&](const float4 *v, int n) {
-    float4 q = v[0];
+
+// What a warp, a CTA or a cluster knows of its part of a row, in the frame k = m c: the sum of 2^(z c - k) by pass 1, the
+// same over the top (each entry once), the teacher's weights p there, and p (log p - ln2 (z c - k)).
+struct alignas(16) Known {
+  float m, sum, top, mass, terms, pad[3];
+};
+// The n parts of `all` in one frame, on every lane of the warp that asks: each lane moves its own there (terms move by ln2 p
+// times the distance), and the sums run over the lanes in one fixed order.
+template <int MOST> __device__ __forceinline__ Known joined(const Known *all, int n, float scale) {
+  const int lane = threadIdx.x & 31;
+  Known q[(MOST + 31) / 32], a{-INFINITY, 0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int i = 0; i < N; ++i) x[i] = (&q.x)[i];
-    for (int k = 1; k < n; ++k) {
-      q = v[k];
-#pragma unroll
-      for (int i = 0; i < N; ++i) x[i] = both(x[i], (&q.x)[i]);
-    }
-  };
-  float4 q;
-#pragma unroll
-  for (int i = 0; i < N; ++i) (&q.x)[i] = x[i] = MAX ? warp_max(x[i]) : warp_sum(x[i]);
-  if (W > 1) {
-    if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = q;
-    __syncthreads();
-    gather(red, W);
+  for (int i = 0; i < (MOST + 31) / 32; ++i) {
+    q[i] = lane + 32 * i < n ? all[lane + 32 * i] : Known{-INFINITY, 0.f, 0.f, 0.f, 0.f};
+    a.m = fmaxf(a.m, q[i].m);
   }
-  if (CLUSTER) {
+  a.m = warp_max(a.m);
 #pragma unroll
-    for (int i = 0; i < N; ++i) (&q.x)[i] = x[i];
-    if (threadIdx.x < 32) {
-      if (threadIdx.x < ranks) *cg::this_cluster().map_shared_rank(share + rank, threadIdx.x) = q;
-      asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
-    } else {   // has published nothing
-      asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
+  for (int i = 0; i < (MOST + 31) / 32; ++i)
+    if (lane + 32 * i < n) {
+      const float d = (q[i].m - a.m) * scale, f = ex2(d);
+      a.sum += q[i].sum * f;
+      a.top += q[i].top * f;
+      a.terms += q[i].terms - kLn2 * d * q[i].mass;
+      a.mass += q[i].mass;
     }
-    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
-    gather(share, ranks);
-  }
+  a.sum = warp_sum(a.sum);
+  a.top = warp_sum(a.top);
+  a.terms = warp_sum(a.terms);
+  a.mass = warp_sum(a.mass);
+  return a;
 }
 
 // Shared memory behind the bitmap: k entries of each.
@@ -206,18 +205,26 @@ struct Entries {
   float *t, *z;   // the teacher's logit / T, the student's logit
 };
 
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_arrive(bool published) {   // without anything published, no wait for earlier stores
+  if (published) asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+  else asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
+}
+
 // HELD: the part fits in shared memory.
 template <typename TZ, int THREADS, bool CLUSTER, bool HELD>
 __global__ void __launch_bounds__(THREADS, 768 / THREADS) distill_kernel(const DistillArgs p) {
   constexpr int N = Vec<TZ>::N, P = Vec<TZ>::P, W = THREADS / 32, hop = kDeep * THREADS;
   extern __shared__ uint4 memory[];   // the part's whole vectors, the bitmap, the entries
-  __shared__ float4 red[3][W], share[3][kMaxCluster];
+  constexpr int kParts = W * (CLUSTER ? kMaxCluster : 1);
+  __shared__ Known share[kParts];   // of each warp of the cluster
+  __shared__ float tops[W], far_red[W], far_share[kMaxCluster];
   uint32_t *bitmap = reinterpret_cast<uint32_t *>(memory + (HELD ? p.per : 0));
   Entries en;
   en.at = reinterpret_cast<int32_t *>(bitmap + p.words);
   en.t = reinterpret_cast<float *>(en.at + p.k);
   en.z = en.t + p.k;
-  const int tid = threadIdx.x, ranks = CLUSTER ? p.cluster : 1;
+  const int tid = threadIdx.x, warp = tid >> 5, ranks = CLUSTER ? p.cluster : 1;
   const uint32_t row = CLUSTER ? blockIdx.x / ranks : blockIdx.x;
   const int rank = CLUSTER ? (int)(blockIdx.x - row * ranks) : 0;
   const TZ *z = static_cast<const TZ *>(p.z) + row * p.ldz;
@@ -240,28 +247,28 @@ __global__ void __launch_bounds__(THREADS, 768 / THREADS) distill_kernel(const D
     tj = teacher(tid);
   }
   const Part<TZ> part(z, p.v, rank, p.per);
-  const int64_t slot0 = part.slot0, slot1 = part.slot1;
+  const uint32_t slot0 = part.slot0, slot1 = part.slot1;
   const bool together = ((reinterpret_cast<uintptr_t>(z) ^ reinterpret_cast<uintptr_t>(dz)) & 15) == 0;
-  const int count = (int)(part.w1 - part.w0);
+  const int count = part.w1 - part.w0;
   const uint4 *from = reinterpret_cast<const uint4 *>(z - part.pad) + part.w0 + tid;
   uint4 *dst = reinterpret_cast<uint4 *>(dz - part.pad) + part.w0 + tid;   // used when z and dz lie together
   const uint4 *src = HELD ? memory + tid : from;
 
   // every CTA of the cluster runs before anybody writes into its shared memory
-  if (CLUSTER) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
+  if (CLUSTER) cluster_arrive(false);
   const auto nothing = [&]() {   // no loss, a zero gradient
     if (tid == 0 && rank == 0 && p.loss) p.loss[row] = 0.f;
     if (dz) {
       if (together)
         for (int j = 0; j < count - tid; j += THREADS) __stcs(dst + j, make_uint4(0, 0, 0, 0));
       else
-        for (int64_t e = part.w0 * N + tid; e < part.w1 * N; e += THREADS) narrow(dz + e - part.pad, 0.f);
+        for (int64_t e = (int64_t)part.w0 * N + tid; e < (int64_t)part.w1 * N; e += THREADS) narrow(dz + e - part.pad, 0.f);
       if (part.edge >= 0) narrow(dz + part.edge - part.pad, 0.f);
     }
   };
   for (int c = tid; c < p.words / 4; c += THREADS) reinterpret_cast<uint4 *>(bitmap)[c] = make_uint4(0, 0, 0, 0);
   if (w == 0.f) {
-    if (CLUSTER) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+    if (CLUSTER) cluster_wait();
     nothing();
     return;
   }
@@ -270,10 +277,14 @@ __global__ void __launch_bounds__(THREADS, 768 / THREADS) distill_kernel(const D
     const uint32_t to = smem_u32(memory + tid);
     for (int j = 0; j < count - tid; j += THREADS)
       asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to + j * 16), "l"(from + j) : "memory");
+    asm volatile("cp.async.wait_all;" ::: "memory");
   }
   __syncthreads();
-  // the top: its entries, which of them lie in this part, the bitmap
-  float x[4] = {-kFar, -INFINITY, 0.f, 0.f};   // maxima of z and of t over the top; whether an entry is listed twice
+  // The top: its entries, which of them lie in this part, the bitmap.  In tail mode what is held of them becomes
+  // -infinity, so that the passes need not ask.
+  TZ *held = reinterpret_cast<TZ *>(memory) - (int64_t)part.w0 * N;   // slot s is held[s]
+  float tmax = -INFINITY;
+  bool again = false;   // whether an entry of the thread is listed twice
   for (int j = tid; j < p.k; j += THREADS) {
     if (j != tid) {
       at = listed(j);
@@ -285,18 +296,24 @@ __global__ void __launch_bounds__(THREADS, 768 / THREADS) distill_kernel(const D
     const bool here = there && slot >= slot0 && slot < slot1;
     en.at[j] = here ? (int32_t)at : -1;
     en.t[j] = tj;
-    if (there) x[1] = fmaxf(x[1], tj == tj ? tj : INFINITY);   // (a NaN is there as well)
+    if (there) tmax = fmaxf(tmax, tj == tj ? tj : INFINITY);   // (a NaN is there as well)
     if (here) {
       const uint32_t b = (uint32_t)((slot - slot0) & (kMaxBits - 1));
-      if (atomicOr(bitmap + (b >> 5), 1u << (b & 31)) >> (b & 31) & 1) x[2] = 1.f;
-      const float zj = widen(z[at]);
-      en.z[j] = zj;
-      x[0] = fmaxf(x[0], zj);
+      again |= atomicOr(bitmap + (b >> 5), 1u << (b & 31)) >> (b & 31) & 1;
+      en.z[j] = widen(z[at]);
+      if (HELD && tail && slot >= (int64_t)part.w0 * N && slot < (int64_t)part.w1 * N) narrow(held + slot, -INFINITY);
     }
   }
-  __syncthreads();
-  if (HELD) asm volatile("cp.async.wait_all;" ::: "memory");   // a thread uses what it has copied itself
-  if (CLUSTER) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+  tmax = warp_max(tmax);
+  if ((tid & 31) == 0) tops[warp] = tmax;
+  const bool twice = __syncthreads_or(again);
+#pragma unroll
+  for (int i = 0; i < W; ++i) tmax = fmaxf(tmax, tops[i]);
+  if (CLUSTER) cluster_wait();
+  if (tmax == -INFINITY) {   // no teacher entry
+    nothing();
+    return;
+  }
 
   // which of the N slots from s on (a multiple of N) are in the top
   const uint8_t *bytes = reinterpret_cast<const uint8_t *>(bitmap);
@@ -321,129 +338,160 @@ __global__ void __launch_bounds__(THREADS, 768 / THREADS) distill_kernel(const D
     seen.k = seen.m * p.scale;
     seen.sum.x = ex2(fmaf(edge, p.scale, -seen.k));
   }
-  const int64_t s0 = (part.w0 + tid) * N;
-  int base = 0;
-  for (; base + hop <= count; base += hop) {
+  const int64_t s0 = (int64_t)(part.w0 + tid) * N;
+  for (int base = 0; base < count; base += hop) {
     Vec<TZ> a[kDeep];
+    const int left = count - base - tid;
+    if (base + hop <= count) {
 #pragma unroll
-    for (int u = 0; u < kDeep; ++u) a[u].w = src[base + u * THREADS];
-    if (tail) {
-      uint32_t mask[kDeep], any = 0;
+      for (int u = 0; u < kDeep; ++u) a[u].w = src[base + u * THREADS];
+    } else {
 #pragma unroll
-      for (int u = 0; u < kDeep; ++u) any |= mask[u] = in_top(s0 + (int64_t)(base + u * THREADS) * N);
-      if (any)
+      for (int u = 0; u < kDeep; ++u) {
+        a[u] = all_least<TZ>();
+        if (u * THREADS < left) a[u].w = src[base + u * THREADS];
+      }
+    }
+    if (!HELD && tail) {
 #pragma unroll
-        for (int u = 0; u < kDeep; ++u) strike(a[u], mask[u]);
+      for (int u = 0; u < kDeep; ++u) {
+        const uint32_t mask = u * THREADS < left ? in_top(s0 + (int64_t)(base + u * THREADS) * N) : 0;
+        if (mask) strike(a[u], mask);
+      }
     }
     seen.take<kDeep>(a, p.scale);
   }
-  for (int j = base; j < count - tid; j += THREADS) {
-    Vec<TZ> a;
-    a.w = src[j];
-    if (tail) {
-      const uint32_t mask = in_top(s0 + (int64_t)j * N);
-      if (mask) strike(a, mask);
-    }
-    seen.take<1>(&a, p.scale);
-  }
-  x[0] = fmaxf(x[0], seen.m);
-  over_row<3, true, W, CLUSTER>(x, red[0], share[0], rank, ranks);
-  if (x[1] == -INFINITY) {   // no teacher entry
-    nothing();
-    return;
-  }
-  float M = x[0];
-  const bool twice = x[2] != 0.f;
-  const float norm = tail ? lse : x[1];
-  float sum = seen.sum.x + seen.sum.y;
-  const bool far = !(fabsf(M) < kFar);
-  if (far) {   // logits beyond +-kFar only (or infinite, or NaN): once more, element by element
-    float top[1] = {-INFINITY};
-    const int64_t s1 = min(slot1, p.v + part.pad);
-    for (int64_t s = max(slot0, (int64_t)part.pad) + tid; s < s1; s += THREADS) top[0] = fmaxf(top[0], widen(z[s - part.pad]));
-    over_row<1, true, W, CLUSTER>(top, red[1], share[1], rank, ranks);
-    M = top[0] == -INFINITY ? 0.f : top[0];
-    sum = 0.f;
-    for (int64_t s = max(slot0, (int64_t)part.pad) + tid; s < s1; s += THREADS)
-      if (counts(s)) sum += ex2((widen(z[s - part.pad]) - M) * p.scale);
-  }
-  const float K = M * p.scale;
-  const auto exponent = [&](float v) { return far ? (v - M) * p.scale : fmaf(v, p.scale, -K); };
-  // sums: of 2^(z c - K) by pass 1 and over the top, each entry once; of the teacher's weights and of their terms of the
-  // loss
-  x[0] = far ? sum : sum * ex2(seen.k - K);
-  x[1] = x[2] = x[3] = 0.f;
-  for (int j = tid; j < p.k; j += THREADS) {
-    if (en.at[j] < 0) continue;
+  // the warp's part in its own frame, then everybody's
+  Known all_of;
+  float m = seen.m;
+  for (int j = tid; j < p.k; j += THREADS)
+    if (en.at[j] >= 0) m = fmaxf(m, en.z[j]);
+  all_of.m = warp_max(m);
+  const float kw = all_of.m * p.scale, norm = tail ? lse : tmax;
+  float sums[4] = {(seen.sum.x + seen.sum.y) * ex2(seen.k - kw), 0.f, 0.f, 0.f};
+  const auto entry = [&](int j, float y) {   // what entry j adds, its exponent being y
     bool first = true;
     if (twice)
       for (int e = 0; e < j; ++e) first &= en.at[e] != en.at[j];
-    const float y = exponent(en.z[j]);
-    if (tail && first) x[1] += ex2(y);
+    if (tail && first) sums[1] += ex2(y);
     const float lp = en.t[j] - norm, pj = expf(lp);
-    x[2] += pj;
-    if (pj > 0.f) x[3] += pj * (lp - kLn2 * y);
+    sums[2] += pj;
+    if (pj > 0.f) sums[3] += pj * (lp - kLn2 * y);
+  };
+  for (int j = tid; j < p.k; j += THREADS)
+    if (en.at[j] >= 0) entry(j, fmaf(en.z[j], p.scale, -kw));
+  const auto gather = [&]() {
+    all_of.sum = warp_sum(sums[0]);
+    all_of.top = warp_sum(sums[1]);
+    all_of.mass = warp_sum(sums[2]);
+    all_of.terms = warp_sum(sums[3]);
+    const int lane = tid & 31;
+    if (CLUSTER) {
+      if (lane < ranks) *cg::this_cluster().map_shared_rank(share + rank * W + warp, lane) = all_of;
+      cluster_arrive(true);
+      cluster_wait();
+    } else if (W > 1) {
+      if (lane == 0) share[warp] = all_of;
+      __syncthreads();
+    }
+    if (CLUSTER || W > 1) all_of = joined<kParts>(share, W * ranks, p.scale);
+  };
+  gather();
+  float M = all_of.m;
+  const bool far = !(fabsf(M) < kFar);
+  const auto exponent = [&](float v) { return far ? (v - M) * p.scale : fmaf(v, p.scale, -(M * p.scale)); };
+  if (far) {   // logits beyond +-kFar only (or infinite, or NaN): once more, element by element
+    float top = -INFINITY;
+    const int64_t s1 = min((int64_t)slot1, p.v + part.pad);
+    for (int64_t s = max((int64_t)slot0, (int64_t)part.pad) + tid; s < s1; s += THREADS) top = fmaxf(top, widen(z[s - part.pad]));
+    top = warp_max(top);
+    if ((tid & 31) == 0) far_red[warp] = top;
+    __syncthreads();
+    for (int i = 0; i < W; ++i) top = fmaxf(top, far_red[i]);
+    if (CLUSTER) {
+      if (tid < ranks) *cg::this_cluster().map_shared_rank(far_share + rank, tid) = top;
+      cluster_arrive(tid < 32);
+      cluster_wait();
+      for (int r = 0; r < ranks; ++r) top = fmaxf(top, far_share[r]);
+    }
+    M = top == -INFINITY ? 0.f : top;
+    sums[0] = sums[1] = sums[2] = sums[3] = 0.f;
+    for (int64_t s = max((int64_t)slot0, (int64_t)part.pad) + tid; s < s1; s += THREADS)
+      if (counts(s)) sums[0] += ex2(exponent(widen(z[s - part.pad])));
+    for (int j = tid; j < p.k; j += THREADS)
+      if (en.at[j] >= 0) entry(j, exponent(en.z[j]));
+    all_of.m = 0.f;   // one frame for all
+    if (CLUSTER) {    // everybody has read the first parts
+      cluster_arrive(false);
+      cluster_wait();
+    } else {
+      __syncthreads();
+    }
+    gather();
   }
-  over_row<4, false, W, CLUSTER>(x, red[2], share[2], rank, ranks);
-  const float out = x[0], total = x[0] + x[1];
-  const float mass = tail ? 1.f : x[2];   // what the teacher's weights are divided by
-  const float rest = tail ? fmaxf(0.f, 1.f - x[2]) : 0.f;
+  const float out = all_of.sum, total = all_of.sum + all_of.top;
+  const float mass = tail ? 1.f : all_of.mass;   // what the teacher's weights are divided by
+  const float rest = tail ? fmaxf(0.f, 1.f - all_of.mass) : 0.f;
   if (tid == 0 && rank == 0 && p.loss) {
-    float l = tail ? x[3] + x[2] * logf(total) : x[3] / mass - logf(mass) + logf(total);
+    float l = tail ? all_of.terms + all_of.mass * logf(total) : all_of.terms / mass - logf(mass) + logf(total);
     if (rest > 0.f) l += rest * logf(rest / (out / total));
     if (total == 0.f) l = INFINITY;
     p.loss[row] = w * l;
   }
-  if (dz) {
-    // pass 2
-    const float scale = w / p.temperature;
-    const float inside = total == 0.f ? 0.f : scale / total;
-    const float outside = rest > 0.f && out > 0.f ? inside - scale * (rest / out) : inside;
-    if (together && !far) {
-      const Val<2> shift = all<2>(-K), by = all<2>(p.scale), factor = all<2>(outside);
-      const auto turn = [&](Vec<TZ> v) {
+  if (!dz) return;
+  // pass 2
+  const float scale = w / p.temperature;
+  const float inside = total == 0.f ? 0.f : scale / total;
+  const float outside = rest > 0.f && out > 0.f ? inside - scale * (rest / out) : inside;
+  if (together && !far) {
+    const Val<2> shift = all<2>(-(M * p.scale)), by = all<2>(p.scale), factor = all<2>(outside);
+    const auto turn = [&](Vec<TZ> v) {
 #pragma unroll
-        for (int i = 0; i < P; ++i) {
-          Val<2> y = fma(pair(v, i), by, shift);
-          y.x = ex2(y.x);
-          y.y = ex2(y.y);
-          set_pair(v, i, mul(y, factor));
-        }
-        return v.w;
-      };
-      for (base = 0; base + hop <= count; base += hop) {
-        Vec<TZ> a[kDeep];
+      for (int i = 0; i < P; ++i) {
+        Val<2> y = fma(pair(v, i), by, shift);
+        y.x = ex2(y.x);
+        y.y = ex2(y.y);
+        set_pair(v, i, mul(y, factor));
+      }
+      return v.w;
+    };
+    for (int base = 0; base < count; base += hop) {
+      Vec<TZ> a[kDeep];
+      if (base + hop <= count) {
 #pragma unroll
         for (int u = 0; u < kDeep; ++u) a[u].w = src[base + u * THREADS];
 #pragma unroll
         for (int u = 0; u < kDeep; ++u) __stcs(dst + base + u * THREADS, turn(a[u]));
+      } else {
+        const int left = count - base - tid;
+#pragma unroll
+        for (int u = 0; u < kDeep; ++u)
+          if (u * THREADS < left) a[u].w = src[base + u * THREADS];
+#pragma unroll
+        for (int u = 0; u < kDeep; ++u)
+          if (u * THREADS < left) __stcs(dst + base + u * THREADS, turn(a[u]));
       }
-      for (int j = base; j < count - tid; j += THREADS) {
-        Vec<TZ> a;
-        a.w = src[j];
-        __stcs(dst + j, turn(a));
-      }
-      if (part.edge >= 0) narrow(dz + part.edge - part.pad, ex2(exponent(edge)) * outside);
-    } else {   // element by element, from memory (where dz is z, each thread reads what it writes over)
-      const int64_t s1 = min(slot1, p.v + part.pad);
-      for (int64_t s = max(slot0, (int64_t)part.pad) + tid; s < s1; s += THREADS)
-        narrow(dz + s - part.pad, ex2(exponent(widen(z[s - part.pad]))) * outside);
     }
-    __syncthreads();
-    for (int j = tid; j < p.k; j += THREADS) {
-      if (en.at[j] < 0) continue;
-      float pc = expf(en.t[j] - norm);
-      bool first = true;
-      if (twice) {   // an entry listed twice counts with both weights, in the order of the list
-        pc = 0.f;
-        for (int e = 0; e < p.k; ++e)
-          if (en.at[e] == en.at[j]) {
-            first &= e >= j;
-            pc += expf(en.t[e] - norm);
-          }
-      }
-      if (first) narrow(dz + en.at[j], ex2(exponent(en.z[j])) * inside - scale * (pc / mass));
+    if (part.edge >= 0) narrow(dz + part.edge - part.pad, ex2(exponent(edge)) * outside);
+  } else {   // element by element, from memory (where dz is z, each thread reads what it writes over)
+    const int64_t s1 = min((int64_t)slot1, p.v + part.pad);
+    for (int64_t s = max((int64_t)slot0, (int64_t)part.pad) + tid; s < s1; s += THREADS)
+      narrow(dz + s - part.pad, ex2(exponent(widen(z[s - part.pad]))) * outside);
+  }
+  __syncthreads();
+  for (int j = tid; j < p.k; j += THREADS) {
+    if (en.at[j] < 0) continue;
+    float pc = expf(en.t[j] - norm);
+    bool first = true;
+    if (twice) {   // an entry listed twice counts with both weights, in the order of the list
+      pc = 0.f;
+      for (int e = 0; e < p.k; ++e)
+        if (en.at[e] == en.at[j]) {
+          first &= e >= j;
+          pc += expf(en.t[e] - norm);
+        }
     }
+    if (first) narrow(dz + en.at[j], ex2(exponent(en.z[j])) * inside - scale * (pc / mass));
   }
 }
 
