@@ -530,7 +530,7 @@ template <typename TZ> cudaError_t launch_rows(DistillArgs p, int64_t r, cudaStr
   if (p.cluster > 1) return launch<TZ, 128, true, true>(p, r, s);
   // few vectors a thread for short rows, so that many of them are at work on an SM
   if (per <= 8 * 32) return launch<TZ, 32, false, true>(p, r, s);
-  return per <= 8 * 64 ? launch<TZ, 64, false, true>(p, r, s) : launch<TZ, 128, false, true>(p, r, s);
+  return per <= 16 * 64 ? launch<TZ, 64, false, true>(p, r, s) : launch<TZ, 128, false, true>(p, r, s);
 }
 
 ceca_status_t distill(const void *z, const void *idx, const void *t, const float *teacher_lse, const float *weight,

@@ -4,11 +4,15 @@
 //
 // Both directions move rows and do one multiplication or addition per element, so bytes bound them.  The
 // gradient lists every table row's positions in ascending order (token_list_kernel), then each row of dE is
-// summed over its list and written once (embed_grad_kernel): no atomics on values, one order of additions.
+// summed over its list and written once (embed_grad_kernel).  A list longer than kChunk is cut: another kernel sums the
+// pieces of it that lie in each kChunk places of the list, and the row is their sum.  No atomics on values, one order of
+// additions.
 #include <cuda_runtime.h>
 
 #include <algorithm>
+#include <atomic>
 #include <cstdint>
+#include <type_traits>
 
 #include "ceca.h"
 #include "tma.h"
@@ -28,26 +32,75 @@ struct EmbedArgs {
   int32_t accumulate;
   int32_t *row_start;  // n x (v + 1): where each table row's positions begin in `list`
   int32_t *list;       // n x t: positions, by token and then ascending
+  float *pieces;       // n x chunks x 2 x d: sums of the pieces of long lists
   int32_t bins;        // table rows per block of token_list_kernel
+  int32_t chunks;      // kChunk places each, of an agent's list; 0 when no list can be long
+  int32_t slices;      // of a row
 };
 
-constexpr int kLookupThreads = 256;
+constexpr int kThreads = 256, kWarps = kThreads / 32;
+constexpr int kChunk = 32;     // a list up to here is one warp's work
+constexpr int kGroup = 4;      // table rows that a warp of embed_grad_kernel takes together
+constexpr int kLookupPacks = 4;
+constexpr int kDeep = 4;       // rows of dout that a warp has on their way at a time
 constexpr int kListThreads = 512;
 constexpr int kListWarps = kListThreads / 32;
 constexpr int kMaxBins = 2048;
 
-template <typename TE, typename TO, typename TI>
-__global__ void __launch_bounds__(kLookupThreads) embed_lookup_kernel(const EmbedArgs p) {
+// V adjacent elements, moved at once: V * sizeof(T) is 16 bytes for the wider of a call's two types (V = 1: rows on any
+// boundary).
+template <typename T, int V> struct alignas(V * sizeof(T)) Pack {
+  T e[V];
+};
+template <typename T, int V> __device__ __forceinline__ void add_to(float *acc, const Pack<T, V> &v) {
+#pragma unroll
+  for (int i = 0; i < V; ++i) acc[i] += widen(v.e[i]);
+}
+template <typename T, int V> __device__ __forceinline__ void put(T *p, const float *x) {
+  Pack<T, V> v;
+#pragma unroll
+  for (int i = 0; i < V; ++i) narrow(&v.e[i], x[i]);
+  *reinterpret_cast<Pack<T, V> *>(p) = v;
+}
+template <typename T, int V> __device__ __forceinline__ Pack<T, V> get(const T *p) { return *reinterpret_cast<const Pack<T, V> *>(p); }
+// A warp works on a slice of a row at a time: U packs of a lane, 32 V elements apart.
+template <int V> struct Slice {
+  static constexpr int U = V == 8 ? 2 : V == 4 ? 4 : 8, kElements = 32 * U * V;
+};
+
+template <typename TE, typename TO, typename TI, int V>
+__global__ void __launch_bounds__(kThreads) embed_lookup_kernel(const EmbedArgs p) {
+  constexpr int U = kLookupPacks;
   const int lane = threadIdx.x & 31;
-  const int64_t rows = (int64_t)p.n * p.t;
-  const int64_t step = (int64_t)gridDim.x * (kLookupThreads / 32);
-  for (int64_t row = (int64_t)blockIdx.x * (kLookupThreads / 32) + (threadIdx.x >> 5); row < rows; row += step) {
-    const int64_t i = row / p.t, s = row - i * p.t;
-    const int64_t tok = static_cast<const TI *>(p.tokens)[i * p.tokens_agent + s];
-    TO *o = static_cast<TO *>(p.dst) + i * p.out_agent + s * p.out_row;
+  const int64_t units = (int64_t)p.n * p.t * p.slices, step = (int64_t)gridDim.x * kWarps;
+  const auto token = [&](int64_t unit) -> int64_t {   // of the unit's position
+    const int64_t row = p.slices == 1 ? unit : unit / p.slices, i = row / p.t;
+    return static_cast<const TI *>(p.tokens)[i * p.tokens_agent + (row - i * p.t)];
+  };
+  int64_t unit = (int64_t)blockIdx.x * kWarps + (threadIdx.x >> 5);
+  int64_t tok = unit < units ? token(unit) : 0;
+  for (; unit < units; unit += step) {
+    const int64_t coming = unit + step < units ? token(unit + step) : 0;   // on its way before the rows are
+    const int64_t row = p.slices == 1 ? unit : unit / p.slices, i = row / p.t;
+    const int64_t c0 = (unit - row * p.slices) * (32 * U * V) + lane * V;
     const bool some = tok >= 0 && tok < p.v;
-    const TE *e = static_cast<const TE *>(p.src) + i * p.table_agent + (some ? tok : 0) * p.table_row;
-    for (int64_t c = lane; c < p.d; c += 32) narrow(o + c, some ? p.scale * widen(e[c]) : 0.f);
+    const TE *e = static_cast<const TE *>(p.src) + i * p.table_agent + (some ? tok : 0) * p.table_row + c0;
+    TO *o = static_cast<TO *>(p.dst) + i * p.out_agent + (row - i * p.t) * p.out_row + c0;
+    Pack<TE, V> v[U];
+    if (some) {
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        if (c0 + u * 32 * V < p.d) v[u] = get<TE, V>(e + u * 32 * V);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (c0 + u * 32 * V < p.d) {
+        float x[V];
+#pragma unroll
+        for (int k = 0; k < V; ++k) x[k] = some ? p.scale * widen(v[u].e[k]) : 0.f;
+        put<TO, V>(o + u * 32 * V, x);
+      }
+    tok = coming;
   }
 }
 
@@ -72,6 +125,7 @@ __global__ void __launch_bounds__(kListThreads) token_list_kernel(const EmbedArg
   if (threadIdx.x == 0) below_all = 0;
   __syncthreads();
   int32_t below = 0;
+#pragma unroll 4
   for (int64_t s = s0 + lane; s < s1; s += 32) {
     const int64_t w = tok[s];
     below += w >= 0 && w < lo;
@@ -114,8 +168,10 @@ __global__ void __launch_bounds__(kListThreads) token_list_kernel(const EmbedArg
   __syncthreads();
 
   int32_t *list = p.list + i * p.t;
+  int64_t coming = s0 + lane < s1 ? (int64_t)tok[s0 + lane] : -1;
   for (int64_t s = s0; s < s1; s += 32) {
-    const int64_t w = s + lane < s1 ? (int64_t)tok[s + lane] : -1;
+    const int64_t w = coming;
+    coming = s + 32 + lane < s1 ? (int64_t)tok[s + 32 + lane] : -1;
     const bool in = w >= lo && w < lo + bins;
     const uint32_t some = __ballot_sync(0xffffffffu, in);
     if (in) {
@@ -130,26 +186,168 @@ __global__ void __launch_bounds__(kListThreads) token_list_kernel(const EmbedArg
   }
 }
 
-template <typename TE, typename TO>
-__global__ void __launch_bounds__(kLookupThreads) embed_grad_kernel(const EmbedArgs p) {
-  const int lane = threadIdx.x & 31;
-  const int64_t rows = (int64_t)p.n * p.v;
-  const int64_t step = (int64_t)gridDim.x * (kLookupThreads / 32);
-  for (int64_t row = (int64_t)blockIdx.x * (kLookupThreads / 32) + (threadIdx.x >> 5); row < rows; row += step) {
-    const int64_t i = row / p.v, w = row - i * p.v;
-    const int32_t *start = p.row_start + i * (p.v + 1) + w;
-    const int32_t b = start[0], e = start[1];
-    if (p.accumulate && b == e) continue;
-    const int32_t *list = p.list + i * p.t;
-    const TO *o = static_cast<const TO *>(p.src) + i * p.out_agent;
-    TE *g = static_cast<TE *>(p.dst) + i * p.table_agent + w * p.table_row;
-    for (int64_t c = lane; c < p.d; c += 32) {
-      float acc = 0.f;
-      for (int32_t j = b; j < e; ++j) acc += widen(o[list[j] * p.out_row + c]);
-      acc *= p.scale;
-      if (p.accumulate) acc += widen(g[c]);
-      narrow(g + c, acc);
+// Sum over a part of a list, or of the pieces, by the warps of a CTA in turn; every warp ends up with its own packs of it
+// in `acc` of warp 0.  `load(j, c)` adds entry j's packs.
+template <int V, typename Add> __device__ __forceinline__ void sum_by_warps(float (*acc)[V], int count, float (*shared)[Slice<V>::kElements], Add add) {
+  constexpr int U = Slice<V>::U;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int per = (count + kWarps - 1) / kWarps, from = min(count, warp * per), to = min(count, from + per);
+#pragma unroll
+  for (int u = 0; u < U; ++u)
+#pragma unroll
+    for (int k = 0; k < V; ++k) acc[u][k] = 0.f;
+#pragma unroll 4
+  for (int j = from; j < to; ++j) add(j);
+  __syncthreads();   // the last sum has been read
+#pragma unroll
+  for (int u = 0; u < U; ++u)
+#pragma unroll
+    for (int k = 0; k < V; ++k) shared[warp][(u * V + k) * 32 + lane] = acc[u][k];
+  __syncthreads();
+  if (warp == 0)
+    for (int w = 1; w < kWarps; ++w)
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int k = 0; k < V; ++k) acc[u][k] += shared[w][(u * V + k) * 32 + lane];
+}
+
+// The places [j kChunk, (j + 1) kChunk) of agent i's list: a long list of a token begins, ends or goes through there, so it
+// holds the first place or the last.
+struct Chunk {
+  int32_t from, to;          // the places
+  int32_t first, last;       // the tokens at the first and the last of them
+};
+template <typename TI> __device__ __forceinline__ Chunk chunk_of(const EmbedArgs &p, int64_t i, int j) {
+  const int32_t *start = p.row_start + i * (p.v + 1), *list = p.list + i * p.t;
+  const TI *tok = static_cast<const TI *>(p.tokens) + i * p.tokens_agent;
+  Chunk c;
+  c.from = j * kChunk;
+  c.to = (int32_t)min((int64_t)c.from + kChunk, (int64_t)start[p.v]);
+  c.first = c.last = -1;
+  if (c.from < c.to) {
+    c.first = (int32_t)tok[list[c.from]];
+    c.last = (int32_t)tok[list[c.to - 1]];
+  }
+  return c;
+}
+
+// Block (j, slice, i): the pieces of long lists in chunk j, [0] of the token at its first place and [1] of another one at its
+// last.
+template <typename TO, typename TI, int V> __global__ void __launch_bounds__(kThreads) embed_pieces_kernel(const EmbedArgs p) {
+  constexpr int U = Slice<V>::U;
+  __shared__ float shared[kWarps][Slice<V>::kElements];
+  const int64_t i = blockIdx.z;
+  const int j = blockIdx.x;
+  const Chunk c = chunk_of<TI>(p, i, j);
+  const int32_t *start = p.row_start + i * (p.v + 1), *list = p.list + i * p.t;
+  const int64_t c0 = (int64_t)blockIdx.y * Slice<V>::kElements + (threadIdx.x & 31) * V;
+  const TO *o = static_cast<const TO *>(p.src) + i * p.out_agent + c0;
+  for (int piece = 0; piece < 2; ++piece) {
+    const int32_t w = piece ? c.last : c.first;
+    if (w < 0 || (piece && c.last == c.first)) return;
+    const int32_t b = start[w], e = start[w + 1];
+    if (e - b <= kChunk) continue;
+    const int32_t from = max(b, c.from), to = min(e, c.to);
+    float acc[U][V];
+    sum_by_warps<V>(acc, to - from, shared, [&](int k) {
+      const TO *r = o + list[from + k] * p.out_row;
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        if (c0 + u * 32 * V < p.d) add_to(acc[u], get<TO, V>(r + u * 32 * V));
+    });
+    if (threadIdx.x < 32) {
+      float *out = p.pieces + ((i * p.chunks + j) * 2 + piece) * p.d + c0;
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int k = 0; k < V; ++k)
+          if (c0 + u * 32 * V < p.d) out[u * 32 * V + k] = acc[u][k];
     }
+  }
+}
+
+// The slice's packs of a finished row.
+template <typename TE, int V> __device__ __forceinline__ void finish_row(const EmbedArgs &p, TE *g, int64_t c0, float (*acc)[V]) {
+#pragma unroll
+  for (int u = 0; u < Slice<V>::U; ++u)
+    if (c0 + u * 32 * V < p.d) {
+      float x[V];
+#pragma unroll
+      for (int k = 0; k < V; ++k) x[k] = acc[u][k] * p.scale;
+      if (p.accumulate) add_to(x, get<TE, V>(g + u * 32 * V));
+      put<TE, V>(g + u * 32 * V, x);
+    }
+}
+
+// Blocks (x, slice, agent).  The first p.chunks of x: the row whose long list begins in chunk x, the sum of its pieces.  The
+// others: kGroup rows for each warp, whose lists lie one behind the other.
+template <typename TE, typename TO, typename TI, int V>
+__global__ void __launch_bounds__(kThreads) embed_grad_kernel(const EmbedArgs p) {
+  constexpr int U = Slice<V>::U;
+  const int lane = threadIdx.x & 31;
+  const int64_t i = blockIdx.z;
+  const int64_t c0 = (int64_t)blockIdx.y * Slice<V>::kElements + lane * V;
+  const int32_t *start = p.row_start + i * (p.v + 1), *list = p.list + i * p.t;
+  TE *table = static_cast<TE *>(p.dst) + i * p.table_agent + c0;
+  float acc[U][V];
+  if ((int)blockIdx.x < p.chunks) {
+    __shared__ float shared[kWarps][Slice<V>::kElements];
+    const int j = blockIdx.x;
+    const int32_t w = chunk_of<TI>(p, i, j).last;
+    if (w < 0) return;
+    const int32_t b = start[w], e = start[w + 1];
+    if (e - b <= kChunk || b < j * kChunk) return;
+    const int count = (e - 1) / kChunk - j + 1, piece0 = b > j * kChunk;
+    const float *pieces = p.pieces + (i * p.chunks + j) * 2 * p.d + c0;
+    sum_by_warps<V>(acc, count, shared, [&](int k) {
+      const float *r = pieces + (2 * (int64_t)k + (k == 0 ? piece0 : 0)) * p.d;
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int q = 0; q < V; ++q)
+          if (c0 + u * 32 * V < p.d) acc[u][q] += r[u * 32 * V + q];
+    });
+    if (threadIdx.x < 32) finish_row<TE, V>(p, table + w * p.table_row, c0, acc);
+    return;
+  }
+  const int64_t r0 = ((int64_t)(blockIdx.x - p.chunks) * kWarps + (threadIdx.x >> 5)) * kGroup;
+  if (r0 >= p.v) return;
+  const int rows = (int)min((int64_t)kGroup, p.v - r0);
+  const int32_t begin = start[r0 + min(lane, rows)];
+  const int32_t first = __shfl_sync(0xffffffffu, begin, 0), end = __shfl_sync(0xffffffffu, begin, rows);
+  int32_t window = first;   // places [window, window + 32) are in `place`
+  int32_t place = first + lane < end ? list[first + lane] : 0;
+  const TO *o = static_cast<const TO *>(p.src) + i * p.out_agent + c0;
+  for (int g = 0; g < rows; ++g) {
+    const int32_t b = __shfl_sync(0xffffffffu, begin, g), e = __shfl_sync(0xffffffffu, begin, g + 1);
+    if (e - b > kChunk || (p.accumulate && b == e)) continue;
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int k = 0; k < V; ++k) acc[u][k] = 0.f;
+    for (int32_t j = b; j < e; j += kDeep) {
+      if (j + kDeep > window + 32) {
+        window = j;
+        place = window + lane < end ? list[window + lane] : 0;
+      }
+      Pack<TO, V> v[kDeep][U];
+#pragma unroll
+      for (int q = 0; q < kDeep; ++q) {
+        const TO *r = o + __shfl_sync(0xffffffffu, place, (j + q - window) & 31) * p.out_row;
+        if (j + q < e)
+#pragma unroll
+          for (int u = 0; u < U; ++u)
+            if (c0 + u * 32 * V < p.d) v[q][u] = get<TO, V>(r + u * 32 * V);
+      }
+#pragma unroll
+      for (int q = 0; q < kDeep; ++q)
+        if (j + q < e)
+#pragma unroll
+          for (int u = 0; u < U; ++u)
+            if (c0 + u * 32 * V < p.d) add_to(acc[u], v[q][u]);
+    }
+    finish_row<TE, V>(p, table + (r0 + g) * p.table_row, c0, acc);
   }
 }
 
@@ -159,6 +357,8 @@ int32_t list_bins(int32_t n, int64_t v) {
   const int64_t blocks = std::max<int64_t>(ceil_div(v, kMaxBins), ceil_div(2 * 148, n));
   return (int32_t)std::max<int64_t>(1, ceil_div(v, blocks));
 }
+
+int64_t chunks_of(int64_t t) { return t > kChunk ? ceil_div(t, kChunk) : 0; }
 
 size_t round16(size_t bytes) { return (bytes + 15) / 16 * 16; }
 
@@ -170,18 +370,48 @@ bool embed_args_ok(int32_t n, int64_t t, int64_t v, int64_t d, int64_t table_age
          is_type(table_type) && is_index(tokens_type) && is_type(out_type);
 }
 
-int grid_of(int64_t rows) {
-  return (int)std::min<int64_t>(ceil_div(rows, kLookupThreads / 32), (int64_t)sm_count() * 8);
+// Elements of a pack: both tensors' packs must lie on a boundary of their own size.
+int pack_of(const EmbedArgs &p, const void *table, int64_t te, const void *out, int64_t to) {
+  const int v = te == 2 && to == 2 ? 8 : 4;
+  const auto fits = [&](const void *base, int64_t agent, int64_t row, int64_t size) {
+    return (uintptr_t)base % (v * size) == 0 && (p.n == 1 || agent % v == 0) && row % v == 0;
+  };
+  return p.d % v == 0 && fits(table, p.table_agent, p.table_row, te) && fits(out, p.out_agent, p.out_row, to) ? v : 1;
 }
 
-template <typename TE, typename TO> void launch_lookup(const EmbedArgs &p, bool i64, cudaStream_t s) {
-  const int g = grid_of((int64_t)p.n * p.t);
-  if (i64) embed_lookup_kernel<TE, TO, int64_t><<<g, kLookupThreads, 0, s>>>(p);
-  else embed_lookup_kernel<TE, TO, int32_t><<<g, kLookupThreads, 0, s>>>(p);
+template <typename TE, typename TO, typename TI, int V> cudaError_t launch_lookup(EmbedArgs p, cudaStream_t s) {
+  p.slices = (int32_t)ceil_div(p.d, 32 * kLookupPacks * V);
+  const int64_t units = (int64_t)p.n * p.t * p.slices;
+  const int grid = (int)std::min<int64_t>(ceil_div(units, kWarps), (int64_t)sm_count() * 8);
+  embed_lookup_kernel<TE, TO, TI, V><<<grid, kThreads, 0, s>>>(p);
+  return cudaGetLastError();
 }
 
-template <typename TE, typename TO> void launch_grad(const EmbedArgs &p, cudaStream_t s) {
-  embed_grad_kernel<TE, TO><<<grid_of((int64_t)p.n * p.v), kLookupThreads, 0, s>>>(p);
+template <typename TE, typename TO, typename TI, int V> cudaError_t launch_grad(EmbedArgs p, cudaStream_t s) {
+  p.slices = (int32_t)ceil_div(p.d, Slice<V>::kElements);
+  if (p.slices > 65535) return cudaErrorInvalidValue;
+  if (p.chunks > 0) {
+    embed_pieces_kernel<TO, TI, V><<<dim3(p.chunks, p.slices, p.n), kThreads, 0, s>>>(p);
+    const cudaError_t e = cudaGetLastError();
+    if (e != cudaSuccess) return e;
+  }
+  const int64_t blocks = p.chunks + ceil_div(p.v, kWarps * kGroup);
+  embed_grad_kernel<TE, TO, TI, V><<<dim3((unsigned)blocks, p.slices, p.n), kThreads, 0, s>>>(p);
+  return cudaGetLastError();
+}
+
+// Calls go(TE, TO, TI, V) for the types of a call.
+template <typename TE, typename TO, typename Go> cudaError_t with_index(bool i64, int pack, Go go) {
+  constexpr int V = sizeof(TE) == 2 && sizeof(TO) == 2 ? 8 : 4;
+  if (i64) return pack == 1 ? go(TE(), TO(), int64_t(), std::integral_constant<int, 1>()) : go(TE(), TO(), int64_t(), std::integral_constant<int, V>());
+  return pack == 1 ? go(TE(), TO(), int32_t(), std::integral_constant<int, 1>()) : go(TE(), TO(), int32_t(), std::integral_constant<int, V>());
+}
+template <typename Go> ceca_status_t with_types(int32_t te, int32_t to, int32_t ti, int pack, Go go) {
+  const bool i64 = ti == DSGD_I64;
+  cudaError_t e;
+  if (te == DSGD_F32) e = to == DSGD_F32 ? with_index<float, float>(i64, pack, go) : with_index<float, bf16>(i64, pack, go);
+  else e = to == DSGD_F32 ? with_index<bf16, float>(i64, pack, go) : with_index<bf16, bf16>(i64, pack, go);
+  return e == cudaSuccess ? CECA_OK : CECA_ERR_CUDA;
 }
 
 template <typename TI> cudaError_t launch_list(const EmbedArgs &p, cudaStream_t s) {
@@ -216,20 +446,16 @@ extern "C" ceca_status_t dsgd_embed_lookup(const void *E, const void *tokens, vo
   p.table_agent = agent_stride; p.table_row = row_stride; p.tokens_agent = tokens_stride;
   p.out_agent = out_agent_stride; p.out_row = out_row_stride; p.scale = scale;
   const cudaStream_t s = static_cast<cudaStream_t>(stream);
-  const bool i64 = tokens_type == DSGD_I64;
-  if (table_type == DSGD_F32) {
-    if (out_type == DSGD_F32) launch_lookup<float, float>(p, i64, s);
-    else launch_lookup<float, bf16>(p, i64, s);
-  } else {
-    if (out_type == DSGD_F32) launch_lookup<bf16, float>(p, i64, s);
-    else launch_lookup<bf16, bf16>(p, i64, s);
-  }
-  return cudaGetLastError() == cudaSuccess ? CECA_OK : CECA_ERR_CUDA;
+  const int pack = pack_of(p, E, type_bytes(table_type), out, type_bytes(out_type));
+  return with_types(table_type, out_type, tokens_type, pack, [&](auto te, auto to, auto ti, auto v) {
+    return launch_lookup<decltype(te), decltype(to), decltype(ti), v.value>(p, s);
+  });
 }
 
 extern "C" size_t dsgd_embed_workspace_bytes(int32_t n, int64_t t, int64_t v, int64_t d) {
   if (!embed_args_ok(n, t, v, d, 0, d, 0, 0, d, DSGD_F32, DSGD_I32, DSGD_F32)) return 0;
-  return round16(sizeof(int32_t) * (size_t)n * (size_t)(v + 1)) + round16(sizeof(int32_t) * (size_t)n * (size_t)t);
+  return round16(sizeof(int32_t) * (size_t)n * (size_t)(v + 1)) + round16(sizeof(int32_t) * (size_t)n * (size_t)t) +
+         sizeof(float) * 2 * (size_t)n * (size_t)chunks_of(t) * (size_t)d;
 }
 
 extern "C" ceca_status_t dsgd_embed_grad(const void *dout, const void *tokens, void *dE, int32_t n, int64_t t,
@@ -250,16 +476,14 @@ extern "C" ceca_status_t dsgd_embed_grad(const void *dout, const void *tokens, v
   p.out_agent = out_agent_stride; p.out_row = out_row_stride; p.scale = scale; p.accumulate = accumulate != 0;
   p.row_start = static_cast<int32_t *>(workspace);
   p.list = reinterpret_cast<int32_t *>(static_cast<char *>(workspace) + round16(sizeof(int32_t) * (size_t)n * (size_t)(v + 1)));
+  p.pieces = reinterpret_cast<float *>(reinterpret_cast<char *>(p.list) + round16(sizeof(int32_t) * (size_t)n * (size_t)t));
   p.bins = list_bins(n, v);
+  p.chunks = (int32_t)chunks_of(t);
   const cudaStream_t s = static_cast<cudaStream_t>(stream);
   if ((tokens_type == DSGD_I64 ? launch_list<int64_t>(p, s) : launch_list<int32_t>(p, s)) != cudaSuccess)
     return CECA_ERR_CUDA;
-  if (table_type == DSGD_F32) {
-    if (out_type == DSGD_F32) launch_grad<float, float>(p, s);
-    else launch_grad<float, bf16>(p, s);
-  } else {
-    if (out_type == DSGD_F32) launch_grad<bf16, float>(p, s);
-    else launch_grad<bf16, bf16>(p, s);
-  }
-  return cudaGetLastError() == cudaSuccess ? CECA_OK : CECA_ERR_CUDA;
+  const int pack = pack_of(p, dE, type_bytes(table_type), dout, type_bytes(out_type));
+  return with_types(table_type, out_type, tokens_type, pack, [&](auto te, auto to, auto ti, auto v) {
+    return launch_grad<decltype(te), decltype(to), decltype(ti), v.value>(p, s);
+  });
 }
