@@ -3,10 +3,12 @@
 //   out[i, s, :] = scale E_i[tok[i, s], :]          dE_i[w, :] = scale sum_{s : tok[i, s] = w} dout[i, s, :]
 //
 // Both directions move rows and do one multiplication or addition per element, so bytes bound them.  The
-// gradient lists every table row's positions in ascending order (token_list_kernel), then each row of dE is
-// summed over its list and written once (embed_grad_kernel).  A list longer than kChunk is cut: another kernel sums the
-// pieces of it that lie in each kChunk places of the list, and the row is their sum.  No atomics on values, one order of
-// additions.
+// gradient runs in three launches without atomics on values, in one order of additions:
+//   token_list_kernel   lists every table row's positions in ascending order, by token;
+//   embed_grad_kernel   cuts the list into chunks of kChunk places.  A warp takes the rows that begin in its chunk, or,
+//                       of a row with more than kChunk positions, the piece that lies in it: however the tokens are
+//                       distributed, its work is the same.  Other CTAs fill the rows that no position holds;
+//   embed_join_kernel   adds up the pieces of the rows that have several.
 #include <cuda_runtime.h>
 
 #include <algorithm>
@@ -32,34 +34,68 @@ struct EmbedArgs {
   int32_t accumulate;
   int32_t *row_start;  // n x (v + 1): where each table row's positions begin in `list`
   int32_t *list;       // n x t: positions, by token and then ascending
+  int32_t *owner;      // n x t: the token of each
   float *pieces;       // n x chunks x 2 x d: sums of the pieces of long lists
   int32_t bins;        // table rows per block of token_list_kernel
-  int32_t chunks;      // kChunk places each, of an agent's list; 0 when no list can be long
+  int32_t chunks;      // kChunk places each, of an agent's list
   int32_t slices;      // of a row
+  int32_t fills;       // CTAs that fill kFill rows each with zeros
 };
 
 constexpr int kThreads = 256, kWarps = kThreads / 32;
-constexpr int kChunk = 32;     // a list up to here is one warp's work
-constexpr int kGroup = 4;      // table rows that a warp of embed_grad_kernel takes together
+constexpr int kChunk = 32;
+constexpr int kFill = 64;      // table rows
 constexpr int kLookupPacks = 4;
 constexpr int kDeep = 4;       // rows of dout that a warp has on their way at a time
 constexpr int kListThreads = 512;
 constexpr int kListWarps = kListThreads / 32;
 constexpr int kMaxBins = 2048;
 
-// V adjacent elements, moved at once: V * sizeof(T) is 16 bytes for the wider of a call's two types (V = 1: rows on any
-// boundary).
-template <typename T, int V> struct alignas(V * sizeof(T)) Pack {
-  T e[V];
+// V adjacent elements, moved at once: V * sizeof(T) is 16 bytes for the narrower of a call's types, or 8 (V = 1: rows on
+// any boundary).
+template <typename T, int V> struct Pack;
+template <int V> struct alignas(V * 4) Pack<float, V> {
+  float e[V];
+  __device__ __forceinline__ void get(float *x) const {
+#pragma unroll
+    for (int i = 0; i < V; ++i) x[i] = e[i];
+  }
+  __device__ __forceinline__ void set(const float *x) {
+#pragma unroll
+    for (int i = 0; i < V; ++i) e[i] = x[i];
+  }
+};
+template <> struct Pack<bf16, 1> {
+  bf16 e;
+  __device__ __forceinline__ void get(float *x) const { *x = __bfloat162float(e); }
+  __device__ __forceinline__ void set(const float *x) { e = __float2bfloat16_rn(*x); }
+};
+template <int V> struct alignas(V * 2) Pack<bf16, V> {
+  uint32_t w[V / 2];
+  __device__ __forceinline__ void get(float *x) const {   // a bf16 is the upper half of the fp32 of the same value
+#pragma unroll
+    for (int i = 0; i < V / 2; ++i) {
+      x[2 * i] = __uint_as_float(w[i] << 16);
+      x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+    }
+  }
+  __device__ __forceinline__ void set(const float *x) {
+#pragma unroll
+    for (int i = 0; i < V / 2; ++i) {
+      const __nv_bfloat162 h = __floats2bfloat162_rn(x[2 * i], x[2 * i + 1]);
+      w[i] = *reinterpret_cast<const uint32_t *>(&h);
+    }
+  }
 };
 template <typename T, int V> __device__ __forceinline__ void add_to(float *acc, const Pack<T, V> &v) {
+  float x[V];
+  v.get(x);
 #pragma unroll
-  for (int i = 0; i < V; ++i) acc[i] += widen(v.e[i]);
+  for (int i = 0; i < V; ++i) acc[i] += x[i];
 }
 template <typename T, int V> __device__ __forceinline__ void put(T *p, const float *x) {
   Pack<T, V> v;
-#pragma unroll
-  for (int i = 0; i < V; ++i) narrow(&v.e[i], x[i]);
+  v.set(x);
   *reinterpret_cast<Pack<T, V> *>(p) = v;
 }
 template <typename T, int V> __device__ __forceinline__ Pack<T, V> get(const T *p) { return *reinterpret_cast<const Pack<T, V> *>(p); }
@@ -91,13 +127,21 @@ __global__ void __launch_bounds__(kThreads) embed_lookup_kernel(const EmbedArgs 
 #pragma unroll
       for (int u = 0; u < U; ++u)
         if (c0 + u * 32 * V < p.d) v[u] = get<TE, V>(e + u * 32 * V);
+    } else {
+      const float zero[V] = {};
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        if (c0 + u * 32 * V < p.d) put<TO, V>(o + u * 32 * V, zero);
+      tok = coming;
+      continue;
     }
 #pragma unroll
     for (int u = 0; u < U; ++u)
       if (c0 + u * 32 * V < p.d) {
         float x[V];
+        v[u].get(x);
 #pragma unroll
-        for (int k = 0; k < V; ++k) x[k] = some ? p.scale * widen(v[u].e[k]) : 0.f;
+        for (int k = 0; k < V; ++k) x[k] *= p.scale;
         put<TO, V>(o + u * 32 * V, x);
       }
     tok = coming;
@@ -125,7 +169,7 @@ __global__ void __launch_bounds__(kListThreads) token_list_kernel(const EmbedArg
   if (threadIdx.x == 0) below_all = 0;
   __syncthreads();
   int32_t below = 0;
-#pragma unroll 4
+#pragma unroll 8
   for (int64_t s = s0 + lane; s < s1; s += 32) {
     const int64_t w = tok[s];
     below += w >= 0 && w < lo;
@@ -167,22 +211,28 @@ __global__ void __launch_bounds__(kListThreads) token_list_kernel(const EmbedArg
   }
   __syncthreads();
 
-  int32_t *list = p.list + i * p.t;
-  int64_t coming = s0 + lane < s1 ? (int64_t)tok[s0 + lane] : -1;
-  for (int64_t s = s0; s < s1; s += 32) {
-    const int64_t w = coming;
-    coming = s + 32 + lane < s1 ? (int64_t)tok[s + 32 + lane] : -1;
-    const bool in = w >= lo && w < lo + bins;
-    const uint32_t some = __ballot_sync(0xffffffffu, in);
-    if (in) {
-      const int32_t r = (int32_t)(w - lo);
-      const uint32_t same = __match_any_sync(some, r);
-      const int32_t rank = __popc(same & ((1u << lane) - 1));
-      list[mine[r] + rank] = (int32_t)(s + lane);
-      __syncwarp(some);
-      if (rank == 0) mine[r] += __popc(same);
+  int32_t *list = p.list + i * p.t, *owner = p.owner + i * p.t;
+  constexpr int kAhead = 8;   // groups of 32 tokens on their way at a time
+  for (int64_t s = s0; s < s1; s += 32 * kAhead) {
+    int64_t w[kAhead];
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) w[k] = s + 32 * k + lane < s1 ? (int64_t)tok[s + 32 * k + lane] : -1;
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) {
+      const bool in = w[k] >= lo && w[k] < lo + bins;
+      const uint32_t some = __ballot_sync(0xffffffffu, in);
+      if (some == 0) continue;
+      if (in) {
+        const int32_t r = (int32_t)(w[k] - lo);
+        const uint32_t same = __match_any_sync(some, r);
+        const int32_t rank = __popc(same & ((1u << lane) - 1)), at = mine[r] + rank;
+        list[at] = (int32_t)(s + 32 * k + lane);
+        owner[at] = (int32_t)w[k];
+        __syncwarp(some);
+        if (rank == 0) mine[r] += __popc(same);
+      }
+      __syncwarp();
     }
-    __syncwarp();
   }
 }
 
@@ -212,61 +262,6 @@ template <int V, typename Add> __device__ __forceinline__ void sum_by_warps(floa
         for (int k = 0; k < V; ++k) acc[u][k] += shared[w][(u * V + k) * 32 + lane];
 }
 
-// The places [j kChunk, (j + 1) kChunk) of agent i's list: a long list of a token begins, ends or goes through there, so it
-// holds the first place or the last.
-struct Chunk {
-  int32_t from, to;          // the places
-  int32_t first, last;       // the tokens at the first and the last of them
-};
-template <typename TI> __device__ __forceinline__ Chunk chunk_of(const EmbedArgs &p, int64_t i, int j) {
-  const int32_t *start = p.row_start + i * (p.v + 1), *list = p.list + i * p.t;
-  const TI *tok = static_cast<const TI *>(p.tokens) + i * p.tokens_agent;
-  Chunk c;
-  c.from = j * kChunk;
-  c.to = (int32_t)min((int64_t)c.from + kChunk, (int64_t)start[p.v]);
-  c.first = c.last = -1;
-  if (c.from < c.to) {
-    c.first = (int32_t)tok[list[c.from]];
-    c.last = (int32_t)tok[list[c.to - 1]];
-  }
-  return c;
-}
-
-// Block (j, slice, i): the pieces of long lists in chunk j, [0] of the token at its first place and [1] of another one at its
-// last.
-template <typename TO, typename TI, int V> __global__ void __launch_bounds__(kThreads) embed_pieces_kernel(const EmbedArgs p) {
-  constexpr int U = Slice<V>::U;
-  __shared__ float shared[kWarps][Slice<V>::kElements];
-  const int64_t i = blockIdx.z;
-  const int j = blockIdx.x;
-  const Chunk c = chunk_of<TI>(p, i, j);
-  const int32_t *start = p.row_start + i * (p.v + 1), *list = p.list + i * p.t;
-  const int64_t c0 = (int64_t)blockIdx.y * Slice<V>::kElements + (threadIdx.x & 31) * V;
-  const TO *o = static_cast<const TO *>(p.src) + i * p.out_agent + c0;
-  for (int piece = 0; piece < 2; ++piece) {
-    const int32_t w = piece ? c.last : c.first;
-    if (w < 0 || (piece && c.last == c.first)) return;
-    const int32_t b = start[w], e = start[w + 1];
-    if (e - b <= kChunk) continue;
-    const int32_t from = max(b, c.from), to = min(e, c.to);
-    float acc[U][V];
-    sum_by_warps<V>(acc, to - from, shared, [&](int k) {
-      const TO *r = o + list[from + k] * p.out_row;
-#pragma unroll
-      for (int u = 0; u < U; ++u)
-        if (c0 + u * 32 * V < p.d) add_to(acc[u], get<TO, V>(r + u * 32 * V));
-    });
-    if (threadIdx.x < 32) {
-      float *out = p.pieces + ((i * p.chunks + j) * 2 + piece) * p.d + c0;
-#pragma unroll
-      for (int u = 0; u < U; ++u)
-#pragma unroll
-        for (int k = 0; k < V; ++k)
-          if (c0 + u * 32 * V < p.d) out[u * 32 * V + k] = acc[u][k];
-    }
-  }
-}
-
 // The slice's packs of a finished row.
 template <typename TE, int V> __device__ __forceinline__ void finish_row(const EmbedArgs &p, TE *g, int64_t c0, float (*acc)[V]) {
 #pragma unroll
@@ -280,75 +275,106 @@ template <typename TE, int V> __device__ __forceinline__ void finish_row(const E
     }
 }
 
-// Blocks (x, slice, agent).  The first p.chunks of x: the row whose long list begins in chunk x, the sum of its pieces.  The
-// others: kGroup rows for each warp, whose lists lie one behind the other.
-template <typename TE, typename TO, typename TI, int V>
-__global__ void __launch_bounds__(kThreads) embed_grad_kernel(const EmbedArgs p) {
+// Blocks (x, slice, agent): first a chunk for each warp, then kFill rows for each CTA.
+template <typename TE, typename TO, int V> __global__ void __launch_bounds__(kThreads, 2) embed_grad_kernel(const EmbedArgs p) {
   constexpr int U = Slice<V>::U;
-  const int lane = threadIdx.x & 31;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int64_t i = blockIdx.z;
   const int64_t c0 = (int64_t)blockIdx.y * Slice<V>::kElements + lane * V;
-  const int32_t *start = p.row_start + i * (p.v + 1), *list = p.list + i * p.t;
+  const int32_t *start = p.row_start + i * (p.v + 1), *list = p.list + i * p.t, *owner = p.owner + i * p.t;
   TE *table = static_cast<TE *>(p.dst) + i * p.table_agent + c0;
-  float acc[U][V];
-  if ((int)blockIdx.x < p.chunks) {
-    __shared__ float shared[kWarps][Slice<V>::kElements];
-    const int j = blockIdx.x;
-    const int32_t w = chunk_of<TI>(p, i, j).last;
-    if (w < 0) return;
-    const int32_t b = start[w], e = start[w + 1];
-    if (e - b <= kChunk || b < j * kChunk) return;
-    const int count = (e - 1) / kChunk - j + 1, piece0 = b > j * kChunk;
-    const float *pieces = p.pieces + (i * p.chunks + j) * 2 * p.d + c0;
-    sum_by_warps<V>(acc, count, shared, [&](int k) {
-      const float *r = pieces + (2 * (int64_t)k + (k == 0 ? piece0 : 0)) * p.d;
+  const int work = gridDim.x - p.fills;
+  if ((int)blockIdx.x >= work) {
+    const int64_t r0 = (int64_t)(blockIdx.x - work) * kFill;
+    constexpr int kRows = kFill / kWarps;   // of each warp: warp, warp + kWarps, ...
+    const int64_t row = r0 + warp + lane * kWarps;
+    const bool empty = lane < kRows && row < p.v && start[row] == start[row + 1];
+    uint32_t todo = __ballot_sync(0xffffffffu, empty);
+    const float zero[V] = {};
+    for (; todo; todo &= todo - 1) {
+      TE *g = table + (r0 + warp + (__ffs(todo) - 1) * kWarps) * p.table_row;
 #pragma unroll
       for (int u = 0; u < U; ++u)
-#pragma unroll
-        for (int q = 0; q < V; ++q)
-          if (c0 + u * 32 * V < p.d) acc[u][q] += r[u * 32 * V + q];
-    });
-    if (threadIdx.x < 32) finish_row<TE, V>(p, table + w * p.table_row, c0, acc);
+        if (c0 + u * 32 * V < p.d) put<TE, V>(g + u * 32 * V, zero);
+    }
     return;
   }
-  const int64_t r0 = ((int64_t)(blockIdx.x - p.chunks) * kWarps + (threadIdx.x >> 5)) * kGroup;
-  if (r0 >= p.v) return;
-  const int rows = (int)min((int64_t)kGroup, p.v - r0);
-  const int32_t begin = start[r0 + min(lane, rows)];
-  const int32_t first = __shfl_sync(0xffffffffu, begin, 0), end = __shfl_sync(0xffffffffu, begin, rows);
-  int32_t window = first;   // places [window, window + 32) are in `place`
-  int32_t place = first + lane < end ? list[first + lane] : 0;
+  const int j = blockIdx.x * kWarps + warp;
+  const int32_t total = start[p.v], from = j * kChunk, to = min(from + kChunk, total);
+  if (from >= total) return;
+  // the chunk's places and the next ones, for rows that go on there; each lane knows where its place's row begins and ends
+  const int32_t place0 = from + lane < total ? list[from + lane] : 0, place1 = from + 32 + lane < total ? list[from + 32 + lane] : 0;
+  const int32_t w = from + lane < to ? owner[from + lane] : 0;
+  const int32_t begin = from + lane < to ? start[w] : 0, end = from + lane < to ? start[w + 1] : 0;
   const TO *o = static_cast<const TO *>(p.src) + i * p.out_agent + c0;
-  for (int g = 0; g < rows; ++g) {
-    const int32_t b = __shfl_sync(0xffffffffu, begin, g), e = __shfl_sync(0xffffffffu, begin, g + 1);
-    if (e - b > kChunk || (p.accumulate && b == e)) continue;
+  for (int32_t at = from; at < to;) {
+    const int32_t b = __shfl_sync(0xffffffffu, begin, at - from), e = __shfl_sync(0xffffffffu, end, at - from);
+    const int32_t row = __shfl_sync(0xffffffffu, w, at - from);
+    const bool piece = e - b > kChunk;
+    const int32_t s0 = piece ? at : b, s1 = piece ? min(e, to) : e;
+    const int32_t here = at;
+    at = min(e, to);
+    if (!piece && b < from) continue;   // the warp of the chunk before has it
+    float acc[U][V];
 #pragma unroll
     for (int u = 0; u < U; ++u)
 #pragma unroll
       for (int k = 0; k < V; ++k) acc[u][k] = 0.f;
-    for (int32_t j = b; j < e; j += kDeep) {
-      if (j + kDeep > window + 32) {
-        window = j;
-        place = window + lane < end ? list[window + lane] : 0;
-      }
+    for (int32_t s = s0; s < s1; s += kDeep) {
       Pack<TO, V> v[kDeep][U];
 #pragma unroll
       for (int q = 0; q < kDeep; ++q) {
-        const TO *r = o + __shfl_sync(0xffffffffu, place, (j + q - window) & 31) * p.out_row;
-        if (j + q < e)
+        const int32_t k = s + q - from, p0 = __shfl_sync(0xffffffffu, place0, k & 31), p1 = __shfl_sync(0xffffffffu, place1, k & 31);
+        const TO *r = o + (k < 32 ? p0 : p1) * p.out_row;
+        if (s + q < s1)
 #pragma unroll
           for (int u = 0; u < U; ++u)
             if (c0 + u * 32 * V < p.d) v[q][u] = get<TO, V>(r + u * 32 * V);
       }
 #pragma unroll
       for (int q = 0; q < kDeep; ++q)
-        if (j + q < e)
+        if (s + q < s1)
 #pragma unroll
           for (int u = 0; u < U; ++u)
             if (c0 + u * 32 * V < p.d) add_to(acc[u], v[q][u]);
     }
-    finish_row<TE, V>(p, table + (r0 + g) * p.table_row, c0, acc);
+    if (piece) {   // [0] where it begins the chunk, [1] where it ends it (both: [0])
+      float *out = p.pieces + ((i * p.chunks + j) * 2 + (here > from)) * p.d + c0;
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+#pragma unroll
+        for (int k = 0; k < V; ++k)
+          if (c0 + u * 32 * V < p.d) out[u * 32 * V + k] = acc[u][k];
+    } else {
+      finish_row<TE, V>(p, table + row * p.table_row, c0, acc);
+    }
   }
+}
+
+// Block (j, slice, agent): the row with several pieces whose list begins in chunk j, if there is one: it ends the chunk.
+template <typename TE, int V> __global__ void __launch_bounds__(kThreads) embed_join_kernel(const EmbedArgs p) {
+  constexpr int U = Slice<V>::U;
+  __shared__ float shared[kWarps][Slice<V>::kElements];
+  const int64_t i = blockIdx.z;
+  const int j = blockIdx.x;
+  const int32_t *start = p.row_start + i * (p.v + 1);
+  const int32_t total = start[p.v], from = j * kChunk, to = min(from + kChunk, total);
+  if (from >= total) return;
+  const int32_t w = p.owner[i * p.t + to - 1];
+  const int32_t b = start[w], e = start[w + 1];
+  if (e - b <= kChunk || b < from) return;
+  const int64_t c0 = (int64_t)blockIdx.y * Slice<V>::kElements + (threadIdx.x & 31) * V;
+  const float *pieces = p.pieces + (i * p.chunks + j) * 2 * p.d + c0;
+  float acc[U][V];
+  sum_by_warps<V>(acc, (e - 1) / kChunk - j + 1, shared, [&](int k) {
+    const float *r = pieces + (2 * (int64_t)k + (k == 0 && b > from)) * p.d;
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int q = 0; q < V; ++q)
+        if (c0 + u * 32 * V < p.d) acc[u][q] += r[u * 32 * V + q];
+  });
+  if (threadIdx.x < 32) finish_row<TE, V>(p, static_cast<TE *>(p.dst) + i * p.table_agent + w * p.table_row + c0, c0, acc);
 }
 
 // Table rows per list block: at most kMaxBins (its counters then fill 128 KB), and so few that the blocks of
@@ -358,7 +384,7 @@ int32_t list_bins(int32_t n, int64_t v) {
   return (int32_t)std::max<int64_t>(1, ceil_div(v, blocks));
 }
 
-int64_t chunks_of(int64_t t) { return t > kChunk ? ceil_div(t, kChunk) : 0; }
+int64_t chunks_of(int64_t t) { return ceil_div(t, kChunk); }
 
 size_t round16(size_t bytes) { return (bytes + 15) / 16 * 16; }
 
@@ -387,16 +413,13 @@ template <typename TE, typename TO, typename TI, int V> cudaError_t launch_looku
   return cudaGetLastError();
 }
 
-template <typename TE, typename TO, typename TI, int V> cudaError_t launch_grad(EmbedArgs p, cudaStream_t s) {
+template <typename TE, typename TO, int V> cudaError_t launch_grad(EmbedArgs p, cudaStream_t s) {
   p.slices = (int32_t)ceil_div(p.d, Slice<V>::kElements);
   if (p.slices > 65535) return cudaErrorInvalidValue;
-  if (p.chunks > 0) {
-    embed_pieces_kernel<TO, TI, V><<<dim3(p.chunks, p.slices, p.n), kThreads, 0, s>>>(p);
-    const cudaError_t e = cudaGetLastError();
-    if (e != cudaSuccess) return e;
-  }
-  const int64_t blocks = p.chunks + ceil_div(p.v, kWarps * kGroup);
-  embed_grad_kernel<TE, TO, TI, V><<<dim3((unsigned)blocks, p.slices, p.n), kThreads, 0, s>>>(p);
+  p.fills = p.accumulate ? 0 : (int32_t)ceil_div(p.v, kFill);
+  const unsigned blocks = (unsigned)(ceil_div(p.chunks, kWarps) + p.fills);
+  if (blocks > 0) embed_grad_kernel<TE, TO, V><<<dim3(blocks, p.slices, p.n), kThreads, 0, s>>>(p);
+  if (p.chunks > 1) embed_join_kernel<TE, V><<<dim3(p.chunks - 1, p.slices, p.n), kThreads, 0, s>>>(p);
   return cudaGetLastError();
 }
 
@@ -454,7 +477,7 @@ extern "C" ceca_status_t dsgd_embed_lookup(const void *E, const void *tokens, vo
 
 extern "C" size_t dsgd_embed_workspace_bytes(int32_t n, int64_t t, int64_t v, int64_t d) {
   if (!embed_args_ok(n, t, v, d, 0, d, 0, 0, d, DSGD_F32, DSGD_I32, DSGD_F32)) return 0;
-  return round16(sizeof(int32_t) * (size_t)n * (size_t)(v + 1)) + round16(sizeof(int32_t) * (size_t)n * (size_t)t) +
+  return round16(sizeof(int32_t) * (size_t)n * (size_t)(v + 1)) + 2 * round16(sizeof(int32_t) * (size_t)n * (size_t)t) +
          sizeof(float) * 2 * (size_t)n * (size_t)chunks_of(t) * (size_t)d;
 }
 
@@ -476,14 +499,15 @@ extern "C" ceca_status_t dsgd_embed_grad(const void *dout, const void *tokens, v
   p.out_agent = out_agent_stride; p.out_row = out_row_stride; p.scale = scale; p.accumulate = accumulate != 0;
   p.row_start = static_cast<int32_t *>(workspace);
   p.list = reinterpret_cast<int32_t *>(static_cast<char *>(workspace) + round16(sizeof(int32_t) * (size_t)n * (size_t)(v + 1)));
-  p.pieces = reinterpret_cast<float *>(reinterpret_cast<char *>(p.list) + round16(sizeof(int32_t) * (size_t)n * (size_t)t));
+  p.owner = reinterpret_cast<int32_t *>(reinterpret_cast<char *>(p.list) + round16(sizeof(int32_t) * (size_t)n * (size_t)t));
+  p.pieces = reinterpret_cast<float *>(reinterpret_cast<char *>(p.owner) + round16(sizeof(int32_t) * (size_t)n * (size_t)t));
   p.bins = list_bins(n, v);
   p.chunks = (int32_t)chunks_of(t);
   const cudaStream_t s = static_cast<cudaStream_t>(stream);
   if ((tokens_type == DSGD_I64 ? launch_list<int64_t>(p, s) : launch_list<int32_t>(p, s)) != cudaSuccess)
     return CECA_ERR_CUDA;
   const int pack = pack_of(p, dE, type_bytes(table_type), dout, type_bytes(out_type));
-  return with_types(table_type, out_type, tokens_type, pack, [&](auto te, auto to, auto ti, auto v) {
-    return launch_grad<decltype(te), decltype(to), decltype(ti), v.value>(p, s);
+  return with_types(table_type, out_type, tokens_type, pack, [&](auto te, auto to, auto, auto v) {
+    return launch_grad<decltype(te), decltype(to), v.value>(p, s);
   });
 }
