@@ -5,9 +5,9 @@
 // Both directions move rows and do one multiplication or addition per element, so bytes bound them.  The
 // gradient runs in three launches without atomics on values, in one order of additions:
 //   token_list_kernel   lists every table row's positions in ascending order, by token;
-//   embed_grad_kernel   cuts the list into chunks of kChunk places.  A warp takes the rows that begin in its chunk, or,
-//                       of a row with more than kChunk positions, the piece that lies in it: however the tokens are
-//                       distributed, its work is the same.  Other CTAs fill the rows that no position holds;
+//   embed_grad_kernel   cuts the list into chunks of up to 32 places.  A warp takes the rows that begin in its chunk, or,
+//                       of a row with more positions than a chunk has places, the piece
+//                       that lies in it: however the tokens are distributed, its work is the same.  Other CTAs fill the rows that no position holds;
 //   embed_join_kernel   adds up the pieces of the rows that have several.
 #include <cuda_runtime.h>
 
@@ -37,19 +37,20 @@ struct EmbedArgs {
   int32_t *owner;      // n x t: the token of each
   float *pieces;       // n x chunks x 2 x d: sums of the pieces of long lists
   int32_t bins;        // table rows per block of token_list_kernel
-  int32_t chunks;      // kChunk places each, of an agent's list
+  int32_t chunk;       // places of the list for a warp, at most 32
+  int32_t chunks;      // of an agent's list
   int32_t slices;      // of a row
   int32_t fills;       // CTAs that fill kFill rows each with zeros
 };
 
 constexpr int kThreads = 256, kWarps = kThreads / 32;
-constexpr int kChunk = 32;
 constexpr int kFill = 64;      // table rows
+constexpr int kJoin = 8;       // chunks
 constexpr int kLookupPacks = 4;
 constexpr int kDeep = 4;       // rows of dout that a warp has on their way at a time
-constexpr int kListThreads = 512;
+constexpr int kListThreads = 1024;
 constexpr int kListWarps = kListThreads / 32;
-constexpr int kMaxBins = 2048;
+constexpr int kMaxBins = kListThreads;   // a row for each thread
 
 // V adjacent elements, moved at once: V * sizeof(T) is 16 bytes for the narrower of a call's types, or 8 (V = 1: rows on
 // any boundary).
@@ -154,7 +155,7 @@ __global__ void __launch_bounds__(kThreads) embed_lookup_kernel(const EmbedArgs 
 // the list is ascending within a row; nothing is exchanged between blocks.
 template <typename TI>
 __global__ void __launch_bounds__(kListThreads) token_list_kernel(const EmbedArgs p) {
-  extern __shared__ int32_t count[];   // [kListWarps][bins]
+  extern __shared__ __align__(16) int32_t count[];   // [kListWarps][bins, rounded up to 4]
   __shared__ int32_t part[kListWarps], below_all;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int64_t i = blockIdx.y;
@@ -163,30 +164,32 @@ __global__ void __launch_bounds__(kListThreads) token_list_kernel(const EmbedArg
   const TI *tok = static_cast<const TI *>(p.tokens) + i * p.tokens_agent;
   const int64_t seg = (p.t + kListThreads - 1) / kListThreads * 32;
   const int64_t s0 = warp * seg, s1 = min(p.t, s0 + seg);
-  int32_t *mine = count + warp * p.bins;
+  int32_t *mine = count + warp * ((p.bins + 3) & ~3);
 
-  for (int k = threadIdx.x; k < kListWarps * p.bins; k += kListThreads) count[k] = 0;
+  const int pitch = (p.bins + 3) & ~3;
+  for (int k = threadIdx.x; k < kListWarps * pitch / 4; k += kListThreads) reinterpret_cast<int4 *>(count)[k] = make_int4(0, 0, 0, 0);
   if (threadIdx.x == 0) below_all = 0;
   __syncthreads();
+  // (compared as unsigned numbers: negative tokens lie above every row)
+  using U = typename std::make_unsigned<TI>::type;
+  const U ulo = (U)lo, ubins = (U)bins;
   int32_t below = 0;
 #pragma unroll 8
   for (int64_t s = s0 + lane; s < s1; s += 32) {
-    const int64_t w = tok[s];
-    below += w >= 0 && w < lo;
-    if (w >= lo && w < lo + bins) atomicAdd(mine + (w - lo), 1);
+    const U w = (U)tok[s], r = w - ulo;
+    below += w < ulo;
+    if (r < ubins) atomicAdd(mine + r, 1);
   }
   below = __reduce_add_sync(0xffffffffu, below);
   if (lane == 0) atomicAdd(&below_all, below);
   __syncthreads();
 
   // counts become the places where each (row, warp) begins: exclusive sums over the rows, warps within
-  constexpr int kPer = kMaxBins / kListThreads;
+  const int r = threadIdx.x;
   int32_t sum = 0;
-  for (int j = 0; j < kPer; ++j) {
-    const int r = threadIdx.x * kPer + j;
-    if (r < bins)
-      for (int w = 0; w < kListWarps; ++w) sum += count[w * p.bins + r];
-  }
+  if (r < bins)
+#pragma unroll 8
+    for (int w = 0; w < kListWarps; ++w) sum += count[w * pitch + r];
   int32_t upto = sum;
   for (int o = 1; o < 32; o <<= 1) {
     const int32_t y = __shfl_up_sync(0xffffffffu, upto, o);
@@ -194,40 +197,39 @@ __global__ void __launch_bounds__(kListThreads) token_list_kernel(const EmbedArg
   }
   if (lane == 31) part[warp] = upto;
   __syncthreads();
-  int32_t at = below_all + upto - sum;
-  for (int w = 0; w < warp; ++w) at += part[w];
-  int32_t *start = p.row_start + i * (p.v + 1) + lo;
-  for (int j = 0; j < kPer; ++j) {
-    const int r = threadIdx.x * kPer + j;
-    if (r < bins) {
-      start[r] = at;
-      for (int w = 0; w < kListWarps; ++w) {
-        const int32_t c = count[w * p.bins + r];
-        count[w * p.bins + r] = at;
-        at += c;
-      }
-      if (r == bins - 1 && lo + bins == p.v) start[bins] = at;
+  int32_t before = lane < warp ? part[lane] : 0;
+  before = __reduce_add_sync(0xffffffffu, before);
+  int32_t at = below_all + before + upto - sum;
+  if (r < bins) {
+    int32_t *start = p.row_start + i * (p.v + 1) + lo;
+    start[r] = at;
+#pragma unroll 8
+    for (int w = 0; w < kListWarps; ++w) {
+      const int32_t c = count[w * pitch + r];
+      count[w * pitch + r] = at;
+      at += c;
     }
+    if (r == bins - 1 && lo + bins == p.v) start[bins] = at;
   }
   __syncthreads();
 
   int32_t *list = p.list + i * p.t, *owner = p.owner + i * p.t;
   constexpr int kAhead = 8;   // groups of 32 tokens on their way at a time
   for (int64_t s = s0; s < s1; s += 32 * kAhead) {
-    int64_t w[kAhead];
+    U w[kAhead];
 #pragma unroll
-    for (int k = 0; k < kAhead; ++k) w[k] = s + 32 * k + lane < s1 ? (int64_t)tok[s + 32 * k + lane] : -1;
+    for (int k = 0; k < kAhead; ++k) w[k] = s + 32 * k + lane < s1 ? (U)tok[s + 32 * k + lane] - ulo : ubins;
 #pragma unroll
     for (int k = 0; k < kAhead; ++k) {
-      const bool in = w[k] >= lo && w[k] < lo + bins;
+      const bool in = w[k] < ubins;
       const uint32_t some = __ballot_sync(0xffffffffu, in);
       if (some == 0) continue;
       if (in) {
-        const int32_t r = (int32_t)(w[k] - lo);
+        const int32_t r = (int32_t)w[k];
         const uint32_t same = __match_any_sync(some, r);
         const int32_t rank = __popc(same & ((1u << lane) - 1)), at = mine[r] + rank;
         list[at] = (int32_t)(s + 32 * k + lane);
-        owner[at] = (int32_t)w[k];
+        owner[at] = (int32_t)lo + r;
         __syncwarp(some);
         if (rank == 0) mine[r] += __popc(same);
       }
@@ -299,92 +301,110 @@ template <typename TE, typename TO, int V> __global__ void __launch_bounds__(kTh
     }
     return;
   }
-  const int j = blockIdx.x * kWarps + warp;
-  const int32_t total = start[p.v], from = j * kChunk, to = min(from + kChunk, total);
+  const int j = blockIdx.x * kWarps + warp, chunk = p.chunk;
+  const int32_t total = start[p.v], from = j * chunk, to = min(from + chunk, total);
   if (from >= total) return;
-  // the chunk's places and the next ones, for rows that go on there; each lane knows where its place's row begins and ends
+  // the chunk's places and the next ones, for a row that goes on there; each lane knows where its place's row begins and ends
   const int32_t place0 = from + lane < total ? list[from + lane] : 0, place1 = from + 32 + lane < total ? list[from + 32 + lane] : 0;
-  const int32_t w = from + lane < to ? owner[from + lane] : 0;
-  const int32_t begin = from + lane < to ? start[w] : 0, end = from + lane < to ? start[w + 1] : 0;
+  const int32_t w = owner[min(from + lane, to - 1)];
+  const int32_t begin = start[w], end = start[w + 1];
   const TO *o = static_cast<const TO *>(p.src) + i * p.out_agent + c0;
-  for (int32_t at = from; at < to;) {
-    const int32_t b = __shfl_sync(0xffffffffu, begin, at - from), e = __shfl_sync(0xffffffffu, end, at - from);
-    const int32_t row = __shfl_sync(0xffffffffu, w, at - from);
-    const bool piece = e - b > kChunk;
-    const int32_t s0 = piece ? at : b, s1 = piece ? min(e, to) : e;
-    const int32_t here = at;
-    at = min(e, to);
-    if (!piece && b < from) continue;   // the warp of the chunk before has it
-    float acc[U][V];
+  // the places [s0, s1) are this warp's: not those of a whole row that the warp of the chunk before has, but all of a whole
+  // row that goes on after the chunk
+  const int32_t b0 = __shfl_sync(0xffffffffu, begin, 0), e0 = __shfl_sync(0xffffffffu, end, 0);
+  const int32_t bl = __shfl_sync(0xffffffffu, begin, 31), el = __shfl_sync(0xffffffffu, end, 31);
+  const int32_t s0 = b0 < from && e0 - b0 <= chunk ? min(e0, to) : from;
+  const int32_t s1 = el - bl > chunk || bl < from ? to : el;
+  float acc[U][V];
 #pragma unroll
-    for (int u = 0; u < U; ++u)
+  for (int u = 0; u < U; ++u)
 #pragma unroll
-      for (int k = 0; k < V; ++k) acc[u][k] = 0.f;
-    for (int32_t s = s0; s < s1; s += kDeep) {
-      Pack<TO, V> v[kDeep][U];
+    for (int k = 0; k < V; ++k) acc[u][k] = 0.f;
+  for (int32_t s = s0; s < s1; s += kDeep) {
+    Pack<TO, V> v[kDeep][U];
 #pragma unroll
-      for (int q = 0; q < kDeep; ++q) {
-        const int32_t k = s + q - from, p0 = __shfl_sync(0xffffffffu, place0, k & 31), p1 = __shfl_sync(0xffffffffu, place1, k & 31);
-        const TO *r = o + (k < 32 ? p0 : p1) * p.out_row;
-        if (s + q < s1)
+    for (int q = 0; q < kDeep; ++q) {
+      const int32_t k = s + q - from, p0 = __shfl_sync(0xffffffffu, place0, k & 31), p1 = __shfl_sync(0xffffffffu, place1, k & 31);
+      const TO *r = o + (k < 32 ? p0 : p1) * p.out_row;
+      if (s + q < s1)
 #pragma unroll
-          for (int u = 0; u < U; ++u)
-            if (c0 + u * 32 * V < p.d) v[q][u] = get<TO, V>(r + u * 32 * V);
-      }
-#pragma unroll
-      for (int q = 0; q < kDeep; ++q)
-        if (s + q < s1)
-#pragma unroll
-          for (int u = 0; u < U; ++u)
-            if (c0 + u * 32 * V < p.d) add_to(acc[u], v[q][u]);
+        for (int u = 0; u < U; ++u)
+          if (c0 + u * 32 * V < p.d) v[q][u] = get<TO, V>(r + u * 32 * V);
     }
-    if (piece) {   // [0] where it begins the chunk, [1] where it ends it (both: [0])
-      float *out = p.pieces + ((i * p.chunks + j) * 2 + (here > from)) * p.d + c0;
+#pragma unroll
+    for (int q = 0; q < kDeep; ++q) {
+      if (s + q >= s1) break;
+      const int k = min(s + q, to - 1) - from;   // a place after the chunk is of the chunk's last row
+      const int32_t b = __shfl_sync(0xffffffffu, begin, k), e = __shfl_sync(0xffffffffu, end, k), row = __shfl_sync(0xffffffffu, w, k);
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        if (c0 + u * 32 * V < p.d) add_to(acc[u], v[q][u]);
+      if (s + q + 1 < e && s + q + 1 < s1) continue;   // the row, or its piece, goes on
+      if (e - b > chunk) {   // a piece: [0] where it begins the chunk, [1] where it only ends it
+        float *out = p.pieces + ((i * p.chunks + j) * 2 + (b > from)) * p.d + c0;
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+          for (int x = 0; x < V; ++x)
+            if (c0 + u * 32 * V < p.d) out[u * 32 * V + x] = acc[u][x];
+      } else {
+        finish_row<TE, V>(p, table + row * p.table_row, c0, acc);
+      }
 #pragma unroll
       for (int u = 0; u < U; ++u)
 #pragma unroll
-        for (int k = 0; k < V; ++k)
-          if (c0 + u * 32 * V < p.d) out[u * 32 * V + k] = acc[u][k];
-    } else {
-      finish_row<TE, V>(p, table + row * p.table_row, c0, acc);
+        for (int x = 0; x < V; ++x) acc[u][x] = 0.f;
     }
   }
 }
 
-// Block (j, slice, agent): the row with several pieces whose list begins in chunk j, if there is one: it ends the chunk.
+// Block (x, slice, agent): the rows with several pieces whose lists begin in the chunks [x kJoin, (x + 1) kJoin).  Such a row
+// ends its chunk.
 template <typename TE, int V> __global__ void __launch_bounds__(kThreads) embed_join_kernel(const EmbedArgs p) {
   constexpr int U = Slice<V>::U;
   __shared__ float shared[kWarps][Slice<V>::kElements];
   const int64_t i = blockIdx.z;
-  const int j = blockIdx.x;
+  const int lane = threadIdx.x & 31;
   const int32_t *start = p.row_start + i * (p.v + 1);
-  const int32_t total = start[p.v], from = j * kChunk, to = min(from + kChunk, total);
-  if (from >= total) return;
-  const int32_t w = p.owner[i * p.t + to - 1];
-  const int32_t b = start[w], e = start[w + 1];
-  if (e - b <= kChunk || b < from) return;
-  const int64_t c0 = (int64_t)blockIdx.y * Slice<V>::kElements + (threadIdx.x & 31) * V;
-  const float *pieces = p.pieces + (i * p.chunks + j) * 2 * p.d + c0;
-  float acc[U][V];
-  sum_by_warps<V>(acc, (e - 1) / kChunk - j + 1, shared, [&](int k) {
-    const float *r = pieces + (2 * (int64_t)k + (k == 0 && b > from)) * p.d;
+  const int32_t total = start[p.v], mine = ((int)blockIdx.x * kJoin + lane) * p.chunk;
+  int32_t w = 0, b = 0, e = 0;
+  if (lane < kJoin && mine < total) {
+    w = p.owner[i * p.t + min(mine + p.chunk, total) - 1];
+    b = start[w];
+    e = start[w + 1];
+  }
+  uint32_t todo = __ballot_sync(0xffffffffu, e - b > p.chunk && b >= mine);   // the same in every warp
+  const int64_t c0 = (int64_t)blockIdx.y * Slice<V>::kElements + lane * V;
+  for (; todo; todo &= todo - 1) {
+    const int k0 = __ffs(todo) - 1, j = blockIdx.x * kJoin + k0;
+    const int32_t row = __shfl_sync(0xffffffffu, w, k0), from = __shfl_sync(0xffffffffu, b, k0), to = __shfl_sync(0xffffffffu, e, k0);
+    const float *pieces = p.pieces + (i * p.chunks + j) * 2 * p.d + c0;
+    float acc[U][V];
+    sum_by_warps<V>(acc, (to - 1) / p.chunk - j + 1, shared, [&](int k) {
+      const float *r = pieces + (2 * (int64_t)k + (k == 0 && from > j * p.chunk)) * p.d;
 #pragma unroll
-    for (int u = 0; u < U; ++u)
+      for (int u = 0; u < U; ++u)
 #pragma unroll
-      for (int q = 0; q < V; ++q)
-        if (c0 + u * 32 * V < p.d) acc[u][q] += r[u * 32 * V + q];
-  });
-  if (threadIdx.x < 32) finish_row<TE, V>(p, static_cast<TE *>(p.dst) + i * p.table_agent + w * p.table_row + c0, c0, acc);
+        for (int q = 0; q < V; ++q)
+          if (c0 + u * 32 * V < p.d) acc[u][q] += r[u * 32 * V + q];
+    });
+    if (threadIdx.x < 32) finish_row<TE, V>(p, static_cast<TE *>(p.dst) + i * p.table_agent + row * p.table_row + c0, c0, acc);
+  }
 }
 
-// Table rows per list block: at most kMaxBins (its counters then fill 128 KB), and so few that the blocks of
-// all agents cover the GPU.
+// Table rows per list block: few blocks scan all of an agent's tokens in vain, but a block's own tokens take longest, and
+// frequent tokens lie together; two blocks an SM are best over the range.
 int32_t list_bins(int32_t n, int64_t v) {
   const int64_t blocks = std::max<int64_t>(ceil_div(v, kMaxBins), ceil_div(2 * 148, n));
   return (int32_t)std::max<int64_t>(1, ceil_div(v, blocks));
 }
 
-int64_t chunks_of(int64_t t) { return ceil_div(t, kChunk); }
+// Places of a chunk: 32, or fewer where that would leave the SMs without work.
+int32_t chunk_of(int32_t n, int64_t t, int64_t d) {
+  int32_t c = 32;
+  while (c > 8 && n * ceil_div(t, c) * ceil_div(d, 512) < 16 * 148) c /= 2;
+  return c;
+}
 
 size_t round16(size_t bytes) { return (bytes + 15) / 16 * 16; }
 
@@ -419,7 +439,7 @@ template <typename TE, typename TO, int V> cudaError_t launch_grad(EmbedArgs p, 
   p.fills = p.accumulate ? 0 : (int32_t)ceil_div(p.v, kFill);
   const unsigned blocks = (unsigned)(ceil_div(p.chunks, kWarps) + p.fills);
   if (blocks > 0) embed_grad_kernel<TE, TO, V><<<dim3(blocks, p.slices, p.n), kThreads, 0, s>>>(p);
-  if (p.chunks > 1) embed_join_kernel<TE, V><<<dim3(p.chunks - 1, p.slices, p.n), kThreads, 0, s>>>(p);
+  if (p.chunks > 1) embed_join_kernel<TE, V><<<dim3((unsigned)ceil_div(p.chunks, kJoin), p.slices, p.n), kThreads, 0, s>>>(p);
   return cudaGetLastError();
 }
 
@@ -443,7 +463,7 @@ template <typename TI> cudaError_t launch_list(const EmbedArgs &p, cudaStream_t 
                                             sizeof(int32_t) * kListWarps * kMaxBins, &done);
   if (e != cudaSuccess) return e;
   const dim3 grid((unsigned)ceil_div(p.v, p.bins), (unsigned)p.n);
-  token_list_kernel<TI><<<grid, kListThreads, sizeof(int32_t) * kListWarps * p.bins, s>>>(p);
+  token_list_kernel<TI><<<grid, kListThreads, sizeof(int32_t) * kListWarps * ((p.bins + 3) / 4 * 4), s>>>(p);
   return cudaGetLastError();
 }
 
@@ -478,7 +498,7 @@ extern "C" ceca_status_t dsgd_embed_lookup(const void *E, const void *tokens, vo
 extern "C" size_t dsgd_embed_workspace_bytes(int32_t n, int64_t t, int64_t v, int64_t d) {
   if (!embed_args_ok(n, t, v, d, 0, d, 0, 0, d, DSGD_F32, DSGD_I32, DSGD_F32)) return 0;
   return round16(sizeof(int32_t) * (size_t)n * (size_t)(v + 1)) + 2 * round16(sizeof(int32_t) * (size_t)n * (size_t)t) +
-         sizeof(float) * 2 * (size_t)n * (size_t)chunks_of(t) * (size_t)d;
+         sizeof(float) * 2 * (size_t)n * (size_t)ceil_div(t, chunk_of(n, t, d)) * (size_t)d;
 }
 
 extern "C" ceca_status_t dsgd_embed_grad(const void *dout, const void *tokens, void *dE, int32_t n, int64_t t,
@@ -502,7 +522,8 @@ extern "C" ceca_status_t dsgd_embed_grad(const void *dout, const void *tokens, v
   p.owner = reinterpret_cast<int32_t *>(reinterpret_cast<char *>(p.list) + round16(sizeof(int32_t) * (size_t)n * (size_t)t));
   p.pieces = reinterpret_cast<float *>(reinterpret_cast<char *>(p.owner) + round16(sizeof(int32_t) * (size_t)n * (size_t)t));
   p.bins = list_bins(n, v);
-  p.chunks = (int32_t)chunks_of(t);
+  p.chunk = chunk_of(n, t, d);
+  p.chunks = (int32_t)ceil_div(t, p.chunk);
   const cudaStream_t s = static_cast<cudaStream_t>(stream);
   if ((tokens_type == DSGD_I64 ? launch_list<int64_t>(p, s) : launch_list<int32_t>(p, s)) != cudaSuccess)
     return CECA_ERR_CUDA;
