@@ -80,13 +80,12 @@ __global__ void __launch_bounds__(32 * WARPS, 16 / WARPS) recurrence_kernel(cons
     stage = stage + 1 == kStages ? 0 : stage + 1;
     const int left = (int)max((int64_t)0, min((int64_t)kRun, p.t - s0));   // steps of the run that exist
     V a[kRun], b[kRun], A = all<C>(1.f), H = all<C>(0.f);
-    const bool xo = L == HALVES && odd_step(x, p.x_step, s0), xa = L == HALVES && p.x_step & 1;
-    const bool fo = L == HALVES && odd_step(f, p.f_step, s0), fa = L == HALVES && p.f_step & 1;
+    const Skew xk(x, p.x_step * sizeof(T), s0), fk(f, p.f_step * sizeof(T), s0);
 #pragma unroll
     for (int j = 0; j < kRun; ++j) {
       V na;
-      gates(take<L>(fr.at(j, fo ^ (fa && (j & 1)))), &a[j], &na);
-      b[j] = mul(na, take<L>(xr.at(j, xo ^ (xa && (j & 1)))));
+      gates(take<L>(fr.at(j, fk)), &a[j], &na);
+      b[j] = mul(na, take<L>(xr.at(j, xk)));
     }
     if (left < kRun) {   // steps beyond the end change nothing
 #pragma unroll

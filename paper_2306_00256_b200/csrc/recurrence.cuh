@@ -86,52 +86,63 @@ template <int L> __device__ __forceinline__ void store(float *p, Val<Lanes<L>::k
 __device__ __forceinline__ void copy16(uint32_t to, const void *from, int have) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(have) : "memory");
 }
-__device__ __forceinline__ void copy4(uint32_t to, const void *from, int have) {
-  asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(to), "l"(from), "r"(have) : "memory");
+__device__ __forceinline__ void copy16(uint32_t to, const void *from) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
 }
 __device__ __forceinline__ void copies_end() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int LEFT> __device__ __forceinline__ void copies_wait() {
   asm volatile("cp.async.wait_group %0;" ::"n"(LEFT) : "memory");
 }
 
-// The kRun steps of one stream for one warp, brought by that warp itself: nobody else waits for them.  WIDE copies
-// 16 bytes at a time, four steps an instruction; otherwise a step is copied word by word, from the word that holds its
-// first byte (HALVES: a step may begin in the middle of it, and then ends in a 33rd word).
+// Where the steps of a run begin between 16-byte boundaries: the first one, and how far it moves from step to step.
+struct Skew {
+  uint32_t first, step;
+  __device__ __forceinline__ Skew(const void *p, int64_t step_bytes, int64_t s0)
+      : first((uint32_t)(reinterpret_cast<uintptr_t>(p) + step_bytes * s0)), step((uint32_t)step_bytes) {}
+  __device__ __forceinline__ uint32_t of(int j) const { return (first + j * step) & 15; }
+};
+
+// The kRun steps of one stream for one warp, brought by that warp itself: nobody else waits for them.  WIDE: every step
+// begins on a 16-byte boundary.  Otherwise a step's 128 bytes are copied as the nine 16-byte words that hold them, and
+// found at the step's skew; of a first word, what lies before the step is another channel's or another tensor's, in the
+// same allocation (none begins inside such a word), and is not used.
 template <int L, bool WIDE> struct Run {
   using T = typename Lanes<L>::T;
-  static constexpr int kPitch = L == HALVES ? 132 : 128;
+  static constexpr int kPitch = WIDE ? 128 : 144;
   alignas(16) char bytes[kRun * kPitch];
 
   // p: the stream's first channel of this warp at step 0; width: bytes of a step that exist from there on (up to 128)
   __device__ __forceinline__ void fetch(const T *p, int64_t step, int64_t s0, int64_t t, int width) {
     const int lane = threadIdx.x & 31;
     const uint32_t to = smem_u32(bytes);
-    const int left = s0 < 0 ? 0 : (int)min((int64_t)kRun, t - s0);
+    const int left = s0 < 0 ? 0 : (int)max((int64_t)0, min((int64_t)kRun, t - s0));
+    const int64_t hop = step * (int64_t)sizeof(T);
+    const char *base = reinterpret_cast<const char *>(p) + s0 * hop;
     if constexpr (WIDE) {
       const int row = lane >> 3, col = (lane & 7) * 16;
-      const int have = max(0, min(16, width - col));
-      const char *from = reinterpret_cast<const char *>(p + (s0 + row) * step) + col;
-      const int64_t hop = 4 * step * (int64_t)sizeof(T);
+      const char *from = base + row * hop + col;
+      const uint32_t at = to + row * kPitch + col;
+      if (left == kRun && width == 128) {
 #pragma unroll
-      for (int k = 0; k < kRun / 4; ++k, from += hop) {
-        const bool in = row + 4 * k < left && have > 0;
-        copy16(to + (row + 4 * k) * kPitch + col, in ? from : reinterpret_cast<const char *>(p), in ? have : 0);
+        for (int k = 0; k < kRun / 4; ++k) copy16(at + 4 * k * kPitch, from + 4 * k * hop);
+      } else {
+        const int have = max(0, min(16, width - col));
+        for (int k = 0; k < kRun / 4; ++k)
+          if (row + 4 * k < left && have > 0) copy16(at + 4 * k * kPitch, from + 4 * k * hop, have);
       }
     } else {
-      const T *from = p + s0 * step;
-      for (int k = 0; k < left; ++k, from += step) {
-        const uintptr_t at = reinterpret_cast<uintptr_t>(from);
-        const int skew = L == HALVES ? (int)(at & 2) : 0;
-        const char *words = reinterpret_cast<const char *>(at - skew);
-        const int have = min(4, width + skew - 4 * lane);
-        if (have > 0) copy4(to + k * kPitch + 4 * lane, words + 4 * lane, have);
-        if (L == HALVES && lane == 0 && width + skew > 128) copy4(to + k * kPitch + 128, words + 128, width + skew - 128);
+#pragma unroll
+      for (int k = lane; k < kRun * 9; k += 32) {
+        const int row = k / 9, col = (k - row * 9) * 16;
+        const char *from = base + row * hop;
+        const int skew = (int)(reinterpret_cast<uintptr_t>(from) & 15), have = min(16, width + skew - col);
+        if (row < left && have > 0) copy16(to + row * kPitch + col, from - skew + col, have);
       }
     }
   }
-  // the lane's first channel of step j; `odd`: whether the step begins in the middle of a word
-  __device__ __forceinline__ const T *at(int j, bool odd) const {
-    return reinterpret_cast<const T *>(bytes + j * kPitch) + (threadIdx.x & 31) * Lanes<L>::kFirst + (L == HALVES && odd);
+  // the lane's first channel of step j
+  __device__ __forceinline__ const T *at(int j, const Skew &skew) const {
+    return reinterpret_cast<const T *>(bytes + j * kPitch + (WIDE ? 0 : skew.of(j))) + (threadIdx.x & 31) * Lanes<L>::kFirst;
   }
 };
 
@@ -203,7 +214,7 @@ template <int L> struct Place {
   Live live;
   __device__ __forceinline__ explicit Place(const RecurArgs &p) {
     lane = threadIdx.x & 31;
-    warp = threadIdx.x >> 5;
+    warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0);   // one value for the warp, and known to be
     const uint32_t which = blockIdx.x / (uint32_t)p.segs;
     seg = (int)(blockIdx.x - which * p.segs);
     i = which / (uint32_t)p.blocks;
@@ -236,11 +247,6 @@ __device__ __forceinline__ Val<Lanes<L>::kVals> arriving(const RecurArgs &p, con
   return none;
 }
 
-// Whether step s of a stream of bf16 begins in the middle of a word.
-__device__ __forceinline__ bool odd_step(const void *p, int64_t step, int64_t s) {
-  return ((reinterpret_cast<uintptr_t>(p) >> 1) + step * s) & 1;
-}
-
 // How far the steps of a tensor are aligned: 16, 4 or fewer bytes.
 inline int alignment(const void *base, int64_t seq, int64_t step, int32_t type) {
   const int64_t e = type_bytes(type);
@@ -254,9 +260,9 @@ inline int alignment(const void *base, int64_t seq, int64_t step, int32_t type) 
 // maps a first kernel finds (it reads two of the streams once more).
 constexpr int64_t kSms = 148, kWanted = 12 * kSms, kMaxSegs = 128;
 struct Split { int warps, segs; };
-inline Split split(int64_t chains, int64_t t) {
+inline Split split(int64_t chains, int64_t t, int most) {
   const int64_t runs = ceil_div(t, kRun);
-  for (int w = 4; w <= 16; w *= 2)
+  for (int w = 4; w <= most; w *= 2)
     if (chains * w >= kWanted && w <= std::max<int64_t>(4, runs)) return {w, 1};
   return {4, (int)std::max<int64_t>(1, std::min({4 * kSms / chains, ceil_div(runs, 4), kMaxSegs}))};
 }
@@ -274,7 +280,8 @@ inline cudaError_t launch_kernel(void (*kernel)(const RecurArgs), const RecurArg
 template <typename Go, int L, bool WIDE> cudaError_t choose_split(Go &go) {
   RecurArgs &p = go.p;
   p.blocks = (int32_t)ceil_div(p.d, Lanes<L>::kChannels);
-  const Split s = split(go.b * p.blocks, p.t);
+  constexpr int kMost = WIDE ? 16 : 8;   // warps that the shared memory of a CTA has room for
+  const Split s = split(go.b * p.blocks, p.t, kMost);
   p.n_tiles = ceil_div(p.t, s.warps * kRun);
   p.seg_tiles = ceil_div(p.n_tiles, s.segs);
   p.segs = (int32_t)ceil_div(p.n_tiles, p.seg_tiles);
@@ -283,7 +290,8 @@ template <typename Go, int L, bool WIDE> cudaError_t choose_split(Go &go) {
     const cudaError_t e = go.template maps<L, WIDE>();
     if (e != cudaSuccess) return e;
   }
-  if (s.warps == 16) return go.template run<L, WIDE, 16>();
+  if constexpr (WIDE)
+    if (s.warps == 16) return go.template run<L, WIDE, 16>();
   return s.warps == 8 ? go.template run<L, WIDE, 8>() : go.template run<L, WIDE, 4>();
 }
 template <typename Go> ceca_status_t choose(Go go, int in, int out, int32_t type) {
@@ -294,9 +302,9 @@ template <typename Go> ceca_status_t choose(Go go, int in, int out, int32_t type
   return e == cudaSuccess ? CECA_OK : CECA_ERR_CUDA;
 }
 
-// Enough for every layout: the widest channel blocks make the most segments.
+// Enough for every layout: the widest channel blocks and the fewest warps make the most segments.
 inline size_t maps_bytes(int64_t b, int64_t t, int64_t d) {
-  const int segs = split(b * ceil_div(d, 64), t).segs;
+  const int segs = split(b * ceil_div(d, 64), t, 8).segs;
   return segs == 1 ? 0 : sizeof(float) * 2 * (size_t)b * (size_t)(segs + 1) * (size_t)d;
 }
 
@@ -353,13 +361,12 @@ template <int L, bool WIDE, bool REVERSE> __global__ void __launch_bounds__(128,
     stage = stage + 1 == kStages ? 0 : stage + 1;
     const int64_t s0 = where(k);
     const int left = (int)max((int64_t)0, min((int64_t)kRun, p.t - s0));
-    const bool xo = L == HALVES && odd_step(x, x_step, s0), xa = L == HALVES && x_step & 1;
-    const bool fo = L == HALVES && odd_step(f, p.f_step, s0), fa = L == HALVES && p.f_step & 1;
+    const Skew xk(x, x_step * sizeof(T), s0), fk(f, p.f_step * sizeof(T), s0);
     cut |= cuts != 0;
     auto step = [&](int j, bool begins_here) {
       V a, na;
-      gates(take<L>(fr.at(j, fo ^ (fa && (j & 1)))), &a, &na);
-      const V xv = take<L>(xr.at(j, xo ^ (xa && (j & 1))));
+      gates(take<L>(fr.at(j, fk)), &a, &na);
+      const V xv = take<L>(xr.at(j, xk));
       if (REVERSE) H = begins_here ? all<C>(0.f) : mul(a, add(xv, H));
       else H = begins_here ? mul(na, xv) : fma(a, H, mul(na, xv));
       A = mul(A, a);

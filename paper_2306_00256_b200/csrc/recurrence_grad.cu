@@ -71,14 +71,12 @@ __global__ void __launch_bounds__(32 * WARPS, 16 / WARPS) recurrence_grad_kernel
     const Run<L, WIDE> &xr = mine[stage][0], &fr = mine[stage][1], &gr = mine[stage][2];
     stage = stage + 1 == kStages ? 0 : stage + 1;
     const int left = (int)max((int64_t)0, min((int64_t)kRun, p.t - s0));
-    const bool xo = L == HALVES && odd_step(x, p.x_step, s0), xa = p.x_step & 1;
-    const bool fo = L == HALVES && odd_step(f, p.f_step, s0), fa = p.f_step & 1;
-    const bool go = L == HALVES && odd_step(dh, p.dh_step, s0), ga = p.dh_step & 1;
-    auto xv = [&](int j) { return take<L>(xr.at(j, xo ^ (xa && (j & 1)))); };
-    auto gv = [&](int j) { return take<L>(gr.at(j, go ^ (ga && (j & 1)))); };
+    const Skew xk(x, p.x_step * sizeof(T), s0), fk(f, p.f_step * sizeof(T), s0), gk(dh, p.dh_step * sizeof(T), s0);
+    auto xv = [&](int j) { return take<L>(xr.at(j, xk)); };
+    auto gv = [&](int j) { return take<L>(gr.at(j, gk)); };
     V a[kRun], na[kRun], A = all<C>(1.f), H = all<C>(0.f), D = all<C>(0.f);
 #pragma unroll
-    for (int j = 0; j < kRun; ++j) gates(take<L>(fr.at(j, fo ^ (fa && (j & 1)))), &a[j], &na[j]);
+    for (int j = 0; j < kRun; ++j) gates(take<L>(fr.at(j, fk)), &a[j], &na[j]);
     if (left < kRun || cuts) {
 #pragma unroll
       for (int j = 0; j < kRun; ++j) {

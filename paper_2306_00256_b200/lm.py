@@ -24,6 +24,13 @@ def _empty(shape, dtype, like, stream):
         return torch.empty(shape, dtype=dtype, device=like.device)
 
 
+def _like(t, dtype, stream):
+    """An uninitialised dense tensor of t's shape; the short way where t says it all."""
+    if stream is None and t.dtype == dtype and t.is_contiguous():
+        return torch.empty_like(t)
+    return _empty(t.shape, dtype, t, stream)
+
+
 def _here(stream, first, *others):
     """The stream to launch on, as a number; all tensors must live on the current device."""
     device = first.get_device()
@@ -144,12 +151,12 @@ def dsgd_recurrence(x, f, h0=None, starts=None, h=None, h_last=None, save=False,
     p0 = None if h0 is None else _dense(h0, "h0", (b, d))
     ps = None if starts is None else _starts(starts, (b, t))
     if h is None:
-        h = _empty(shape, dtype, x, stream)
+        h = _like(x, dtype, stream)
     elif h.shape != shape or h.dtype != dtype:
         raise ValueError("h must have the shape and type of x")
     sh = _rows(h, "h")[1]
     if h_last is None:
-        h_last = _empty((b, d), _F32, x, stream)
+        h_last = _empty((b, d), _F32, x, stream) if h0 is None else _like(h0, _F32, stream)
         pl = h_last.data_ptr()
     else:
         pl = _dense(h_last, "h_last", (b, d))
@@ -179,13 +186,13 @@ def dsgd_recurrence_grad(x, f, dh, marks, h0=None, starts=None, dh_last=None, dx
     outs = []
     for g, name in ((dx, "dx"), (df, "df")):
         if g is None:
-            g = _empty(shape, dtype, x, stream)
+            g = _like(x, dtype, stream)
         elif g.shape != shape or g.dtype != dtype:
             raise ValueError("%s must have the shape and type of x" % name)
         outs.append((g, _rows(g, name)[1]))
     (dx, sdx), (df, sdf) = outs
     if dh0 is None:
-        dh0 = _empty((b, d), _F32, x, stream)
+        dh0 = _empty((b, d), _F32, x, stream) if dh_last is None else _like(dh_last, _F32, stream)
         p0 = dh0.data_ptr()
     else:
         p0 = _dense(dh0, "dh0", (b, d))
@@ -207,7 +214,7 @@ def _distill(z, idx, t, teacher_lse, weight, loss, dz, stream):
     pe = None if teacher_lse is None else _dense(teacher_lse, "teacher_lse", (r,))
     pw = None if weight is None else _dense(weight, "weight", (r,))
     if loss is None:
-        loss = _empty(r, _F32, z, stream)
+        loss = _empty(r, _F32, z, stream) if weight is None else _like(weight, _F32, stream)
         pl = loss.data_ptr()
     else:
         pl = _dense(loss, "loss", (r,))
@@ -227,7 +234,7 @@ def dsgd_distill_grad(z, idx, t, teacher_lse=None, weight=None, temperature=1.0,
     """(loss, dz): dsgd_distill_loss and the gradient of its sum over rows with respect to z, in one pass.  dz may be z."""
     at, sizes, types, s, loss = _distill(z, idx, t, teacher_lse, weight, loss, dz, stream)
     if dz is None:
-        dz = _empty(z.shape, z.dtype, z, stream)
+        dz = _like(z, z.dtype, stream)
     elif dz.shape != z.shape or dz.dtype != z.dtype:
         raise ValueError("dz must have the shape and type of z")
     _check(library().dsgd_distill_grad(*at, dz.data_ptr(), *sizes, _rows(dz, "dz")[1][0], *types, temperature, s), "dsgd_distill_grad")
