@@ -111,7 +111,8 @@ template <int L, bool WIDE> struct Run {
   static constexpr int kPitch = WIDE ? 128 : 144;
   alignas(16) char bytes[kRun * kPitch];
 
-  // p: the stream's first channel of this warp at step 0; width: bytes of a step that exist from there on (up to 128)
+  // p: the stream's first channel of this warp at step 0; width: bytes of a step that exist from there on (up to 128).
+  // Steps and channels that do not exist become zeros.
   __device__ __forceinline__ void fetch(const T *p, int64_t step, int64_t s0, int64_t t, int width) {
     const int lane = threadIdx.x & 31;
     const uint32_t to = smem_u32(bytes);
@@ -127,8 +128,10 @@ template <int L, bool WIDE> struct Run {
         for (int k = 0; k < kRun / 4; ++k) copy16(at + 4 * k * kPitch, from + 4 * k * hop);
       } else {
         const int have = max(0, min(16, width - col));
-        for (int k = 0; k < kRun / 4; ++k)
-          if (row + 4 * k < left && have > 0) copy16(at + 4 * k * kPitch, from + 4 * k * hop, have);
+        for (int k = 0; k < kRun / 4; ++k) {
+          const bool in = row + 4 * k < left && have > 0;
+          copy16(at + 4 * k * kPitch, in ? from + 4 * k * hop : reinterpret_cast<const char *>(p), in ? have : 0);
+        }
       }
     } else {
 #pragma unroll
@@ -136,7 +139,8 @@ template <int L, bool WIDE> struct Run {
         const int row = k / 9, col = (k - row * 9) * 16;
         const char *from = base + row * hop;
         const int skew = (int)(reinterpret_cast<uintptr_t>(from) & 15), have = min(16, width + skew - col);
-        if (row < left && have > 0) copy16(to + row * kPitch + col, from - skew + col, have);
+        const bool in = row < left && have > 0;
+        copy16(to + row * kPitch + col, in ? from - skew + col : reinterpret_cast<const char *>((uintptr_t)p & ~(uintptr_t)15), in ? have : 0);
       }
     }
   }

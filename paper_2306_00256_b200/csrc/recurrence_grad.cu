@@ -76,25 +76,30 @@ __global__ void __launch_bounds__(32 * WARPS, 16 / WARPS) recurrence_grad_kernel
     auto gv = [&](int j) { return take<L>(gr.at(j, gk)); };
     V a[kRun], na[kRun], A = all<C>(1.f), H = all<C>(0.f), D = all<C>(0.f);
 #pragma unroll
-    for (int j = 0; j < kRun; ++j) gates(take<L>(fr.at(j, fk)), &a[j], &na[j]);
-    if (left < kRun || cuts) {
+    for (int j = 0; j < kRun; ++j) {
+      gates(take<L>(fr.at(j, fk)), &a[j], &na[j]);
+      A = mul(A, a[j]);
+    }
+    if (left < kRun) {   // steps beyond the end change nothing
+      A = all<C>(1.f);
 #pragma unroll
       for (int j = 0; j < kRun; ++j) {
         if (j >= left) { a[j] = all<C>(1.f); na[j] = all<C>(0.f); }
-        const V b = j < left ? mul(na[j], xv(j)) : all<C>(0.f);
-        H = cuts >> j & 1 ? b : fma(a[j], H, b);
         A = mul(A, a[j]);
       }
-#pragma unroll
-      for (int j = kRun - 1; j >= 0; --j)
-        if (j < left) D = cuts >> j & 1 ? all<C>(0.f) : mul(a[j], add(gv(j), D));
-      if (cuts) A = all<C>(kCut);
-    } else {
+    }
+    if (cuts) {
 #pragma unroll
       for (int j = 0; j < kRun; ++j) {
-        H = fma(a[j], H, mul(na[j], xv(j)));
-        A = mul(A, a[j]);
+        const V b = mul(na[j], xv(j));
+        H = cuts >> j & 1 ? b : fma(a[j], H, b);
       }
+#pragma unroll
+      for (int j = kRun - 1; j >= 0; --j) D = cuts >> j & 1 ? all<C>(0.f) : mul(a[j], add(gv(j), D));
+      A = all<C>(kCut);
+    } else {
+#pragma unroll
+      for (int j = 0; j < kRun; ++j) H = fma(a[j], H, mul(na[j], xv(j)));
 #pragma unroll
       for (int j = kRun - 1; j >= 0; --j) D = mul(a[j], add(gv(j), D));
     }
@@ -108,21 +113,26 @@ __global__ void __launch_bounds__(32 * WARPS, 16 / WARPS) recurrence_grad_kernel
     // q: the state before each step, less x
     V q[kRun];
     T *ox = dx + (s0 + kRun - 1) * p.dx_step, *of = df + (s0 + kRun - 1) * p.df_step;
-    if (left < kRun || cuts) {
+    const auto give = [&](int j, V gx, V gf) {
+      const Live in{me.live.x && j < left, me.live.y && j < left};
+      put<L>(ox, gx, in);
+      put<L>(of, gf, in);
+      ox -= p.dx_step;
+      of -= p.df_step;
+    };
+    if (cuts) {
 #pragma unroll
       for (int j = 0; j < kRun; ++j) {
-        const V xj = j < left ? xv(j) : all<C>(0.f), b = mul(na[j], xj);
+        const V xj = xv(j), b = mul(na[j], xj);
         const bool cut = cuts >> j & 1;
         q[j] = sub(cut ? all<C>(0.f) : v, xj);
         v = cut ? b : fma(a[j], v, b);
       }
 #pragma unroll
-      for (int j = kRun - 1; j >= 0; --j, ox -= p.dx_step, of -= p.df_step) {
-        if (j >= left) continue;
+      for (int j = kRun - 1; j >= 0; --j) {
         l = add(gv(j), l);
         const V gx = mul(na[j], l), al = mul(a[j], l);
-        put<L>(ox, gx, me.live);
-        put<L>(of, mul(mul(a[j], gx), q[j]), me.live);
+        give(j, gx, mul(mul(na[j], al), q[j]));
         l = cuts >> j & 1 ? all<C>(0.f) : al;
       }
     } else {
@@ -133,11 +143,11 @@ __global__ void __launch_bounds__(32 * WARPS, 16 / WARPS) recurrence_grad_kernel
         v = fma(a[j], v, mul(na[j], xj));
       }
 #pragma unroll
-      for (int j = kRun - 1; j >= 0; --j, ox -= p.dx_step, of -= p.df_step) {
+      for (int j = kRun - 1; j >= 0; --j) {
         l = add(gv(j), l);
-        put<L>(ox, mul(na[j], l), me.live);
+        const V gx = mul(na[j], l);
         l = mul(a[j], l);
-        put<L>(of, mul(mul(na[j], l), q[j]), me.live);
+        give(j, gx, mul(mul(na[j], l), q[j]));
       }
     }
   }
