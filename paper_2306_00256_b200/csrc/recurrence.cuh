@@ -134,13 +134,22 @@ template <int L, bool WIDE> struct Run {
         }
       }
     } else {
-#pragma unroll
-      for (int k = lane; k < kRun * 9; k += 32) {
+      const auto copy = [&](int k) {
         const int row = k / 9, col = (k - row * 9) * 16;
         const char *from = base + row * hop;
         const int skew = (int)(reinterpret_cast<uintptr_t>(from) & 15), have = min(16, width + skew - col);
-        const bool in = row < left && have > 0;
-        copy16(to + row * kPitch + col, in ? from - skew + col : reinterpret_cast<const char *>((uintptr_t)p & ~(uintptr_t)15), in ? have : 0);
+        if (have > 0) copy16(to + row * kPitch + col, from - skew + col, have);
+      };
+      if (left == kRun) {
+#pragma unroll
+        for (int i = 0; i < kRun * 9 / 32; ++i) copy(lane + 32 * i);
+        if (lane < kRun * 9 % 32) copy(lane + kRun * 9 / 32 * 32);
+      } else {
+#pragma unroll 1
+        for (int k = lane; k < kRun * 9; k += 32) {
+          if (k / 9 < left) copy(k);
+          else *reinterpret_cast<uint4 *>(bytes + k * 16) = make_uint4(0, 0, 0, 0);
+        }
       }
     }
   }
@@ -284,8 +293,7 @@ inline cudaError_t launch_kernel(void (*kernel)(const RecurArgs), const RecurArg
 template <typename Go, int L, bool WIDE> cudaError_t choose_split(Go &go) {
   RecurArgs &p = go.p;
   p.blocks = (int32_t)ceil_div(p.d, Lanes<L>::kChannels);
-  constexpr int kMost = WIDE ? 16 : 8;   // warps that the shared memory of a CTA has room for
-  const Split s = split(go.b * p.blocks, p.t, kMost);
+  const Split s = split(go.b * p.blocks, p.t, Go::template most<WIDE>());
   p.n_tiles = ceil_div(p.t, s.warps * kRun);
   p.seg_tiles = ceil_div(p.n_tiles, s.segs);
   p.segs = (int32_t)ceil_div(p.n_tiles, p.seg_tiles);
@@ -294,9 +302,11 @@ template <typename Go, int L, bool WIDE> cudaError_t choose_split(Go &go) {
     const cudaError_t e = go.template maps<L, WIDE>();
     if (e != cudaSuccess) return e;
   }
-  if constexpr (WIDE)
+  if constexpr (Go::template most<WIDE>() >= 16)
     if (s.warps == 16) return go.template run<L, WIDE, 16>();
-  return s.warps == 8 ? go.template run<L, WIDE, 8>() : go.template run<L, WIDE, 4>();
+  if constexpr (Go::template most<WIDE>() >= 8)
+    if (s.warps == 8) return go.template run<L, WIDE, 8>();
+  return go.template run<L, WIDE, 4>();
 }
 template <typename Go> ceca_status_t choose(Go go, int in, int out, int32_t type) {
   cudaError_t e;
@@ -308,7 +318,7 @@ template <typename Go> ceca_status_t choose(Go go, int in, int out, int32_t type
 
 // Enough for every layout: the widest channel blocks and the fewest warps make the most segments.
 inline size_t maps_bytes(int64_t b, int64_t t, int64_t d) {
-  const int segs = split(b * ceil_div(d, 64), t, 8).segs;
+  const int segs = split(b * ceil_div(d, 64), t, 4).segs;
   return segs == 1 ? 0 : sizeof(float) * 2 * (size_t)b * (size_t)(segs + 1) * (size_t)d;
 }
 

@@ -114,6 +114,13 @@ __global__ void __launch_bounds__(32 * WARPS, 16 / WARPS) recurrence_grad_kernel
     V q[kRun];
     T *ox = dx + (s0 + kRun - 1) * p.dx_step, *of = df + (s0 + kRun - 1) * p.df_step;
     const auto give = [&](int j, V gx, V gf) {
+      if (L == HALVES && left == kRun) {   // (spares two predicates a step)
+        put<L>(ox, gx, me.live);
+        put<L>(of, gf, me.live);
+        ox -= p.dx_step;
+        of -= p.df_step;
+        return;
+      }
       const Live in{me.live.x && j < left, me.live.y && j < left};
       put<L>(ox, gx, in);
       put<L>(of, gf, in);
@@ -159,6 +166,8 @@ struct Backward {
   RecurArgs p;
   int64_t b;
   cudaStream_t s;
+  // the most warps of a CTA that its shared memory has room for
+  template <bool WIDE> static constexpr int most() { return WIDE ? 16 : 8; }
   template <int L, bool WIDE> cudaError_t maps() {
     static std::atomic<uint64_t> done{0};
     return launch_kernel(recurrence_map_kernel<L, WIDE, true>, p, b, 4, sizeof(MapShared<L, WIDE>), &done, s);
