@@ -295,7 +295,8 @@ ceca_status_t dsgd_embed_lookup(const void *E, const void *tokens, void *out, in
  * the sum is added to what the row holds instead, and rows without a token are not touched.
  * The positions of each token are listed in ascending order first, and the sums run over that list in an
  * order that depends on the arguments alone: results are identical from run to run.
- * workspace: device, 16-byte aligned, at least dsgd_embed_workspace_bytes(n, t, v, d) bytes.
+ * workspace: device, 16-byte aligned, at least dsgd_embed_workspace_bytes(n, t, v, d) bytes (0, and then NULL
+ * will do, for short sequences).
  * Errors: as above, and CECA_ERR_WORKSPACE; agent_stride must keep the agents' tables apart (n > 1).
  */
 ceca_status_t dsgd_embed_grad(const void *dout, const void *tokens, void *dE, int32_t n, int64_t t, int64_t v,
@@ -304,7 +305,7 @@ ceca_status_t dsgd_embed_grad(const void *dout, const void *tokens, void *dE, in
                               int32_t tokens_type, int32_t out_type, float scale, int32_t accumulate,
                               void *workspace, size_t workspace_bytes, void *stream);
 
-/* Host function.  Minimum workspace size of dsgd_embed_grad in bytes (0 for sizes it refuses). */
+/* Host function.  Minimum workspace size of dsgd_embed_grad in bytes (0 also for sizes it refuses). */
 size_t dsgd_embed_workspace_bytes(int32_t n, int64_t t, int64_t v, int64_t d);
 
 /*

@@ -103,19 +103,21 @@ template <int D> __device__ __forceinline__ float top_of(const Vec<bf16> *v) {
   return fmaxf(__low2float(m), __high2float(m));
 }
 
-// What one thread has seen: sum counts 2^(z c - k), k = m c.
+// What one thread has seen: sum counts 2^(z c - k), k = m c.  m is the largest of the first vectors that are not masked, not of all: a frame
+// does not have to be the maximum, only near enough that no sum overflows, and if one does the row goes the way of `far`.
 struct Seen {
   float m = -kFar, k;
   Val<2> sum{0.f, 0.f};
   __device__ __forceinline__ explicit Seen(float scale) { k = m * scale; }
-  template <int D, typename T> __device__ __forceinline__ void take(const Vec<T> *a, float scale) {
+  template <int D, typename T> __device__ __forceinline__ void frame(const Vec<T> *a, float scale) {
     const float top = top_of<D>(a);
     if (top > m) {
-      const float was = k;
+      sum = mul(sum, all<2>(ex2(k - top * scale)));   // (an edge element may be in it)
       m = top;
       k = m * scale;
-      sum = mul(sum, all<2>(ex2(was - k)));
     }
+  }
+  template <int D, typename T> __device__ __forceinline__ void take(const Vec<T> *a, float scale) {
     const Val<2> shift = all<2>(-k), by = all<2>(scale);
 #pragma unroll
     for (int u = 0; u < D; ++u)
@@ -359,6 +361,7 @@ __global__ void __launch_bounds__(THREADS, 768 / THREADS) distill_kernel(const D
         if (mask) strike(a[u], mask);
       }
     }
+    if (seen.m == -kFar) seen.frame<kDeep>(a, p.scale);   // nothing but masked logits before
     seen.take<kDeep>(a, p.scale);
   }
   // the warp's part in its own frame, then everybody's
@@ -398,9 +401,9 @@ __global__ void __launch_bounds__(THREADS, 768 / THREADS) distill_kernel(const D
   };
   gather();
   float M = all_of.m;
-  const bool far = !(fabsf(M) < kFar);
+  const bool far = !(fabsf(M) < kFar && all_of.sum < INFINITY);
   const auto exponent = [&](float v) { return far ? (v - M) * p.scale : fmaf(v, p.scale, -(M * p.scale)); };
-  if (far) {   // logits beyond +-kFar only (or infinite, or NaN): once more, element by element
+  if (far) {   // logits beyond +-kFar only, an overflow (or infinities, or NaN): once more, element by element
     float top = -INFINITY;
     const int64_t s1 = min((int64_t)slot1, p.v + part.pad);
     for (int64_t s = max((int64_t)slot0, (int64_t)part.pad) + tid; s < s1; s += THREADS) top = fmaxf(top, widen(z[s - part.pad]));

@@ -67,6 +67,17 @@ def _starts(starts, shape):
     return _dense(starts, "starts", shape, _U8)
 
 
+def _workspace(bytes_of, sizes, workspace, like, stream):
+    """(tensor or None, address, bytes): the caller's workspace, or one allocated here where the sizes need it."""
+    if workspace is None:
+        size = bytes_of(*sizes)
+        if size == 0:
+            return None, None, 0
+        workspace = _empty(size, _U8, like, stream)
+        return workspace, workspace.data_ptr(), size
+    return workspace, workspace.data_ptr(), workspace.numel() * workspace.element_size()
+
+
 def _check(status, where):
     if status != 0:
         raise CecaError(status, where)
@@ -98,7 +109,7 @@ def dsgd_embed_workspace_bytes(n, t, v, d):
 def dsgd_embed_grad(dout, tokens, dE, scale=1.0, accumulate=False, workspace=None, stream=None):
     """The gradient of dsgd_embed_lookup: writes (or, with accumulate, adds) scale times the sum of dout's rows
     over each token's positions into dE [n, v, d], and returns it.  workspace: device memory of
-    dsgd_embed_workspace_bytes(n, t, v, d) bytes, allocated here when it is None."""
+    dsgd_embed_workspace_bytes(n, t, v, d) bytes, allocated here when it is None and the sizes need one."""
     if dE.dim() != 3 or tokens.dim() != 2 or tokens.shape[0] != dE.shape[0]:
         raise ValueError("dE must be [n, v, d] and tokens [n, t]")
     (n, v, d), t = dE.shape, tokens.shape[1]
@@ -107,13 +118,9 @@ def dsgd_embed_grad(dout, tokens, dE, scale=1.0, accumulate=False, workspace=Non
     (te, se), (ti, st), (to, so) = _rows(dE, "dE"), _rows(tokens, "tokens", _INDEX), _rows(dout, "dout")
     s = _here(stream, dE, tokens, dout, workspace)
     lib = library()
-    if workspace is None:
-        size = lib.dsgd_embed_workspace_bytes(n, t, v, d)
-        workspace = _empty(size, _U8, dE, stream)
-    else:
-        size = workspace.numel() * workspace.element_size()
+    workspace, pw, size = _workspace(lib.dsgd_embed_workspace_bytes, (n, t, v, d), workspace, dE, stream)
     _check(lib.dsgd_embed_grad(dout.data_ptr(), tokens.data_ptr(), dE.data_ptr(), n, t, v, d, se[0], se[1], st[0], so[0], so[1],
-                               te, ti, to, scale, 1 if accumulate else 0, workspace.data_ptr(), size, s), "dsgd_embed_grad")
+                               te, ti, to, scale, 1 if accumulate else 0, pw, size, s), "dsgd_embed_grad")
     return dE
 
 
@@ -125,23 +132,12 @@ def dsgd_recurrence_workspace_bytes(b, t, d):
     return int(library().dsgd_recurrence_workspace_bytes(b, t, d))
 
 
-def _recurrence_workspace(lib, workspace, x, shape, stream):
-    """(tensor or None, address, bytes): the caller's workspace, or one allocated here where the sizes need it."""
-    if workspace is None:
-        size = lib.dsgd_recurrence_workspace_bytes(*shape)
-        if size == 0:
-            return None, None, 0
-        workspace = _empty(size, _U8, x, stream)
-        return workspace, workspace.data_ptr(), size
-    return workspace, workspace.data_ptr(), workspace.numel() * workspace.element_size()
-
-
 def dsgd_recurrence(x, f, h0=None, starts=None, h=None, h_last=None, save=False, workspace=None, stream=None):
     """h[:, s] = keep * h[:, s-1] + (1 - sigmoid(f[:, s])) * x[:, s], keep = sigmoid(f[:, s]) or 0 where starts is set,
     for x, f [b, t, d] of one type (float32 or bfloat16).  h0: float32 [b, d]; starts: uint8 or bool [b, t].
     Returns (h, h_last, marks): h like x, h_last the float32 state after the last step, marks what
     dsgd_recurrence_grad starts from (None unless save).  One new token is t = 1 with h0 = h_last = the kept state.
-    workspace: device memory of dsgd_recurrence_workspace_bytes(b, t, d) bytes, allocated here when it is None."""
+    workspace: device memory of dsgd_recurrence_workspace_bytes(b, t, d) bytes, allocated here when it is None and the sizes need one."""
     shape, dtype = x.shape, x.dtype
     if len(shape) != 3 or f.shape != shape or f.dtype != dtype:
         raise ValueError("x and f must be [b, t, d] of one type")
@@ -162,7 +158,7 @@ def dsgd_recurrence(x, f, h0=None, starts=None, h=None, h_last=None, save=False,
         pl = _dense(h_last, "h_last", (b, d))
     lib = library()
     marks = _empty((b, lib.dsgd_recurrence_marks(t), d), _F32, x, stream) if save else None
-    workspace, pw, size = _recurrence_workspace(lib, workspace, x, shape, stream)
+    workspace, pw, size = _workspace(lib.dsgd_recurrence_workspace_bytes, shape, workspace, x, stream)
     _check(lib.dsgd_recurrence(x.data_ptr(), f.data_ptr(), p0, ps, h.data_ptr(), pl, None if marks is None else marks.data_ptr(), b,
                                t, d, sx[0], sx[1], sf[0], sf[1], sh[0], sh[1], code, pw, size, s), "dsgd_recurrence")
     return h, h_last, marks
@@ -196,7 +192,7 @@ def dsgd_recurrence_grad(x, f, dh, marks, h0=None, starts=None, dh_last=None, dx
         p0 = dh0.data_ptr()
     else:
         p0 = _dense(dh0, "dh0", (b, d))
-    workspace, pw, size = _recurrence_workspace(lib, workspace, x, shape, stream)
+    workspace, pw, size = _workspace(lib.dsgd_recurrence_workspace_bytes, shape, workspace, x, stream)
     _check(lib.dsgd_recurrence_grad(x.data_ptr(), f.data_ptr(), dh.data_ptr(), pm, ps, pl, dx.data_ptr(), df.data_ptr(), p0, b, t, d,
                                     sx[0], sx[1], sf[0], sf[1], sg[0], sg[1], sdx[0], sdx[1], sdf[0], sdf[1], code, pw, size, s),
            "dsgd_recurrence_grad")

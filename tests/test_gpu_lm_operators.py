@@ -55,6 +55,7 @@ def _untouched(view, buf):
 EMBED = [  # n, t, v, d
     (1, 1, 1, 1), (2, 5, 3, 7), (3, 64, 100, 32), (1, 300, 17, 129), (4, 129, 1025, 64), (2, 1000, 5000, 96),
     (5, 33, 513, 250), (1, 2000, 40, 260), (2, 77, 4099, 1031), (1, 40, 70000, 16), (1, 4097, 300, 512), (3, 9, 65, 2056),
+    (2, 256, 30, 40), (1, 257, 30, 1048), (1, 9000, 20000, 24),
 ]
 
 
@@ -92,9 +93,10 @@ def test_embedding_lookup_and_gradient(n, t, v, d, te, to, ti):
 
 @pytest.mark.parametrize("te,to", [(F32, F32), (BF16, BF16), (F32, BF16)])
 @pytest.mark.parametrize("pad,offset", [(0, 0), (8, 16), (3, 1), (5, 2)])
-def test_embedding_in_a_block_of_parameter_columns(te, to, pad, offset):
+@pytest.mark.parametrize("t", [50, 300])
+def test_embedding_in_a_block_of_parameter_columns(te, to, pad, offset, t):
     # the table of every agent is a block of columns of its row of X, and out a padded activation
-    n, t, v, d = 3, 50, 41, 64
+    n, v, d = 3, 41, 64
     ld = v * d + 100 + pad
     E, _ = _inside((n, v, d), (ld, d, 1), offset, te)
     E.copy_(_randn((n, v, d), te, 5))
@@ -134,9 +136,10 @@ def test_embedding_of_empty_positions_only():
 
 @pytest.mark.parametrize("te,to", [(F32, BF16), (BF16, F32)])
 @pytest.mark.parametrize("hot", [1, 2, 5])
-def test_embedding_gradient_of_a_few_frequent_tokens(te, to, hot):
-    # lists far longer than a block takes, next to rows with none
-    n, t, v, d = 2, 9001, 50, 72
+@pytest.mark.parametrize("t", [200, 9001])
+def test_embedding_gradient_of_a_few_frequent_tokens(te, to, hot, t):
+    # lists far longer than a warp takes, next to rows with none
+    n, v, d = 2, 50, 72
     tok = (torch.arange(n * t).reshape(n, t) % hot * 7).to(torch.int32).to(DEV)
     dout = _randn((n, t, d), to, 8)
     dE = torch.empty((n, v, d), dtype=te, device=DEV)

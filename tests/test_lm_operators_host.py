@@ -90,7 +90,7 @@ def test_lookup_refuses(change):
 @pytest.mark.parametrize("change,status", [(c, INVALID) for c in [
     dict(dout=None), dict(tokens=None), dict(dE=None), dict(n=0), dict(t=-1), dict(t=BIG), dict(v=0), dict(v=BIG), dict(d=0), dict(agent=127), dict(agent=0),
     dict(row=15), dict(tok=-1), dict(o_row=-1), dict(te=2), dict(ti=-1), dict(to=9)]] + [
-    (dict(ws=None), WORKSPACE), (dict(size=8), WORKSPACE), (dict(ws=ctypes.c_void_p(4104)), WORKSPACE)])
+    (dict(t=4000, ws=None), WORKSPACE), (dict(t=4000, size=8), WORKSPACE), (dict(t=4000, ws=ctypes.c_void_p(4104)), WORKSPACE)])
 def test_lookup_gradient_refuses(change, status):
     assert _call("dsgd_embed_grad", GRAD, **change) == status
 
@@ -142,7 +142,7 @@ def test_sizes():
     assert ceca.dsgd_recurrence_marks(100000) > ceca.dsgd_recurrence_marks(1000) >= 1
     assert ceca.dsgd_recurrence_workspace_bytes(64, 1000, 2048) == 0 and ceca.dsgd_recurrence_workspace_bytes(1, 1, 64) == 0
     assert ceca.dsgd_recurrence_workspace_bytes(0, 100, 64) == 0
-    assert ceca.dsgd_embed_workspace_bytes(2, 100, 1000, 64) >= 4 * (2 * 100 + 2 * 1001)
+    assert ceca.dsgd_embed_workspace_bytes(2, 1000, 1000, 64) >= 4 * (2 * 1000 + 2 * 1001) and ceca.dsgd_embed_workspace_bytes(2, 1, 1000, 64) == 0
     for bad in ((0, 1, 1, 1), (1, -1, 1, 1), (1, 1, 0, 1), (1, 1, 1, 0), (1, BIG, 1, 1)):
         assert ceca.dsgd_embed_workspace_bytes(*bad) == 0
 
