@@ -302,8 +302,9 @@ __global__ void __launch_bounds__(THREADS, 768 / THREADS) distill_kernel(const D
     if (here) {
       const uint32_t b = (uint32_t)((slot - slot0) & (kMaxBits - 1));
       again |= atomicOr(bitmap + (b >> 5), 1u << (b & 31)) >> (b & 31) & 1;
-      en.z[j] = widen(z[at]);
-      if (HELD && tail && slot >= (int64_t)part.w0 * N && slot < (int64_t)part.w1 * N) narrow(held + slot, -INFINITY);
+      const bool kept = HELD && slot >= (int64_t)part.w0 * N && slot < (int64_t)part.w1 * N;
+      en.z[j] = kept && !tail ? widen(held[slot]) : widen(z[at]);   // (listed twice, it is -infinity there by now)
+      if (kept && tail) narrow(held + slot, -INFINITY);
     }
   }
   tmax = warp_max(tmax);
@@ -520,6 +521,13 @@ template <typename TZ, int THREADS, bool CLUSTER, bool HELD> cudaError_t launch(
 template <typename TZ> cudaError_t launch_rows(DistillArgs p, int64_t r, cudaStream_t s) {
   constexpr int N = Vec<TZ>::N;
   const int64_t vectors = ceil_div(p.v + N - 1, N);   // of the row on the least fortunate boundary
+  // The loss alone needs no second pass, and nothing held: a CTA streams a row, as long as there are rows for all SMs.
+  if (!p.dz && r >= 4 * sm_count() && 16 * vectors > kHeld / 2) {
+    p.cluster = 1;
+    p.per = (int32_t)vectors;
+    p.words = (int32_t)(std::min(kMaxBits, ceil_div(vectors * N, 128) * 128) / 32);
+    return launch<TZ, 128, false, false>(p, r, s);
+  }
   // CTAs per row: what holds the row, and more where the rows leave SMs empty and a part is still 16 vectors a thread
   p.cluster = 1;
   while (p.cluster < kMaxCluster && (16 * ceil_div(vectors, p.cluster) > kHeld ||
