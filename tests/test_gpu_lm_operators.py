@@ -416,6 +416,25 @@ def test_distillation_loss_and_gradient(r, v, k, dtype, tail, temperature, tt, t
     _distill_check(z, idx, t, lse, None, temperature, "no weights: ")
 
 
+@pytest.mark.parametrize("r,v", [(600, 9001), (2400, 130), (900, 1001), (700, 3000)])   # more rows than the GPU holds at a time
+@pytest.mark.parametrize("dtype,tail", [(F32, True), (BF16, False), (BF16, True)])
+def test_distillation_of_many_rows(r, v, dtype, tail):
+    z, idx, t, lse, w = _distill_inputs(r, v, 5, dtype, tail, 21)
+    w[::7] = 0
+    idx[5, 3], idx[5, 4] = 9, 9
+    _distill_check(z, idx, t, lse, w, 1.0)
+
+
+@pytest.mark.parametrize("v", [70000, 250000])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_distillation_logits_further_apart_than_an_exponential_reaches(v, dtype):
+    # what a thread sees first says nothing about what comes later: sums of 2^((z - m) c) from its first logits overflow
+    z, idx, t, _, _ = _distill_inputs(2, v, 6, dtype, False, 23)
+    z[0, -300:] += 400.0
+    z[1, v // 2] = 1000.0
+    _distill_check(z, idx, t, None, None, 1.0)
+
+
 @pytest.mark.parametrize("dtype", [F32, BF16])
 @pytest.mark.parametrize("tail", [False, True])
 @pytest.mark.parametrize("v", [300, 40001])
