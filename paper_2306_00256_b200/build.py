@@ -1,4 +1,5 @@
-"""Builds the CUDA library (sm_100a only) in-tree with nvcc: libceca_b200.so next to this file."""
+"""Builds in-tree, next to this file: the CUDA library (sm_100a only) with nvcc, libceca_b200.so, and the Python module of
+the language-model operators with g++ and torch's headers, _lm_module.so."""
 import glob
 import os
 import subprocess
@@ -7,6 +8,9 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libceca_b200.so")
+MODULE_NAME = "_lm_module"
+MODULE = os.path.join(HERE, MODULE_NAME + ".so")
+MODULE_SOURCE = os.path.join(CSRC, "lm_module.cc")
 
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "-Xptxas=-v", "-shared", "-Xcompiler", "-fPIC", "--threads", "8"]
@@ -17,11 +21,37 @@ def sources():
 
 
 def is_stale():
-    if not os.path.exists(LIB):
+    if not os.path.exists(LIB) or not os.path.exists(MODULE):
         return True
-    deps = (sources() + glob.glob(os.path.join(CSRC, "*.h")) + glob.glob(os.path.join(CSRC, "*.cuh")) +
-            [os.path.join(ROOT, "include", "ceca.h")])
-    return any(os.path.getmtime(f) > os.path.getmtime(LIB) for f in deps)
+    header = os.path.join(ROOT, "include", "ceca.h")
+    deps = sources() + glob.glob(os.path.join(CSRC, "*.h")) + glob.glob(os.path.join(CSRC, "*.cuh")) + [header]
+    return (any(os.path.getmtime(f) > os.path.getmtime(LIB) for f in deps) or
+            any(os.path.getmtime(f) > os.path.getmtime(MODULE) for f in (MODULE_SOURCE, header)))
+
+
+def module_command(out):
+    """The g++ command of the Python module: torch's own headers and libraries, the CUDA library by its place."""
+    import sysconfig
+
+    import torch
+    root = os.path.join(os.path.dirname(torch.__file__))
+    includes = [os.path.join(root, "include"), os.path.join(root, "include", "torch", "csrc", "api", "include"),
+                sysconfig.get_paths()["include"], os.path.join(os.environ.get("CUDA_HOME", "/usr/local/cuda"), "include"),
+                os.path.join(ROOT, "include")]
+    libs = os.path.join(root, "lib")
+    return (["g++", "-O2", "-std=c++17", "-shared", "-fPIC", "-DTORCH_EXTENSION_NAME=" + MODULE_NAME, "-DTORCH_API_INCLUDE_EXTENSION_H",
+             "-D_GLIBCXX_USE_CXX11_ABI=%d" % int(torch._C._GLIBCXX_USE_CXX11_ABI)] + ["-I" + i for i in includes] +
+            [MODULE_SOURCE, "-o", out, "-L" + libs, "-ltorch_python", "-ltorch", "-ltorch_cpu", "-lc10_cuda", "-lc10",
+             "-L" + HERE, "-l:" + os.path.basename(LIB), "-Wl,-rpath,$ORIGIN:" + libs])
+
+
+def _run(what, cmd, verbose):
+    res = subprocess.run(cmd, capture_output=True, text=True)
+    if verbose or res.returncode != 0:
+        print(res.stdout)
+        print(res.stderr)
+    if res.returncode != 0:
+        raise RuntimeError(what + " failed")
 
 
 def build(force=False, verbose=False):
@@ -29,14 +59,11 @@ def build(force=False, verbose=False):
         return LIB
     nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
     tmp = LIB + ".tmp.%d" % os.getpid()
-    cmd = [nvcc] + NVCC_FLAGS + ["-I", os.path.join(ROOT, "include"), "-I", CSRC, "-o", tmp] + sources()
-    res = subprocess.run(cmd, capture_output=True, text=True)
-    if verbose or res.returncode != 0:
-        print(res.stdout)
-        print(res.stderr)
-    if res.returncode != 0:
-        raise RuntimeError("nvcc failed")
+    _run("nvcc", [nvcc] + NVCC_FLAGS + ["-I", os.path.join(ROOT, "include"), "-I", CSRC, "-o", tmp] + sources(), verbose)
     os.replace(tmp, LIB)
+    tmp = MODULE + ".tmp.%d" % os.getpid()
+    _run("g++", module_command(tmp), verbose)
+    os.replace(tmp, MODULE)
     return LIB
 
 
