@@ -50,7 +50,6 @@ constexpr int kFill = 64;      // table rows
 constexpr int kJoin = 8;       // chunks
 constexpr int kFew = 256;      // positions
 constexpr int kFewRows = 16;   // table rows of a CTA
-constexpr int kLookupPacks = 4;
 constexpr int kDeep = 4;       // rows of dout that a warp has on their way at a time
 constexpr int kListThreads = 1024;
 constexpr int kListWarps = kListThreads / 32;
@@ -109,9 +108,11 @@ template <int V> struct Slice {
   static constexpr int U = V == 8 ? 2 : V == 4 ? 4 : 8, kElements = 32 * U * V;
 };
 
+template <int V> constexpr int kLookupPacks = V == 1 ? 16 : 4;   // that a lane has on their way at a time
+
 template <typename TE, typename TO, typename TI, int V>
 __global__ void __launch_bounds__(kThreads) embed_lookup_kernel(const EmbedArgs p) {
-  constexpr int U = kLookupPacks;
+  constexpr int U = kLookupPacks<V>;
   const int lane = threadIdx.x & 31;
   const int64_t units = (int64_t)p.n * p.t * p.slices, step = (int64_t)gridDim.x * kWarps;
   const auto token = [&](int64_t unit) -> int64_t {   // of the unit's position
@@ -255,6 +256,22 @@ template <typename TE, int V> __device__ __forceinline__ void finish_row(const E
     }
 }
 
+// Zeros for the columns [c, c + count) of a row, by a warp: rows on any boundary get 16 bytes at a time too.
+template <typename TE, int V> __device__ __forceinline__ void zero_row(TE *g, int64_t count) {
+  const int lane = threadIdx.x & 31;
+  if (V > 1) {
+    const float zero[V] = {};
+    for (int64_t c = lane * V; c < count; c += 32 * V) put<TE, V>(g + c, zero);
+    return;
+  }
+  const int64_t head = min(count, (int64_t)((16 - (reinterpret_cast<uintptr_t>(g) & 15)) & 15) / (int64_t)sizeof(TE));
+  constexpr int N = 16 / sizeof(TE);
+  const int64_t whole = (count - head) / N, tail = head + whole * N;
+  if (lane < head) narrow(g + lane, 0.f);
+  for (int64_t k = lane; k < whole; k += 32) reinterpret_cast<uint4 *>(g + head)[k] = make_uint4(0, 0, 0, 0);
+  if (tail + lane < count) narrow(g + tail + lane, 0.f);
+}
+
 // Block (x, slice, agent): kFewRows rows, a warp each in turn, for agents with at most kFew positions.
 template <typename TE, typename TO, typename TI, int V> __global__ void __launch_bounds__(kThreads) embed_few_kernel(const EmbedArgs p) {
   constexpr int U = Slice<V>::U;
@@ -347,13 +364,9 @@ template <typename TE, typename TO, int V> __global__ void __launch_bounds__(kTh
     const int64_t row = r0 + warp + lane * kWarps;
     const bool empty = lane < kRows && row < p.v && start[row] == start[row + 1];
     uint32_t todo = __ballot_sync(0xffffffffu, empty);
-    const float zero[V] = {};
-    for (; todo; todo &= todo - 1) {
-      TE *g = table + (r0 + warp + (__ffs(todo) - 1) * kWarps) * p.table_row;
-#pragma unroll
-      for (int u = 0; u < U; ++u)
-        if (c0 + u * 32 * V < p.d) put<TE, V>(g + u * 32 * V, zero);
-    }
+    const int64_t width = min((int64_t)Slice<V>::kElements, p.d - (int64_t)blockIdx.y * Slice<V>::kElements);
+    for (; todo; todo &= todo - 1)
+      zero_row<TE, V>(table - lane * V + (r0 + warp + (__ffs(todo) - 1) * kWarps) * p.table_row, width);
     return;
   }
   const int j = blockIdx.x * kWarps + warp, chunk = p.chunk;
@@ -481,7 +494,7 @@ int pack_of(const EmbedArgs &p, const void *table, int64_t te, const void *out, 
 }
 
 template <typename TE, typename TO, typename TI, int V> cudaError_t launch_lookup(EmbedArgs p, cudaStream_t s) {
-  p.slices = (int32_t)ceil_div(p.d, 32 * kLookupPacks * V);
+  p.slices = (int32_t)ceil_div(p.d, 32 * kLookupPacks<V> * V);
   const int64_t units = (int64_t)p.n * p.t * p.slices;
   const int grid = (int)std::min<int64_t>(ceil_div(units, kWarps), (int64_t)sm_count() * 8);
   embed_lookup_kernel<TE, TO, TI, V><<<grid, kThreads, 0, s>>>(p);
