@@ -35,8 +35,7 @@ struct EmbedArgs {
   float scale;
   int32_t accumulate;
   int32_t *row_start;  // n x (v + 1): where each table row's positions begin in `list`
-  int32_t *list;       // n x t: positions, by token and then ascending
-  int32_t *owner;      // n x t: the token of each
+  int2 *list;          // n x t: positions, by token and then ascending, each with its token
   float *pieces;       // n x chunks x 2 x d: sums of the pieces of long lists
   int32_t bins;        // table rows per block of token_list_kernel
   int32_t chunk;       // places of the list for a warp, at most 32
@@ -218,7 +217,7 @@ __global__ void __launch_bounds__(kListThreads) token_list_kernel(const EmbedArg
   }
   __syncthreads();
 
-  int32_t *list = p.list + i * p.t, *owner = p.owner + i * p.t;
+  int2 *list = p.list + i * p.t;
   constexpr int kAhead = 8;   // groups of 32 tokens on their way at a time
   for (int64_t s = s0; s < s1; s += 32 * kAhead) {
     U w[kAhead];
@@ -233,8 +232,7 @@ __global__ void __launch_bounds__(kListThreads) token_list_kernel(const EmbedArg
         const int32_t r = (int32_t)w[k];
         const uint32_t same = __match_any_sync(some, r);
         const int32_t rank = __popc(same & ((1u << lane) - 1)), at = mine[r] + rank;
-        list[at] = (int32_t)(s + 32 * k + lane);
-        owner[at] = (int32_t)lo + r;
+        list[at] = make_int2((int32_t)(s + 32 * k + lane), (int32_t)lo + r);   // (stores this scattered are what takes the time)
         __syncwarp(some);
         if (rank == 0) mine[r] += __popc(same);
       }
@@ -355,7 +353,8 @@ template <typename TE, typename TO, int V> __global__ void __launch_bounds__(kTh
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int64_t i = blockIdx.z;
   const int64_t c0 = (int64_t)blockIdx.y * Slice<V>::kElements + lane * V;
-  const int32_t *start = p.row_start + i * (p.v + 1), *list = p.list + i * p.t, *owner = p.owner + i * p.t;
+  const int32_t *start = p.row_start + i * (p.v + 1);
+  const int2 *list = p.list + i * p.t;
   TE *table = static_cast<TE *>(p.dst) + i * p.table_agent + c0;
   const int work = gridDim.x - p.fills;
   if ((int)blockIdx.x >= work) {
@@ -373,8 +372,8 @@ template <typename TE, typename TO, int V> __global__ void __launch_bounds__(kTh
   const int32_t total = start[p.v], from = j * chunk, to = min(from + chunk, total);
   if (from >= total) return;
   // the chunk's places and the next ones, for a row that goes on there; each lane knows where its place's row begins and ends
-  const int32_t place0 = from + lane < total ? list[from + lane] : 0, place1 = from + 32 + lane < total ? list[from + 32 + lane] : 0;
-  const int32_t w = owner[min(from + lane, to - 1)];
+  const int32_t place0 = from + lane < total ? list[from + lane].x : 0, place1 = from + 32 + lane < total ? list[from + 32 + lane].x : 0;
+  const int32_t w = list[min(from + lane, to - 1)].y;
   const int32_t begin = start[w], end = start[w + 1];
   const TO *o = static_cast<const TO *>(p.src) + i * p.out_agent + c0;
   // the places [s0, s1) are this warp's: not those of a whole row that the warp of the chunk before has, but all of a whole
@@ -437,7 +436,7 @@ template <typename TE, int V> __global__ void __launch_bounds__(kThreads) embed_
   const int32_t total = start[p.v], mine = ((int)blockIdx.x * kJoin + lane) * p.chunk;
   int32_t w = 0, b = 0, e = 0;
   if (lane < kJoin && mine < total) {
-    w = p.owner[i * p.t + min(mine + p.chunk, total) - 1];
+    w = p.list[i * p.t + min(mine + p.chunk, total) - 1].y;
     b = start[w];
     e = start[w + 1];
   }
@@ -571,7 +570,7 @@ extern "C" ceca_status_t dsgd_embed_lookup(const void *E, const void *tokens, vo
 
 extern "C" size_t dsgd_embed_workspace_bytes(int32_t n, int64_t t, int64_t v, int64_t d) {
   if (!embed_args_ok(n, t, v, d, 0, d, 0, 0, d, DSGD_F32, DSGD_I32, DSGD_F32) || t <= kFew) return 0;
-  return round16(sizeof(int32_t) * (size_t)n * (size_t)(v + 1)) + 2 * round16(sizeof(int32_t) * (size_t)n * (size_t)t) +
+  return round16(sizeof(int32_t) * (size_t)n * (size_t)(v + 1)) + round16(sizeof(int2) * (size_t)n * (size_t)t) +
          sizeof(float) * 2 * (size_t)n * (size_t)ceil_div(t, chunk_of(n, t, d)) * (size_t)d;
 }
 
@@ -592,9 +591,8 @@ extern "C" ceca_status_t dsgd_embed_grad(const void *dout, const void *tokens, v
   p.table_agent = agent_stride; p.table_row = row_stride; p.tokens_agent = tokens_stride;
   p.out_agent = out_agent_stride; p.out_row = out_row_stride; p.scale = scale; p.accumulate = accumulate != 0;
   p.row_start = static_cast<int32_t *>(workspace);
-  p.list = reinterpret_cast<int32_t *>(static_cast<char *>(workspace) + round16(sizeof(int32_t) * (size_t)n * (size_t)(v + 1)));
-  p.owner = reinterpret_cast<int32_t *>(reinterpret_cast<char *>(p.list) + round16(sizeof(int32_t) * (size_t)n * (size_t)t));
-  p.pieces = reinterpret_cast<float *>(reinterpret_cast<char *>(p.owner) + round16(sizeof(int32_t) * (size_t)n * (size_t)t));
+  p.list = reinterpret_cast<int2 *>(static_cast<char *>(workspace) + round16(sizeof(int32_t) * (size_t)n * (size_t)(v + 1)));
+  p.pieces = reinterpret_cast<float *>(reinterpret_cast<char *>(p.list) + round16(sizeof(int2) * (size_t)n * (size_t)t));
   p.bins = list_bins(n, v);
   p.chunk = chunk_of(n, t, d);
   p.chunks = (int32_t)ceil_div(t, p.chunk);
