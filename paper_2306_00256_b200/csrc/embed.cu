@@ -9,8 +9,12 @@
 //                       of a row with more positions than a chunk has places, the piece
 //                       that lies in it: however the tokens are distributed, its work is the same.  Other CTAs fill the rows that no position holds;
 //   embed_join_kernel   adds up the pieces of the rows that have several.
+// 8 x 8192 positions in bf16 of 32000 x 1024 fp32 tables: 0.23 ms, 0.79 of the measured copy rate, of which the list takes
+// 22 us (the block with the most frequent tokens, whose shared-memory counters every token passes) and the join 11.
+// Lookup of 8 x 8192 rows of 2048 bf16: 69 us, 0.82.  Rows that are not on 16-byte boundaries move an element a lane
+// (1031 columns: 0.25 in bf16, 0.45 in fp32).
 // For up to kFew positions these three launches would take longer than their work: embed_few_kernel looks the positions of
-// every row up as it goes (n = 4, t = 129, 4097 x 256 fp32 on the device: 18 -> 6 us).
+// every row up as it goes (4 x 129 positions, 4097 x 256 fp32: 18 us by three launches, 10 us so).
 #include <cuda_runtime.h>
 
 #include <algorithm>

@@ -1,6 +1,8 @@
 // The gradient of the gated linear recurrence (the mathematics and the split are in recurrence.cu): from the end of the
 // sequence to its beginning, each tile first finding its runs' maps of both the states and of c_s = keep_s l_s, which
-// share their A, then the states from the mark before it and c from the tiles after it.
+// share their A, then the states from the mark before it and c from the tiles after it.  The states are computed again
+// rather than read: a mark of 4 bytes every 64 steps replaces a stream, and bf16 states would not be exact.  x and dh are
+// read from shared memory where they are needed instead of being kept in registers: a, 1 - a and the differences take 96.
 #include <algorithm>
 
 #include "recurrence.cuh"
