@@ -36,7 +36,7 @@ constexpr int kFewSteps = 16;   // sequences up to here: one thread per channel
 
 // Shared memory of a CTA: the runs on their way, then the exchange.
 template <int L, bool WIDE, int WARPS> struct Shared {
-  static constexpr int kStages = WARPS == 16 || (WARPS == 8 && !WIDE) ? 2 : 3;
+  static constexpr int kStages = WARPS == 16 || !WIDE ? 2 : 3;
   Run<L, WIDE> runs[WARPS][kStages][2];   // x and f
   Exchange<L, WARPS> ex;
 };
@@ -173,6 +173,7 @@ struct Forward {
   cudaStream_t s;
   // the most warps of a CTA that its shared memory has room for
   template <bool WIDE> static constexpr int most() { return WIDE ? 16 : 8; }
+  template <bool WIDE> static constexpr int resident() { return 4; }   // CTAs of 4 warps on an SM
   template <int L, bool WIDE> cudaError_t maps() {
     static std::atomic<uint64_t> done{0};
     return launch_kernel(recurrence_map_kernel<L, WIDE, false>, p, b, 4, sizeof(MapShared<L, WIDE>), &done, s);

@@ -269,15 +269,16 @@ inline int alignment(const void *base, int64_t seq, int64_t step, int32_t type) 
 
 // How a call is split: the warps of a CTA and the segments of a sequence.  An SM holds 16 warps of the kernels that
 // compute the outputs and wants at least 12, better in CTAs of 4 whose phases overlap.  Where there are too few channel
-// blocks for that, a CTA gets 8 or 16 warps; where these do not do either, the sequences are cut into segments, whose
-// maps a first kernel finds (it reads two of the streams once more).
+// blocks for that, a CTA gets 8 or 16 warps, up to `most`; where these do not do either, the sequences are cut into
+// segments, as many as make `resident` CTAs of 4 warps for every SM, whose maps a first kernel finds (it reads two of the
+// streams once more).
 constexpr int64_t kSms = 148, kWanted = 12 * kSms, kMaxSegs = 128;
 struct Split { int warps, segs; };
-inline Split split(int64_t chains, int64_t t, int most) {
+inline Split split(int64_t chains, int64_t t, int most, int resident) {
   const int64_t runs = ceil_div(t, kRun);
   for (int w = 4; w <= most; w *= 2)
     if (chains * w >= kWanted && w <= std::max<int64_t>(4, runs)) return {w, 1};
-  return {4, (int)std::max<int64_t>(1, std::min({4 * kSms / chains, ceil_div(runs, 4), kMaxSegs}))};
+  return {4, (int)std::max<int64_t>(1, std::min({resident * kSms / chains, ceil_div(runs, 4), kMaxSegs}))};
 }
 
 inline cudaError_t launch_kernel(void (*kernel)(const RecurArgs), const RecurArgs &p, int64_t b, int warps, int bytes,
@@ -293,7 +294,7 @@ inline cudaError_t launch_kernel(void (*kernel)(const RecurArgs), const RecurArg
 template <typename Go, int L, bool WIDE> cudaError_t choose_split(Go &go) {
   RecurArgs &p = go.p;
   p.blocks = (int32_t)ceil_div(p.d, Lanes<L>::kChannels);
-  const Split s = split(go.b * p.blocks, p.t, Go::template most<WIDE>());
+  const Split s = split(go.b * p.blocks, p.t, Go::template most<WIDE>(), Go::template resident<WIDE>());
   p.n_tiles = ceil_div(p.t, s.warps * kRun);
   p.seg_tiles = ceil_div(p.n_tiles, s.segs);
   p.segs = (int32_t)ceil_div(p.n_tiles, p.seg_tiles);
@@ -318,14 +319,14 @@ template <typename Go> ceca_status_t choose(Go go, int in, int out, int32_t type
 
 // Enough for every layout: the widest channel blocks and the fewest warps make the most segments.
 inline size_t maps_bytes(int64_t b, int64_t t, int64_t d) {
-  const int segs = split(b * ceil_div(d, 64), t, 4).segs;
+  const int segs = split(b * ceil_div(d, 64), t, 4, 4).segs;
   return segs == 1 ? 0 : sizeof(float) * 2 * (size_t)b * (size_t)(segs + 1) * (size_t)d;
 }
 
 // The map of each segment.  A warp takes a quarter of it step by step; REVERSE: for c_s = keep_s (dh_s + c_{s+1}) from the end,
 // with dh in x's place.  Entry 0 (of the maps in the direction of the recurrence) is what reaches the first segment.
 template <int L, bool WIDE> struct MapShared {
-  static constexpr int kStages = 3;
+  static constexpr int kStages = WIDE ? 3 : 2;   // so that four CTAs fit on an SM
   Run<L, WIDE> runs[4][kStages][2];
   Exchange<L, 4> ex;
 };

@@ -170,6 +170,7 @@ struct Backward {
   cudaStream_t s;
   // the most warps of a CTA that its shared memory has room for
   template <bool WIDE> static constexpr int most() { return WIDE ? 16 : 8; }
+  template <bool WIDE> static constexpr int resident() { return WIDE ? 4 : 3; }   // CTAs of 4 warps on an SM
   template <int L, bool WIDE> cudaError_t maps() {
     static std::atomic<uint64_t> done{0};
     return launch_kernel(recurrence_map_kernel<L, WIDE, true>, p, b, 4, sizeof(MapShared<L, WIDE>), &done, s);
