@@ -176,11 +176,11 @@ struct Forward {
   template <bool WIDE> static constexpr int resident() { return 4; }   // CTAs of 4 warps on an SM
   template <int L, bool WIDE> cudaError_t maps() {
     static std::atomic<uint64_t> done{0};
-    return launch_kernel(recurrence_map_kernel<L, WIDE, false>, p, b, 4, sizeof(MapShared<L, WIDE>), &done, s);
+    return launch_kernel(recurrence_map_kernel<L, WIDE, false>, p, b, 4, sizeof(MapShared<L, WIDE>), &done, false, s);
   }
   template <int L, bool WIDE, int WARPS> cudaError_t run() {
     static std::atomic<uint64_t> done{0};
-    return launch_kernel(recurrence_kernel<L, WIDE, WARPS>, p, b, WARPS, sizeof(Shared<L, WIDE, WARPS>), &done, s);
+    return launch_kernel(recurrence_kernel<L, WIDE, WARPS>, p, b, WARPS, sizeof(Shared<L, WIDE, WARPS>), &done, p.segs > 1, s);
   }
 };
 

@@ -247,6 +247,7 @@ template <int L, int WARPS>
 __device__ __forceinline__ Val<Lanes<L>::kVals> arriving(const RecurArgs &p, const Place<L> &me, Exchange<L, WARPS> &ex, int entries) {
   constexpr int C = Lanes<L>::kVals;
   using V = Val<C>;
+  after_first();
   const int per = (entries + WARPS - 1) / WARPS, from = me.warp * per, to = min(entries, from + per);
   V A = all<C>(1.f), H = all<C>(0.f);
 #pragma unroll 4
@@ -282,10 +283,12 @@ inline Split split(int64_t chains, int64_t t, int most, int resident) {
 }
 
 inline cudaError_t launch_kernel(void (*kernel)(const RecurArgs), const RecurArgs &p, int64_t b, int warps, int bytes,
-                                 std::atomic<uint64_t> *done, cudaStream_t s) {
+                                 std::atomic<uint64_t> *done, bool after, cudaStream_t s) {
   const cudaError_t e = set_max_shared_once(reinterpret_cast<const void *>(kernel), bytes, done);
   if (e != cudaSuccess) return e;
-  kernel<<<(unsigned)(b * p.blocks * p.segs), 32 * warps, bytes, s>>>(p);
+  const unsigned grid = (unsigned)(b * p.blocks * p.segs);
+  if (after) return launch_after<RecurArgs>(kernel, p, dim3(grid), 32 * warps, bytes, s);
+  kernel<<<grid, 32 * warps, bytes, s>>>(p);
   return cudaGetLastError();
 }
 
@@ -339,6 +342,7 @@ template <int L, bool WIDE, bool REVERSE> __global__ void __launch_bounds__(128,
   static_assert(sizeof(Sh) <= kMaxShared);
   extern __shared__ __align__(16) char memory[];
   Sh &sh = *reinterpret_cast<Sh *>(memory);
+  follow_early();
   const Place<L> me(p);
   const int64_t x_step = REVERSE ? p.dh_step : p.x_step;
   const T *x = (REVERSE ? static_cast<const T *>(p.dh) + me.i * p.dh_seq : static_cast<const T *>(p.x) + me.i * p.x_seq) + me.first;

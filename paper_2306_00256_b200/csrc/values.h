@@ -82,4 +82,26 @@ inline bool is_index(int32_t t) { return t == DSGD_I32 || t == DSGD_I64; }
 inline int64_t type_bytes(int32_t t) { return t == DSGD_BF16 ? 2 : 4; }
 inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
+#ifdef __CUDACC__
+// A kernel that another one of the same call follows lets it begin early (follow_early); that one, launched with
+// launch_after, does what does not depend on the first and then waits for its end (after_first).
+__device__ __forceinline__ void follow_early() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+__device__ __forceinline__ void after_first() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+
+template <typename Args>
+inline cudaError_t launch_after(void (*kernel)(const Args), const Args &p, dim3 grid, int threads, int bytes, cudaStream_t s) {
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3(threads);
+  cfg.dynamicSmemBytes = bytes;
+  cfg.stream = s;
+  cudaLaunchAttribute at{};
+  at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at.val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = &at;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kernel, p);
+}
+#endif
+
 }  // namespace ceca
