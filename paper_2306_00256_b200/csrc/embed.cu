@@ -42,6 +42,7 @@ struct EmbedArgs {
   int2 *list;          // n x t: positions, by token and then ascending, each with its token
   float *pieces;       // n x chunks x 2 x d: sums of the pieces of long lists
   int32_t bins;        // table rows per block of token_list_kernel
+  int64_t part;        // tokens that it places, a multiple of 32 for each warp
   int32_t chunk;       // places of the list for a warp, at most 32
   int32_t chunks;      // of an agent's list
   int32_t slices;      // of a row
@@ -50,7 +51,7 @@ struct EmbedArgs {
 
 constexpr int kThreads = 256, kWarps = kThreads / 32;
 constexpr int kFill = 64;      // table rows
-constexpr int kJoin = 8;       // chunks
+constexpr int kJoin = 2;       // chunks
 constexpr int kFew = 256;      // positions
 constexpr int kFewRows = 16;   // table rows of a CTA
 constexpr int kDeep = 4;       // rows of dout that a warp has on their way at a time
@@ -157,37 +158,42 @@ __global__ void __launch_bounds__(kThreads) embed_lookup_kernel(const EmbedArgs 
   }
 }
 
-// Block (x, i) lists the positions of the table rows [lo, hi) of agent i.  It scans all of the agent's tokens
-// twice: once to count them per (warp, row) and to count those below lo, which is where its part of the list
-// begins, and once to place them.  A warp owns a contiguous segment of the positions and takes it in order, so
-// the list is ascending within a row; nothing is exchanged between blocks.
+// Block (x, i, part) lists those positions of the table rows [lo, hi) of agent i that lie in a part of the agent's tokens.
+// It counts the row's tokens before, in and after the part, and those below lo, which is where its rows' lists
+// begin; then it places its part's.  A warp owns a contiguous segment of the part and takes it in order, so a list is
+// ascending; nothing is exchanged between blocks.  Counting all tokens in every block is cheap; placing them is not (ranks
+// among the lanes of a warp, stores anywhere), and frequent tokens lie together in one block: parts divide that.
 template <typename TI>
 __global__ void __launch_bounds__(kListThreads) token_list_kernel(const EmbedArgs p) {
-  extern __shared__ __align__(16) int32_t count[];   // [kListWarps][bins, rounded up to 4]
-  __shared__ int32_t part[kListWarps], below_all;
+  extern __shared__ __align__(16) int32_t count[];   // [kListWarps + 2][pitch]: of each warp, before and after the part
+  __shared__ int32_t sums[kListWarps], below_all;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int64_t i = blockIdx.y;
   const int64_t lo = (int64_t)blockIdx.x * p.bins;
-  const int32_t bins = (int32_t)min((int64_t)p.bins, p.v - lo);
+  const int32_t bins = (int32_t)min((int64_t)p.bins, p.v - lo), pitch = (p.bins + 3) & ~3;
   const TI *tok = static_cast<const TI *>(p.tokens) + i * p.tokens_agent;
-  const int64_t seg = (p.t + kListThreads - 1) / kListThreads * 32;
-  const int64_t s0 = warp * seg, s1 = min(p.t, s0 + seg);
-  int32_t *mine = count + warp * ((p.bins + 3) & ~3);
+  const int64_t p0 = min(p.t, blockIdx.z * p.part), p1 = min(p.t, p0 + p.part);
+  const int64_t seg = p.part / kListWarps, s0 = min(p1, p0 + warp * seg), s1 = min(p1, s0 + seg);
+  int32_t *mine = count + warp * pitch, *before = count + kListWarps * pitch, *after = before + pitch;
 
-  const int pitch = (p.bins + 3) & ~3;
-  for (int k = threadIdx.x; k < kListWarps * pitch / 4; k += kListThreads) reinterpret_cast<int4 *>(count)[k] = make_int4(0, 0, 0, 0);
+  for (int k = threadIdx.x; k < (kListWarps + 2) * pitch / 4; k += kListThreads) reinterpret_cast<int4 *>(count)[k] = make_int4(0, 0, 0, 0);
   if (threadIdx.x == 0) below_all = 0;
   __syncthreads();
   // (compared as unsigned numbers: negative tokens lie above every row)
   using U = typename std::make_unsigned<TI>::type;
   const U ulo = (U)lo, ubins = (U)bins;
   int32_t below = 0;
-#pragma unroll 8
-  for (int64_t s = s0 + lane; s < s1; s += 32) {
+  const auto tally = [&](int64_t s, int32_t *counts) {
     const U w = (U)tok[s], r = w - ulo;
     below += w < ulo;
-    if (r < ubins) atomicAdd(mine + r, 1);
-  }
+    if (r < ubins) atomicAdd(counts + r, 1);
+  };
+#pragma unroll 8
+  for (int64_t s = s0 + lane; s < s1; s += 32) tally(s, mine);
+#pragma unroll 4
+  for (int64_t s = threadIdx.x; s < p0; s += kListThreads) tally(s, before);
+#pragma unroll 4
+  for (int64_t s = p1 + threadIdx.x; s < p.t; s += kListThreads) tally(s, after);
   below = __reduce_add_sync(0xffffffffu, below);
   if (lane == 0) atomicAdd(&below_all, below);
   __syncthreads();
@@ -197,27 +203,30 @@ __global__ void __launch_bounds__(kListThreads) token_list_kernel(const EmbedArg
   int32_t sum = 0;
   if (r < bins)
 #pragma unroll 8
-    for (int w = 0; w < kListWarps; ++w) sum += count[w * pitch + r];
+    for (int w = 0; w < kListWarps + 2; ++w) sum += count[w * pitch + r];
   int32_t upto = sum;
   for (int o = 1; o < 32; o <<= 1) {
     const int32_t y = __shfl_up_sync(0xffffffffu, upto, o);
     if (lane >= o) upto += y;
   }
-  if (lane == 31) part[warp] = upto;
+  if (lane == 31) sums[warp] = upto;
   __syncthreads();
-  int32_t before = lane < warp ? part[lane] : 0;
-  before = __reduce_add_sync(0xffffffffu, before);
-  int32_t at = below_all + before + upto - sum;
+  int32_t lower = lane < warp ? sums[lane] : 0;
+  lower = __reduce_add_sync(0xffffffffu, lower);
+  int32_t at = below_all + lower + upto - sum;
   if (r < bins) {
-    int32_t *start = p.row_start + i * (p.v + 1) + lo;
-    start[r] = at;
+    if (blockIdx.z == 0) {
+      int32_t *start = p.row_start + i * (p.v + 1) + lo;
+      start[r] = at;
+      if (r == bins - 1 && lo + bins == p.v) start[bins] = at + sum;
+    }
+    at += before[r];
 #pragma unroll 8
     for (int w = 0; w < kListWarps; ++w) {
       const int32_t c = count[w * pitch + r];
       count[w * pitch + r] = at;
       at += c;
     }
-    if (r == bins - 1 && lo + bins == p.v) start[bins] = at;
   }
   __syncthreads();
 
@@ -233,12 +242,12 @@ __global__ void __launch_bounds__(kListThreads) token_list_kernel(const EmbedArg
       const uint32_t some = __ballot_sync(0xffffffffu, in);
       if (some == 0) continue;
       if (in) {
-        const int32_t r = (int32_t)w[k];
-        const uint32_t same = __match_any_sync(some, r);
-        const int32_t rank = __popc(same & ((1u << lane) - 1)), at = mine[r] + rank;
-        list[at] = make_int2((int32_t)(s + 32 * k + lane), (int32_t)lo + r);   // (stores this scattered are what takes the time)
+        const int32_t row = (int32_t)w[k];
+        const uint32_t same = __match_any_sync(some, row);
+        const int32_t rank = __popc(same & ((1u << lane) - 1)), place = mine[row] + rank;
+        list[place] = make_int2((int32_t)(s + 32 * k + lane), (int32_t)lo + row);
         __syncwarp(some);
-        if (rank == 0) mine[r] += __popc(same);
+        if (rank == 0) mine[row] += __popc(same);
       }
       __syncwarp();
     }
@@ -293,40 +302,43 @@ template <typename TE, typename TO, typename TI, int V> __global__ void __launch
   const uint32_t some = present;
   const TO *o = static_cast<const TO *>(p.src) + i * p.out_agent + c0;
   for (int r = warp; r < kFewRows && r0 + r < p.v; r += kWarps) {
-    if (p.accumulate && !(some >> r & 1)) continue;
-    float acc[U][V] = {};
-    if (some >> r & 1) {
-      int count = 0;
-      for (int k = 0; k < p.t; k += 32) {
-        const bool mine = tok[k + lane] == r;
-        const uint32_t them = __ballot_sync(0xffffffffu, mine);
-        if (mine) places[warp][count + __popc(them & ((1u << lane) - 1))] = (uint8_t)(k + lane);
-        count += __popc(them);
-      }
-      __syncwarp();
-      for (int s = 0; s < count; s += kDeep) {
-        Pack<TO, V> v[kDeep][U];
-#pragma unroll
-        for (int q = 0; q < kDeep; ++q)
-          if (s + q < count)
-#pragma unroll
-            for (int u = 0; u < U; ++u)
-              if (c0 + u * 32 * V < p.d) v[q][u] = get<TO, V>(o + places[warp][s + q] * p.out_row + u * 32 * V);
-#pragma unroll
-        for (int q = 0; q < kDeep; ++q)
-          if (s + q < count)
-#pragma unroll
-            for (int u = 0; u < U; ++u)
-              if (c0 + u * 32 * V < p.d) add_to(acc[u], v[q][u]);
-      }
-      __syncwarp();
+    TE *g = static_cast<TE *>(p.dst) + i * p.table_agent + (r0 + r) * p.table_row;
+    if (!(some >> r & 1)) {
+      const int64_t first = (int64_t)blockIdx.y * Slice<V>::kElements;
+      if (!p.accumulate) zero_row<TE, V>(g + first, min((int64_t)Slice<V>::kElements, p.d - first));
+      continue;
     }
-    finish_row<TE, V>(p, static_cast<TE *>(p.dst) + i * p.table_agent + (r0 + r) * p.table_row + c0, c0, acc);
+    float acc[U][V] = {};
+    int count = 0;
+    for (int k = 0; k < p.t; k += 32) {
+      const bool mine = tok[k + lane] == r;
+      const uint32_t them = __ballot_sync(0xffffffffu, mine);
+      if (mine) places[warp][count + __popc(them & ((1u << lane) - 1))] = (uint8_t)(k + lane);
+      count += __popc(them);
+    }
+    __syncwarp();
+    for (int s = 0; s < count; s += kDeep) {
+      Pack<TO, V> v[kDeep][U];
+#pragma unroll
+      for (int q = 0; q < kDeep; ++q)
+        if (s + q < count)
+#pragma unroll
+          for (int u = 0; u < U; ++u)
+            if (c0 + u * 32 * V < p.d) v[q][u] = get<TO, V>(o + places[warp][s + q] * p.out_row + u * 32 * V);
+#pragma unroll
+      for (int q = 0; q < kDeep; ++q)
+        if (s + q < count)
+#pragma unroll
+          for (int u = 0; u < U; ++u)
+            if (c0 + u * 32 * V < p.d) add_to(acc[u], v[q][u]);
+    }
+    __syncwarp();
+    finish_row<TE, V>(p, g + c0, c0, acc);
   }
 }
 
-// Sum over a part of a list, or of the pieces, by the warps of a CTA in turn; every warp ends up with its own packs of it
-// in `acc` of warp 0.  `load(j, c)` adds entry j's packs.
+// The sum of `count` entries, a contiguous share of them by each warp of a CTA; warp 0 ends up with it in `acc`.  `add(j)` adds
+// entry j's packs to acc.
 template <int V, typename Add> __device__ __forceinline__ void sum_by_warps(float (*acc)[V], int count, float (*shared)[Slice<V>::kElements], Add add) {
   constexpr int U = Slice<V>::U;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -463,11 +475,14 @@ template <typename TE, int V> __global__ void __launch_bounds__(kThreads) embed_
   }
 }
 
-// Table rows per list block: few blocks scan all of an agent's tokens in vain, but a block's own tokens take longest, and
-// frequent tokens lie together; two blocks an SM are best over the range.
-int32_t list_bins(int32_t n, int64_t v) {
-  const int64_t blocks = std::max<int64_t>(ceil_div(v, kMaxBins), ceil_div(2 * 148, n));
-  return (int32_t)std::max<int64_t>(1, ceil_div(v, blocks));
+// How the list kernel is split: into parts of the tokens (of 4096 at least: each counts all of them) as far as two blocks an
+// SM allow, then into ranges of table rows, which are at most kMaxBins.
+struct ListSplit { int32_t bins, parts; };
+ListSplit list_split(int32_t n, int64_t t, int64_t v) {
+  const int64_t room = 2 * 148 / n, least = ceil_div(v, kMaxBins);
+  const int64_t parts = std::max<int64_t>(1, std::min({room / least, ceil_div(t, 4096), (int64_t)8}));
+  const int64_t blocks = std::max<int64_t>({least, room / parts, 1});
+  return {(int32_t)ceil_div(v, blocks), (int32_t)parts};
 }
 
 // Places of a chunk: 32, or fewer where that would leave the SMs without work.
@@ -506,11 +521,11 @@ template <typename TE, typename TO, typename TI, int V> cudaError_t launch_looku
 
 template <typename TI> cudaError_t launch_list(const EmbedArgs &p, cudaStream_t s) {
   static std::atomic<uint64_t> done{0};
-  const cudaError_t e = set_max_shared_once(reinterpret_cast<const void *>(token_list_kernel<TI>),
-                                            sizeof(int32_t) * kListWarps * kMaxBins, &done);
+  const auto bytes = [](int bins) { return (int)sizeof(int32_t) * (kListWarps + 2) * ((bins + 3) / 4 * 4); };
+  const cudaError_t e = set_max_shared_once(reinterpret_cast<const void *>(token_list_kernel<TI>), bytes(kMaxBins), &done);
   if (e != cudaSuccess) return e;
-  const dim3 grid((unsigned)ceil_div(p.v, p.bins), (unsigned)p.n);
-  token_list_kernel<TI><<<grid, kListThreads, sizeof(int32_t) * kListWarps * ((p.bins + 3) / 4 * 4), s>>>(p);
+  const dim3 grid((unsigned)ceil_div(p.v, p.bins), (unsigned)p.n, (unsigned)ceil_div(p.t, p.part));
+  token_list_kernel<TI><<<grid, kListThreads, bytes(p.bins), s>>>(p);
   return cudaGetLastError();
 }
 
@@ -597,7 +612,9 @@ extern "C" ceca_status_t dsgd_embed_grad(const void *dout, const void *tokens, v
   p.row_start = static_cast<int32_t *>(workspace);
   p.list = reinterpret_cast<int2 *>(static_cast<char *>(workspace) + round16(sizeof(int32_t) * (size_t)n * (size_t)(v + 1)));
   p.pieces = reinterpret_cast<float *>(reinterpret_cast<char *>(p.list) + round16(sizeof(int2) * (size_t)n * (size_t)t));
-  p.bins = list_bins(n, v);
+  const ListSplit split = list_split(n, t, v);
+  p.bins = split.bins;
+  p.part = std::max<int64_t>(1, ceil_div(t, (int64_t)split.parts * kListThreads)) * kListThreads;
   p.chunk = chunk_of(n, t, d);
   p.chunks = (int32_t)ceil_div(t, p.chunk);
   const cudaStream_t s = static_cast<cudaStream_t>(stream);
