@@ -277,8 +277,8 @@ typedef enum { DSGD_I32 = 0, DSGD_I64 = 1 } dsgd_index_t;
  * row is zero.  out: device, out_type; position s of agent i starts at out + i*out_agent_stride +
  * s*out_row_stride.  Strides count elements; rows themselves are contiguous, and neither the rows of
  * out nor those of E may overlap.  t = 0 is allowed and does nothing.
- * Errors: CECA_ERR_INVALID_ARG (NULL where data is needed, n, v or d < 1, t < 0, v or t >= 2^31, a row
- * stride below d, a negative stride, a bad type).
+ * Errors: CECA_ERR_INVALID_ARG (NULL where data is needed, n, v or d < 1, n > 65535, t < 0, v >= 2^31,
+ * t >= 2^31 - 1024, a row stride below d, a negative stride, a bad type).
  * Speed: 128-bit accesses need every row to start on a 16-byte boundary; other layouts run a narrower
  * form.
  */

@@ -497,7 +497,8 @@ size_t round16(size_t bytes) { return (bytes + 15) / 16 * 16; }
 bool embed_args_ok(int32_t n, int64_t t, int64_t v, int64_t d, int64_t table_agent, int64_t table_row,
                    int64_t tokens_agent, int64_t out_agent, int64_t out_row, int32_t table_type,
                    int32_t tokens_type, int32_t out_type) {
-  return n >= 1 && n <= 65535 && t >= 0 && t < ((int64_t)1 << 31) && v >= 1 && v < ((int64_t)1 << 31) && d >= 1 &&
+  // (places and positions are 32-bit numbers, up to a few chunks beyond t)
+  return n >= 1 && n <= 65535 && t >= 0 && t < ((int64_t)1 << 31) - 1024 && v >= 1 && v < ((int64_t)1 << 31) && d >= 1 &&
          table_agent >= 0 && table_row >= d && tokens_agent >= 0 && out_agent >= 0 && out_row >= 0 &&
          is_type(table_type) && is_index(tokens_type) && is_type(out_type);
 }

@@ -190,6 +190,7 @@ def test_embedding_rows_beyond_32_bit_offsets():
 RECUR = [  # b, t, d
     (1, 1, 1), (2, 1, 64), (300, 1, 40), (3, 2, 33), (1, 5, 256), (2, 31, 8), (1, 127, 70), (2, 128, 64), (1, 129, 72), (4, 200, 520),
     (1, 1025, 24), (2, 513, 136), (1, 3000, 5), (1, 2500, 64), (7, 385, 16), (1, 17, 2048), (3, 16, 1000), (1, 6000, 32),
+    (60, 100, 520), (30, 300, 520), (14, 300, 520), (8, 290, 520), (30, 150, 521), (16, 140, 521),   # channels enough for 4, 8 and 16 warps
 ]
 
 
@@ -423,6 +424,16 @@ def test_distillation_of_many_rows(r, v, dtype, tail):
     w[::7] = 0
     idx[5, 3], idx[5, 4] = 9, 9
     _distill_check(z, idx, t, lse, w, 1.0)
+
+
+def test_distillation_over_more_entries_than_the_bitmap_has_bits():
+    # parts of more than 2^20 logits: entries 2^20 apart share a bit
+    v = 9_000_001
+    z, idx, t, _, _ = _distill_inputs(1, v, 40, F32, False, 25)
+    idx[0, 5], idx[0, 6], idx[0, 7] = 5, 5 + (1 << 20), 11
+    lse = torch.logsumexp(t.masked_fill((idx < 0) | (idx >= v), -float("inf")), 1) + 0.2
+    _distill_check(z, idx, t, lse, None, 1.0)
+    _distill_check(z, idx, t, None, None, 1.0)
 
 
 @pytest.mark.parametrize("v", [70000, 250000])
