@@ -10,11 +10,11 @@
 //                       that lies in it: however the tokens are distributed, its work is the same.  Other CTAs fill the rows that no position holds;
 //   embed_join_kernel   adds up the pieces of the rows that have several.
 // 8 x 8192 positions in bf16 of 32000 x 1024 fp32 tables: 0.23 ms, 0.79 of the measured copy rate, of which the list takes
-// 22 us (the block with the most frequent tokens, whose shared-memory counters every token passes) and the join 11.
-// Lookup of 8 x 8192 rows of 2048 bf16: 69 us, 0.82.  Rows that are not on 16-byte boundaries move an element a lane
-// (1031 columns: 0.25 in bf16, 0.45 in fp32).
+// 22 to 24 us (the block with the most frequent tokens, whose shared-memory counters every token passes) and the join 10.
+// Lookup of 8 x 8192 rows of 2048 bf16: 68 us, 0.83.  bf16 rows on 8-byte boundaries move four elements a lane (1044 columns,
+// lookup and gradient: 67 and 194 us, 107 and 299 with one), rows on other boundaries one (1031 columns: 0.27 in bf16, 0.5 in fp32).
 // For up to kFew positions these three launches would take longer than their work: embed_few_kernel looks the positions of
-// every row up as it goes (4 x 129 positions, 4097 x 256 fp32: 18 us by three launches, 10 us so).
+// every row up as it goes (4 x 129 positions, 4097 x 256 fp32: 18 us by three launches, 9 to 10 us so).
 #include <cuda_runtime.h>
 
 #include <algorithm>
@@ -59,8 +59,8 @@ constexpr int kListThreads = 1024;
 constexpr int kListWarps = kListThreads / 32;
 constexpr int kMaxBins = kListThreads;   // a row for each thread
 
-// V adjacent elements, moved at once: V * sizeof(T) is 16 bytes for the narrower of a call's types, or 8 (V = 1: rows on
-// any boundary).
+// V adjacent elements, moved at once: 8 where both of a call's types are bf16, otherwise 4; where rows lie on 8-byte
+// boundaries only, 4 in bf16; 1 for rows on any boundary.
 template <typename T, int V> struct Pack;
 template <int V> struct alignas(V * 4) Pack<float, V> {
   float e[V];
@@ -505,11 +505,12 @@ bool embed_args_ok(int32_t n, int64_t t, int64_t v, int64_t d, int64_t table_age
 
 // Elements of a pack: both tensors' packs must lie on a boundary of their own size.
 int pack_of(const EmbedArgs &p, const void *table, int64_t te, const void *out, int64_t to) {
-  const int v = te == 2 && to == 2 ? 8 : 4;
-  const auto fits = [&](const void *base, int64_t agent, int64_t row, int64_t size) {
+  const auto fits = [&](int v, const void *base, int64_t agent, int64_t row, int64_t size) {
     return (uintptr_t)base % (v * size) == 0 && (p.n == 1 || agent % v == 0) && row % v == 0;
   };
-  return p.d % v == 0 && fits(table, p.table_agent, p.table_row, te) && fits(out, p.out_agent, p.out_row, to) ? v : 1;
+  for (int v = te == 2 && to == 2 ? 8 : 4; v >= 4; v /= 2)
+    if (p.d % v == 0 && fits(v, table, p.table_agent, p.table_row, te) && fits(v, out, p.out_agent, p.out_row, to)) return v;
+  return 1;
 }
 
 template <typename TE, typename TO, typename TI, int V> cudaError_t launch_lookup(EmbedArgs p, cudaStream_t s) {
@@ -548,9 +549,13 @@ template <typename TE, typename TO, typename TI, int V> cudaError_t launch_grad(
 
 // Calls go(TE, TO, TI, V) for the types of a call.
 template <typename TE, typename TO, typename Go> cudaError_t with_index(bool i64, int pack, Go go) {
-  constexpr int V = sizeof(TE) == 2 && sizeof(TO) == 2 ? 8 : 4;
-  if (i64) return pack == 1 ? go(TE(), TO(), int64_t(), std::integral_constant<int, 1>()) : go(TE(), TO(), int64_t(), std::integral_constant<int, V>());
-  return pack == 1 ? go(TE(), TO(), int32_t(), std::integral_constant<int, 1>()) : go(TE(), TO(), int32_t(), std::integral_constant<int, V>());
+  const auto with_pack = [&](auto ti) {
+    if (pack == 1) return go(TE(), TO(), ti, std::integral_constant<int, 1>());
+    if constexpr (sizeof(TE) == 2 && sizeof(TO) == 2)
+      if (pack == 8) return go(TE(), TO(), ti, std::integral_constant<int, 8>());
+    return go(TE(), TO(), ti, std::integral_constant<int, 4>());
+  };
+  return i64 ? with_pack(int64_t()) : with_pack(int32_t());
 }
 template <typename Go> ceca_status_t with_types(int32_t te, int32_t to, int32_t ti, int pack, Go go) {
   const bool i64 = ti == DSGD_I64;

@@ -55,7 +55,7 @@ def _untouched(view, buf):
 EMBED = [  # n, t, v, d
     (1, 1, 1, 1), (2, 5, 3, 7), (3, 64, 100, 32), (1, 300, 17, 129), (4, 129, 1025, 64), (2, 1000, 5000, 96),
     (5, 33, 513, 250), (1, 2000, 40, 260), (2, 77, 4099, 1031), (1, 40, 70000, 16), (1, 4097, 300, 512), (3, 9, 65, 2056),
-    (2, 256, 30, 40), (1, 257, 30, 1048), (1, 9000, 20000, 24),
+    (2, 256, 30, 40), (1, 257, 30, 1048), (1, 9000, 20000, 24), (3, 70, 65, 100), (1, 700, 300, 1044),
 ]
 
 
