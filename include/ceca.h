@@ -314,6 +314,7 @@ size_t dsgd_embed_workspace_bytes(int32_t n, int64_t t, int64_t v, int64_t d);
  *   a = sigmoid(f[i, s, c]),   h[i, s, c] = keep * h[i, s-1, c] + (1 - a) * x[i, s, c]
  * with keep = a, except keep = 0 at a step that begins a document (starts[i, s] != 0): whatever the state
  * was, an infinity or NaN included, does not reach past it.  h[i, -1, c] = h0[i, c], or 0 when h0 is NULL.
+ * A NaN in f is a NaN in h from its step to the next document, as one in x is.
  * x, f, h: device, `type`; step s of sequence i starts at p + i*p_seq_stride + s*p_step_stride, its d
  * channels contiguous (so x and f may be halves of one projection).  h0, h_last: device fp32, b x d
  * dense; starts: device, one byte per step, b x t dense, may be NULL.  h_last receives the fp32 state
