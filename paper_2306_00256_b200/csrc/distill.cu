@@ -43,6 +43,9 @@ constexpr float kLn2 = 0.6931471805599453f;
 // Beyond this the rounding of M c (2^-24 of it) could itself overflow an exponential.  Logits of this size are masks of
 // the type's lowest value; a row that has no other gets its own, slower sums of 2^((z - M) c).
 constexpr float kFar = 1e8f;
+// A thread looks for a larger frame as long as it has seen no logit above this, so that additive masks (of -1e4, say) end up in
+// no frame beside real logits; and the sum at which a thread that has settled starts again.
+constexpr float kLow = -2e3f, kLeave = 0x1p80f;
 
 struct DistillArgs {
   const void *z, *idx, *t;
@@ -107,16 +110,20 @@ template <int D> __device__ __forceinline__ float top_of(const Vec<bf16> *v) {
   return fmaxf(__low2float(m), __high2float(m));
 }
 
-// What one thread has seen: sum counts 2^(z c - k), k = m c.  m is the largest of the first vectors that are not masked, not of all: a frame
-// does not have to be the maximum, only near enough that no sum overflows, and if one does the row goes the way of `far`.
+// What one thread has seen: sum counts 2^(z c - k), k = m c.  m is the largest of the first vectors that are not masked, not of
+// all: a frame does not have to be the maximum, only so near to it that the sum stays below kLeave.  (A sum that does not is
+// taken again, in the frame of the maximum.)  Then what a factor below 2^-126 makes nothing of when frames are joined is
+// below 2^-46 of the sum in the other frame, and no product with the joined sum or its reciprocal leaves the normal numbers.
 struct Seen {
   float m = -kFar, k;
   Val<2> sum{0.f, 0.f};
-  __device__ __forceinline__ explicit Seen(float scale) { k = m * scale; }
+  __device__ __forceinline__ Seen(float top, float scale) : m(fmaxf(top, -kFar)) { k = m * scale; }
+  __device__ __forceinline__ bool settled() const { return m > kLow; }
+  __device__ __forceinline__ bool beyond() const { return sum.x + sum.y > kLeave; }
   template <int D, typename T> __device__ __forceinline__ void frame(const Vec<T> *a, float scale) {
     const float top = top_of<D>(a);
     if (top > m) {
-      sum = mul(sum, all<2>(ex2(k - top * scale)));   // (an edge element may be in it)
+      sum = mul(sum, all<2>(ex2(k - top * scale)));   // (an edge element, or masked ones, may be in it)
       m = top;
       k = m * scale;
     }
@@ -339,12 +346,9 @@ __global__ void __launch_bounds__(THREADS, 768 / THREADS) distill_kernel(const D
   const auto counts = [&](int64_t s) { return !tail || !(in_top(s / N * N) >> (s % N) & 1); };   // in pass 1's sum
 
   // pass 1: maximum and sum, in tail mode over the entries outside the top
-  Seen seen(p.scale);
-  if (part.edge >= 0 && counts(part.edge)) {
-    seen.m = fmaxf(seen.m, edge);
-    seen.k = seen.m * p.scale;
-    seen.sum.x = ex2(fmaf(edge, p.scale, -seen.k));
-  }
+  const bool edge_counts = part.edge >= 0 && counts(part.edge);
+  Seen seen(edge_counts ? edge : -INFINITY, p.scale);
+  if (edge_counts) seen.sum.x = ex2(fmaf(edge, p.scale, -seen.k));
   const int64_t s0 = (int64_t)(part.w0 + tid) * N;
   for (int base = 0; base < count; base += hop) {
     Vec<TZ> a[kDeep];
@@ -366,8 +370,27 @@ __global__ void __launch_bounds__(THREADS, 768 / THREADS) distill_kernel(const D
         if (mask) strike(a[u], mask);
       }
     }
-    if (seen.m == -kFar) seen.frame<kDeep>(a, p.scale);   // nothing but masked logits before
+    if (!seen.settled()) seen.frame<kDeep>(a, p.scale);
     seen.take<kDeep>(a, p.scale);
+  }
+  if (seen.beyond()) {   // once more, a vector at a time
+    const auto vector = [&](int j) {
+      Vec<TZ> a{src[j]};
+      const uint32_t mask = !HELD && tail ? in_top(s0 + (int64_t)j * N) : 0;
+      if (mask) strike(a, mask);
+      return a;
+    };
+    float top = edge_counts ? edge : -INFINITY;
+    for (int j = 0; j < count - tid; j += THREADS) {
+      const Vec<TZ> a = vector(j);
+      top = fmaxf(top, top_of<1>(&a));
+    }
+    seen = Seen(top, p.scale);
+    if (edge_counts) seen.sum.x = ex2(fmaf(edge, p.scale, -seen.k));
+    for (int j = 0; j < count - tid; j += THREADS) {
+      const Vec<TZ> a = vector(j);
+      seen.take<1>(&a, p.scale);
+    }
   }
   // the warp's part in its own frame, then everybody's
   Known all_of;
@@ -408,7 +431,7 @@ __global__ void __launch_bounds__(THREADS, 768 / THREADS) distill_kernel(const D
   float M = all_of.m;
   const bool far = !(fabsf(M) < kFar && all_of.sum < INFINITY);
   const auto exponent = [&](float v) { return far ? (v - M) * p.scale : fmaf(v, p.scale, -(M * p.scale)); };
-  if (far) {   // logits beyond +-kFar only, an overflow (or infinities, or NaN): once more, element by element
+  if (far) {   // logits beyond +-kFar only, infinities or NaN: once more, element by element
     float top = -INFINITY;
     const int64_t s1 = min((int64_t)slot1, p.v + part.pad);
     for (int64_t s = max((int64_t)slot0, (int64_t)part.pad) + tid; s < s1; s += THREADS) top = fmaxf(top, widen(z[s - part.pad]));

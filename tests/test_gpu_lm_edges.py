@@ -6,7 +6,7 @@ import torch
 
 import paper_2306_00256_b200 as ceca
 from oracle import lm
-from test_gpu_lm_operators import BF16, DEV, F32, NAN, _close, _np, _randn
+from test_gpu_lm_operators import BF16, DEV, F32, NAN, _close, _gen, _np, _randn
 
 pytestmark = pytest.mark.gpu
 
@@ -37,3 +37,77 @@ def test_recurrence_a_gate_that_is_not_a_number_is_seen(dtype, d, t, at, cut, b)
     want = lm.recurrence_grad(_np(x), _np(f), _np(dh), _np(h0), _np(st), _np(dl), dtype == BF16)
     for g, k in ((dx, "dx"), (df, "df"), (dh0, "dh0")):
         _close(g, want[k], k)
+
+
+# ------------------------------------------------------------------------------------------------ distillation
+
+# a period and how much of its beginning is low: what the threads of one warp, of one CTA, of a cluster see first
+APART = [(F32, 1000, 1000, 520), (F32, 3000, 3000, 1030), (BF16, 50000, 50000, 8200), (F32, 50000, 6252, 2100), (BF16, 400000, 50000, 8200)]
+
+
+def _rows_apart(v, period, low, gaps, top, seed):
+    """Rows of N(0, 1) whose first logits in every period lie `gap` below one logit of `top` in the middle of a period."""
+    z = torch.randn((len(gaps), v), generator=_gen(seed))
+    peak = (v // period // 2) * period + (low + period) // 2
+    where = torch.arange(v) % period < low
+    for i, gap in enumerate(gaps):
+        z[i, where] += top - gap
+        z[i, peak] = top
+    return z, peak
+
+
+@pytest.mark.parametrize("dtype,v,period,low", APART)
+@pytest.mark.parametrize("listed", [True, False])
+@pytest.mark.parametrize("top,alone", [(10.0, False), (10.0, True), (60.0, False)])
+def test_distillation_whatever_the_threads_see_first(dtype, v, period, low, listed, top, alone):
+    gaps = [40.0, 55.0, 62.0, 70.0] + [80.0 + 0.25 * i for i in range(61)] + [120.0, 300.0, 10000.0]
+    if v > 100000:
+        gaps = gaps[::4] + [87.5, 88.0, 88.25, 88.5]
+    z, peak = _rows_apart(v, period, low, gaps, top, 31)
+    r = len(gaps)
+    idx = torch.stack([torch.randperm(v, generator=_gen(32 + i))[:5] for i in range(r)])
+    idx[idx == peak] = 0
+    if listed:
+        idx[:, 2] = peak
+    t = torch.randn((r, 5), generator=_gen(33)) + 2.0
+    w = torch.full((r,), 1e-4)
+    z, idx, t, w = z.to(dtype).to(DEV), idx.to(DEV), t.to(DEV), w.to(DEV)
+    want = lm.distill(_np(z), _np(idx), _np(t), None, _np(w), 1.0, dtype == BF16)
+    if alone:   # as many rows as the GPU needs to stream them, for the loss alone
+        many = 700 // r + 1
+        loss = ceca.dsgd_distill_loss(z.repeat(many, 1), idx.repeat(many, 1), t.repeat(many, 1), None, w.repeat(many))
+        _close(loss, tuple(np.tile(a, many) for a in want["loss"]), "loss alone")
+        return
+    loss, dz = ceca.dsgd_distill_grad(z, idx, t, None, w)
+    _close(loss, want["loss"], "loss")
+    _close(dz, want["dz"], "dz")
+
+
+def _time_of(call, n=10):
+    for _ in range(3):
+        call()
+    a, b = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+    times = []
+    for _ in range(n):
+        a.record()
+        call()
+        b.record()
+        torch.cuda.synchronize()
+        times.append(a.elapsed_time(b))
+    return sorted(times)[n // 2]
+
+
+@pytest.mark.parametrize("dtype,v", [(BF16, 32000), (F32, 128000), (F32, 8001)])
+def test_distillation_a_finite_mask_costs_what_an_infinite_one_does(dtype, v):
+    # an additive mask of -1e4 over most of the vocabulary, its first part included: a factor 2 leaves room for noise
+    r, k = 2048, 8
+    z = torch.randn((r, v), generator=_gen(41)).to(dtype).to(DEV)
+    gone = torch.arange(v, device=DEV) % 4096 < 3800
+    idx = (torch.arange(k, device=DEV) * 4096 % (v // 4096 * 4096) + 3900 + torch.arange(k, device=DEV)).expand(r, k).contiguous()
+    t = torch.randn((r, k), generator=_gen(42)).to(DEV)
+    out = torch.empty_like(z)
+    hard, soft = z.masked_fill(gone, -float("inf")), torch.where(gone, z.float() - 1e4, z.float()).to(dtype)
+    for a, b in zip(ceca.dsgd_distill_grad(hard[:9], idx[:9], t[:9]), ceca.dsgd_distill_grad(soft[:9], idx[:9], t[:9])):
+        assert torch.equal(a, b)
+    cost = [_time_of(lambda: ceca.dsgd_distill_grad(m, idx, t, dz=out)) for m in (hard, soft)]
+    assert cost[1] <= 2 * cost[0], cost
