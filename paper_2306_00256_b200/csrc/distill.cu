@@ -40,6 +40,7 @@ constexpr int64_t kHeld = 32 << 10, kMostHeld = 104 << 10;
 constexpr int64_t kMaxBits = 1 << 20;   // of the bitmap; longer parts wrap around in it
 constexpr int kDeep = 4;                // vectors a thread works on at a time
 constexpr float kLn2 = 0.6931471805599453f;
+constexpr float kLift = 32.f;   // binades by which pass 2 raises its exponentials: over a low temperature, a q below 2^-126 is a gradient that is not
 // Beyond this the rounding of M c (2^-24 of it) could itself overflow an exponential.  Logits of this size are masks of
 // the type's lowest value; a row that has no other gets its own, slower sums of 2^((z - M) c).
 constexpr float kFar = 1e8f;
@@ -472,10 +473,14 @@ __global__ void __launch_bounds__(THREADS, 768 / THREADS) distill_kernel(const D
   if (!dz) return;
   // pass 2
   const float scale = w / p.temperature;
-  const float inside = total == 0.f ? 0.f : scale / total;
-  const float outside = rest > 0.f && out > 0.f ? inside - scale * (rest / out) : inside;
+  // exponentials for q: 2^kLift q, about (the frame moves by the total's binade as well), and factors that much less, by what the
+  // frame has really moved
+  const float low = __fmul_rn(M, p.scale) + ((float)((__float_as_int(total) >> 23) - 127) - kLift), drop = ex2(far ? -kLift : low - __fmul_rn(M, p.scale));
+  const auto raised = [&](float v) { return ex2(far ? fmaf(v - M, p.scale, kLift) : fmaf(v, p.scale, -low)); };
+  const float inside = total == 0.f ? 0.f : scale / total * drop;
+  const float outside = rest > 0.f && out > 0.f ? inside - scale * (rest / out) * drop : inside;
   if (together && !far) {
-    const Val<2> shift = all<2>(-(M * p.scale)), by = all<2>(p.scale), factor = all<2>(outside);
+    const Val<2> shift = all<2>(-low), by = all<2>(p.scale), factor = all<2>(outside);
     const auto turn = [&](Vec<TZ> v) {
 #pragma unroll
       for (int i = 0; i < P; ++i) {
@@ -503,11 +508,11 @@ __global__ void __launch_bounds__(THREADS, 768 / THREADS) distill_kernel(const D
           if (u * THREADS < left) __stcs(dst + base + u * THREADS, turn(a[u]));
       }
     }
-    if (part.edge >= 0) narrow(dz + part.edge - part.pad, ex2(exponent(edge)) * outside);
+    if (part.edge >= 0) narrow(dz + part.edge - part.pad, raised(edge) * outside);
   } else {   // element by element, from memory (where dz is z, each thread reads what it writes over)
     const int64_t s1 = min((int64_t)slot1, p.v + part.pad);
     for (int64_t s = max((int64_t)slot0, (int64_t)part.pad) + tid; s < s1; s += THREADS)
-      narrow(dz + s - part.pad, ex2(exponent(widen(z[s - part.pad]))) * outside);
+      narrow(dz + s - part.pad, raised(widen(z[s - part.pad])) * outside);
   }
   __syncthreads();
   for (int j = tid; j < p.k; j += THREADS) {
@@ -522,7 +527,7 @@ __global__ void __launch_bounds__(THREADS, 768 / THREADS) distill_kernel(const D
           pc += expf(en.t[e] - norm);
         }
     }
-    if (first) narrow(dz + en.at[j], ex2(exponent(en.z[j])) * inside - scale * (pc / mass));
+    if (first) narrow(dz + en.at[j], raised(en.z[j]) * inside - scale * (pc / mass));
   }
 }
 

@@ -6,7 +6,7 @@ import torch
 
 import paper_2306_00256_b200 as ceca
 from oracle import lm
-from test_gpu_lm_operators import BF16, DEV, F32, NAN, _close, _gen, _np, _randn
+from test_gpu_lm_operators import BF16, DEV, F32, NAN, _close, _distill_inputs, _gen, _np, _randn
 
 pytestmark = pytest.mark.gpu
 
@@ -111,3 +111,15 @@ def test_distillation_a_finite_mask_costs_what_an_infinite_one_does(dtype, v):
         assert torch.equal(a, b)
     cost = [_time_of(lambda: ceca.dsgd_distill_grad(m, idx, t, dz=out)) for m in (hard, soft)]
     assert cost[1] <= 2 * cost[0], cost
+
+
+@pytest.mark.parametrize("dtype,v", [(F32, 700), (F32, 33000), (BF16, 5000), (F32, 50001)])
+@pytest.mark.parametrize("temperature", [0.2, 0.05, 0.01, 0.002])
+def test_distillation_small_shares_at_low_temperatures(dtype, v, temperature):
+    # q below the smallest normal number, over the temperature, is a gradient that is not
+    z, idx, t, _, _ = _distill_inputs(4, v, 6, dtype, False, 45)
+    T = float(np.float32(temperature))
+    want = lm.distill(_np(z), _np(idx), _np(t * T), None, None, T, dtype == BF16)
+    loss, dz = ceca.dsgd_distill_grad(z, idx, t * T, None, None, T)
+    _close(loss, want["loss"], "loss")
+    _close(dz, want["dz"], "dz")
