@@ -373,7 +373,8 @@ ceca_status_t dsgd_recurrence_grad(const void *x, const void *f, const void *dh,
  *   dz[i, c] = (w_i / T) * (q_c - sum of p_j over { j : idx_j = c })        at the top's entries,
  *   dz[i, c] = (w_i / T) * (q_c, less p0 q_c / q0 with a teacher_lse)       elsewhere
  * (no factor T^2: fold it into the weight).  An entry that a row lists twice counts with both p_j.  Logits of
- * -infinity have q = 0; a row of nothing else has q = 0 throughout.
+ * -infinity have q = 0; a row of nothing else has q = 0 throughout.  A logit below -9.3e7 T counts as -infinity in
+ * a row that has larger ones.
  * z, dz: device, logits_type, r x v with row strides ldz, lddz >= v; idx: device, index_type, r x k with
  * row stride ldi >= k; t: device, teacher_type, r x k with row stride ldt >= k; teacher_lse, weight, loss:
  * device fp32, r elements.  dz may be z with the same row stride (another one: CECA_ERR_UNSUPPORTED).

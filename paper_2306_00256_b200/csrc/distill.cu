@@ -10,7 +10,7 @@
 // entries outside the top alone: q0 must not come from a difference of sums that may be nearly equal, so what is held of
 // the top is struck out first, and the few entries are gathered and summed apart.  The threads' sums, each in a frame of
 // its own, meet in one exchange.  The second pass writes w / T (1 / S [- p0 / S0]) exp((z - M) / T) everywhere, and the
-// top's entries are then written over.  Exponents are taken to base 2, z c - M c with c = log2(e) / T in one fma.
+// top's entries are then written over.  Exponents are taken to base 2, z c - k with c = log2(e) / T and k = M c in one fma.
 //
 // 8192 rows of 128000 bf16 logits: 0.84 ms, 0.76 of the measured copy rate; two exponentials per logit keep the special
 // function units busy for 0.48 ms of it.  2047 rows of 50001: 88 us, 0.71; 4096 rows of 32000 fp32 logits: 0.19 ms, 0.84.
@@ -41,12 +41,14 @@ constexpr int64_t kMaxBits = 1 << 20;   // of the bitmap; longer parts wrap arou
 constexpr int kDeep = 4;                // vectors a thread works on at a time
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kLift = 32.f;   // binades by which pass 2 raises its exponentials: over a low temperature, a q below 2^-126 is a gradient that is not
-// Beyond this the rounding of M c (2^-24 of it) could itself overflow an exponential.  Logits of this size are masks of
-// the type's lowest value; a row that has no other gets its own, slower sums of 2^((z - M) c).
-constexpr float kFar = 1e8f;
-// A thread looks for a larger frame as long as it has seen no logit above this, so that additive masks (of -1e4, say) end up in
+// Exponents of this size: z c - k is exact but for its own rounding whatever k is, so a frame's k is m c rounded (kept as it is
+// rounded: all that move between frames, or that use one later, go by k).  That rounding shifts a frame by up to half an ulp of k,
+// 8 here and harmless; beyond, an exponential could overflow by it.  Logits below -kFar / c are masks; a row that has no others, or one
+// above kFar / c, gets its own, slower sums of 2^((z - M) c).
+constexpr float kFar = 0x1p27f;
+// A thread looks for a larger frame as long as it has seen no exponent above this, so that additive masks (of -1e4, say) end up in
 // no frame beside real logits; and the sum at which a thread that has settled starts again.
-constexpr float kLow = -2e3f, kLeave = 0x1p80f;
+constexpr float kLow = -3e3f, kLeave = 0x1p80f;
 
 struct DistillArgs {
   const void *z, *idx, *t;
@@ -115,18 +117,18 @@ template <int D> __device__ __forceinline__ float top_of(const Vec<bf16> *v) {
 // all: a frame does not have to be the maximum, only so near to it that the sum stays below kLeave.  (A sum that does not is
 // taken again, in the frame of the maximum.)  Then what a factor below 2^-126 makes nothing of when frames are joined is
 // below 2^-46 of the sum in the other frame, and no product with the joined sum or its reciprocal leaves the normal numbers.
+__device__ __forceinline__ float frame_of(float top, float scale) { return __fmul_rn(top, scale); }   // (not part of an fma)
 struct Seen {
-  float m = -kFar, k;
+  float k;
   Val<2> sum{0.f, 0.f};
-  __device__ __forceinline__ Seen(float top, float scale) : m(fmaxf(top, -kFar)) { k = m * scale; }
-  __device__ __forceinline__ bool settled() const { return m > kLow; }
+  __device__ __forceinline__ Seen(float top, float scale) : k(fmaxf(frame_of(top, scale), -kFar)) {}
+  __device__ __forceinline__ bool settled() const { return k > kLow; }
   __device__ __forceinline__ bool beyond() const { return sum.x + sum.y > kLeave; }
   template <int D, typename T> __device__ __forceinline__ void frame(const Vec<T> *a, float scale) {
-    const float top = top_of<D>(a);
-    if (top > m) {
-      sum = mul(sum, all<2>(ex2(k - top * scale)));   // (an edge element, or masked ones, may be in it)
-      m = top;
-      k = m * scale;
+    const float to = frame_of(top_of<D>(a), scale);
+    if (to > k) {
+      sum = mul(sum, all<2>(ex2(k - to)));   // (an edge element, or masked ones, may be in it)
+      k = to;
     }
   }
   template <int D, typename T> __device__ __forceinline__ void take(const Vec<T> *a, float scale) {
@@ -181,26 +183,26 @@ __device__ __forceinline__ float warp_sum(float x) {
   return x;
 }
 
-// What a warp, a CTA or a cluster knows of its part of a row, in the frame k = m c: the sum of 2^(z c - k) by pass 1, the
+// What a warp, a CTA or a cluster knows of its part of a row, in the frame k: the sum of 2^(z c - k) by pass 1, the
 // same over the top (each entry once), the teacher's weights p there, and p (log p - ln2 (z c - k)).
 struct alignas(16) Known {
-  float m, sum, top, mass, terms, pad[3];
+  float k, sum, top, mass, terms, pad[3];
 };
 // The n parts of `all` in one frame, on every lane of the warp that asks: each lane moves its own there (terms move by ln2 p
 // times the distance), and the sums run over the lanes in one fixed order.
-template <int MOST> __device__ __forceinline__ Known joined(const Known *all, int n, float scale) {
+template <int MOST> __device__ __forceinline__ Known joined(const Known *all, int n) {
   const int lane = threadIdx.x & 31;
   Known q[(MOST + 31) / 32], a{-INFINITY, 0.f, 0.f, 0.f, 0.f};
 #pragma unroll
   for (int i = 0; i < (MOST + 31) / 32; ++i) {
     q[i] = lane + 32 * i < n ? all[lane + 32 * i] : Known{-INFINITY, 0.f, 0.f, 0.f, 0.f};
-    a.m = fmaxf(a.m, q[i].m);
+    a.k = fmaxf(a.k, q[i].k);
   }
-  a.m = warp_max(a.m);
+  a.k = warp_max(a.k);
 #pragma unroll
   for (int i = 0; i < (MOST + 31) / 32; ++i)
     if (lane + 32 * i < n) {
-      const float d = (q[i].m - a.m) * scale, f = ex2(d);
+      const float d = q[i].k - a.k, f = ex2(d);
       a.sum += q[i].sum * f;
       a.top += q[i].top * f;
       a.terms += q[i].terms - kLn2 * d * q[i].mass;
@@ -395,11 +397,11 @@ __global__ void __launch_bounds__(THREADS, 768 / THREADS) distill_kernel(const D
   }
   // the warp's part in its own frame, then everybody's
   Known all_of;
-  float m = seen.m;
+  float k = seen.k;
   for (int j = tid; j < p.k; j += THREADS)
-    if (en.at[j] >= 0) m = fmaxf(m, en.z[j]);
-  all_of.m = warp_max(m);
-  const float kw = all_of.m * p.scale, norm = tail ? lse : tmax;
+    if (en.at[j] >= 0) k = fmaxf(k, frame_of(en.z[j], p.scale));
+  all_of.k = warp_max(k);
+  const float kw = all_of.k, norm = tail ? lse : tmax;
   float sums[4] = {(seen.sum.x + seen.sum.y) * ex2(seen.k - kw), 0.f, 0.f, 0.f};
   const auto entry = [&](int j, float y) {   // what entry j adds, its exponent being y
     bool first = true;
@@ -426,13 +428,14 @@ __global__ void __launch_bounds__(THREADS, 768 / THREADS) distill_kernel(const D
       if (lane == 0) share[warp] = all_of;
       __syncthreads();
     }
-    if (CLUSTER || W > 1) all_of = joined<kParts>(share, W * ranks, p.scale);
+    if (CLUSTER || W > 1) all_of = joined<kParts>(share, W * ranks);
   };
   gather();
-  float M = all_of.m;
-  const bool far = !(fabsf(M) < kFar && all_of.sum < INFINITY);
-  const auto exponent = [&](float v) { return far ? (v - M) * p.scale : fmaf(v, p.scale, -(M * p.scale)); };
-  if (far) {   // logits beyond +-kFar only, infinities or NaN: once more, element by element
+  const float K = all_of.k;
+  const bool far = !(fabsf(K) < kFar && all_of.sum < INFINITY);
+  float M = 0.f;
+  const auto exponent = [&](float v) { return far ? (v - M) * p.scale : fmaf(v, p.scale, -K); };
+  if (far) {   // exponents beyond +-kFar, infinities or NaN: once more, element by element
     float top = -INFINITY;
     const int64_t s1 = min((int64_t)slot1, p.v + part.pad);
     for (int64_t s = max((int64_t)slot0, (int64_t)part.pad) + tid; s < s1; s += THREADS) top = fmaxf(top, widen(z[s - part.pad]));
@@ -452,7 +455,7 @@ __global__ void __launch_bounds__(THREADS, 768 / THREADS) distill_kernel(const D
       if (counts(s)) sums[0] += ex2(exponent(widen(z[s - part.pad])));
     for (int j = tid; j < p.k; j += THREADS)
       if (en.at[j] >= 0) entry(j, exponent(en.z[j]));
-    all_of.m = 0.f;   // one frame for all
+    all_of.k = 0.f;   // one frame for all
     if (CLUSTER) {    // everybody has read the first parts
       cluster_arrive(false);
       cluster_wait();
@@ -475,7 +478,7 @@ __global__ void __launch_bounds__(THREADS, 768 / THREADS) distill_kernel(const D
   const float scale = w / p.temperature;
   // exponentials for q: 2^kLift q, about (the frame moves by the total's binade as well), and factors that much less, by what the
   // frame has really moved
-  const float low = __fmul_rn(M, p.scale) + ((float)((__float_as_int(total) >> 23) - 127) - kLift), drop = ex2(far ? -kLift : low - __fmul_rn(M, p.scale));
+  const float low = K + ((float)((__float_as_int(total) >> 23) - 127) - kLift), drop = ex2(far ? -kLift : low - K);
   const auto raised = [&](float v) { return ex2(far ? fmaf(v - M, p.scale, kLift) : fmaf(v, p.scale, -low)); };
   const float inside = total == 0.f ? 0.f : scale / total * drop;
   const float outside = rest > 0.f && out > 0.f ? inside - scale * (rest / out) * drop : inside;

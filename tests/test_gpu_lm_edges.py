@@ -123,3 +123,37 @@ def test_distillation_small_shares_at_low_temperatures(dtype, v, temperature):
     loss, dz = ceca.dsgd_distill_grad(z, idx, t * T, None, None, T)
     _close(loss, want["loss"], "loss")
     _close(dz, want["dz"], "dz")
+
+
+def _check_offset(dtype, v, tail, temperature, offset):
+    z, idx, t, lse, w = _distill_inputs(4, v, 6, F32, tail, 51, F32, torch.int32, temperature)
+    z = (z + offset).to(dtype)
+    t = t * temperature   # (what the teacher sends for this temperature)
+    if tail:
+        here = (idx >= 0) & (idx < v)
+        lse = torch.logsumexp((t.double() / float(np.float32(temperature))).masked_fill(~here, -float("inf")), 1).float() + 0.2
+    T = float(np.float32(temperature))
+    want = lm.distill(_np(z), _np(idx), _np(t), _np(lse), None, T, dtype == BF16)
+    loss, dz = ceca.dsgd_distill_grad(z, idx, t, lse, None, T)
+    _close(loss, want["loss"], "loss")
+    _close(dz, want["dz"], "dz")
+    _close(ceca.dsgd_distill_loss(z, idx, t, lse, None, T), want["loss"], "loss alone")
+
+
+OFFSET_SIZES = [(F32, 700), (F32, 3000), (F32, 33000), (F32, 50001), (BF16, 33000)]
+
+
+@pytest.mark.parametrize("dtype,v", OFFSET_SIZES)
+@pytest.mark.parametrize("tail", [False, True])
+@pytest.mark.parametrize("offset", [100.0, -100.0, 1e3, -1e3, 1e4, -1e4, 1e5, 1e7, -1e7, 9e7])
+def test_distillation_of_logits_that_share_an_offset(dtype, v, tail, offset):
+    _check_offset(dtype, v, tail, 1.0, offset)   # softmax does not know it
+
+
+LOW = [(0.05, 1e3), (0.01, 3e5), (0.01, 1e6), (0.01, -1e6), (1e-5, 30.0), (1e-7, 30.0), (100.0, 1e9)]
+
+
+@pytest.mark.parametrize("dtype,v", OFFSET_SIZES)
+@pytest.mark.parametrize("temperature,offset", LOW)
+def test_distillation_of_an_offset_at_a_low_temperature(dtype, v, temperature, offset):
+    _check_offset(dtype, v, False, temperature, offset)   # which makes a large one of any
