@@ -98,6 +98,11 @@ def recurrence_grad(x, f, dh, h0=None, starts=None, dh_last=None, bf16=False):
 # ------------------------------------------------------------------------------------------- distillation
 
 
+def _logsumexp(x):
+    top = x.max() if x.size else -np.inf
+    return top if top == -np.inf else top + np.log(np.exp(x - top).sum())
+
+
 def distill(z, idx, t, teacher_lse=None, weight=None, temperature=1.0, bf16=False):
     """{name: (want, tolerance)} of loss and dz, row by row."""
     r, v = z.shape
@@ -149,17 +154,17 @@ def distill(z, idx, t, teacher_lse=None, weight=None, temperature=1.0, bf16=Fals
             target = pc
             et = rp * pc + len(js) * U * pc
             if teacher_lse is not None:
-                q0 = q[~inside].sum()
+                lq0 = _logsumexp(logq[~inside])   # q0 itself may be too small for 64 bits
+                share = np.where(~inside, np.exp(logq - lq0), 0.0) if lq0 > -np.inf else np.zeros(v)
                 if p0 > 0:
-                    lr = np.log(p0 / q0)
+                    lr = np.log(p0) - lq0
                     kl += p0 * lr
                     ekl += ep0 * (abs(lr) + 1) + p0 * (2 * rq + 8 * U * (abs(lr) + 1)) + U * abs(p0 * lr)
-                    share = np.where(~inside, q / q0, 0.0) if q0 > 0 else np.zeros(v)
                     target = np.where(inside, pc, p0 * share)
                     et = np.where(inside, et, share * (ep0 + p0 * 3 * rq))
-                elif ep0 > 0 and q0 > 0:   # the true rest may be rounded up to ep0
-                    ekl += ep0 * (abs(np.log(ep0 / q0)) + 1)
-                    et = np.where(inside, et, q / q0 * ep0)
+                elif ep0 > 0 and lq0 > -np.inf:   # the true rest may be rounded up to ep0
+                    ekl += ep0 * (abs(np.log(ep0) - lq0) + 1)
+                    et = np.where(inside, et, share * ep0)
         loss[i], tl[i] = w * kl, abs(w) * ekl
         dz[i] = w / temperature * (q - target)
         tz[i] = abs(w) / temperature * (3 * rq * q + et + 3 * U * (q + target))

@@ -8,9 +8,11 @@
 // work on, asynchronously, so a row is read once.  (Rows above 832 KB are read twice, the second time mostly from L2; for
 // the loss alone nothing needs to be held.)  A first pass sums exponentials per thread, with a teacher_lse over the
 // entries outside the top alone: q0 must not come from a difference of sums that may be nearly equal, so what is held of
-// the top is struck out first, and the few entries are gathered and summed apart.  The threads' sums, each in a frame of
-// its own, meet in one exchange.  The second pass writes w / T (1 / S [- p0 / S0]) exp((z - M) / T) everywhere, and the
-// top's entries are then written over.  Exponents are taken to base 2, z c - k with c = log2(e) / T and k = M c in one fma.
+// the top is struck out first, and the few entries are gathered and summed apart, in a frame of their own: the student's
+// mass outside a top that towers over it may be too small for fp32, its logarithm and the shares of it are not.  The threads'
+// sums, each in a frame of its own, meet in one exchange.  The second pass writes w / T (q / S - p0 / S0) exp((z - M) / T)
+// everywhere, with S0 and M of pass 1 and q its share of everything, and the top's entries are then written over.  Exponents are taken to
+// base 2, z c - k with c = log2(e) / T and k = M c in one fma.
 //
 // 8192 rows of 128000 bf16 logits: 0.84 ms, 0.76 of the measured copy rate; two exponentials per logit keep the special
 // function units busy for 0.48 ms of it.  2047 rows of 50001: 88 us, 0.71; 4096 rows of 32000 fp32 logits: 0.19 ms, 0.84.
@@ -183,28 +185,31 @@ __device__ __forceinline__ float warp_sum(float x) {
   return x;
 }
 
-// What a warp, a CTA or a cluster knows of its part of a row, in the frame k: the sum of 2^(z c - k) by pass 1, the
-// same over the top (each entry once), the teacher's weights p there, and p (log p - ln2 (z c - k)).
+// What a warp, a CTA or a cluster knows of its part of a row: the sum of 2^(z c - k) by pass 1, and of the top, whose frame kt is
+// another because either may lie beyond an exponential's reach from the other, the same sum (each entry once), the
+// teacher's weights p, and p (log p - ln2 (z c - kt)).
 struct alignas(16) Known {
-  float k, sum, top, mass, terms, pad[3];
+  float k, kt, sum, top, mass, terms, pad[2];
 };
-// The n parts of `all` in one frame, on every lane of the warp that asks: each lane moves its own there (terms move by ln2 p
-// times the distance), and the sums run over the lanes in one fixed order.
+// The n parts of `all` in one frame of each kind, on every lane of the warp that asks: each lane moves its own there (terms
+// move by ln2 p times the distance), and the sums run over the lanes in one fixed order.
 template <int MOST> __device__ __forceinline__ Known joined(const Known *all, int n) {
   const int lane = threadIdx.x & 31;
-  Known q[(MOST + 31) / 32], a{-INFINITY, 0.f, 0.f, 0.f, 0.f};
+  Known q[(MOST + 31) / 32], a{-INFINITY, -INFINITY};
 #pragma unroll
   for (int i = 0; i < (MOST + 31) / 32; ++i) {
-    q[i] = lane + 32 * i < n ? all[lane + 32 * i] : Known{-INFINITY, 0.f, 0.f, 0.f, 0.f};
+    q[i] = lane + 32 * i < n ? all[lane + 32 * i] : Known{-INFINITY, -INFINITY};
     a.k = fmaxf(a.k, q[i].k);
+    a.kt = fmaxf(a.kt, q[i].kt);
   }
   a.k = warp_max(a.k);
+  a.kt = warp_max(a.kt);
 #pragma unroll
   for (int i = 0; i < (MOST + 31) / 32; ++i)
     if (lane + 32 * i < n) {
-      const float d = q[i].k - a.k, f = ex2(d);
-      a.sum += q[i].sum * f;
-      a.top += q[i].top * f;
+      const float d = q[i].kt - a.kt;
+      a.sum += q[i].sum * ex2(q[i].k - a.k);
+      a.top += q[i].top * ex2(d);
       a.terms += q[i].terms - kLn2 * d * q[i].mass;
       a.mass += q[i].mass;
     }
@@ -234,7 +239,8 @@ __global__ void __launch_bounds__(THREADS, 768 / THREADS) distill_kernel(const D
   extern __shared__ uint4 memory[];   // the part's whole vectors, the bitmap, the entries
   constexpr int kParts = W * (CLUSTER ? kMaxCluster : 1);
   __shared__ Known share[kParts];   // of each warp of the cluster
-  __shared__ float tops[W], far_red[W], far_share[kMaxCluster];
+  __shared__ float tops[W];
+  __shared__ float2 far_red[W], far_share[kMaxCluster];
   uint32_t *bitmap = reinterpret_cast<uint32_t *>(memory + (HELD ? p.per : 0));
   Entries en;
   en.at = reinterpret_cast<int32_t *>(bitmap + p.words);
@@ -395,14 +401,16 @@ __global__ void __launch_bounds__(THREADS, 768 / THREADS) distill_kernel(const D
       seen.take<1>(&a, p.scale);
     }
   }
-  // the warp's part in its own frame, then everybody's
+  // the warp's part in frames of its own, then everybody's
   Known all_of;
-  float k = seen.k;
+  float kt = -kFar;
   for (int j = tid; j < p.k; j += THREADS)
-    if (en.at[j] >= 0) k = fmaxf(k, frame_of(en.z[j], p.scale));
-  all_of.k = warp_max(k);
-  const float kw = all_of.k, norm = tail ? lse : tmax;
-  float sums[4] = {(seen.sum.x + seen.sum.y) * ex2(seen.k - kw), 0.f, 0.f, 0.f};
+    if (en.at[j] >= 0) kt = fmaxf(kt, frame_of(en.z[j], p.scale));
+  all_of.k = warp_max(seen.k);
+  all_of.kt = warp_max(kt);
+  kt = all_of.kt;
+  const float norm = tail ? lse : tmax;
+  float sums[4] = {(seen.sum.x + seen.sum.y) * ex2(seen.k - all_of.k), 0.f, 0.f, 0.f};
   const auto entry = [&](int j, float y) {   // what entry j adds, its exponent being y
     bool first = true;
     if (twice)
@@ -413,7 +421,7 @@ __global__ void __launch_bounds__(THREADS, 768 / THREADS) distill_kernel(const D
     if (pj > 0.f) sums[3] += pj * (lp - kLn2 * y);
   };
   for (int j = tid; j < p.k; j += THREADS)
-    if (en.at[j] >= 0) entry(j, fmaf(en.z[j], p.scale, -kw));
+    if (en.at[j] >= 0) entry(j, fmaf(en.z[j], p.scale, -kt));
   const auto gather = [&]() {
     all_of.sum = warp_sum(sums[0]);
     all_of.top = warp_sum(sums[1]);
@@ -431,31 +439,47 @@ __global__ void __launch_bounds__(THREADS, 768 / THREADS) distill_kernel(const D
     if (CLUSTER || W > 1) all_of = joined<kParts>(share, W * ranks);
   };
   gather();
-  const float K = all_of.k;
-  const bool far = !(fabsf(K) < kFar && all_of.sum < INFINITY);
-  float M = 0.f;
-  const auto exponent = [&](float v) { return far ? (v - M) * p.scale : fmaf(v, p.scale, -K); };
+  // The frames: K of pass 1's sum, Kt of the top's, Ka of everything, and how far below Ka the others lie (without a
+  // teacher_lse pass 1 has seen everything, and Kt may lie above).  A far row's are 0, and its logits less these M.
+  const float K = all_of.k, Kt = all_of.kt, Ka = tail ? fmaxf(K, Kt) : K;
+  float M = 0.f, Mt = 0.f, Ma = 0.f, under = K - Ka, under_top = Kt - Ka;
+  const bool far = !(fabsf(fmaxf(K, Kt)) < kFar && all_of.sum < INFINITY);
   if (far) {   // exponents beyond +-kFar, infinities or NaN: once more, element by element
-    float top = -INFINITY;
     const int64_t s1 = min((int64_t)slot1, p.v + part.pad);
-    for (int64_t s = max((int64_t)slot0, (int64_t)part.pad) + tid; s < s1; s += THREADS) top = fmaxf(top, widen(z[s - part.pad]));
-    top = warp_max(top);
-    if ((tid & 31) == 0) far_red[warp] = top;
+    M = Mt = -INFINITY;
+    for (int64_t s = max((int64_t)slot0, (int64_t)part.pad) + tid; s < s1; s += THREADS)
+      if (counts(s)) M = fmaxf(M, widen(z[s - part.pad]));
+    for (int j = tid; j < p.k; j += THREADS)
+      if (en.at[j] >= 0) Mt = fmaxf(Mt, en.z[j]);
+    M = warp_max(M);
+    Mt = warp_max(Mt);
+    if ((tid & 31) == 0) far_red[warp] = make_float2(M, Mt);
     __syncthreads();
-    for (int i = 0; i < W; ++i) top = fmaxf(top, far_red[i]);
+    const auto greatest = [&](const float2 *of, int n) {
+      for (int i = 0; i < n; ++i) {
+        M = fmaxf(M, of[i].x);
+        Mt = fmaxf(Mt, of[i].y);
+      }
+    };
+    greatest(far_red, W);
     if (CLUSTER) {
-      if (tid < ranks) *cg::this_cluster().map_shared_rank(far_share + rank, tid) = top;
+      if (tid < ranks) *cg::this_cluster().map_shared_rank(far_share + rank, tid) = make_float2(M, Mt);
       cluster_arrive(tid < 32);
       cluster_wait();
-      for (int r = 0; r < ranks; ++r) top = fmaxf(top, far_share[r]);
+      greatest(far_share, ranks);
     }
-    M = top == -INFINITY ? 0.f : top;
+    Ma = tail ? fmaxf(M, Mt) : M;   // where there is nothing, there are no distances either
+    under = M == -INFINITY ? 0.f : (M - Ma) * p.scale;
+    under_top = Mt == -INFINITY || Ma == -INFINITY ? 0.f : (Mt - Ma) * p.scale;
+    if (M == -INFINITY) M = 0.f;
+    if (Mt == -INFINITY) Mt = 0.f;
+    if (Ma == -INFINITY) Ma = 0.f;
     sums[0] = sums[1] = sums[2] = sums[3] = 0.f;
     for (int64_t s = max((int64_t)slot0, (int64_t)part.pad) + tid; s < s1; s += THREADS)
-      if (counts(s)) sums[0] += ex2(exponent(widen(z[s - part.pad])));
+      if (counts(s)) sums[0] += ex2((widen(z[s - part.pad]) - M) * p.scale);
     for (int j = tid; j < p.k; j += THREADS)
-      if (en.at[j] >= 0) entry(j, exponent(en.z[j]));
-    all_of.k = 0.f;   // one frame for all
+      if (en.at[j] >= 0) entry(j, (en.z[j] - Mt) * p.scale);
+    all_of.k = all_of.kt = 0.f;   // the same frames for all
     if (CLUSTER) {    // everybody has read the first parts
       cluster_arrive(false);
       cluster_wait();
@@ -464,26 +488,32 @@ __global__ void __launch_bounds__(THREADS, 768 / THREADS) distill_kernel(const D
     }
     gather();
   }
-  const float out = all_of.sum, total = all_of.sum + all_of.top;
+  const float out = all_of.sum, total = out * ex2(under) + (tail ? all_of.top * ex2(under_top) : 0.f);
   const float mass = tail ? 1.f : all_of.mass;   // what the teacher's weights are divided by
   const float rest = tail ? fmaxf(0.f, 1.f - all_of.mass) : 0.f;
   if (tid == 0 && rank == 0 && p.loss) {
-    float l = tail ? all_of.terms + all_of.mass * logf(total) : all_of.terms / mass - logf(mass) + logf(total);
-    if (rest > 0.f) l += rest * logf(rest / (out / total));
+    const float log_total = logf(total) - kLn2 * under_top;   // in the top's frame
+    float l = tail ? all_of.terms + all_of.mass * log_total : all_of.terms / mass - logf(mass) + log_total;
+    if (rest > 0.f) l += rest * (logf(rest * (total / out)) - kLn2 * under);
     if (total == 0.f) l = INFINITY;
     p.loss[row] = w * l;
   }
   if (!dz) return;
   // pass 2
   const float scale = w / p.temperature;
-  // exponentials for q: 2^kLift q, about (the frame moves by the total's binade as well), and factors that much less, by what the
-  // frame has really moved
-  const float low = K + ((float)((__float_as_int(total) >> 23) - 127) - kLift), drop = ex2(far ? -kLift : low - K);
-  const auto raised = [&](float v) { return ex2(far ? fmaf(v - M, p.scale, kLift) : fmaf(v, p.scale, -low)); };
-  const float inside = total == 0.f ? 0.f : scale / total * drop;
-  const float outside = rest > 0.f && out > 0.f ? inside - scale * (rest / out) * drop : inside;
+  // Raised exponentials: 2^kLift z's share of a sum, about (a frame moves by the sum's binade as well), and factors that much less, by
+  // what the frame has really moved.  q is a share of everything at the top's entries, of pass 1's sum elsewhere.
+  struct Raised { float low, drop; };
+  const auto raise = [&](float k, float sum) -> Raised {
+    const float low = k + ((float)((__float_as_int(sum) >> 23) - 127) - kLift);
+    return {low, ex2(far ? -kLift : low - k)};
+  };
+  const Raised all_raised = raise(Ka, total), out_raised = raise(K, out);
+  const auto raised = [&](float v, float m, float low) { return ex2(far ? fmaf(v - m, p.scale, kLift) : fmaf(v, p.scale, -low)); };
+  const float part_of_all = total == 0.f ? 0.f : scale / total, inside = part_of_all * all_raised.drop;
+  const float outside = (part_of_all * ex2(under) - (rest > 0.f && out > 0.f ? scale * (rest / out) : 0.f)) * out_raised.drop;
   if (together && !far) {
-    const Val<2> shift = all<2>(-low), by = all<2>(p.scale), factor = all<2>(outside);
+    const Val<2> shift = all<2>(-out_raised.low), by = all<2>(p.scale), factor = all<2>(outside);
     const auto turn = [&](Vec<TZ> v) {
 #pragma unroll
       for (int i = 0; i < P; ++i) {
@@ -511,11 +541,11 @@ __global__ void __launch_bounds__(THREADS, 768 / THREADS) distill_kernel(const D
           if (u * THREADS < left) __stcs(dst + base + u * THREADS, turn(a[u]));
       }
     }
-    if (part.edge >= 0) narrow(dz + part.edge - part.pad, raised(edge) * outside);
+    if (part.edge >= 0) narrow(dz + part.edge - part.pad, raised(edge, M, out_raised.low) * outside);
   } else {   // element by element, from memory (where dz is z, each thread reads what it writes over)
     const int64_t s1 = min((int64_t)slot1, p.v + part.pad);
     for (int64_t s = max((int64_t)slot0, (int64_t)part.pad) + tid; s < s1; s += THREADS)
-      narrow(dz + s - part.pad, raised(widen(z[s - part.pad])) * outside);
+      narrow(dz + s - part.pad, raised(widen(z[s - part.pad]), M, out_raised.low) * outside);
   }
   __syncthreads();
   for (int j = tid; j < p.k; j += THREADS) {
@@ -530,7 +560,7 @@ __global__ void __launch_bounds__(THREADS, 768 / THREADS) distill_kernel(const D
           pc += expf(en.t[e] - norm);
         }
     }
-    if (first) narrow(dz + en.at[j], raised(en.z[j]) * inside - scale * (pc / mass));
+    if (first) narrow(dz + en.at[j], raised(en.z[j], Ma, all_raised.low) * inside - scale * (pc / mass));
   }
 }
 

@@ -157,3 +157,53 @@ LOW = [(0.05, 1e3), (0.01, 3e5), (0.01, 1e6), (0.01, -1e6), (1e-5, 30.0), (1e-7,
 @pytest.mark.parametrize("temperature,offset", LOW)
 def test_distillation_of_an_offset_at_a_low_temperature(dtype, v, temperature, offset):
     _check_offset(dtype, v, False, temperature, offset)   # which makes a large one of any
+
+
+@pytest.mark.parametrize("dtype,v", [(F32, 900), (BF16, 50000), (F32, 50000), (F32, 300001), (F32, 2500001)])
+@pytest.mark.parametrize("temperature", [1.0, 0.25, 0.1])
+def test_distillation_outside_of_a_top_that_towers_over_it(dtype, v, temperature):
+    # q0, the student's mass outside the top, is below what fp32 holds: its logarithm and its shares are not
+    gaps = [20.0, 60.0, 80.0, 86.0, 87.0, 88.0, 90.0, 100.0, 104.0, 150.0, 300.0, 1000.0, -30.0, -95.0, -400.0]
+    if v > 100000:
+        gaps = gaps[::3]
+    r = len(gaps)
+    z = torch.randn((r, v), generator=_gen(61))
+    idx = torch.stack([torch.randperm(v, generator=_gen(62 + i))[:4] for i in range(r)])
+    z[torch.arange(r), idx[:, 1]] = torch.tensor(gaps)
+    t = torch.randn((r, 4), generator=_gen(63)) * temperature
+    idx[:, 3] = -1
+    lse = torch.logsumexp(t[:, :3] / temperature, 1) + 0.3
+    z, idx, t, lse = z.to(dtype).to(DEV), idx.to(DEV), t.to(DEV), lse.to(DEV)
+    T = float(np.float32(temperature))
+    want = lm.distill(_np(z), _np(idx), _np(t), _np(lse), None, T, dtype == BF16)
+    assert np.isfinite(want["loss"][0]).all()
+    loss, dz = ceca.dsgd_distill_grad(z, idx, t, lse, None, T)
+    _close(loss, want["loss"], "loss")
+    _close(dz, want["dz"], "dz")
+    _close(ceca.dsgd_distill_loss(z, idx, t, lse, None, T), want["loss"], "loss alone")
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("v", [600, 40000])
+def test_distillation_outside_of_a_top_among_logits_far_from_zero(dtype, v):
+    # the same where every logit is too far from zero for one multiplication by 1 / T
+    r, base = 4, 3e8 if dtype == F32 else 2.0 ** 28
+    step, temperatures = (32.0, (2.0, 0.5)) if dtype == F32 else (2.0 ** 21, (1.0, 0.25))   # the type's spacing there
+    z = base + step * torch.randint(-3, 4, (r, v), generator=_gen(65)).float()
+    idx = torch.stack([torch.randperm(v, generator=_gen(66 + i))[:4] for i in range(r)])
+    z[torch.arange(r), idx[:, 0]] = base + 40 * step
+    t = torch.randn((r, 4), generator=_gen(67))
+    lse = (torch.logsumexp(t, 1) + 0.3).to(DEV)
+    z, idx, t = z.to(dtype).to(DEV), idx.to(DEV), t.to(DEV)
+    for e in (lse, None):
+        for T in temperatures:
+            want = lm.distill(_np(z), _np(idx), _np(t * T), _np(e), None, T, dtype == BF16)
+            loss, dz = ceca.dsgd_distill_grad(z, idx, t * T, e, None, T)
+            _close(loss, want["loss"], "loss")
+            _close(dz, want["dz"], "dz")
+
+
+@pytest.mark.parametrize("dtype,v", OFFSET_SIZES)
+@pytest.mark.parametrize("temperature,offset", LOW)
+def test_distillation_outside_of_a_top_at_a_low_temperature(dtype, v, temperature, offset):
+    _check_offset(dtype, v, True, temperature, offset)
