@@ -370,8 +370,10 @@ ceca_status_t dsgd_recurrence_grad(const void *x, const void *f, const void *dh,
  *                                   loss[i] = w_i * (sum_j p_j (log p_j - log q[idx_j]) + p0 log(p0 / q0))
  * w_i = weight[i] (1 when weight is NULL).  A row with w_i = 0, or without any teacher entry, has loss 0
  * and a zero gradient, whatever its logits hold.  The gradient is
- *   dz[i, c] = (w_i / T) * (q_c - sum of p_j over { j : idx_j = c })        at the top's entries,
- *   dz[i, c] = (w_i / T) * (q_c, less p0 q_c / q0 with a teacher_lse)       elsewhere
+ *   dz[i, c] = (w_i / T) * (m q_c - sum of p_j over { j : idx_j = c })      at the top's entries,
+ *   dz[i, c] = (w_i / T) * (m q_c, less p0 q_c / q0 with a teacher_lse)     elsewhere
+ * with m = sum_j p_j + p0, all the mass that is compared: 1, or with a teacher_lse sum_j p_j where that is more, as it
+ * can be by the rounding of teacher logits that were sent in fewer bits than their log-sum-exp
  * (no factor T^2: fold it into the weight).  An entry that a row lists twice counts with both p_j.  Logits of
  * -infinity have q = 0; a row of nothing else has q = 0 throughout.  A logit below -9.3e7 T counts as -infinity in
  * a row that has larger ones.

@@ -166,7 +166,12 @@ def distill(z, idx, t, teacher_lse=None, weight=None, temperature=1.0, bf16=Fals
                     ekl += ep0 * (abs(np.log(ep0) - lq0) + 1)
                     et = np.where(inside, et, share * ep0)
         loss[i], tl[i] = w * kl, abs(w) * ekl
-        dz[i] = w / temperature * (q - target)
-        tz[i] = abs(w) / temperature * (3 * rq * q + et + 3 * U * (q + target))
+        # all the mass that is compared is 1, or what the top holds where that is more (or may be rounded to more)
+        all_mass, e_mass = 1.0, 0.0
+        if teacher_lse is not None:
+            all_mass = p.sum() + p0
+            e_mass = ep0 if p.sum() > 1.0 - ep0 else 0.0
+        dz[i] = w / temperature * (all_mass * q - target)
+        tz[i] = abs(w) / temperature * ((3 * rq * all_mass + e_mass) * q + et + 3 * U * (all_mass * q + target))
     with np.errstate(invalid="ignore"):
         return {"loss": _out(loss, tl, False), "dz": _out(dz, tz, bf16)}

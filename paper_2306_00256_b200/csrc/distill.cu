@@ -1,7 +1,7 @@
 // Distillation from a teacher's top logits: loss per row, and its gradient with respect to the student's logits.
 //
 //   q = softmax(z / T),  p_j = exp(t_j / T - N),  loss = w (sum_j p_j (log p_j - log q_j) [+ p0 log(p0 / q0)])
-//   dz = (w / T) (q - p) at the top's entries, (w / T) (q [- p0 q / q0]) elsewhere
+//   dz = (w / T) (m q - p) at the top's entries, (w / T) (m q [- p0 q / q0]) elsewhere, m = sum_j p_j [+ p0]: 1, or more where the top has more
 //
 // A CTA takes a row that fits in shared memory, or a cluster of up to 8 takes a part of it each, 32 KB a CTA, six CTAs an
 // SM whose phases overlap; there are more to a row where there are few rows.  Every thread copies the vectors that it will
@@ -10,8 +10,8 @@
 // entries outside the top alone: q0 must not come from a difference of sums that may be nearly equal, so what is held of
 // the top is struck out first, and the few entries are gathered and summed apart, in a frame of their own: the student's
 // mass outside a top that towers over it may be too small for fp32, its logarithm and the shares of it are not.  The threads'
-// sums, each in a frame of its own, meet in one exchange.  The second pass writes w / T (q / S - p0 / S0) exp((z - M) / T)
-// everywhere, with S0 and M of pass 1 and q its share of everything, and the top's entries are then written over.  Exponents are taken to
+// sums, each in a frame of its own, meet in one exchange.  The second pass writes w / T (m / S - p0 / S0) exp((z - M) / T)
+// everywhere, with S0 and M of pass 1 and S the sum of everything in that frame, and the top's entries are then written over.  Exponents are taken to
 // base 2, z c - k with c = log2(e) / T and k = M c in one fma.
 //
 // 8192 rows of 128000 bf16 logits: 0.84 ms, 0.76 of the measured copy rate; two exponentials per logit keep the special
@@ -491,6 +491,7 @@ __global__ void __launch_bounds__(THREADS, 768 / THREADS) distill_kernel(const D
   const float out = all_of.sum, total = out * ex2(under) + (tail ? all_of.top * ex2(under_top) : 0.f);
   const float mass = tail ? 1.f : all_of.mass;   // what the teacher's weights are divided by
   const float rest = tail ? fmaxf(0.f, 1.f - all_of.mass) : 0.f;
+  const float compared = tail ? fmaxf(1.f, all_of.mass) : 1.f;   // with log q, the top's mass and the rest
   if (tid == 0 && rank == 0 && p.loss) {
     const float log_total = logf(total) - kLn2 * under_top;   // in the top's frame
     float l = tail ? all_of.terms + all_of.mass * log_total : all_of.terms / mass - logf(mass) + log_total;
@@ -510,7 +511,7 @@ __global__ void __launch_bounds__(THREADS, 768 / THREADS) distill_kernel(const D
   };
   const Raised all_raised = raise(Ka, total), out_raised = raise(K, out);
   const auto raised = [&](float v, float m, float low) { return ex2(far ? fmaf(v - m, p.scale, kLift) : fmaf(v, p.scale, -low)); };
-  const float part_of_all = total == 0.f ? 0.f : scale / total, inside = part_of_all * all_raised.drop;
+  const float part_of_all = total == 0.f ? 0.f : scale * compared / total, inside = part_of_all * all_raised.drop;
   const float outside = (part_of_all * ex2(under) - (rest > 0.f && out > 0.f ? scale * (rest / out) : 0.f)) * out_raised.drop;
   if (together && !far) {
     const Val<2> shift = all<2>(-out_raised.low), by = all<2>(p.scale), factor = all<2>(outside);

@@ -207,3 +207,38 @@ def test_distillation_outside_of_a_top_among_logits_far_from_zero(dtype, v):
 @pytest.mark.parametrize("temperature,offset", LOW)
 def test_distillation_outside_of_a_top_at_a_low_temperature(dtype, v, temperature, offset):
     _check_offset(dtype, v, True, temperature, offset)
+
+
+def _mass_inputs(v, teacher, more, r=5, k=6, seed=71):
+    z, idx, t, _, _ = _distill_inputs(r, v, k, F32, False, seed)
+    lse = torch.logsumexp(t.masked_fill((idx < 0) | (idx >= v), -float("inf")), 1)
+    return z, idx, t.to(teacher), lse + more
+
+
+@pytest.mark.parametrize("v", [300, 20001, 60001])
+@pytest.mark.parametrize("teacher,more", [(F32, -0.05), (F32, -0.3), (F32, -2.0), (BF16, 0.0), (BF16, 0.002), (F32, 0.0), (F32, 1e-6)])
+def test_distillation_gradient_where_the_top_holds_more_than_all_mass(v, teacher, more):
+    # the listed mass exceeds 1 by the caller's teacher_lse, or by the rounding of logits that were sent in bf16
+    z, idx, t, lse = _mass_inputs(v, teacher, more)
+    loss, dz = ceca.dsgd_distill_grad(z, idx, t, lse)
+    want = lm.distill(_np(z), _np(idx), _np(t), _np(lse))
+    _close(loss, want["loss"], "loss")
+    _close(dz, want["dz"], "dz")
+
+
+@pytest.mark.parametrize("teacher,more", [(F32, -0.05), (F32, -0.3), (BF16, -0.01)])
+def test_distillation_gradient_of_spent_mass_against_differences(teacher, more):
+    # central differences of the library's own loss; off by its error over h and by a third derivative below the mass
+    v, h = 500, 2e-2
+    z, idx, t, lse = _mass_inputs(v, teacher, more)
+    loss, dz = ceca.dsgd_distill_grad(z, idx, t, lse)
+    off = lm.distill(_np(z), _np(idx), _np(t), _np(lse))["loss"][1].max()
+    for s in range(4):
+        u = _randn(tuple(z.shape), F32, 100 + s)
+        u[:, :3] += 8.0   # (a direction along which the gradient's sum would show)
+        u /= u.norm(dim=1, keepdim=True)
+        up, dn = (ceca.dsgd_distill_loss(z + c * u, idx, t, lse) for c in (h, -h))
+        slip = float(z.abs().max()) * lm.U * 2 * np.sqrt(v) / h
+        assert np.abs(_np(up - dn) / (2 * h) - _np((dz * u).sum(1))).max() <= off / h + 2 * h * h + slip + 1e-5
+    # without a shift of all logits: the loss does not know it, so the gradient sums to nothing
+    assert float(dz.double().sum(1).abs().max()) <= 1e-5
