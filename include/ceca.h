@@ -374,7 +374,8 @@ ceca_status_t dsgd_recurrence_grad(const void *x, const void *f, const void *dh,
  *   dz[i, c] = (w_i / T) * (m q_c, less p0 q_c / q0 with a teacher_lse)     elsewhere
  * with m = sum_j p_j + p0, all the mass that is compared: 1, or with a teacher_lse sum_j p_j where that is more, as it
  * can be by the rounding of teacher logits that were sent in fewer bits than their log-sum-exp
- * (no factor T^2: fold it into the weight).  An entry that a row lists twice counts with both p_j.  Logits of
+ * (no factor T^2: fold it into the weight).  A NaN in t or teacher_lse is one in all that it enters: the loss, and
+ * with a teacher_lse all of the row's dz.  An entry that a row lists twice counts with both p_j.  Logits of
  * -infinity have q = 0; a row of nothing else has q = 0 throughout.  A logit below -9.3e7 T counts as -infinity in
  * a row that has larger ones.
  * z, dz: device, logits_type, r x v with row strides ldz, lddz >= v; idx: device, index_type, r x k with

@@ -138,7 +138,7 @@ def distill(z, idx, t, teacher_lse=None, weight=None, temperature=1.0, bf16=Fals
         lp = ti - norm
         p = np.exp(lp)
         rp = U * (4 * (np.abs(ti).max() + abs(norm)) + 20 + len(js))
-        p0 = max(0.0, 1.0 - p.sum()) if teacher_lse is not None else 0.0
+        p0 = 1.0 - p.sum() if teacher_lse is not None and not p.sum() >= 1.0 else 0.0   # NaN for a NaN
         ep0 = (rp + len(js) * U) * p.sum() + U if teacher_lse is not None else 0.0
         inside = np.zeros(v, bool)
         inside[at] = True

@@ -490,13 +490,14 @@ __global__ void __launch_bounds__(THREADS, 768 / THREADS) distill_kernel(const D
   }
   const float out = all_of.sum, total = out * ex2(under) + (tail ? all_of.top * ex2(under_top) : 0.f);
   const float mass = tail ? 1.f : all_of.mass;   // what the teacher's weights are divided by
-  const float rest = tail ? fmaxf(0.f, 1.f - all_of.mass) : 0.f;
-  const float compared = tail ? fmaxf(1.f, all_of.mass) : 1.f;   // with log q, the top's mass and the rest
+  // (a NaN of the teacher goes on from here: fmaxf would end it)
+  const float rest = tail && !(all_of.mass >= 1.f) ? 1.f - all_of.mass : 0.f;
+  const float compared = tail && !(all_of.mass <= 1.f) ? all_of.mass : 1.f;   // with log q, the top's mass and the rest
   if (tid == 0 && rank == 0 && p.loss) {
     const float log_total = logf(total) - kLn2 * under_top;   // in the top's frame
     float l = tail ? all_of.terms + all_of.mass * log_total : all_of.terms / mass - logf(mass) + log_total;
     if (rest > 0.f) l += rest * (logf(rest * (total / out)) - kLn2 * under);
-    if (total == 0.f) l = INFINITY;
+    if (total == 0.f && all_of.mass == all_of.mass) l = INFINITY;
     p.loss[row] = w * l;
   }
   if (!dz) return;
@@ -511,7 +512,7 @@ __global__ void __launch_bounds__(THREADS, 768 / THREADS) distill_kernel(const D
   };
   const Raised all_raised = raise(Ka, total), out_raised = raise(K, out);
   const auto raised = [&](float v, float m, float low) { return ex2(far ? fmaf(v - m, p.scale, kLift) : fmaf(v, p.scale, -low)); };
-  const float part_of_all = total == 0.f ? 0.f : scale * compared / total, inside = part_of_all * all_raised.drop;
+  const float part_of_all = (total == 0.f ? 0.f : scale / total) * compared, inside = part_of_all * all_raised.drop;
   const float outside = (part_of_all * ex2(under) - (rest > 0.f && out > 0.f ? scale * (rest / out) : 0.f)) * out_raised.drop;
   if (together && !far) {
     const Val<2> shift = all<2>(-out_raised.low), by = all<2>(p.scale), factor = all<2>(outside);

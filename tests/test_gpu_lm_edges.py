@@ -242,3 +242,22 @@ def test_distillation_gradient_of_spent_mass_against_differences(teacher, more):
         assert np.abs(_np(up - dn) / (2 * h) - _np((dz * u).sum(1))).max() <= off / h + 2 * h * h + slip + 1e-5
     # without a shift of all logits: the loss does not know it, so the gradient sums to nothing
     assert float(dz.double().sum(1).abs().max()) <= 1e-5
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("v", [90, 20001, 60001])
+def test_distillation_a_teacher_that_is_not_a_number_is_seen(dtype, v):
+    z, idx, t, lse, _ = _distill_inputs(4, v, 5, dtype, True, 81)
+    idx[:, 1:3] = torch.arange(2, device=DEV, dtype=idx.dtype)
+    t[1, 0] = NAN
+    lse[2] = NAN
+    loss, dz = ceca.dsgd_distill_grad(z, idx, t, lse)
+    want = lm.distill(_np(z[::3]), _np(idx[::3]), _np(t[::3]), _np(lse[::3]), None, 1.0, dtype == BF16)
+    _close(loss[::3], want["loss"], "loss")
+    _close(dz[::3], want["dz"], "dz")
+    assert bool(torch.isnan(loss[1:3]).all()) and bool(torch.isnan(dz[1:3].float()).all())
+    # renormalised, a NaN spoils the entries; q, which is all there is elsewhere, has nothing to do with it
+    loss, dz = ceca.dsgd_distill_grad(z, idx, t)
+    inside = torch.zeros((v,), dtype=torch.bool, device=DEV)
+    inside[idx[1][(idx[1] >= 0) & (idx[1] < v)].long()] = True
+    assert bool(torch.isnan(loss[1])) and bool(torch.isnan(dz[1, inside].float()).all()) and bool(torch.isfinite(dz[1, ~inside].float()).all())
