@@ -261,3 +261,19 @@ def test_distillation_a_teacher_that_is_not_a_number_is_seen(dtype, v):
     inside = torch.zeros((v,), dtype=torch.bool, device=DEV)
     inside[idx[1][(idx[1] >= 0) & (idx[1] < v)].long()] = True
     assert bool(torch.isnan(loss[1])) and bool(torch.isnan(dz[1, inside].float()).all()) and bool(torch.isfinite(dz[1, ~inside].float()).all())
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("tail", [False, True])
+@pytest.mark.parametrize("r,v", [(9, 700), (700, 5001), (40, 130001)])
+def test_distillation_repeats_to_the_bit_beside_rows_that_are_not_numbers(dtype, tail, r, v):
+    z, idx, t, lse, w = _distill_inputs(r, v, 6, dtype, tail, 91)
+    z[3, 5], z[4, v - 1] = NAN, float("inf")
+    bits = (lambda a: a.view(torch.int32)) if dtype == F32 else (lambda a: a.view(torch.int16))
+    loss, dz = ceca.dsgd_distill_grad(z, idx, t, lse, w)
+    assert bool(torch.isnan(loss[3:5]).all()) and bool(torch.isfinite(loss[5:]).all()) and bool(torch.isfinite(dz[5:].float()).all())
+    only = ceca.dsgd_distill_loss(z, idx, t, lse, w)
+    for _ in range(3):
+        again, gz = ceca.dsgd_distill_grad(z, idx, t, lse, w)
+        assert torch.equal(again.view(torch.int32), loss.view(torch.int32)) and torch.equal(bits(gz), bits(dz))
+        assert torch.equal(ceca.dsgd_distill_loss(z, idx, t, lse, w).view(torch.int32), only.view(torch.int32))
