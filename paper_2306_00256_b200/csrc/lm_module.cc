@@ -90,6 +90,7 @@ struct Workspace {
   Workspace(const Maybe &given, size_t wanted, const Tensor &like) {
     if (given) {
       held = *given;
+      need(held.is_contiguous(), "workspace must be contiguous");   // all memory from its first byte to its last is written
       bytes = (size_t)held.numel() * held.element_size();
     } else if (wanted) {
       held = empty({(int64_t)wanted}, at::kByte, like);

@@ -277,3 +277,26 @@ def test_distillation_repeats_to_the_bit_beside_rows_that_are_not_numbers(dtype,
         again, gz = ceca.dsgd_distill_grad(z, idx, t, lse, w)
         assert torch.equal(again.view(torch.int32), loss.view(torch.int32)) and torch.equal(bits(gz), bits(dz))
         assert torch.equal(ceca.dsgd_distill_loss(z, idx, t, lse, w).view(torch.int32), only.view(torch.int32))
+
+
+# ------------------------------------------------------------------------------------------------ arguments
+
+
+def test_a_workspace_with_gaps_is_refused():
+    # its memory between the elements is not the call's
+    tok = torch.zeros((1, 2000), dtype=torch.int32, device=DEV)
+    dout, dE = torch.zeros((1, 2000, 16), device=DEV), torch.zeros((1, 50, 16), device=DEV)
+    size = ceca.dsgd_embed_workspace_bytes(1, 2000, 50, 16)
+    ws = torch.full((2 * size,), 77, dtype=torch.uint8, device=DEV)
+    with pytest.raises(ValueError):
+        ceca.dsgd_embed_grad(dout, tok, dE, workspace=ws[::2])
+    x = torch.zeros((1, 5000, 16), device=DEV)
+    size = ceca.dsgd_recurrence_workspace_bytes(1, 5000, 16)
+    more = torch.full((2 * size,), 77, dtype=torch.uint8, device=DEV)
+    with pytest.raises(ValueError):
+        ceca.dsgd_recurrence(x, x, workspace=more[::2])
+    marks = ceca.dsgd_recurrence(x, x, save=True)[2]
+    with pytest.raises(ValueError):
+        ceca.dsgd_recurrence_grad(x, x, x, marks, workspace=more[::2])
+    torch.cuda.synchronize()
+    assert bool((ws == 77).all()) and bool((more == 77).all())
