@@ -49,7 +49,7 @@ def library():
     global _lib
     if _lib is not None:
         return _lib
-    path = _build.build() if (_build.is_stale() and os.environ.get("CECA_NO_BUILD") != "1") else _build.LIB
+    path = _build.build_library() if (_build.is_stale() and os.environ.get("CECA_NO_BUILD") != "1") else _build.LIB
     lib = ctypes.CDLL(path)
     vp, i32, i64, f32 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_float
     lib.ceca_schedule.argtypes = [i32, i32, i64, ctypes.POINTER(Round), vp, vp]

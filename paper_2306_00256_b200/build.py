@@ -1,16 +1,19 @@
 """Builds in-tree, next to this file: the CUDA library (sm_100a only) with nvcc, libceca_b200.so, and the Python module of
-the language-model operators with g++ and torch's headers, _lm_module.so."""
+the language-model operators with g++ and torch's headers, _lm_module.*.so.  The library needs neither of those, and is
+built without the module where only the ctypes binding is used."""
 import glob
+import importlib.metadata
 import os
 import subprocess
+import sys
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libceca_b200.so")
 MODULE_NAME = "_lm_module"
-MODULE = os.path.join(HERE, MODULE_NAME + ".so")
 MODULE_SOURCE = os.path.join(CSRC, "lm_module.cc")
+HEADER = os.path.join(ROOT, "include", "ceca.h")
 
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "-Xptxas=-v", "-shared", "-Xcompiler", "-fPIC", "--threads", "8"]
@@ -20,13 +23,21 @@ def sources():
     return sorted(glob.glob(os.path.join(CSRC, "*.cu")) + glob.glob(os.path.join(CSRC, "*.cpp")))
 
 
+def module_path():
+    """The module for this Python and this torch, whose binary interfaces it uses: another version of either gets its own."""
+    return os.path.join(HERE, "%s.%s.torch-%s.so" % (MODULE_NAME, sys.implementation.cache_tag, importlib.metadata.version("torch")))
+
+
+def _older(path, deps):
+    return not os.path.exists(path) or any(os.path.getmtime(f) > os.path.getmtime(path) for f in deps)
+
+
 def is_stale():
-    if not os.path.exists(LIB) or not os.path.exists(MODULE):
-        return True
-    header = os.path.join(ROOT, "include", "ceca.h")
-    deps = sources() + glob.glob(os.path.join(CSRC, "*.h")) + glob.glob(os.path.join(CSRC, "*.cuh")) + [header]
-    return (any(os.path.getmtime(f) > os.path.getmtime(LIB) for f in deps) or
-            any(os.path.getmtime(f) > os.path.getmtime(MODULE) for f in (MODULE_SOURCE, header)))
+    return _older(LIB, sources() + glob.glob(os.path.join(CSRC, "*.h")) + glob.glob(os.path.join(CSRC, "*.cuh")) + [HEADER])
+
+
+def module_is_stale():
+    return _older(module_path(), [MODULE_SOURCE, HEADER])
 
 
 def module_command(out):
@@ -54,16 +65,29 @@ def _run(what, cmd, verbose):
         raise RuntimeError(what + " failed")
 
 
-def build(force=False, verbose=False):
+def build_library(force=False, verbose=False):
     if not force and not is_stale():
         return LIB
     nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
     tmp = LIB + ".tmp.%d" % os.getpid()
     _run("nvcc", [nvcc] + NVCC_FLAGS + ["-I", os.path.join(ROOT, "include"), "-I", CSRC, "-o", tmp] + sources(), verbose)
     os.replace(tmp, LIB)
-    tmp = MODULE + ".tmp.%d" % os.getpid()
+    return LIB
+
+
+def build_module(force=False, verbose=False):
+    path = module_path()
+    if not force and not module_is_stale():
+        return path
+    tmp = path + ".tmp.%d" % os.getpid()
     _run("g++", module_command(tmp), verbose)
-    os.replace(tmp, MODULE)
+    os.replace(tmp, path)
+    return path
+
+
+def build(force=False, verbose=False):
+    build_library(force, verbose)
+    build_module(force, verbose)
     return LIB
 
 

@@ -4,6 +4,7 @@ The marshalling itself is C++ (csrc/lm_module.cc, built next to the library).  O
 in, and workspaces, are allocated by torch on the stream that the call runs on; everything else is as in binding.py:
 the current stream by default, ValueError for tensors that do not fit, CecaError for what the library refuses."""
 import importlib.util
+import os
 
 from . import build as _build
 from .binding import library
@@ -13,8 +14,9 @@ _module = None
 
 def _load():
     global _module
-    library()   # builds what is missing
-    spec = importlib.util.spec_from_file_location(_build.MODULE_NAME, _build.MODULE)
+    library()   # which the module links with
+    path = _build.build_module() if (_build.module_is_stale() and os.environ.get("CECA_NO_BUILD") != "1") else _build.module_path()
+    spec = importlib.util.spec_from_file_location(_build.MODULE_NAME, path)
     module = importlib.util.module_from_spec(spec)
     spec.loader.exec_module(module)
     _module = module

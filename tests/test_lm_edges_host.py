@@ -31,3 +31,12 @@ def test_distillation_statement_against_differences_whatever_mass_the_top_holds(
         u, h = np.random.default_rng(seed).standard_normal(z.shape), 1e-5
         up, dn = (lm.distill(z + c * u, idx, t, lse, w, temperature)["loss"][0].sum() for c in (h, -h))
         assert abs((up - dn) / (2 * h) - (g * u).sum()) <= 1e-8 * max(1.0, abs((g * u).sum()))
+
+
+def test_the_module_is_built_for_one_python_and_one_torch(monkeypatch):
+    from paper_2306_00256_b200 import build
+    here = build.module_path()
+    assert torch.__version__ in here and not build.module_is_stale()
+    monkeypatch.setattr(build.importlib.metadata, "version", lambda name: "0.0.1")
+    assert build.module_path() != here and build.module_is_stale()
+    assert not build.is_stale()   # the library has nothing to do with it
