@@ -277,7 +277,7 @@ typedef enum { DSGD_I32 = 0, DSGD_I64 = 1 } dsgd_index_t;
  * row is zero.  out: device, out_type; position s of agent i starts at out + i*out_agent_stride +
  * s*out_row_stride.  Strides count elements; rows themselves are contiguous, and neither the rows of
  * out nor those of E may overlap.  t = 0 is allowed and does nothing.
- * Errors: CECA_ERR_INVALID_ARG (NULL where data is needed, n, v or d < 1, n > 65535, t < 0, v >= 2^31,
+ * Errors: CECA_ERR_INVALID_ARG (NULL where data is needed, n, v or d < 1, n > 65535, t < 0, v or d >= 2^31,
  * t >= 2^31 - 1024, a row stride below d, a negative stride, a bad type).
  * Speed: 128-bit accesses need every row to start on a 16-byte boundary; other layouts run a narrower
  * form.
@@ -297,7 +297,8 @@ ceca_status_t dsgd_embed_lookup(const void *E, const void *tokens, void *out, in
  * order that depends on the arguments alone: results are identical from run to run.
  * workspace: device, 16-byte aligned, at least dsgd_embed_workspace_bytes(n, t, v, d) bytes (0, and then NULL
  * will do, for short sequences).
- * Errors: as above, and CECA_ERR_WORKSPACE; agent_stride must keep the agents' tables apart (n > 1).
+ * Errors: as above, CECA_ERR_UNSUPPORTED (d > 65535 * 256) and CECA_ERR_WORKSPACE; agent_stride must keep the
+ * agents' tables apart (n > 1).
  */
 ceca_status_t dsgd_embed_grad(const void *dout, const void *tokens, void *dE, int32_t n, int64_t t, int64_t v,
                               int64_t d, int64_t agent_stride, int64_t row_stride, int64_t tokens_stride,
@@ -376,8 +377,8 @@ ceca_status_t dsgd_recurrence_grad(const void *x, const void *f, const void *dh,
  * can be by the rounding of teacher logits that were sent in fewer bits than their log-sum-exp
  * (no factor T^2: fold it into the weight).  A NaN in t or teacher_lse is one in all that it enters: the loss, and
  * with a teacher_lse all of the row's dz.  An entry that a row lists twice counts with both p_j.  Logits of
- * -infinity have q = 0; a row of nothing else has q = 0 throughout.  A logit below -9.3e7 T counts as -infinity in
- * a row that has larger ones.
+ * -infinity have q = 0; a row of nothing else has q = 0 throughout.  A logit below -9.3e7 T has q = 0 too in a row
+ * that has larger ones.
  * z, dz: device, logits_type, r x v with row strides ldz, lddz >= v; idx: device, index_type, r x k with
  * row stride ldi >= k; t: device, teacher_type, r x k with row stride ldt >= k; teacher_lse, weight, loss:
  * device fp32, r elements.  dz may be z with the same row stride (another one: CECA_ERR_UNSUPPORTED).

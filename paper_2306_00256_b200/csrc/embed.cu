@@ -53,6 +53,7 @@ constexpr int kThreads = 256, kWarps = kThreads / 32;
 constexpr int kFill = 64;      // table rows
 constexpr int kJoin = 2;       // chunks
 constexpr int kFew = 256;      // positions
+constexpr int64_t kMaxWidth = 65535 * 256;   // columns of a gradient: its slices are a dimension of the grid
 constexpr int kFewRows = 16;   // table rows of a CTA
 constexpr int kDeep = 4;       // rows of dout that a warp has on their way at a time
 constexpr int kListThreads = 1024;
@@ -498,7 +499,7 @@ bool embed_args_ok(int32_t n, int64_t t, int64_t v, int64_t d, int64_t table_age
                    int64_t tokens_agent, int64_t out_agent, int64_t out_row, int32_t table_type,
                    int32_t tokens_type, int32_t out_type) {
   // (places and positions are 32-bit numbers, up to a few chunks beyond t)
-  return n >= 1 && n <= 65535 && t >= 0 && t < ((int64_t)1 << 31) - 1024 && v >= 1 && v < ((int64_t)1 << 31) && d >= 1 &&
+  return n >= 1 && n <= 65535 && t >= 0 && t < ((int64_t)1 << 31) - 1024 && v >= 1 && v < ((int64_t)1 << 31) && d >= 1 && d < ((int64_t)1 << 31) &&
          table_agent >= 0 && table_row >= d && tokens_agent >= 0 && out_agent >= 0 && out_row >= 0 &&
          is_type(table_type) && is_index(tokens_type) && is_type(out_type);
 }
@@ -533,7 +534,6 @@ template <typename TI> cudaError_t launch_list(const EmbedArgs &p, cudaStream_t 
 
 template <typename TE, typename TO, typename TI, int V> cudaError_t launch_grad(EmbedArgs p, cudaStream_t s) {
   p.slices = (int32_t)ceil_div(p.d, Slice<V>::kElements);
-  if (p.slices > 65535) return cudaErrorInvalidValue;
   if (p.t <= kFew) {
     embed_few_kernel<TE, TO, TI, V><<<dim3((unsigned)ceil_div(p.v, kFewRows), p.slices, p.n), kThreads, 0, s>>>(p);
     return cudaGetLastError();
@@ -594,7 +594,7 @@ extern "C" ceca_status_t dsgd_embed_lookup(const void *E, const void *tokens, vo
 }
 
 extern "C" size_t dsgd_embed_workspace_bytes(int32_t n, int64_t t, int64_t v, int64_t d) {
-  if (!embed_args_ok(n, t, v, d, 0, d, 0, 0, d, DSGD_F32, DSGD_I32, DSGD_F32) || t <= kFew) return 0;
+  if (!embed_args_ok(n, t, v, d, 0, d, 0, 0, d, DSGD_F32, DSGD_I32, DSGD_F32) || t <= kFew || d > kMaxWidth) return 0;
   return round16(sizeof(int32_t) * (size_t)n * (size_t)(v + 1)) + round16(sizeof(int2) * (size_t)n * (size_t)t) +
          sizeof(float) * 2 * (size_t)n * (size_t)ceil_div(t, chunk_of(n, t, d)) * (size_t)d;
 }
@@ -608,6 +608,7 @@ extern "C" ceca_status_t dsgd_embed_grad(const void *dout, const void *tokens, v
                      table_type, tokens_type, out_type) ||
       !dE || (t > 0 && (!dout || !tokens)) || (n > 1 && agent_stride < (v - 1) * row_stride + d))
     return CECA_ERR_INVALID_ARG;
+  if (d > kMaxWidth) return CECA_ERR_UNSUPPORTED;
   const size_t need = dsgd_embed_workspace_bytes(n, t, v, d);
   if (need > 0 && (!workspace || workspace_bytes < need || (uintptr_t)workspace % 16)) return CECA_ERR_WORKSPACE;
   EmbedArgs p{};

@@ -40,3 +40,15 @@ def test_the_module_is_built_for_one_python_and_one_torch(monkeypatch):
     monkeypatch.setattr(build.importlib.metadata, "version", lambda name: "0.0.1")
     assert build.module_path() != here and build.module_is_stale()
     assert not build.is_stale()   # the library has nothing to do with it
+
+
+def test_rows_wider_than_the_embedding_supports_are_refused():
+    from test_lm_operators_host import GRAD, INVALID, LOOKUP, UNSUPPORTED, _call
+    import paper_2306_00256_b200 as ceca
+    wide, huge = 65535 * 256 + 1, 1 << 31
+    for t in (4, 4000):
+        more = {"t": t, "agent": 1 << 45, "tok": t, "o_agent": 1 << 50}
+        assert _call("dsgd_embed_grad", GRAD, d=wide, row=wide, o_row=wide, **more) == UNSUPPORTED
+        assert _call("dsgd_embed_grad", GRAD, d=huge, row=huge, o_row=huge, **more) == INVALID
+        assert _call("dsgd_embed_lookup", LOOKUP, d=huge, row=huge, o_row=huge, **more) == INVALID
+    assert ceca.dsgd_embed_workspace_bytes(2, 4000, 8, wide) == 0 and ceca.dsgd_embed_workspace_bytes(2, 4000, 8, wide - 1) > 0
