@@ -42,7 +42,6 @@ constexpr int64_t kHeld = 32 << 10, kMostHeld = 104 << 10;
 constexpr int64_t kMaxBits = 1 << 20;   // of the bitmap; longer parts wrap around in it
 constexpr int kDeep = 4;                // vectors a thread works on at a time
 constexpr float kLn2 = 0.6931471805599453f;
-constexpr float kLift = 32.f;   // binades by which pass 2 raises its exponentials: over a low temperature, a q below 2^-126 is a gradient that is not
 // Exponents of this size: z c - k is exact but for its own rounding whatever k is, so a frame's k is m c rounded (kept as it is
 // rounded: all that move between frames, or that use one later, go by k).  That rounding shifts a frame by up to half an ulp of k,
 // 8 here and harmless; beyond, an exponential could overflow by it.  Logits below -kFar / c are masks; a row that has no others, or one
@@ -503,19 +502,24 @@ __global__ void __launch_bounds__(THREADS, 768 / THREADS) distill_kernel(const D
   if (!dz) return;
   // pass 2
   const float scale = w / p.temperature;
-  // Raised exponentials: 2^kLift z's share of a sum, about (a frame moves by the sum's binade as well), and factors that much less, by
-  // what the frame has really moved.  q is a share of everything at the top's entries, of pass 1's sum elsewhere.
-  struct Raised { float low, drop; };
-  const auto raise = [&](float k, float sum) -> Raised {
-    const float low = k + ((float)((__float_as_int(sum) >> 23) - 127) - kLift);
-    return {low, ex2(far ? -kLift : low - k)};
-  };
-  const Raised all_raised = raise(Ka, total), out_raised = raise(K, out);
-  const auto raised = [&](float v, float m, float low) { return ex2(far ? fmaf(v - m, p.scale, kLift) : fmaf(v, p.scale, -low)); };
-  const float part_of_all = (total == 0.f ? 0.f : scale / total) * compared, inside = part_of_all * all_raised.drop;
-  const float outside = (part_of_all * ex2(under) - (rest > 0.f && out > 0.f ? scale * (rest / out) : 0.f)) * out_raised.drop;
+  // The frames of the second pass, and what their exponentials are multiplied by besides: q is a share of everything at the top's
+  // entries, of pass 1's sum elsewhere.  Over a low temperature a q below 2^-126 is a gradient that is not, so frames are lowered by
+  // the binades of w / T; and where a sum shows a frame far below its maximum, they are raised by the sum's, so that the factor
+  // stays a normal number.  Not otherwise: an exponent's rounding grows with it, and is least for the largest q in a frame that is the maximum.
+  float low = K, low_all = Ka, drop = 1.f, drop_all = 1.f, lift = 0.f;
+  if (fabsf(scale) >= 2.f || fmaxf(out, total) >= 0x1p32f) {
+    const auto binade = [](float x) { return (float)((__float_as_int(fabsf(x)) >> 23) - 127); };
+    lift = fminf(fmaxf(binade(scale), 0.f), 32.f);
+    low = K + ((out >= 0x1p32f ? binade(out) : 0.f) - lift);
+    low_all = Ka + ((total >= 0x1p32f ? binade(total) : 0.f) - lift);
+    drop = ex2(far ? -lift : low - K);
+    drop_all = ex2(far ? -lift : low_all - Ka);
+  }
+  const auto raised = [&](float v, float m, float low) { return ex2(far ? fmaf(v - m, p.scale, lift) : fmaf(v, p.scale, -low)); };
+  const float part_of_all = (total == 0.f ? 0.f : scale / total) * compared, inside = part_of_all * drop_all;
+  const float outside = (part_of_all * ex2(under) - (rest > 0.f && out > 0.f ? scale * (rest / out) : 0.f)) * drop;
   if (together && !far) {
-    const Val<2> shift = all<2>(-out_raised.low), by = all<2>(p.scale), factor = all<2>(outside);
+    const Val<2> shift = all<2>(-low), by = all<2>(p.scale), factor = all<2>(outside);
     const auto turn = [&](Vec<TZ> v) {
 #pragma unroll
       for (int i = 0; i < P; ++i) {
@@ -543,11 +547,11 @@ __global__ void __launch_bounds__(THREADS, 768 / THREADS) distill_kernel(const D
           if (u * THREADS < left) __stcs(dst + base + u * THREADS, turn(a[u]));
       }
     }
-    if (part.edge >= 0) narrow(dz + part.edge - part.pad, raised(edge, M, out_raised.low) * outside);
+    if (part.edge >= 0) narrow(dz + part.edge - part.pad, raised(edge, M, low) * outside);
   } else {   // element by element, from memory (where dz is z, each thread reads what it writes over)
     const int64_t s1 = min((int64_t)slot1, p.v + part.pad);
     for (int64_t s = max((int64_t)slot0, (int64_t)part.pad) + tid; s < s1; s += THREADS)
-      narrow(dz + s - part.pad, raised(widen(z[s - part.pad]), M, out_raised.low) * outside);
+      narrow(dz + s - part.pad, raised(widen(z[s - part.pad]), M, low) * outside);
   }
   __syncthreads();
   for (int j = tid; j < p.k; j += THREADS) {
@@ -562,7 +566,7 @@ __global__ void __launch_bounds__(THREADS, 768 / THREADS) distill_kernel(const D
           pc += expf(en.t[e] - norm);
         }
     }
-    if (first) narrow(dz + en.at[j], raised(en.z[j], Ma, all_raised.low) * inside - scale * (pc / mass));
+    if (first) narrow(dz + en.at[j], raised(en.z[j], Ma, low_all) * inside - scale * (pc / mass));
   }
 }
 

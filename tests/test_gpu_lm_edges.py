@@ -279,6 +279,18 @@ def test_distillation_repeats_to_the_bit_beside_rows_that_are_not_numbers(dtype,
         assert torch.equal(ceca.dsgd_distill_loss(z, idx, t, lse, w).view(torch.int32), only.view(torch.int32))
 
 
+@pytest.mark.parametrize("v", [500, 1000, 4000, 20000])
+@pytest.mark.parametrize("tail", [False, True])
+@pytest.mark.parametrize("seed", [1, 2, 3])
+def test_distillation_gradient_is_good_to_fp32(v, tail, seed):
+    # What makes the norm of dz are shares within a few binades of the largest: exponents below 8, off by 2^-22 ln 2 at most and by
+    # half of that mostly, an exponential of 2 ulp, the sum's own error and two products: 4 U in the norm leaves room
+    z, idx, t, lse, w = _distill_inputs(64, v, 8, F32, tail, 300 + seed)
+    _, dz = ceca.dsgd_distill_grad(z, idx, t, lse, w)
+    want = lm.distill(_np(z), _np(idx), _np(t), _np(lse), _np(w))["dz"][0]
+    assert np.linalg.norm(_np(dz) - want) <= 4 * lm.U * np.linalg.norm(want)
+
+
 # ------------------------------------------------------------------------------------------------ arguments
 
 
