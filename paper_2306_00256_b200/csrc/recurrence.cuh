@@ -162,20 +162,17 @@ template <int L, bool WIDE> struct Run {
 // a = sigmoid(f) and na = sigmoid(-f): with e = exp(-f), a = 1 / (1 + e) and na = e a.  Each is within a few ulp of itself plus
 // |f| ulp or so: the product f log2(e) is rounded before its exponential is taken, which is a choice (its low half would
 // take two more instructions a gate, and where |f| is large enough to matter one of the two is next to 0 and the other next to 1).
-// The exponent stops at 126, where e and its reciprocal are both still normal numbers and na rounds to 1; the saturating
-// subtraction then makes a exactly 0 and changes no a above 2^-100.  A NaN goes through: the lesser number of it and 126 is a
-// NaN here, and so are e and na; the saturation would make a zero of it, so 0 * na is added, which changes no other a.
-constexpr float kNegLog2e = -1.4426950408889634f, kLeast = 0x1p-125f;
-__device__ __forceinline__ float least_or_nan(float x, float y) {
-  float r;
-  asm("min.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(x), "f"(y));
-  return r;
-}
+// The exponent stops at 126, where e and its reciprocal are both still normal numbers and na rounds to 1; the
+// subtraction then makes a exactly 0 and changes no a above 2^-101.  (a does not leave [0, 1]: the reciprocal of 1 is 1, that of
+// 2^126 is 2^-126, and between them its last place does not reach beyond either.)  A NaN is not above 126 and goes
+// through.
+constexpr float kNegLog2e = -1.4426950408889634f, kLeast = 0x1p-126f;
+__device__ __forceinline__ float least_or_nan(float x, float y) { return x > y ? y : x; }
 __device__ __forceinline__ void gates(Val<1> f, Val<1> *a, Val<1> *na) {
   const float e = ex2(least_or_nan(f.x * kNegLog2e, 126.f));
   const float r = rcp(1.f + e);
   na->x = e * r;
-  a->x = fmaf(na->x, 0.f, __saturatef(r - kLeast));
+  a->x = r - kLeast;
 }
 __device__ __forceinline__ void gates(Val<2> f, Val<2> *a, Val<2> *na) {
   Val<2> e = mul(f, all<2>(kNegLog2e));
@@ -185,9 +182,7 @@ __device__ __forceinline__ void gates(Val<2> f, Val<2> *a, Val<2> *na) {
   r.x = rcp(r.x);
   r.y = rcp(r.y);
   *na = mul(e, r);
-  r.x = __saturatef(r.x - kLeast);
-  r.y = __saturatef(r.y - kLeast);
-  *a = fma(*na, all<2>(0.f), r);
+  *a = add(r, all<2>(-kLeast));
 }
 
 // A run's map applied to what comes into it, and the map of a run with one more map (wa, wh) after it.

@@ -39,6 +39,23 @@ def test_recurrence_a_gate_that_is_not_a_number_is_seen(dtype, d, t, at, cut, b)
         _close(g, want[k], k)
 
 
+@pytest.mark.parametrize("lo,hi", [(-88.5, -86.5), (-104.0, -101.0), (14.0, 20.0), (86.5, 89.0)])
+def test_recurrence_gates_of_every_number_where_they_are_next_to_zero_or_one(lo, hi):
+    # every fp32 number of the range: neither gate leaves [0, 1], each is within its bound of the sigmoid
+    ends = np.array(sorted((lo, hi), key=abs), np.float32).view(np.int32)
+    f = torch.from_numpy(np.arange(ends[0], ends[1] + 1, dtype=np.int32).view(np.float32)).to(DEV).view(1, 1, -1)
+    one = torch.ones_like(f)
+    h, _, marks = ceca.dsgd_recurrence(one, f, save=True)   # 1 - a
+    _, _, a = ceca.dsgd_recurrence_grad(one, f, one, marks)
+    h, a, f64 = _np(h)[0, 0], _np(a)[0], _np(f)[0, 0]
+    assert a.min() >= 0 and a.max() <= 1 and h.min() >= 0 and h.max() <= 1 + 4 * lm.U
+    bound = lm.U * (12 + 2.4 * np.minimum(np.abs(f64), 90.0))
+    want, rest = 1 / (1 + np.exp(-f64)), 1 / (1 + np.exp(f64))
+    assert (np.abs(a - want) <= bound * want + 2.0 ** -124).all() and (np.abs(h - rest) <= bound * rest + 2.0 ** -124).all()
+    if hi < 0:
+        assert a.min() == 0 and h.min() >= 1 - 4 * lm.U   # shut for good, and open
+
+
 # ------------------------------------------------------------------------------------------------ distillation
 
 # a period and how much of its beginning is low: what the threads of one warp, of one CTA, of a cluster see first
