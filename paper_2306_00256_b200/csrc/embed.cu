@@ -11,8 +11,9 @@
 //   embed_join_kernel   adds up the pieces of the rows that have several.
 // 8 x 8192 positions in bf16 of 32000 x 1024 fp32 tables: 0.23 ms, 0.79 of the measured copy rate, of which the list takes
 // 22 to 24 us (the block with the most frequent tokens, whose shared-memory counters every token passes) and the join 10.
-// Lookup of 8 x 8192 rows of 2048 bf16: 68 us, 0.83.  bf16 rows on 8-byte boundaries move four elements a lane (1044 columns,
-// lookup and gradient: 67 and 194 us, 107 and 299 with one), rows on other boundaries one (1031 columns: 0.27 in bf16, 0.5 in fp32).
+// Lookup of 8 x 8192 rows of 2048 bf16: 68 us, 0.84.  bf16 rows on 8-byte boundaries move four elements a lane (1044 columns,
+// lookup and gradient: 67 and 192 us, 107 and 299 with one), rows on other boundaries one (1031 columns: lookup 0.27 in bf16, 0.53 in
+// fp32, gradient 0.35 and 0.57).  Accumulating, the 8 x 8192 positions take 0.16 ms, 0.33: list, pieces and join, few rows to write.
 // For up to kFew positions these three launches would take longer than their work: embed_few_kernel looks the positions of
 // every row up as it goes (4 x 129 positions, 4097 x 256 fp32: 18 us by three launches, 9 to 10 us so).
 #include <cuda_runtime.h>

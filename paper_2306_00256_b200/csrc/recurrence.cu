@@ -17,9 +17,10 @@
 // Bytes bound it: 6 per element in bf16 forward, 10 for the gradient.  Lanes are channels so that the scan itself needs no
 // shuffles, two bf16 channels to a lane so that it runs on f32x2 instructions, and runs are 16 steps because the exchange
 // between warps costs the same for every run.  64 x 512 x 2048 bf16: forward 67 us (0.92 of the measured copy rate),
-// gradient 129 us (0.79; 40 instructions an element, of which 12 are the gates and the two scans); in fp32 128 us (0.96)
-// and 220 us (0.93).  8 x 4096 x 2048 bf16, 256 channel blocks and so CTAs of 8 warps: 76 us (0.80) and 144 us (0.71).
-// Few channels pay for the maps: 1 x 32768 x 1024 bf16 forward 66 us, of which 30 are the first kernel.  Clusters of CTAs
+// gradient 128 us (0.80; 39 instructions an element, of which 12 are the gates and the two scans); in fp32 127 to 129 us (0.96)
+// and 221 us (0.93).  8 x 4096 x 2048 bf16, 256 channel blocks and so CTAs of 8 warps, 256 of them on 296 places: 76 us (0.81) and
+// 144 us (0.71), with documents' starts 79 and 146.  Few channels pay for the maps: 1 x 32768 x 1024 bf16 forward 66 us, of which 30
+// are the first kernel.  Clusters of CTAs
 // that exchanged the tiles' maps through distributed shared memory read everything once, but took 97 us there: their
 // barrier was on the path from tile to tile.
 //

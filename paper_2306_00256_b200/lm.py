@@ -2,7 +2,10 @@
 
 The marshalling itself is C++ (csrc/lm_module.cc, built next to the library).  Outputs that are not passed
 in, and workspaces, are allocated by torch on the stream that the call runs on; everything else is as in binding.py:
-the current stream by default, ValueError for tensors that do not fit, CecaError for what the library refuses."""
+the current stream by default, ValueError for tensors that do not fit, CecaError for what the library refuses.
+
+They build no graph for automatic differentiation: an input may have requires_grad, the outputs never do, and each gradient
+is a call of its own (wrap the pair in a torch.autograd.Function where a graph is wanted)."""
 import importlib.util
 import os
 
@@ -68,7 +71,8 @@ def dsgd_recurrence_grad(x, f, dh, marks, h0=None, starts=None, dh_last=None, dx
 def dsgd_distill_loss(z, idx, t, teacher_lse=None, weight=None, temperature=1.0, loss=None, stream=None):
     """weight * KL(teacher || softmax(z / temperature)) of each row of z [r, v], the teacher being known by its top
     logits t [r, k] at the vocabulary entries idx [r, k] (an idx outside [0, v): fewer entries).  Without teacher_lse
-    it is renormalised over them; with it, the mass it leaves is compared with the student's outside the top."""
+    it is renormalised over them; with it, the mass it leaves is compared with the student's outside the top.  (Taken
+    before t was rounded to fewer bits, it may leave the top more than all mass; loss and gradient go by the mass there is.)"""
     return (_module or _load()).distill(z, idx, t, teacher_lse, weight, temperature, loss, False, None, stream)
 
 
