@@ -306,13 +306,13 @@ def run(s):
     if own:
         import paper_2306_00256_b200 as ceca
         if op == "keep8":
-            return ceca.dsgd_unpack8(ceca.dsgd_pack8(s["x"]), s["d"], s["x"].dtype)
+            return ceca.dsgd_bring8(ceca.dsgd_keep8(s["x"]), s["d"], s["x"].dtype)
         if op in ("block", "block_train"):
             act = {"none": None, "sigmoid": ceca.GATE_SIGMOID, "silu": ceca.GATE_SILU}[s["gate"]]
-            more = {"gate_act": act or ceca.GATE_SIGMOID, "scale": s["scale"], "eps": EPS}
+            more = {"gate_act": act or ceca.GATE_SIGMOID, "scale": s["scale"]}
             train, kept = op == "block_train", (s["h"], s["y"], s["gate_"])
-            h, u, stats, packed = ceca.dsgd_block_norm(s["h"], s["y"], s["w_pre"], s["w_post"], gate=s["gate_"], save=train,
-                                                       keep8=train and s["kept"] == "8bit", **more)
+            h, u, stats, packed = ceca.dsgd_block_norm(s["h"], s["y"], s["w_pre"], s["w_post"], gate=s["gate_"], eps=EPS,
+                                                       save=train, keep8=train and s["kept"] == "8bit", **more)
             out = {"h": h, "u": u}
             if train:
                 hk, yk, ak = kept if packed is None else packed
