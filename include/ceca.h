@@ -396,6 +396,143 @@ ceca_status_t dsgd_distill_grad(const void *z, const void *idx, const void *t, c
                                 int64_t ldz, int64_t ldi, int64_t ldt, int64_t lddz, int32_t logits_type,
                                 int32_t index_type, int32_t teacher_type, float temperature, void *stream);
 
+/* A device tensor of n x t rows: row s of agent i starts at `at` + i*agent_stride + s*row_stride elements of its own type.
+ * Its d elements are contiguous. */
+typedef struct {
+  void *at;
+  int64_t agent_stride, row_stride;
+} dsgd_rows_t;
+
+/* What a gate's values go through: sigmoid(a), or a sigmoid(a). */
+typedef enum { DSGD_GATE_SIGMOID = 0, DSGD_GATE_SILU = 1 } dsgd_gate_t;
+
+/*
+ * Activations kept in 8 bits between a forward and a backward pass (not in the paper).  Channels are kept in blocks of 32 (the last
+ * one of a row may be shorter) that share an exponent: with 2^E <= max |x| < 2^(E+1) over a block, x is held as
+ *   q = x / 2^(E-6), rounded to the nearest whole number (even on ties) and cut to [-127, 127],
+ * and stands for q 2^(E-6).  E is -121 where all of a block is below 2^-121.  A block that holds an infinity or a NaN stands for NaNs.
+ * All values are exact in fp32 and in bf16.
+ * A kept row is dsgd_kept_row_bytes(d) = d + ceil(d/32) bytes, rounded up to a multiple of 16: the q as int8, the exponents as bytes E + 127
+ * (255 for a block of NaNs), zeros.  A kept tensor is n x t such rows, dense and 16-byte aligned.
+ * dsgd_keep8 writes the kept form of x, dsgd_bring8 the values it stands for.
+ * Errors: CECA_ERR_INVALID_ARG (NULL where data is needed, n or d < 1, n > 65535, t < 0, t or d >= 2^31 - 1024, a row stride below d, a negative
+ * stride, a bad type), CECA_ERR_ALIGNMENT (kept).  t = 0 does nothing.
+ */
+ceca_status_t dsgd_keep8(dsgd_rows_t x, void *kept, int32_t n, int64_t t, int64_t d, int32_t type, void *stream);
+ceca_status_t dsgd_bring8(const void *kept, dsgd_rows_t x, int32_t n, int64_t t, int64_t d, int32_t type, void *stream);
+
+/* Host function.  Bytes of one kept row of d channels (0 for d < 1). */
+int64_t dsgd_kept_row_bytes(int64_t d);
+
+/*
+ * The end of one block of a residual model and the start of the next (not in the paper; the models of the language-model
+ * workload), row by row for n agents with t rows each:
+ *   g = sigmoid(gate) or gate sigmoid(gate) (gate_act), or 1 without a gate
+ *   h_out = h + scale_i g * w_post_i * y / rms(y),     u = w_pre_i * h_out / rms(h_out),     rms(x)^2 = mean(x^2) + eps
+ * h is the residual stream, y the block's output, u the next block's input; w_post, w_pre [d] and the number scale (1 when NULL)
+ * are each agent's own.  Without y (at == NULL) h_out is h and is not written: the first norm of a model.  Without w_pre there is
+ * no u: a block that no norm follows.  u is computed from h_out before that is rounded for its storage.
+ * h, h_out: stream_type; y, gate, u: act_type; all n x t rows.  w_pre, w_post, scale: weights_type, agent i's at i*stride
+ * (so they may be blocks of columns of X).
+ * stats: device fp32, n x t x 2 dense, receives 1 / rms(y) and 1 / rms(h_out) for the gradient; may be NULL.
+ * h8, y8, gate8: device, kept tensors (dsgd_keep8) of h, y and gate, each may be NULL: what the gradient reads in their place.
+ * h_out may be h, u may be y or gate where the types and strides are the same (each element is read before it is written; other overlaps
+ * are not allowed).  t = 0 does nothing.
+ * Errors: CECA_ERR_INVALID_ARG (NULL where data is needed, n or d < 1, n > 65535, t < 0, t or d >= 2^31 - 1024, a row stride below d, a negative
+ * stride, eps not positive and finite, neither y nor w_pre, a gate without y, a bad type), CECA_ERR_ALIGNMENT (h8, y8, gate8).
+ * Speed: best where d is a multiple of 8 and every row starts on a 16-byte boundary.
+ */
+ceca_status_t dsgd_block_norm(dsgd_rows_t h, dsgd_rows_t y, dsgd_rows_t gate, const void *w_pre, const void *w_post, const void *scale,
+                              int64_t w_pre_stride, int64_t w_post_stride, int64_t scale_stride, dsgd_rows_t h_out, dsgd_rows_t u,
+                              float *stats, void *h8, void *y8, void *gate8, int32_t n, int64_t t, int64_t d, int32_t stream_type,
+                              int32_t act_type, int32_t weights_type, int32_t gate_act, float eps, void *stream);
+
+/*
+ * The gradient of dsgd_block_norm.  du, dh_out: the gradients with respect to u and h_out (dh_out: 0 when its `at` is NULL; du is needed
+ * with w_pre).  With yn = y / rms(y), hn = h_out / rms(h_out), both by the saved stats, and h_out computed again in fp32 from h, y and gate:
+ *   dh = dh_out + (w_pre du - hn mean(hn w_pre du)) / rms(h_out)
+ *   dy = (e - yn mean(yn e)) / rms(y),  e = scale g w_post dh;     dgate = scale g' w_post yn dh
+ *   dw_pre = sum over rows of hn du;    dw_post = scale S,  dscale = sum over channels of w_post S,  S = sum over rows of yn g dh
+ * h, y, gate: the forward call's, or with kept != 0 their kept forms h8, y8, gate8 (the strides are then not read): the gradient is taken
+ * at the values that they stand for, with the statistics of the whole ones.
+ * dh, dh_out: stream_type; du, dy, dgate, and y and gate when whole: act_type.  dw_pre, dw_post: weights_type, agent i's at i*stride, so
+ * they may be blocks of columns of G; dscale: weights_type, may be NULL.  With accumulate != 0 the three are added to.  dh is needed, dy
+ * with y, dgate with gate, dw_pre with w_pre, dw_post with y.  dh may be h or dh_out, dy may be y, gate or du, dgate may be gate, y or du, where types and strides
+ * are the same.  du and dh_out may have strides of 0.
+ * workspace: device, 16-byte aligned, dsgd_block_norm_workspace_bytes(n, t, d) bytes.  Sums over rows are taken in an order that
+ * depends on the sizes alone: results are identical from run to run.  t = 0: the weights' gradients are 0.
+ * Errors: as dsgd_block_norm, and CECA_ERR_WORKSPACE.
+ */
+ceca_status_t dsgd_block_norm_grad(dsgd_rows_t h, dsgd_rows_t y, dsgd_rows_t gate, int32_t kept, const void *w_pre, const void *w_post,
+                                   const void *scale, int64_t w_pre_stride, int64_t w_post_stride, int64_t scale_stride, const float *stats,
+                                   dsgd_rows_t du, dsgd_rows_t dh_out, dsgd_rows_t dh, dsgd_rows_t dy, dsgd_rows_t dgate, void *dw_pre,
+                                   void *dw_post, void *dscale, int64_t dw_pre_stride, int64_t dw_post_stride, int64_t dscale_stride,
+                                   int32_t accumulate, int32_t n, int64_t t, int64_t d, int32_t stream_type, int32_t act_type,
+                                   int32_t weights_type, int32_t gate_act, void *workspace, size_t workspace_bytes, void *stream);
+
+/* Host function.  Minimum workspace size of dsgd_block_norm_grad in bytes (0 also for sizes it refuses). */
+size_t dsgd_block_norm_workspace_bytes(int32_t n, int64_t t, int64_t d);
+
+/*
+ * The log-probability of one token of each row of logits (not in the paper; what the two losses below start from, and what a caller
+ * saves of an older or a reference model for them):
+ *   logp[i] = log softmax(z[i, :] / T)[tokens[i]]
+ * A token outside [0, v) marks an empty position (a prompt's, or padding): its logp is 0 and its logits are not read.  Logits of
+ * -infinity have probability 0; a row of nothing else gives -infinity; one of +infinity or a NaN gives NaN.  A logit below -9.3e7 T has probability 0 too in a row whose others
+ * are larger.
+ * z: device, logits_type, r x v with row stride ldz >= v; tokens: device, index_type, r; logp: device fp32, r.
+ * workspace: device, 16-byte aligned, dsgd_token_workspace_bytes(r, v, pairs) bytes (pairs = 0 but for the preference loss), here and in the losses below.
+ * Errors of all five: CECA_ERR_INVALID_ARG (NULL where data is needed, r < 0, r >= 2^28, v < 1, v >= 2^31 - 1024, a row stride below the row,
+ * temperature not positive and finite, a bad type, and what each call names), CECA_ERR_WORKSPACE.
+ */
+ceca_status_t dsgd_token_logprob(const void *z, const void *tokens, float *logp, int64_t r, int64_t v, int64_t ldz, int32_t logits_type,
+                                 int32_t index_type, float temperature, void *workspace, size_t workspace_bytes, void *stream);
+
+/* Host function.  Minimum workspace size in bytes of dsgd_token_logprob and of the calls below (0 also for sizes they refuse). */
+size_t dsgd_token_workspace_bytes(int64_t r, int64_t v, int64_t pairs);
+
+/*
+ * Clipped policy loss with a KL term, row by row (a row is a position of a sampled sequence).  With l = logp[i] as above, the sampling
+ * policy's o = old_logp[i], the advantage A and the ratio p = exp(l - o):
+ *   loss[i] = w_i ( -min(p A, min(max(p, 1 - clip_low), 1 + clip_high) A)  +  kl (exp(x) - 1 - x) ),   x = ref_logp[i] - l
+ * (no second term without ref_logp or with kl = 0), w_i = weight[i] (1 when NULL).  A row without a token or with w_i = 0 has loss and gradient 0, and
+ * none of its other inputs is looked at.  The gradient is, with c = w_i (-p A where the ratio's own value is the smaller or equal one, else 0, and - kl (exp(x) - 1)):
+ *   dz[i, k] = c / T ((k = tokens[i]) - softmax(z[i, :] / T)[k])
+ * 1 - softmax at the token is taken from the other entries' sum, so that it keeps its digits where the model is sure.
+ * old_logp, advantage, ref_logp (may be NULL), weight (may be NULL), loss, logp (may be NULL; 0 in rows without a token or weight): device fp32, r.
+ * dz: device, logits_type, row stride lddz >= v; it may be z with the same row stride (another one: CECA_ERR_UNSUPPORTED).
+ * Also refused: clip_low not in [0, 1], clip_high or kl negative or not finite.
+ */
+ceca_status_t dsgd_policy_loss(const void *z, const void *tokens, const float *old_logp, const float *advantage, const float *ref_logp,
+                               const float *weight, float *loss, float *logp, int64_t r, int64_t v, int64_t ldz, int32_t logits_type,
+                               int32_t index_type, float temperature, float clip_low, float clip_high, float kl, void *workspace,
+                               size_t workspace_bytes, void *stream);
+ceca_status_t dsgd_policy_grad(const void *z, const void *tokens, const float *old_logp, const float *advantage, const float *ref_logp,
+                               const float *weight, float *loss, float *logp, void *dz, int64_t r, int64_t v, int64_t ldz, int64_t lddz,
+                               int32_t logits_type, int32_t index_type, float temperature, float clip_low, float clip_high, float kl,
+                               void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Preference loss of pairs of sequences.  bounds: device, bounds_type, 2*pairs + 1 row numbers that do not descend: sequence j is the rows
+ * [bounds[j], bounds[j+1]), the preferred one of pair p is j = 2p, the other 2p + 1.  L_j is the sum of logp over the sequence's rows
+ * that have a token, or with average != 0 their mean (0 for a sequence without any), and with m = beta ((L_2p - R_2p) - (L_2p+1 - R_2p+1)),
+ * R = ref_logp (0 when NULL):
+ *   loss[p] = w_p ( -(1 - smoothing) log sigmoid(m) - smoothing log sigmoid(-m) ),   w_p = weight[p] (1 when NULL)
+ * L goes to logp[0..2*pairs).  dz is the gradient of the sum of all losses; it is 0 in rows without a token, of pairs of weight 0, and outside all
+ * sequences.  Bounds outside [0, r] are taken as the nearest of the two.  L is summed in 64 bits in the order of the rows' numbers.
+ * ref_logp: device fp32, 2*pairs, may be NULL; weight, loss: device fp32, pairs, weight may be NULL; logp: device fp32, 2*pairs, may be NULL;
+ * dz as above.  pairs = 0 writes a gradient of 0.
+ * Also refused: pairs < 0 or >= 2^27, beta not finite, smoothing not in [0, 1].
+ */
+ceca_status_t dsgd_preference_loss(const void *z, const void *tokens, const void *bounds, const float *ref_logp, const float *weight,
+                                   float *loss, float *logp, int64_t pairs, int64_t r, int64_t v, int64_t ldz, int32_t logits_type,
+                                   int32_t index_type, int32_t bounds_type, float temperature, float beta, float smoothing, int32_t average,
+                                   void *workspace, size_t workspace_bytes, void *stream);
+ceca_status_t dsgd_preference_grad(const void *z, const void *tokens, const void *bounds, const float *ref_logp, const float *weight,
+                                   float *loss, float *logp, void *dz, int64_t pairs, int64_t r, int64_t v, int64_t ldz, int64_t lddz,
+                                   int32_t logits_type, int32_t index_type, int32_t bounds_type, float temperature, float beta,
+                                   float smoothing, int32_t average, void *workspace, size_t workspace_bytes, void *stream);
+
 typedef enum {
   CECA_WS_CONSENSUS_FUSED = 1,    /* ceca_consensus_rounds, fused = 1                      */
   CECA_WS_CONSENSUS_UNFUSED = 2,  /* ceca_consensus_rounds, fused = 0 with Y_out == NULL   */

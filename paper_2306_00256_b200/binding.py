@@ -19,7 +19,9 @@ EXPORTS = ["ceca_schedule", "ceca_gossip_sgd_step", "ceca_consensus_rounds", "ds
            "dsgd_logreg_grad_static", "dsgd_logreg_grad_static_capacity", "dsgd_lsq_grad",
            "ceca_fused_wait_selftest", "ceca_gossip_sgd_step_bf16", "dsgd_grad_shard_dots", "dsgd_grad_shard_sum",
            "dsgd_grad_shard_apply", "dsgd_embed_lookup", "dsgd_embed_grad", "dsgd_embed_workspace_bytes", "dsgd_recurrence",
-           "dsgd_recurrence_marks", "dsgd_recurrence_grad", "dsgd_recurrence_workspace_bytes", "dsgd_distill_loss", "dsgd_distill_grad"]
+           "dsgd_recurrence_marks", "dsgd_recurrence_grad", "dsgd_recurrence_workspace_bytes", "dsgd_distill_loss", "dsgd_distill_grad",
+           "dsgd_block_norm", "dsgd_block_norm_grad", "dsgd_block_norm_workspace_bytes", "dsgd_bring8", "dsgd_keep8", "dsgd_kept_row_bytes",
+           "dsgd_policy_grad", "dsgd_policy_loss", "dsgd_preference_grad", "dsgd_preference_loss", "dsgd_token_logprob", "dsgd_token_workspace_bytes"]
 
 
 class Round(ctypes.Structure):
@@ -29,6 +31,11 @@ class Round(ctypes.Structure):
                 ("a_num", ctypes.c_int32), ("a_den", ctypes.c_int32),
                 ("b_num", ctypes.c_int32), ("b_den", ctypes.c_int32),
                 ("a", ctypes.c_double), ("b", ctypes.c_double)]
+
+
+class Rows(ctypes.Structure):
+    """Mirror of dsgd_rows_t."""
+    _fields_ = [("at", ctypes.c_void_p), ("agent_stride", ctypes.c_int64), ("row_stride", ctypes.c_int64)]
 
 
 class CecaError(RuntimeError):
@@ -103,6 +110,31 @@ def library():
     lib.dsgd_distill_loss.restype = ctypes.c_int
     lib.dsgd_distill_grad.argtypes = [vp] * 7 + [i64] * 7 + [i32] * 3 + [f32, vp]
     lib.dsgd_distill_grad.restype = ctypes.c_int
+    lib.dsgd_kept_row_bytes.argtypes = [i64]
+    lib.dsgd_kept_row_bytes.restype = i64
+    lib.dsgd_keep8.argtypes = [Rows, vp, i32, i64, i64, i32, vp]
+    lib.dsgd_keep8.restype = ctypes.c_int
+    lib.dsgd_bring8.argtypes = [vp, Rows, i32, i64, i64, i32, vp]
+    lib.dsgd_bring8.restype = ctypes.c_int
+    lib.dsgd_block_norm.argtypes = [Rows] * 3 + [vp] * 3 + [i64] * 3 + [Rows] * 2 + [vp] * 4 + [i32, i64, i64] + [i32] * 4 + [f32, vp]
+    lib.dsgd_block_norm.restype = ctypes.c_int
+    lib.dsgd_block_norm_grad.argtypes = ([Rows] * 3 + [i32] + [vp] * 3 + [i64] * 3 + [vp] + [Rows] * 5 + [vp] * 3 + [i64] * 3 + [i32, i32, i64, i64] +
+                                         [i32] * 4 + [vp, sz, vp])
+    lib.dsgd_block_norm_grad.restype = ctypes.c_int
+    lib.dsgd_block_norm_workspace_bytes.argtypes = [i32, i64, i64]
+    lib.dsgd_block_norm_workspace_bytes.restype = sz
+    lib.dsgd_token_workspace_bytes.argtypes = [i64] * 3
+    lib.dsgd_token_workspace_bytes.restype = sz
+    lib.dsgd_token_logprob.argtypes = [vp] * 3 + [i64] * 3 + [i32] * 2 + [f32, vp, sz, vp]
+    lib.dsgd_token_logprob.restype = ctypes.c_int
+    lib.dsgd_policy_loss.argtypes = [vp] * 8 + [i64] * 3 + [i32] * 2 + [f32] * 4 + [vp, sz, vp]
+    lib.dsgd_policy_loss.restype = ctypes.c_int
+    lib.dsgd_policy_grad.argtypes = [vp] * 9 + [i64] * 4 + [i32] * 2 + [f32] * 4 + [vp, sz, vp]
+    lib.dsgd_policy_grad.restype = ctypes.c_int
+    lib.dsgd_preference_loss.argtypes = [vp] * 7 + [i64] * 4 + [i32] * 3 + [f32] * 3 + [i32, vp, sz, vp]
+    lib.dsgd_preference_loss.restype = ctypes.c_int
+    lib.dsgd_preference_grad.argtypes = [vp] * 8 + [i64] * 5 + [i32] * 3 + [f32] * 3 + [i32, vp, sz, vp]
+    lib.dsgd_preference_grad.restype = ctypes.c_int
     lib.ceca_status_string.argtypes = [ctypes.c_int]
     lib.ceca_status_string.restype = ctypes.c_char_p
     _lib = lib

@@ -12,6 +12,8 @@ import os
 from . import build as _build
 from .binding import library
 
+GATE_SIGMOID, GATE_SILU = 0, 1
+
 _module = None
 
 
@@ -79,3 +81,86 @@ def dsgd_distill_loss(z, idx, t, teacher_lse=None, weight=None, temperature=1.0,
 def dsgd_distill_grad(z, idx, t, teacher_lse=None, weight=None, temperature=1.0, loss=None, dz=None, stream=None):
     """(loss, dz): dsgd_distill_loss and the gradient of its sum over rows with respect to z, in one pass.  dz may be z."""
     return (_module or _load()).distill(z, idx, t, teacher_lse, weight, temperature, loss, True, dz, stream)
+
+
+def dsgd_kept_row_bytes(d):
+    return int(library().dsgd_kept_row_bytes(d))
+
+
+def dsgd_keep8(x, kept=None, stream=None):
+    """x [n, t, d] (float32 or bfloat16) in 8 bits with an exponent for every 32 channels: uint8 [n, t, dsgd_kept_row_bytes(d)].
+    For activations that wait for the backward pass; dsgd_block_norm writes its inputs in this form by itself (keep8=True)."""
+    return (_module or _load()).keep8(x, kept, stream)
+
+
+def dsgd_bring8(kept, d, dtype=None, x=None, stream=None):
+    """The values [n, t, d] that a kept tensor stands for, exactly, in dtype (float32 unless x says otherwise)."""
+    return (_module or _load()).bring8(kept, d, dtype, x, stream)
+
+
+def dsgd_block_norm(h, y, w_pre, w_post, gate=None, gate_act=GATE_SIGMOID, scale=None, eps=1e-6, h_out=None, u=None, save=False, keep8=False,
+                    stream=None):
+    """The end of a residual model's block and the start of the next, for n agents' rows [n, t, d]:
+        h_out = h + scale * g(gate) * w_post * y / rms(y),   u = w_pre * h_out / rms(h_out)
+    h (the residual stream) and h_out have one type, y (the block's output), gate and u one; w_pre, w_post [n, d] and scale [n] are each
+    agent's (blocks of columns of X will do).  y = w_post = None leaves the first line out (a model's first norm), w_pre = None the second.
+    g is the sigmoid of the gate (GATE_SIGMOID) or gate * sigmoid(gate) (GATE_SILU), 1 without one.
+    Returns (h_out, u, stats, kept): stats (None unless save) and kept, with keep8 the kept forms of (h, y, gate), are what
+    dsgd_block_norm_grad takes.  h_out may be h, and u may be y or gate."""
+    return (_module or _load()).block_norm(h, y, w_pre, w_post, gate, gate_act, scale, eps, h_out, u, save, keep8, stream)
+
+
+def dsgd_block_norm_workspace_bytes(n, t, d):
+    return int(library().dsgd_block_norm_workspace_bytes(n, t, d))
+
+
+def dsgd_block_norm_grad(h, y, w_pre, w_post, stats, du, dh_out=None, gate=None, gate_act=GATE_SIGMOID, scale=None, dh=None, dy=None,
+                         dgate=None, dw_pre=None, dw_post=None, dscale=None, accumulate=False, workspace=None, stream=None):
+    """The gradient of dsgd_block_norm from its stats and its inputs h, y and gate, whole or as it kept them in 8 bits: returns
+    (dh, dy, dgate, dw_pre, dw_post, dscale), None for what is not there.  du and dh_out (0 when None) are the gradients with respect to u and
+    h_out.  dw_pre, dw_post [n, d] and dscale [n] may be blocks of columns of G; with accumulate they are added to.  With kept inputs and no
+    dh_out, dh has the type of du unless it is passed in."""
+    return (_module or _load()).block_norm_grad(h, y, w_pre, w_post, stats, du, dh_out, gate, gate_act, scale, dh, dy, dgate, dw_pre, dw_post, dscale,
+                                                accumulate, workspace, stream)
+
+
+def dsgd_token_workspace_bytes(r, v, pairs=0):
+    return int(library().dsgd_token_workspace_bytes(r, v, pairs))
+
+
+def dsgd_token_logprob(z, tokens, temperature=1.0, logp=None, workspace=None, stream=None):
+    """log softmax(z / temperature) of z [r, v] at each row's token (int32 or int64 [r]): float32 [r], 0 where the token is outside [0, v)."""
+    return (_module or _load()).token_logprob(z, tokens, temperature, logp, workspace, stream)
+
+
+def dsgd_policy_loss(z, tokens, old_logp, advantage, ref_logp=None, weight=None, temperature=1.0, clip_low=0.2, clip_high=0.2, kl=0.0, loss=None,
+                     logp=None, workspace=None, stream=None):
+    """weight * (-min(p A, clip(p, 1 - clip_low, 1 + clip_high) A) + kl * (exp(x) - 1 - x)) of each row, p = exp(l - old_logp) and
+    x = ref_logp - l with l the log-probability of the row's token, A the advantage.  Rows without a token or with weight 0 have loss 0.
+    logp: float32 [r], receives l."""
+    return (_module or _load()).policy(z, tokens, old_logp, advantage, ref_logp, weight, temperature, clip_low, clip_high, kl, loss, logp, False, None,
+                                       workspace, stream)
+
+
+def dsgd_policy_grad(z, tokens, old_logp, advantage, ref_logp=None, weight=None, temperature=1.0, clip_low=0.2, clip_high=0.2, kl=0.0, loss=None,
+                     logp=None, dz=None, workspace=None, stream=None):
+    """(loss, dz): dsgd_policy_loss and the gradient of its sum over rows with respect to z.  dz may be z."""
+    return (_module or _load()).policy(z, tokens, old_logp, advantage, ref_logp, weight, temperature, clip_low, clip_high, kl, loss, logp, True, dz,
+                                       workspace, stream)
+
+
+def dsgd_preference_loss(z, tokens, bounds, ref_logp=None, weight=None, temperature=1.0, beta=0.1, smoothing=0.0, average=False, loss=None, logp=None,
+                         workspace=None, stream=None):
+    """The preference loss of pairs of sequences packed into the rows of z [r, v]: sequence j is rows bounds[j] to bounds[j + 1] (int32 or
+    int64 [2 pairs + 1]), 2p the preferred one of pair p.  With L the sum (or average) of its rows' log-probabilities and
+    m = beta * ((L_2p - ref_2p) - (L_2p+1 - ref_2p+1)): weight * (-(1 - smoothing) log sigmoid(m) - smoothing log sigmoid(-m)).
+    Returns (loss [pairs], logp [2 pairs]), logp being the L."""
+    return (_module or _load()).preference(z, tokens, bounds, ref_logp, weight, temperature, beta, smoothing, average, loss, logp, False, None,
+                                           workspace, stream)
+
+
+def dsgd_preference_grad(z, tokens, bounds, ref_logp=None, weight=None, temperature=1.0, beta=0.1, smoothing=0.0, average=False, loss=None, logp=None,
+                         dz=None, workspace=None, stream=None):
+    """(loss, logp, dz): dsgd_preference_loss and the gradient of the sum of its losses with respect to z.  dz may be z."""
+    return (_module or _load()).preference(z, tokens, bounds, ref_logp, weight, temperature, beta, smoothing, average, loss, logp, True, dz,
+                                           workspace, stream)
