@@ -434,12 +434,12 @@ int64_t dsgd_kept_row_bytes(int64_t d);
  * no u: a block that no norm follows.  u is computed from h_out before that is rounded for its storage.
  * h, h_out: stream_type; y, gate, u: act_type; all n x t rows.  w_pre, w_post, scale: weights_type, agent i's at i*stride
  * (so they may be blocks of columns of X).
- * stats: device fp32, n x t x 2 dense, receives 1 / rms(y) and 1 / rms(h_out) for the gradient; may be NULL.
+ * stats: device fp32, n x t x 2 dense, 8-byte aligned, receives 1 / rms(y) and 1 / rms(h_out) for the gradient; may be NULL.
  * h8, y8, gate8: device, kept tensors (dsgd_keep8) of h, y and gate, each may be NULL: what the gradient reads in their place.
  * h_out may be h, u may be y or gate where the types and strides are the same (each element is read before it is written; other overlaps
  * are not allowed).  t = 0 does nothing.
  * Errors: CECA_ERR_INVALID_ARG (NULL where data is needed, n or d < 1, n > 65535, t < 0, t or d >= 2^31 - 1024, a row stride below d, a negative
- * stride, eps not positive and finite, neither y nor w_pre, a gate without y, a bad type), CECA_ERR_ALIGNMENT (h8, y8, gate8).
+ * stride, eps not positive and finite, neither y nor w_pre, a gate without y, a bad type), CECA_ERR_ALIGNMENT (stats, h8, y8, gate8).
  * Speed: best where d is a multiple of 8 and every row starts on a 16-byte boundary.
  */
 ceca_status_t dsgd_block_norm(dsgd_rows_t h, dsgd_rows_t y, dsgd_rows_t gate, const void *w_pre, const void *w_post, const void *scale,

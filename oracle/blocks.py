@@ -127,6 +127,9 @@ def block_norm_grad(h, y, w_pre, w_post, stats, du, dh_out=None, gate=None, act=
         ee = np.abs(by * g) * edh + np.abs(by * dh) * eg + 4 * U * np.abs(e)
         m = (yn * e).mean(-1, keepdims=True)
         em = (np.abs(yn) * ee + np.abs(e) * eyn).mean(-1, keepdims=True) + rows * U * np.abs(yn * e).mean(-1, keepdims=True)
+        if w_pre is not None:   # mean(yn e) may be mean(q (dh_out + r w_pre du)) - r mean(hn w_pre du) mean(q hn), q = s g w_post yn: sums of their own
+            q, m1 = np.abs(by * g * yn), np.abs((hn * flow).mean(-1, keepdims=True))
+            em = em + rows * U * ((q * (np.abs(past) + r * np.abs(flow))).mean(-1, keepdims=True) + r * m1 * (q * np.abs(hn)).mean(-1, keepdims=True))
         dy = rho * (e - yn * m)
         out["dy"] = _out(dy, rho * (ee + np.abs(m) * eyn + np.abs(yn) * em + 3 * U * (np.abs(e) + np.abs(yn * m))) + 2 * U * np.abs(dy), act16)
         if gate is not None:

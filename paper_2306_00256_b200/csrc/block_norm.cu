@@ -192,7 +192,9 @@ __global__ void __launch_bounds__(kThreads) finish_kernel(const BlockArgs p) {
   const int64_t agent = blockIdx.y, c = (int64_t)blockIdx.x * 32 + lane;
   const float scale = p.scale ? load(p.scale, p.weights_type, agent * p.scale_stride) : 1.f;
   float a = 0.f, b = 0.f;
+  after_first();
   if (c < p.d)
+#pragma unroll 8
     for (int q = warp; q < p.part_count; q += kWarps) {
       const float *part = p.parts + ((agent * p.part_count + q) * 2) * p.d + c;
       a += part[0];
@@ -221,10 +223,6 @@ __global__ void __launch_bounds__(kThreads) finish_kernel(const BlockArgs p) {
   }
 }
 
-cudaError_t finish(const BlockArgs &p, cudaStream_t s) {
-  finish_kernel<<<dim3((unsigned)ceil_div(p.d, 32), (unsigned)p.n), kThreads, 0, s>>>(p);
-  return cudaGetLastError();
-}
 
 constexpr int64_t kMost = ((int64_t)1 << 31) - 1024;
 
@@ -248,6 +246,11 @@ bool out_ok(const dsgd_rows_t &x, int32_t n, int64_t d) { return rows_ok(x, d) &
 ceca_status_t status(cudaError_t e) { return e == cudaSuccess ? CECA_OK : CECA_ERR_CUDA; }
 
 }  // namespace
+
+cudaError_t finish_block_grad(const BlockArgs &p, cudaStream_t s) {
+  return launch_after(finish_kernel, p, dim3((unsigned)ceil_div(p.d, 32), (unsigned)p.n), kThreads, 0, s);
+}
+
 }  // namespace ceca
 
 using namespace ceca;
@@ -264,7 +267,8 @@ extern "C" ceca_status_t dsgd_block_norm(dsgd_rows_t h, dsgd_rows_t y, dsgd_rows
   if (t == 0) return CECA_OK;
   if (!h.at || (!y.at && !w_pre) || (y.at && (!w_post || !h_out.at)) || (gate.at && !y.at) || (w_pre && !u.at) || (y8 && !y.at) || (gate8 && !gate.at))
     return CECA_ERR_INVALID_ARG;
-  if ((reinterpret_cast<uintptr_t>(h8) | reinterpret_cast<uintptr_t>(y8) | reinterpret_cast<uintptr_t>(gate8)) & 15) return CECA_ERR_ALIGNMENT;
+  if (((reinterpret_cast<uintptr_t>(h8) | reinterpret_cast<uintptr_t>(y8) | reinterpret_cast<uintptr_t>(gate8)) & 15) || (reinterpret_cast<uintptr_t>(stats) & 7))
+    return CECA_ERR_ALIGNMENT;
   BlockArgs p{};
   p.h = h; p.y = y; p.gate = gate; p.h_out = h_out; p.u = u;
   p.w_pre = w_pre; p.w_post = w_post; p.scale = scale;
@@ -273,12 +277,16 @@ extern "C" ceca_status_t dsgd_block_norm(dsgd_rows_t h, dsgd_rows_t y, dsgd_rows
   p.t = t; p.d = d; p.row_bytes = kept_row_bytes(d); p.n = n;
   p.stream_type = stream_type; p.act_type = act_type; p.weights_type = weights_type; p.silu = gate_act == DSGD_GATE_SILU; p.eps = eps;
   const cudaStream_t s = static_cast<cudaStream_t>(stream);
+  if (d <= kWidest)
+    return status(launch_block_rows(p, d % 8 == 0 && on_words(h, stream_type) && on_words(h_out, stream_type) && on_words(y, act_type) && on_words(gate, act_type) &&
+                                           on_words(u, act_type), s));
   wide_kernel<<<(unsigned)std::min<int64_t>(n * t, (int64_t)sm_count() * 8), kThreads, 0, s>>>(p);
   return status(cudaGetLastError());
 }
 
 extern "C" size_t dsgd_block_norm_workspace_bytes(int32_t n, int64_t t, int64_t d) {
   if (!sizes_ok(n, t, d)) return 0;
+  if (d <= kWidest) return (size_t)n * block_grad_parts(n, t, d) * (8 * (size_t)d + 16);
   const Sizes z = sizes_of(n, t, d);
   return 8 * (size_t)n * t + 4 * (size_t)n * z.part_count * (2 * (size_t)d + z.column_blocks);
 }
@@ -299,6 +307,7 @@ extern "C" ceca_status_t dsgd_block_norm_grad(dsgd_rows_t h, dsgd_rows_t y, dsgd
       (dscale && dscale_stride < (n > 1 ? 1 : 0)))
     return CECA_ERR_INVALID_ARG;
   if (t > 0 && (!h.at || !stats || (w_pre && !du.at) || !dh.at || (y.at && !dy.at) || (gate.at && !dgate.at))) return CECA_ERR_INVALID_ARG;
+  if ((reinterpret_cast<uintptr_t>(stats) & 7) != 0) return CECA_ERR_ALIGNMENT;
   if (kept && ((reinterpret_cast<uintptr_t>(h.at) | reinterpret_cast<uintptr_t>(y.at) | reinterpret_cast<uintptr_t>(gate.at)) & 15))
     return CECA_ERR_ALIGNMENT;
   const size_t need = dsgd_block_norm_workspace_bytes(n, t, d);
@@ -311,19 +320,24 @@ extern "C" ceca_status_t dsgd_block_norm_grad(dsgd_rows_t h, dsgd_rows_t y, dsgd
   p.stats = const_cast<float *>(stats);
   p.t = t; p.d = d; p.row_bytes = kept_row_bytes(d); p.n = n; p.kept = kept != 0; p.accumulate = accumulate != 0;
   p.stream_type = stream_type; p.act_type = act_type; p.weights_type = weights_type; p.silu = gate_act == DSGD_GATE_SILU;
+  const cudaStream_t s = static_cast<cudaStream_t>(stream);
+  p.means = static_cast<float2 *>(workspace);
+  if (d <= kWidest && t > 0) {
+    const bool words = d % 8 == 0 && (kept || (on_words(h, stream_type) && on_words(y, act_type) && on_words(gate, act_type))) && on_words(du, act_type) &&
+                       on_words(dh_out, stream_type) && on_words(dh, stream_type) && on_words(dy, act_type) && on_words(dgate, act_type);
+    return status(launch_block_grad_rows(p, words, s));
+  }
   const Sizes z = sizes_of(n, t, d);
   p.part_rows = z.part_rows;
   p.part_count = (int32_t)z.part_count;
   p.scale_count = (int32_t)(z.part_count * z.column_blocks);
-  p.means = static_cast<float2 *>(workspace);
   p.parts = reinterpret_cast<float *>(p.means + n * t);
   p.scale_parts = p.parts + (size_t)n * z.part_count * 2 * d;
-  const cudaStream_t s = static_cast<cudaStream_t>(stream);
   if (t > 0) {
     const unsigned rows = (unsigned)std::min<int64_t>(n * t, (int64_t)sm_count() * 8);
     wide_means_kernel<<<rows, kThreads, 0, s>>>(p);
     wide_sums_kernel<<<dim3((unsigned)z.column_blocks, (unsigned)std::min<int64_t>(n * z.part_count, 65535)), kThreads, 0, s>>>(p);
     wide_grad_kernel<<<rows, kThreads, 0, s>>>(p);
   }
-  return status(finish(p, s));
+  return status(finish_block_grad(p, s));
 }

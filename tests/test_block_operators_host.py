@@ -176,6 +176,8 @@ def test_block_norm_gradient_refuses(change):
 def test_block_norm_refuses_places_that_do_not_do():
     for k in ("h8", "y8", "gate8"):
         assert _call("dsgd_block_norm", NORM, **{k: ODD}) == ALIGNMENT
+    for name, args in (("dsgd_block_norm", NORM), ("dsgd_block_norm_grad", NGRAD)):
+        assert _call(name, args, stats=ctypes.c_void_p(4100)) == ALIGNMENT
     for k in ("h", "y", "gate"):
         assert _call("dsgd_block_norm_grad", NGRAD, kept=1, **{k: R(at=4104)}) == ALIGNMENT
     size = ceca.dsgd_block_norm_workspace_bytes(2, 4, 16)
