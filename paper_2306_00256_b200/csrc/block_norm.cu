@@ -33,6 +33,9 @@ __device__ __forceinline__ float cta_sum(float x) {
 // ---------------------------------------------------------------------------------------------- rows of any width
 // A CTA works on a row, channel by channel, and reads it once for each thing that it sums.
 
+struct Gate {
+  float g, slope;
+};
 struct Row {
   const BlockArgs &p;
   int64_t agent, row, h, y, gate;
@@ -55,7 +58,11 @@ struct Row {
   __device__ float h_at(int64_t c) const { return value(p.h, h, p.stream_type, c); }
   __device__ float y_at(int64_t c) const { return value(p.y, y, p.act_type, c); }
   __device__ float gate_at(int64_t c) const { return value(p.gate, gate, p.act_type, c); }
-  __device__ Gate g(int64_t c) const { return p.gate.at ? gate_of(gate_at(c), p.silu) : Gate{1.f, 0.f}; }
+  __device__ Gate g(int64_t c) const {
+    if (!p.gate.at) return {1.f, 0.f};
+    const Gates x = gates_of(all<2>(gate_at(c)), p.silu);
+    return {x.g.x, x.slope.x};
+  }
   __device__ float w_pre(int64_t c) const { return load(p.w_pre, p.weights_type, agent * p.w_pre_stride + c); }
   __device__ float w_post(int64_t c) const { return load(p.w_post, p.weights_type, agent * p.w_post_stride + c); }
   __device__ float out(int64_t c, float rho) const {
@@ -83,7 +90,7 @@ __global__ void __launch_bounds__(kThreads) wide_kernel(const BlockArgs p) {
       }
       return cta_sum(s);
     };
-    const auto norm = [&](auto value) { return inverse_rms(squares(value, 1.f), p.d, p.eps, [&](float unit) { return squares(value, unit); }); };
+    const auto norm = [&](auto value) { return inverse_rms(squares(value, 1.f), 1.f / (float)p.d, p.eps, [&](float unit) { return squares(value, unit); }); };
     const float rho = p.y.at ? norm([&](int64_t c) { return x.y_at(c); }) : 0.f;
     const float r = p.w_pre ? norm([&](int64_t c) { return x.out(c, rho); }) : 0.f;
     if (threadIdx.x == 0 && p.stats) {
@@ -243,9 +250,27 @@ bool rows_ok(const dsgd_rows_t &x, int64_t d) { return !x.at || (x.row_stride >=
 // (two agents' rows in one place would be written by both)
 bool out_ok(const dsgd_rows_t &x, int32_t n, int64_t d) { return rows_ok(x, d) && (!x.at || n == 1 || x.agent_stride >= d); }
 
+// Rows in registers, by types and alignment.
+cudaError_t rows(const BlockArgs &p, bool grad, cudaStream_t s) {
+  bool words = p.d % 8 == 0;
+  for (const dsgd_rows_t *x : {&p.h, &p.y, &p.gate}) words = words && (p.kept || on_words(*x, x == &p.h ? p.stream_type : p.act_type));
+  for (const dsgd_rows_t *x : {&p.h_out, &p.dh_out, &p.dh}) words = words && on_words(*x, p.stream_type);
+  for (const dsgd_rows_t *x : {&p.u, &p.du, &p.dy, &p.dgate}) words = words && on_words(*x, p.act_type);
+  if (words && p.stream_type == DSGD_BF16 && p.act_type == DSGD_BF16) return block_rows_bf16(p, grad, s);
+  if (words && p.stream_type == DSGD_F32) return p.act_type == DSGD_F32 ? block_rows_f32(p, grad, s) : block_rows_mixed(p, grad, s);
+  return block_rows_any(p, grad, s);
+}
+
 ceca_status_t status(cudaError_t e) { return e == cudaSuccess ? CECA_OK : CECA_ERR_CUDA; }
 
 }  // namespace
+
+// At least four rows a group: a part costs as much as two rows in memory.  Parts are counted by 148 SMs, not by the device's: the workspace's size is
+// asked for without one.
+int64_t block_grad_parts(int64_t n, int64_t t, int64_t d) {
+  const Shape z = grad_shape_of(d);
+  return std::max<int64_t>(1, std::min(148 * (int64_t)resident_grad(z.group, z.passes) / n, ceil_div(t, 4 * groups_of(z.group))));
+}
 
 cudaError_t finish_block_grad(const BlockArgs &p, cudaStream_t s) {
   return launch_after(finish_kernel, p, dim3((unsigned)ceil_div(p.d, 32), (unsigned)p.n), kThreads, 0, s);
@@ -277,9 +302,7 @@ extern "C" ceca_status_t dsgd_block_norm(dsgd_rows_t h, dsgd_rows_t y, dsgd_rows
   p.t = t; p.d = d; p.row_bytes = kept_row_bytes(d); p.n = n;
   p.stream_type = stream_type; p.act_type = act_type; p.weights_type = weights_type; p.silu = gate_act == DSGD_GATE_SILU; p.eps = eps;
   const cudaStream_t s = static_cast<cudaStream_t>(stream);
-  if (d <= kWidest)
-    return status(launch_block_rows(p, d % 8 == 0 && on_words(h, stream_type) && on_words(h_out, stream_type) && on_words(y, act_type) && on_words(gate, act_type) &&
-                                           on_words(u, act_type), s));
+  if (d <= kWidest) return status(rows(p, false, s));
   wide_kernel<<<(unsigned)std::min<int64_t>(n * t, (int64_t)sm_count() * 8), kThreads, 0, s>>>(p);
   return status(cudaGetLastError());
 }
@@ -322,11 +345,7 @@ extern "C" ceca_status_t dsgd_block_norm_grad(dsgd_rows_t h, dsgd_rows_t y, dsgd
   p.stream_type = stream_type; p.act_type = act_type; p.weights_type = weights_type; p.silu = gate_act == DSGD_GATE_SILU;
   const cudaStream_t s = static_cast<cudaStream_t>(stream);
   p.means = static_cast<float2 *>(workspace);
-  if (d <= kWidest && t > 0) {
-    const bool words = d % 8 == 0 && (kept || (on_words(h, stream_type) && on_words(y, act_type) && on_words(gate, act_type))) && on_words(du, act_type) &&
-                       on_words(dh_out, stream_type) && on_words(dh, stream_type) && on_words(dy, act_type) && on_words(dgate, act_type);
-    return status(launch_block_grad_rows(p, words, s));
-  }
+  if (d <= kWidest && t > 0) return status(rows(p, true, s));
   const Sizes z = sizes_of(n, t, d);
   p.part_rows = z.part_rows;
   p.part_count = (int32_t)z.part_count;

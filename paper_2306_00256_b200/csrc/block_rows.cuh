@@ -1,0 +1,682 @@
+// Internal: the end of a block and the start of the next, and its gradient, for rows that a group of threads holds in registers.
+//
+// A group takes every so-many-th row of an agent.  The next rows are copied to a ring in shared memory while one is computed on, so that loads are always
+// under way; the weights, and the sums of their gradients, stay in registers.
+//
+// Forward: two sums over the group a row, y^2 and h_out^2.  Gradient, with q = s g w_post yn (what the block added), f = w_pre du and t = dh_out + r f:
+// the three sums A = hn f, B = q t, C = q hn at once, then m = A / d, dh = t - r m hn and mean(yn e) = (B - r m C) / d.
+#pragma once
+#include <cuda_runtime.h>
+
+#include <algorithm>
+#include <atomic>
+#include <type_traits>
+
+#include "block_norm.cuh"
+#include "tma.h"
+
+namespace ceca {
+
+constexpr int kKept = 2;      // besides DSGD_F32 and DSGD_BF16
+constexpr int kAnyType = -1;  // of a template: the call says which
+// What a kernel is compiled for: the whole of the formulas without a gate or with one of the two, or any part of them, as the call says.  (Branches
+// between the parts keep loads and products apart that could overlap.)
+enum Parts : int { kPlain, kSigmoid, kSilu, kAnyParts };
+
+__device__ __forceinline__ void copy_16(uint32_t to, const void *from) { asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory"); }
+__device__ __forceinline__ void copy_16(uint32_t to, const void *from, int bytes) {   // zeros behind the first `bytes`
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void copy_8(uint32_t to, const void *from) { asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(to), "l"(from) : "memory"); }
+__device__ __forceinline__ void copy_4(uint32_t to, const void *from) { asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(to), "l"(from) : "memory"); }
+__device__ __forceinline__ void copies_end() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+__device__ __forceinline__ void copies_but(int behind) {   // waits for all groups but the last `behind`
+  switch (behind) {
+    case 0: asm volatile("cp.async.wait_group 0;" ::: "memory"); break;
+    case 1: asm volatile("cp.async.wait_group 1;" ::: "memory"); break;
+    case 2: asm volatile("cp.async.wait_group 2;" ::: "memory"); break;
+    default: asm volatile("cp.async.wait_group 3;" ::: "memory"); break;
+  }
+}
+
+// The channels of a thread of a group of G: with WORDS 8 neighbours (channel 8 (rank + G j) on, in 16-byte words), else every G-th one.
+// They are computed on in pairs.  PASSES: eights a thread.
+template <int G, int PASSES, bool WORDS> struct Lay {
+  static constexpr int kPairs = 4 * PASSES;
+  __device__ static int channel(int rank, int j, int e) { return WORDS ? 8 * (rank + G * j) + e : rank + G * (8 * j + e); }
+};
+struct Pairs8 {
+  Val<2> v[4];
+};
+
+// A place in shared memory for a row of a tensor, or for a kept row, and its copy and reading.  With WORDS each warp copies what it will
+// read; else the group copies the 16-byte words that the row touches (of the first and last one the bytes inside the row count), and
+// must meet between copying and reading.
+template <int G, int PASSES, bool WORDS> struct Place {
+  using L = Lay<G, PASSES, WORDS>;
+  // types: DSGD_F32, DSGD_BF16, kKept
+  static int room(int64_t d, int32_t type) {
+    if (type == kKept) return WORDS ? 12 * G * PASSES : (int)kept_row_bytes(d);
+    return WORDS ? 16 * G * PASSES * (type == DSGD_BF16 ? 1 : 2) : (int)((d * type_bytes(type) + 47) / 16 * 16);
+  }
+  __device__ static void copy(uint32_t to, const uint8_t *from, int32_t type, int d, int rank) {
+    if (WORDS) {
+#pragma unroll
+      for (int j = 0; j < PASSES; ++j) {
+        const int at = rank + G * j;
+        if (8 * at >= d) continue;
+        if (type == kKept) {
+          copy_8(to + 8 * at, from + 8 * at);
+          copy_4(to + 8 * G * PASSES + 4 * at, from + ((d + at / 4) & ~3));
+        } else if (type == DSGD_BF16) {
+          copy_16(to + 16 * at, from + 16 * at);
+        } else if ((at ^ 1) * 8 >= d) {   // (the last one, alone)
+          copy_16(to + 16 * at, from + 32 * at);
+          copy_16(to + 16 * (G * PASSES + (at ^ 1)), from + 32 * at + 16);
+        } else {   // two lanes copy each one's 32 bytes together, so that every copy touches whole sectors
+          const int odd = at & 1, even = at ^ odd;
+          copy_16(to + 16 * (odd * G * PASSES + (even ^ odd)), from + 32 * even + 16 * odd);
+          copy_16(to + 16 * (odd * G * PASSES + ((even + 1) ^ odd)), from + 32 * even + 32 + 16 * odd);
+        }
+      }
+    } else {
+      const int pad = (int)(reinterpret_cast<uintptr_t>(from) & 15), end = pad + (type == kKept ? (int)kept_row_bytes(d) : d * (type == DSGD_BF16 ? 2 : 4));
+      from -= pad;
+      for (int at = 16 * rank; at < end; at += 16 * G) copy_16(to + at, from + at, min(16, end - at));
+    }
+  }
+  // the eight channels of pass j; zeros outside the row
+  __device__ static Pairs8 read(const uint8_t *place, int pad, int32_t type, int d, int rank, int j) {
+    Pairs8 r;
+    if (WORDS) {
+      const int at = rank + G * j;
+      if (8 * at >= d) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) r.v[i] = {0.f, 0.f};
+      } else if (type == kKept) {
+        const uint2 q = reinterpret_cast<const uint2 *>(place)[at];
+        const uint32_t e = reinterpret_cast<const uint32_t *>(place + 8 * G * PASSES)[at] >> 8 * ((d + at / 4) & 3) & 255u;
+        const Val<2> step = all<2>(step8(e));
+#pragma unroll
+        for (int i = 0; i < 4; ++i) r.v[i] = mul(bytes8(i < 2 ? q.x : q.y, 2 * (i & 1)), step);
+      } else if (type == DSGD_BF16) {
+        const uint4 w = reinterpret_cast<const uint4 *>(place)[at];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const uint32_t x = (&w.x)[i];
+          r.v[i] = {__uint_as_float(x << 16), __uint_as_float(x & 0xffff0000u)};
+        }
+      } else {
+        const float4 a = reinterpret_cast<const float4 *>(place)[at], b = reinterpret_cast<const float4 *>(place)[G * PASSES + (at ^ 1)];
+        r.v[0] = {a.x, a.y};
+        r.v[1] = {a.z, a.w};
+        r.v[2] = {b.x, b.y};
+        r.v[3] = {b.z, b.w};
+      }
+    } else {
+      place += pad;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const int c = L::channel(rank, j, e);
+        float x = 0.f;
+        if (c < d) {
+          if (type == kKept) x = (float)(int8_t)place[c] * step8(place[d + c / kBlock8]);
+          else x = type == DSGD_BF16 ? widen(reinterpret_cast<const bf16 *>(place)[c]) : reinterpret_cast<const float *>(place)[c];
+        }
+        (e & 1 ? r.v[e / 2].y : r.v[e / 2].x) = x;
+      }
+    }
+    return r;
+  }
+  // bytes `from` and from + 1 of w, two whole numbers
+  __device__ static Val<2> bytes8(uint32_t w, int from) {
+    w ^= 0x80808080u;   // (x + 128) + 2^23, less 2^23 + 128
+    const Val<2> v = {__uint_as_float(__byte_perm(w, 0x4b000000u, 0x7650u | from)), __uint_as_float(__byte_perm(w, 0x4b000000u, 0x7650u | (from + 1)))};
+    return add(v, all<2>(-8388736.f));
+  }
+  // writes eight channels of a row
+  __device__ static void write(void *row, int32_t type, const Pairs8 &x, int d, int rank, int j) {
+    if (WORDS) {
+      const int at = rank + G * j;
+      if (type == DSGD_F32) {   // two lanes write each one's 32 bytes together
+        const bool odd = at & 1, alone = 8 * (at ^ 1) >= d;
+        float4 a = make_float4(x.v[0].x, x.v[0].y, x.v[1].x, x.v[1].y), b = make_float4(x.v[2].x, x.v[2].y, x.v[3].x, x.v[3].y);
+        const float4 give = odd ? a : b;
+        float4 got;
+        got.x = __shfl_xor_sync(0xffffffffu, give.x, 1);
+        got.y = __shfl_xor_sync(0xffffffffu, give.y, 1);
+        got.z = __shfl_xor_sync(0xffffffffu, give.z, 1);
+        got.w = __shfl_xor_sync(0xffffffffu, give.w, 1);
+        if (8 * at >= d) return;
+        float4 *to = static_cast<float4 *>(row) + 2 * at;
+        if (alone) {
+          to[0] = a;
+          to[1] = b;
+        } else {
+          (odd ? a : b) = got;
+          to[odd ? -1 : 0] = a;   // the second half of the even lane's, or the first of its own
+          to[odd ? 1 : 2] = b;
+        }
+        return;
+      }
+      if (8 * at >= d) return;
+      if (type == DSGD_BF16) {
+        uint4 w;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const __nv_bfloat162 h = __floats2bfloat162_rn(x.v[i].x, x.v[i].y);
+          (&w.x)[i] = *reinterpret_cast<const uint32_t *>(&h);
+        }
+        static_cast<uint4 *>(row)[at] = w;
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const int c = L::channel(rank, j, e);
+        if (c < d) store(row, type, c, e & 1 ? x.v[e / 2].y : x.v[e / 2].x);
+      }
+    }
+  }
+  // keeps a row in 8 bits; whole warps call it
+  __device__ static void keep(uint8_t *row, const Pairs8 *x, int d, int rank) {
+#pragma unroll
+    for (int j = 0; j < PASSES; ++j) keep(row, x[j], d, rank, j);
+    const int from = d + (int)blocks8(d), to = (int)kept_row_bytes(d);   // the bytes behind the exponents
+    if (rank < to - from) row[from + rank] = 0;
+  }
+  __device__ static void keep(uint8_t *row, const Pairs8 &x, int d, int rank, int j) {
+    if (WORDS) {
+      const int at = rank + G * j;
+      uint32_t top = 0;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) top = max(top, max(magnitude(x.v[i].x), magnitude(x.v[i].y)));
+      top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+      top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+      if (8 * at >= d) return;
+      const uint32_t e = exponent8(top);
+      const Val<2> by = all<2>(scale8(e));
+      uint32_t b[8];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const Val<2> v = mul(x.v[i], by);
+        // rounded to the nearest whole number in the low bits of a sum with 1.5 2^23 (a NaN times 0 becomes 0 first: fmaxf drops it, to -127, so it is asked for)
+        b[2 * i] = __float_as_uint(fminf(fmaxf(v.x, -127.f), 127.f) + 12582912.f);
+        b[2 * i + 1] = __float_as_uint(fminf(fmaxf(v.y, -127.f), 127.f) + 12582912.f);
+      }
+      uint2 q;
+      q.x = __byte_perm(__byte_perm(b[0], b[1], 0x0040), __byte_perm(b[2], b[3], 0x0040), 0x5410);
+      q.y = __byte_perm(__byte_perm(b[4], b[5], 0x0040), __byte_perm(b[6], b[7], 0x0040), 0x5410);
+      if (e == 255u) q = make_uint2(0, 0);
+      reinterpret_cast<uint2 *>(row)[at] = q;
+      if (at % 4 == 0) row[d + at / 4] = (uint8_t)e;
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const int c = L::channel(rank, j, e);
+        const float v = e & 1 ? x.v[e / 2].y : x.v[e / 2].x;
+        const uint32_t b = exponent8(__reduce_max_sync(0xffffffffu, magnitude(v)));
+        if (c < d) {
+          row[c] = (uint8_t)(int8_t)hold8(v, scale8(b));
+          if (c % kBlock8 == 0) row[d + c / kBlock8] = (uint8_t)b;
+        }
+      }
+    }
+  }
+};
+
+// The sums over a group of N numbers a thread, in one order, the same on all its threads.  `turn` says which of two places is used: consecutive
+// sums take the other one, so that one barrier is enough.
+template <int G, int N> __device__ __forceinline__ void group_sums(float (&x)[N], float (*place)[4 * (G / 32)], int turn) {
+#pragma unroll
+  for (int o = 16; o; o >>= 1)
+#pragma unroll
+    for (int i = 0; i < N; ++i) x[i] += __shfl_xor_sync(0xffffffffu, x[i], o);
+  if (G == 32) return;
+  constexpr int W = G / 32;
+  const int lane = threadIdx.x & 31;
+  if (lane == 0) {
+    if (N == 1) place[turn][threadIdx.x >> 5] = x[0];
+    else *reinterpret_cast<float4 *>(place[turn] + 4 * (threadIdx.x >> 5)) = make_float4(x[0], x[1 % N], x[2 % N], 0.f);
+  }
+  __syncthreads();
+  // each lane reads one warp's, and the warps' are summed as the lanes' were
+  if (N == 1) {
+    x[0] = place[turn][lane % W];
+#pragma unroll
+    for (int o = W / 2; o; o >>= 1) x[0] += __shfl_xor_sync(0xffffffffu, x[0], o);
+  } else {
+    const float4 v = *reinterpret_cast<const float4 *>(place[turn] + 4 * (lane % W));
+    x[0] = v.x;
+    x[1 % N] = v.y;
+    x[2 % N] = v.z;
+#pragma unroll
+    for (int o = W / 2; o; o >>= 1)
+#pragma unroll
+      for (int i = 0; i < N; ++i) x[i] += __shfl_xor_sync(0xffffffffu, x[i], o);
+  }
+}
+template <int G> __device__ __forceinline__ float group_sum(float x, float (*place)[4 * (G / 32)], int turn) {
+  float v[1] = {x};
+  group_sums<G, 1>(v, place, turn);
+  return v[0];
+}
+
+__device__ __forceinline__ float total(const Pairs8 &a) {
+  const Val<2> s = add(add(a.v[0], a.v[1]), add(a.v[2], a.v[3]));
+  return s.x + s.y;
+}
+
+
+// A tensor's rows that a group takes: the next one to copy, and where one lies.
+struct Walk {
+  const uint8_t *at;
+  int64_t hop;
+  uint32_t low, low_hop;   // of the row that is computed on
+  __device__ Walk(const dsgd_rows_t &x, int64_t agent, int64_t first, int64_t rows, int bytes)
+      : at(static_cast<const uint8_t *>(x.at) + place(x, agent, first) * bytes), hop(rows * x.row_stride * bytes), low((uint32_t)reinterpret_cast<uintptr_t>(at)), low_hop((uint32_t)hop) {}
+  __device__ Walk(const dsgd_rows_t &x, int64_t row, int64_t rows, int64_t row_bytes)   // a kept tensor's
+      : at(static_cast<const uint8_t *>(x.at) + row * row_bytes), hop(rows * row_bytes), low(0), low_hop(0) {}
+  __device__ int pad() const { return low & 15; }
+  __device__ void next() { low += low_hop; }
+};
+
+#define CECA_TYPES                                                           \
+  const int32_t ts = TS == kAnyType ? p.stream_type : TS;                    \
+  const int32_t ta = TA == kAnyType ? p.act_type : TA;                       \
+  const int sb = ts == DSGD_BF16 ? 2 : 4, ab = ta == DSGD_BF16 ? 2 : 4
+
+template <int G, int PASSES, bool WORDS, int TS, int TA, int PARTS>
+__global__ void __launch_bounds__(G * groups_of(G), resident_block(G, PASSES)) block_kernel(const __grid_constant__ BlockArgs p) {
+  using X = Place<G, PASSES, WORDS>;
+  using L = Lay<G, PASSES, WORDS>;
+  extern __shared__ uint4 ring[];
+  __shared__ alignas(16) float sums[2][4 * (G / 32)];
+  constexpr int kGroups = groups_of(G);
+  CECA_TYPES;
+  const int rank = G == 32 ? threadIdx.x & 31 : threadIdx.x, group = G == 32 ? threadIdx.x >> 5 : 0, d = (int)p.d;
+  const int64_t agent = blockIdx.x / p.part_count, first = (blockIdx.x - agent * p.part_count) * kGroups + group, hop = (int64_t)p.part_count * kGroups;
+  constexpr bool kAny = PARTS == kAnyParts;
+  const bool y = !kAny || p.y.at != nullptr, gated = kAny ? p.gate.at != nullptr : PARTS != kPlain, u = !kAny || p.w_pre != nullptr, silu = kAny ? p.silu : PARTS == kSilu;
+  uint8_t *mine = reinterpret_cast<uint8_t *>(ring) + (size_t)group * p.stages * p.stage_bytes;
+  const uint32_t mine32 = smem_u32(mine);
+  const int off_y = p.room[0], off_g = off_y + p.room[1];
+  Walk wh(p.h, agent, first, hop, sb), wy(p.y, agent, first, hop, ab), wg(p.gate, agent, first, hop, ab);
+  const auto bring = [&](int64_t row, int stage) {
+    if (row < p.t) {
+      const uint32_t to = mine32 + stage * p.stage_bytes;
+      X::copy(to, wh.at, ts, d, rank);
+      if (y) X::copy(to + off_y, wy.at, ta, d, rank);
+      if (gated) X::copy(to + off_g, wg.at, ta, d, rank);
+    }
+    wh.at += wh.hop;
+    wy.at += wy.hop;
+    wg.at += wg.hop;
+    copies_end();
+  };
+  for (int i = 0; i + 1 < p.stages; ++i) bring(first + i * hop, i);
+  const float scale = p.scale ? load(p.scale, p.weights_type, agent * p.scale_stride) : 1.f, over_d = 1.f / (float)p.d;
+  Pairs8 wq[PASSES], wp[PASSES];   // scale w_post, w_pre
+#pragma unroll
+  for (int j = 0; j < PASSES; ++j)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const int c = L::channel(rank, j, e);
+      (e & 1 ? wq[j].v[e / 2].y : wq[j].v[e / 2].x) = y && c < d ? scale * load(p.w_post, p.weights_type, agent * p.w_post_stride + c) : 0.f;
+      (e & 1 ? wp[j].v[e / 2].y : wp[j].v[e / 2].x) = u && c < d ? load(p.w_pre, p.weights_type, agent * p.w_pre_stride + c) : 0.f;
+    }
+  const auto norm = [&](const Pairs8 *a, int turn) {
+    const auto squares = [&](float unit) {
+      Pairs8 s{};
+#pragma unroll
+      for (int j = 0; j < PASSES; ++j)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const Val<2> v = unit == 1.f ? a[j].v[k] : mul(a[j].v[k], all<2>(unit));
+          s.v[k] = fma(v, v, s.v[k]);
+        }
+      return total(s);
+    };
+    return inverse_rms(group_sum<G>(squares(1.f), sums, turn), over_d, p.eps, [&](float unit) {
+      if (G > 32) __syncthreads();
+      return group_sum<G>(squares(unit), sums, turn);
+    });
+  };
+  uint8_t *to_h = static_cast<uint8_t *>(p.h_out.at) + place(p.h_out, agent, first) * sb, *to_u = static_cast<uint8_t *>(p.u.at) + place(p.u, agent, first) * ab;
+  const int64_t hop_h = hop * p.h_out.row_stride * sb, hop_u = hop * p.u.row_stride * ab;
+  int64_t kept_at = (agent * p.t + first) * p.row_bytes;
+  float *stats = p.stats ? p.stats + 2 * (agent * p.t + first) : nullptr;
+  int stage = 0;
+  for (int64_t row = first; row < p.t; row += hop) {
+    if (p.stages > 1) bring(row + (p.stages - 1) * hop, stage == 0 ? p.stages - 1 : stage - 1);
+    else bring(row, 0);
+    copies_but(p.stages - 1);
+    if (WORDS || G == 32) __syncwarp();   // (lanes copy for one another)
+    else __syncthreads();
+    const uint8_t *at = mine + stage * p.stage_bytes;
+    stage = stage + 1 == p.stages ? 0 : stage + 1;
+    Pairs8 h[PASSES];
+    float rho = 0.f;
+#pragma unroll
+    for (int j = 0; j < PASSES; ++j) h[j] = X::read(at, wh.pad(), ts, d, rank, j);
+    if (p.h8) X::keep(p.h8 + kept_at, h, d, rank);
+    if (y) {
+      Pairs8 a[PASSES];
+#pragma unroll
+      for (int j = 0; j < PASSES; ++j) a[j] = X::read(at + off_y, wy.pad(), ta, d, rank, j);
+      rho = norm(a, 0);
+      if (p.y8) X::keep(p.y8 + kept_at, a, d, rank);
+      if (gated) {
+        Pairs8 g[PASSES];
+#pragma unroll
+        for (int j = 0; j < PASSES; ++j) g[j] = X::read(at + off_g, wg.pad(), ta, d, rank, j);
+        if (p.gate8) X::keep(p.gate8 + kept_at, g, d, rank);
+#pragma unroll
+        for (int j = 0; j < PASSES; ++j)
+#pragma unroll
+          for (int k = 0; k < 4; ++k) h[j].v[k] = fma(mul(wq[j].v[k], gates_of(g[j].v[k], silu).g), mul(a[j].v[k], all<2>(rho)), h[j].v[k]);
+      } else {
+#pragma unroll
+        for (int j = 0; j < PASSES; ++j)
+#pragma unroll
+          for (int k = 0; k < 4; ++k) h[j].v[k] = fma(wq[j].v[k], mul(a[j].v[k], all<2>(rho)), h[j].v[k]);
+      }
+#pragma unroll
+      for (int j = 0; j < PASSES; ++j) X::write(to_h, ts, h[j], d, rank, j);
+    }
+    float r = 0.f;
+    if (u) {
+      r = norm(h, 1);
+#pragma unroll
+      for (int j = 0; j < PASSES; ++j) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) h[j].v[k] = mul(mul(h[j].v[k], all<2>(r)), wp[j].v[k]);
+        X::write(to_u, ta, h[j], d, rank, j);
+      }
+    }
+    if (stats) {
+      if (rank == 0) *reinterpret_cast<float2 *>(stats) = make_float2(rho, r);
+      stats += 2 * hop;
+    }
+    to_h += hop_h;
+    to_u += hop_u;
+    kept_at += hop * p.row_bytes;
+    wh.next();
+    wy.next();
+    wg.next();
+    if (G > 32 && (!WORDS || !y || !u)) __syncthreads();   // the place is written again only when everybody has read it, and a sum's when everybody has it
+    else __syncwarp();
+  }
+  copies_but(0);
+}
+
+template <int G, int PASSES, bool WORDS, int TS, int TA, bool KEPT, int PARTS>
+__global__ void __launch_bounds__(G * groups_of(G), resident_grad(G, PASSES)) block_grad_kernel(const __grid_constant__ BlockArgs p) {
+  using X = Place<G, PASSES, WORDS>;
+  using L = Lay<G, PASSES, WORDS>;
+  extern __shared__ uint4 ring[];
+  __shared__ alignas(16) float sums[2][4 * (G / 32)];
+  constexpr int kGroups = groups_of(G);
+  CECA_TYPES;
+  const int32_t held_s = KEPT ? kKept : ts, held_a = KEPT ? kKept : ta;
+  const int rank = G == 32 ? threadIdx.x & 31 : threadIdx.x, group = G == 32 ? threadIdx.x >> 5 : 0, d = (int)p.d;
+  const int64_t agent = blockIdx.x / p.part_count, cta = blockIdx.x - agent * p.part_count;
+  const int64_t first = cta * kGroups + group, hop = (int64_t)p.part_count * kGroups;
+  constexpr bool kAny = PARTS == kAnyParts;
+  const bool y = !kAny || p.y.at != nullptr, gated = kAny ? p.gate.at != nullptr : PARTS != kPlain, u = !kAny || p.w_pre != nullptr, silu = kAny ? p.silu : PARTS == kSilu;
+  const bool past = !kAny || p.dh_out.at != nullptr;
+  uint8_t *mine = reinterpret_cast<uint8_t *>(ring) + (size_t)group * p.stages * p.stage_bytes;
+  const uint32_t mine32 = smem_u32(mine);
+  const int off_y = p.room[0], off_g = off_y + p.room[1], off_u = off_g + p.room[2], off_p = off_u + p.room[3];
+  const auto held = [&](const dsgd_rows_t &x, int bytes) {
+    return KEPT ? Walk(x, agent * p.t + first, hop, p.row_bytes) : Walk(x, agent, first, hop, bytes);
+  };
+  Walk wh = held(p.h, sb), wy = held(p.y, ab), wg = held(p.gate, ab), wu(p.du, agent, first, hop, ab), wo(p.dh_out, agent, first, hop, sb);
+  const auto bring = [&](int64_t row, int stage) {
+    if (row < p.t) {
+      const uint32_t to = mine32 + stage * p.stage_bytes;
+      X::copy(to, wh.at, held_s, d, rank);
+      if (y) X::copy(to + off_y, wy.at, held_a, d, rank);
+      if (gated) X::copy(to + off_g, wg.at, held_a, d, rank);
+      if (u) X::copy(to + off_u, wu.at, ta, d, rank);
+      if (past) X::copy(to + off_p, wo.at, ts, d, rank);
+    }
+    wh.at += wh.hop;
+    wy.at += wy.hop;
+    wg.at += wg.hop;
+    wu.at += wu.hop;
+    wo.at += wo.hop;
+    copies_end();
+  };
+  for (int i = 0; i + 1 < p.stages; ++i) bring(first + i * hop, i);
+  const float scale = p.scale ? load(p.scale, p.weights_type, agent * p.scale_stride) : 1.f, over_d = 1.f / (float)p.d;
+  Pairs8 wq[PASSES], wp[PASSES];   // scale w_post, w_pre
+  Pairs8 sum_pre[PASSES], sum_post[PASSES];
+#pragma unroll
+  for (int j = 0; j < PASSES; ++j) {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) sum_pre[j].v[k] = sum_post[j].v[k] = {0.f, 0.f};
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const int c = L::channel(rank, j, e);
+      (e & 1 ? wq[j].v[e / 2].y : wq[j].v[e / 2].x) = y && c < d ? scale * load(p.w_post, p.weights_type, agent * p.w_post_stride + c) : 0.f;
+      (e & 1 ? wp[j].v[e / 2].y : wp[j].v[e / 2].x) = u && c < d ? load(p.w_pre, p.weights_type, agent * p.w_pre_stride + c) : 0.f;
+    }
+  }
+  uint8_t *dh = static_cast<uint8_t *>(p.dh.at) + place(p.dh, agent, first) * sb, *dy = static_cast<uint8_t *>(p.dy.at) + place(p.dy, agent, first) * ab;
+  uint8_t *da = static_cast<uint8_t *>(p.dgate.at) + place(p.dgate, agent, first) * ab;
+  const int64_t hop_h = hop * p.dh.row_stride * sb, hop_y = hop * p.dy.row_stride * ab, hop_a = hop * p.dgate.row_stride * ab;
+  const float2 *stats = reinterpret_cast<const float2 *>(p.stats) + agent * p.t;
+  float2 st = first < p.t ? stats[first] : make_float2(0.f, 0.f);
+  int stage = 0, turn = 0;
+  for (int64_t row = first; row < p.t; row += hop) {
+    if (p.stages > 1) bring(row + (p.stages - 1) * hop, stage == 0 ? p.stages - 1 : stage - 1);
+    else bring(row, 0);
+    const float2 now = st;   // the next row's are on their way
+    if (row + hop < p.t) st = stats[row + hop];
+    const Val<2> rho = all<2>(now.x), r = all<2>(now.y);
+    copies_but(p.stages - 1);
+    if (WORDS || G == 32) __syncwarp();   // (lanes copy for one another)
+    else __syncthreads();
+    const uint8_t *at = mine + stage * p.stage_bytes;
+    stage = stage + 1 == p.stages ? 0 : stage + 1;
+    Pairs8 hn[PASSES], t[PASSES], yn[PASSES], g[PASSES], slope[PASSES];
+    Val<2> a{0.f, 0.f}, b{0.f, 0.f}, c{0.f, 0.f};
+#pragma unroll
+    for (int j = 0; j < PASSES; ++j) {
+      Pairs8 q{};
+      if (y) {
+        yn[j] = X::read(at + off_y, wy.pad(), held_a, d, rank, j);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          yn[j].v[k] = mul(yn[j].v[k], rho);
+          q.v[k] = mul(wq[j].v[k], yn[j].v[k]);
+        }
+        if (gated) {
+          g[j] = X::read(at + off_g, wg.pad(), held_a, d, rank, j);
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            const Gates x = gates_of(g[j].v[k], silu);
+            g[j].v[k] = x.g;
+            slope[j].v[k] = x.slope;
+            q.v[k] = mul(q.v[k], x.g);
+          }
+        }
+      }
+      if (past) {
+        t[j] = X::read(at + off_p, wo.pad(), ts, d, rank, j);
+      } else {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) t[j].v[k] = {0.f, 0.f};
+      }
+      if (u) {
+        hn[j] = X::read(at, wh.pad(), held_s, d, rank, j);
+        const Pairs8 du = X::read(at + off_u, wu.pad(), ta, d, rank, j);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          hn[j].v[k] = mul(add(hn[j].v[k], q.v[k]), r);
+          const Val<2> f = mul(wp[j].v[k], du.v[k]);
+          a = fma(hn[j].v[k], f, a);
+          t[j].v[k] = fma(r, f, t[j].v[k]);
+          c = fma(q.v[k], hn[j].v[k], c);
+          sum_pre[j].v[k] = fma(hn[j].v[k], du.v[k], sum_pre[j].v[k]);
+        }
+      }
+#pragma unroll
+      for (int k = 0; k < 4; ++k) b = fma(q.v[k], t[j].v[k], b);
+    }
+    float s[3] = {a.x + a.y, b.x + b.y, c.x + c.y};
+    group_sums<G, 3>(s, sums, turn);
+    turn ^= 1;
+    const float rm = u ? now.y * s[0] * over_d : 0.f, my = (s[1] - rm * s[2]) * over_d;
+#pragma unroll
+    for (int j = 0; j < PASSES; ++j) {
+      if (u) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) t[j].v[k] = fma(all<2>(-rm), hn[j].v[k], t[j].v[k]);
+      }
+      X::write(dh, ts, t[j], d, rank, j);
+      if (y) {
+        Pairs8 oy, oa;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          Val<2> e = mul(wq[j].v[k], t[j].v[k]), by = t[j].v[k];
+          if (gated) {
+            oa.v[k] = mul(mul(slope[j].v[k], yn[j].v[k]), e);
+            e = mul(g[j].v[k], e);
+            by = mul(g[j].v[k], by);
+          }
+          oy.v[k] = mul(rho, fma(all<2>(-my), yn[j].v[k], e));
+          sum_post[j].v[k] = fma(yn[j].v[k], by, sum_post[j].v[k]);
+        }
+        X::write(dy, ta, oy, d, rank, j);
+        if (gated) X::write(da, ta, oa, d, rank, j);
+      }
+    }
+    dh += hop_h;
+    dy += hop_y;
+    da += hop_a;
+    wh.next();
+    wy.next();
+    wg.next();
+    wu.next();
+    wo.next();
+    __syncwarp();   // (of larger groups all have met since they read the place)
+  }
+  copies_but(0);
+  follow_early();
+  // the group's sums; those of a CTA's groups are joined in their order
+  const int64_t q = agent * p.part_count + cta;
+  float *to = p.parts + 2 * q * p.d, dot = 0.f;
+#pragma unroll
+  for (int j = 0; j < PASSES; ++j)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const int c = L::channel(rank, j, e);
+      const float x = e & 1 ? sum_pre[j].v[e / 2].y : sum_pre[j].v[e / 2].x, z = e & 1 ? sum_post[j].v[e / 2].y : sum_post[j].v[e / 2].x;
+      if (c >= d) continue;
+      if (y) dot = fmaf(load(p.w_post, p.weights_type, agent * p.w_post_stride + c), z, dot);
+      if (kGroups == 1) {
+        to[c] = x;
+        to[p.d + c] = z;
+      }
+    }
+  if (kGroups > 1) {
+    __syncthreads();
+    float *all_of = reinterpret_cast<float *>(ring);   // kGroups x 2 x d
+#pragma unroll
+    for (int j = 0; j < PASSES; ++j)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const int c = L::channel(rank, j, e);
+        if (c >= d) continue;
+        all_of[(2 * group) * d + c] = e & 1 ? sum_pre[j].v[e / 2].y : sum_pre[j].v[e / 2].x;
+        all_of[(2 * group + 1) * d + c] = e & 1 ? sum_post[j].v[e / 2].y : sum_post[j].v[e / 2].x;
+      }
+    __syncthreads();
+    for (int c = threadIdx.x; c < 2 * d; c += 32 * kGroups) {
+      float x = 0.f;
+#pragma unroll
+      for (int i = 0; i < kGroups; ++i) x += all_of[2 * i * d + c];
+      to[c] = x;
+    }
+  }
+  if (p.dscale) {
+    const float s = group_sum<G>(dot, sums, turn);
+    if (rank == 0) p.scale_parts[q * kGroups + group] = s;
+  }
+}
+
+// ---------------------------------------------------------------------------------------------- launches
+
+constexpr int kMostShared = 220 << 10;
+
+template <int G, int PASSES, bool WORDS, int TS, int TA, int PARTS> cudaError_t launch_block(BlockArgs p, cudaStream_t s) {
+  static std::atomic<uint64_t> done{0};
+  using X = Place<G, PASSES, WORDS>;
+  auto kernel = block_kernel<G, PASSES, WORDS, TS, TA, PARTS>;
+  constexpr int kGroups = groups_of(G), kThreads = G * kGroups;
+  const cudaError_t e = set_max_shared_once(reinterpret_cast<const void *>(kernel), kMostShared, &done);
+  if (e != cudaSuccess) return e;
+  p.room[0] = X::room(p.d, p.stream_type);
+  p.room[1] = p.y.at ? X::room(p.d, p.act_type) : 0;
+  p.room[2] = p.gate.at ? X::room(p.d, p.act_type) : 0;
+  p.stage_bytes = p.room[0] + p.room[1] + p.room[2];
+  const int64_t resident = resident_block(G, PASSES);
+  p.stages = (int32_t)std::max<int64_t>(1, std::min<int64_t>(4, (int64_t)(200 << 10) / (resident * kGroups * p.stage_bytes)));
+  const int64_t bytes = (int64_t)p.stages * p.stage_bytes * kGroups;
+  if (bytes > kMostShared) return cudaErrorInvalidConfiguration;
+  p.part_count = (int32_t)std::max<int64_t>(1, std::min((int64_t)sm_count() * resident / p.n, ceil_div(p.t, kGroups)));
+  kernel<<<(unsigned)(p.n * p.part_count), kThreads, (size_t)bytes, s>>>(p);
+  return cudaGetLastError();
+}
+
+template <int G, int PASSES, bool WORDS, int TS, int TA, bool KEPT, int PARTS> cudaError_t launch_block_grad(BlockArgs p, cudaStream_t s) {
+  static std::atomic<uint64_t> done{0};
+  using X = Place<G, PASSES, WORDS>;
+  auto kernel = block_grad_kernel<G, PASSES, WORDS, TS, TA, KEPT, PARTS>;
+  constexpr int kGroups = groups_of(G), kThreads = G * kGroups;
+  cudaError_t e = set_max_shared_once(reinterpret_cast<const void *>(kernel), kMostShared, &done);
+  if (e != cudaSuccess) return e;
+  p.room[0] = X::room(p.d, KEPT ? kKept : p.stream_type);
+  p.room[1] = p.y.at ? X::room(p.d, KEPT ? kKept : p.act_type) : 0;
+  p.room[2] = p.gate.at ? X::room(p.d, KEPT ? kKept : p.act_type) : 0;
+  p.room[3] = p.w_pre ? X::room(p.d, p.act_type) : 0;
+  p.room[4] = p.dh_out.at ? X::room(p.d, p.stream_type) : 0;
+  p.stage_bytes = p.room[0] + p.room[1] + p.room[2] + p.room[3] + p.room[4];
+  p.stages = (int32_t)std::max<int64_t>(1, std::min<int64_t>(4, (int64_t)(200 << 10) / (resident_grad(G, PASSES) * kGroups * p.stage_bytes)));
+  const int64_t bytes = std::max((int64_t)p.stages * p.stage_bytes * kGroups, kGroups > 1 ? kGroups * 8 * p.d : 0);
+  if (bytes > kMostShared) return cudaErrorInvalidConfiguration;
+  p.part_count = (int32_t)block_grad_parts(p.n, p.t, p.d);
+  p.scale_count = p.part_count * kGroups;
+  p.parts = reinterpret_cast<float *>(p.means);   // the workspace
+  p.scale_parts = p.parts + (size_t)p.n * p.part_count * 2 * p.d;
+  kernel<<<(unsigned)(p.n * p.part_count), kThreads, (size_t)bytes, s>>>(p);
+  e = cudaGetLastError();
+  return e == cudaSuccess ? finish_block_grad(p, s) : e;
+}
+
+template <bool WORDS, int TS, int TA> cudaError_t launch_rows(const BlockArgs &p, bool grad, cudaStream_t s) {
+  const auto with = [&](auto widest, auto parts) {
+    constexpr Shape f = shape_of(decltype(widest)::value), g = grad_shape_of(decltype(widest)::value);
+    constexpr int PARTS = decltype(parts)::value;
+    if (!grad) return launch_block<f.group, f.passes, WORDS, TS, TA, PARTS>(p, s);
+    return p.kept ? launch_block_grad<g.group, g.passes, WORDS, TS, TA, true, PARTS>(p, s) : launch_block_grad<g.group, g.passes, WORDS, TS, TA, false, PARTS>(p, s);
+  };
+  const auto by = [&](auto widest) {
+    if constexpr (WORDS) {
+      if (p.y.at && p.w_pre && (!grad || p.dh_out.at)) {
+        if (!p.gate.at) return with(widest, std::integral_constant<int, kPlain>());
+        return p.silu ? with(widest, std::integral_constant<int, kSilu>()) : with(widest, std::integral_constant<int, kSigmoid>());
+      }
+    }
+    return with(widest, std::integral_constant<int, kAnyParts>());
+  };
+  if (p.d <= 256) return by(std::integral_constant<int, 256>());
+  if (p.d <= 512) return by(std::integral_constant<int, 512>());
+  if (p.d <= 1024) return by(std::integral_constant<int, 1024>());
+  if (p.d <= 2048) return by(std::integral_constant<int, 2048>());
+  if (p.d <= 4096) return by(std::integral_constant<int, 4096>());
+  return by(std::integral_constant<int, 8192>());
+}
+
+}  // namespace ceca
