@@ -55,9 +55,9 @@ struct Pairs8 {
 template <int G, int PASSES, bool WORDS> struct Place {
   using L = Lay<G, PASSES, WORDS>;
   // types: DSGD_F32, DSGD_BF16, kKept
-  static int room(int64_t d, int32_t type) {
+  __host__ __device__ static constexpr int room(int64_t d, int32_t type) {
     if (type == kKept) return WORDS ? 12 * G * PASSES : (int)kept_row_bytes(d);
-    return WORDS ? 16 * G * PASSES * (type == DSGD_BF16 ? 1 : 2) : (int)((d * type_bytes(type) + 47) / 16 * 16);
+    return WORDS ? 16 * G * PASSES * (type == DSGD_BF16 ? 1 : 2) : (int)((d * (type == DSGD_BF16 ? 2 : 4) + 47) / 16 * 16);
   }
   __device__ static void copy(uint32_t to, const uint8_t *from, int32_t type, int d, int rank) {
     if (WORDS) {
@@ -224,41 +224,42 @@ template <int G, int PASSES, bool WORDS> struct Place {
   }
 };
 
-// The sums over a group of N numbers a thread, in one order, the same on all its threads.  `turn` says which of two places is used: consecutive
+// The sum over a group, in one order, the same on all its threads.  `turn` says which of two places is used: consecutive
 // sums take the other one, so that one barrier is enough.
-template <int G, int N> __device__ __forceinline__ void group_sums(float (&x)[N], float (*place)[4 * (G / 32)], int turn) {
+template <int G> __device__ __forceinline__ float group_sum(float x, float (*place)[4 * (G / 32)], int turn) {
 #pragma unroll
-  for (int o = 16; o; o >>= 1)
-#pragma unroll
-    for (int i = 0; i < N; ++i) x[i] += __shfl_xor_sync(0xffffffffu, x[i], o);
-  if (G == 32) return;
+  for (int o = 16; o; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
+  if (G == 32) return x;
   constexpr int W = G / 32;
   const int lane = threadIdx.x & 31;
-  if (lane == 0) {
-    if (N == 1) place[turn][threadIdx.x >> 5] = x[0];
-    else *reinterpret_cast<float4 *>(place[turn] + 4 * (threadIdx.x >> 5)) = make_float4(x[0], x[1 % N], x[2 % N], 0.f);
-  }
+  if (lane == 0) place[turn][threadIdx.x >> 5] = x;
   __syncthreads();
-  // each lane reads one warp's, and the warps' are summed as the lanes' were
-  if (N == 1) {
-    x[0] = place[turn][lane % W];
+  x = place[turn][lane % W];   // each lane reads one warp's, and the warps' are summed as the lanes' were
 #pragma unroll
-    for (int o = W / 2; o; o >>= 1) x[0] += __shfl_xor_sync(0xffffffffu, x[0], o);
-  } else {
-    const float4 v = *reinterpret_cast<const float4 *>(place[turn] + 4 * (lane % W));
-    x[0] = v.x;
-    x[1 % N] = v.y;
-    x[2 % N] = v.z;
-#pragma unroll
-    for (int o = W / 2; o; o >>= 1)
-#pragma unroll
-      for (int i = 0; i < N; ++i) x[i] += __shfl_xor_sync(0xffffffffu, x[i], o);
-  }
+  for (int o = W / 2; o; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
+  return x;
 }
-template <int G> __device__ __forceinline__ float group_sum(float x, float (*place)[4 * (G / 32)], int turn) {
-  float v[1] = {x};
-  group_sums<G, 1>(v, place, turn);
-  return v[0];
+// Three sums at once: lanes first share out the numbers (x to lanes 0 to 7, y to 8 to 15, z to 16 to 23; 24 to 31 have a zero), so that most steps move one.
+template <int G> __device__ __forceinline__ float3 group_sums(float3 v, float (*place)[4 * (G / 32)], int turn) {
+  const int lane = threadIdx.x & 31;
+  const bool upper = lane & 16, odd = lane & 8;
+  const float a = __shfl_xor_sync(0xffffffffu, upper ? v.x : v.z, 16), b = __shfl_xor_sync(0xffffffffu, upper ? v.y : 0.f, 16);
+  const float p = (upper ? v.z : v.x) + a, q = upper ? 0.f : v.y + b;
+  float x = (odd ? q : p) + __shfl_xor_sync(0xffffffffu, odd ? p : q, 8);
+#pragma unroll
+  for (int o = 4; o; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
+  if (G > 32) {
+    constexpr int W = G / 32;
+    if ((lane & 7) == 0) place[turn][4 * (threadIdx.x >> 5) + lane / 8] = x;
+    __syncthreads();
+    // lane 8 n + w reads number n of warp w (of 16 warps two), and the warps' are summed as the lanes' were
+    const int w = lane & 7;
+    x = place[turn][4 * (w % W) + lane / 8];
+    if (W > 8) x += place[turn][4 * (8 + w) + lane / 8];
+#pragma unroll
+    for (int o = (W < 8 ? W : 8) / 2; o; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
+  }
+  return make_float3(__shfl_sync(0xffffffffu, x, 0), __shfl_sync(0xffffffffu, x, 8), __shfl_sync(0xffffffffu, x, 16));
 }
 
 __device__ __forceinline__ float total(const Pairs8 &a) {
@@ -280,6 +281,9 @@ struct Walk {
   __device__ void next() { low += low_hop; }
 };
 
+// Each warp's copy of a row's two statistics, in words of 16 bytes.
+__host__ __device__ constexpr int stats_room(int group) { return group == 32 ? 16 : group / 4; }
+
 #define CECA_TYPES                                                           \
   const int32_t ts = TS == kAnyType ? p.stream_type : TS;                    \
   const int32_t ta = TA == kAnyType ? p.act_type : TA;                       \
@@ -297,13 +301,17 @@ __global__ void __launch_bounds__(G * groups_of(G), resident_block(G, PASSES)) b
   const int64_t agent = blockIdx.x / p.part_count, first = (blockIdx.x - agent * p.part_count) * kGroups + group, hop = (int64_t)p.part_count * kGroups;
   constexpr bool kAny = PARTS == kAnyParts;
   const bool y = !kAny || p.y.at != nullptr, gated = kAny ? p.gate.at != nullptr : PARTS != kPlain, u = !kAny || p.w_pre != nullptr, silu = kAny ? p.silu : PARTS == kSilu;
-  uint8_t *mine = reinterpret_cast<uint8_t *>(ring) + (size_t)group * p.stages * p.stage_bytes;
+  // a row's places in a stage of the ring, where they can be known by now
+  const auto room = [&](int i, int32_t type, bool there) { return WORDS && !kAny ? there ? X::room(0, type) : 0 : p.room[i]; };
+  const int off_y = room(0, ts, true), off_g = off_y + room(1, ta, y), stage_bytes = off_g + room(2, ta, gated);
+  uint8_t *mine = reinterpret_cast<uint8_t *>(ring) + (size_t)group * p.stages * stage_bytes;
   const uint32_t mine32 = smem_u32(mine);
-  const int off_y = p.room[0], off_g = off_y + p.room[1];
   Walk wh(p.h, agent, first, hop, sb), wy(p.y, agent, first, hop, ab), wg(p.gate, agent, first, hop, ab);
-  const auto bring = [&](int64_t row, int stage) {
-    if (row < p.t) {
-      const uint32_t to = mine32 + stage * p.stage_bytes;
+  const int rows = first < p.t ? (int)((p.t - 1 - first) / hop) + 1 : 0, ring_bytes = p.stages * stage_bytes;
+  int fill = 0, left = rows;   // the place that is filled next, the rows that are not on their way
+  const auto bring = [&]() {
+    if (--left >= 0) {
+      const uint32_t to = mine32 + fill;
       X::copy(to, wh.at, ts, d, rank);
       if (y) X::copy(to + off_y, wy.at, ta, d, rank);
       if (gated) X::copy(to + off_g, wg.at, ta, d, rank);
@@ -311,9 +319,11 @@ __global__ void __launch_bounds__(G * groups_of(G), resident_block(G, PASSES)) b
     wh.at += wh.hop;
     wy.at += wy.hop;
     wg.at += wg.hop;
+    fill += stage_bytes;
+    if (fill == ring_bytes) fill = 0;
     copies_end();
   };
-  for (int i = 0; i + 1 < p.stages; ++i) bring(first + i * hop, i);
+  for (int i = 0; i + 1 < p.stages; ++i) bring();
   const float scale = p.scale ? load(p.scale, p.weights_type, agent * p.scale_stride) : 1.f, over_d = 1.f / (float)p.d;
   Pairs8 wq[PASSES], wp[PASSES];   // scale w_post, w_pre
 #pragma unroll
@@ -345,15 +355,15 @@ __global__ void __launch_bounds__(G * groups_of(G), resident_block(G, PASSES)) b
   const int64_t hop_h = hop * p.h_out.row_stride * sb, hop_u = hop * p.u.row_stride * ab;
   int64_t kept_at = (agent * p.t + first) * p.row_bytes;
   float *stats = p.stats ? p.stats + 2 * (agent * p.t + first) : nullptr;
-  int stage = 0;
-  for (int64_t row = first; row < p.t; row += hop) {
-    if (p.stages > 1) bring(row + (p.stages - 1) * hop, stage == 0 ? p.stages - 1 : stage - 1);
-    else bring(row, 0);
+  int from = 0;
+  for (int i = 0; i < rows; ++i) {
+    bring();
     copies_but(p.stages - 1);
     if (WORDS || G == 32) __syncwarp();   // (lanes copy for one another)
     else __syncthreads();
-    const uint8_t *at = mine + stage * p.stage_bytes;
-    stage = stage + 1 == p.stages ? 0 : stage + 1;
+    const uint8_t *at = mine + from;
+    from += stage_bytes;
+    if (from == ring_bytes) from = 0;
     Pairs8 h[PASSES];
     float rho = 0.f;
 #pragma unroll
@@ -424,16 +434,22 @@ __global__ void __launch_bounds__(G * groups_of(G), resident_grad(G, PASSES)) bl
   constexpr bool kAny = PARTS == kAnyParts;
   const bool y = !kAny || p.y.at != nullptr, gated = kAny ? p.gate.at != nullptr : PARTS != kPlain, u = !kAny || p.w_pre != nullptr, silu = kAny ? p.silu : PARTS == kSilu;
   const bool past = !kAny || p.dh_out.at != nullptr;
-  uint8_t *mine = reinterpret_cast<uint8_t *>(ring) + (size_t)group * p.stages * p.stage_bytes;
+  const auto room = [&](int i, int32_t type, bool there) { return WORDS && !kAny ? there ? X::room(0, type) : 0 : p.room[i]; };
+  const int off_y = room(0, held_s, true), off_g = off_y + room(1, held_a, y), off_u = off_g + room(2, held_a, gated), off_p = off_u + room(3, ta, u),
+            off_s = off_p + room(4, ts, past), stage_bytes = off_s + stats_room(G);
+  uint8_t *mine = reinterpret_cast<uint8_t *>(ring) + (size_t)group * p.stages * stage_bytes;
   const uint32_t mine32 = smem_u32(mine);
-  const int off_y = p.room[0], off_g = off_y + p.room[1], off_u = off_g + p.room[2], off_p = off_u + p.room[3];
   const auto held = [&](const dsgd_rows_t &x, int bytes) {
     return KEPT ? Walk(x, agent * p.t + first, hop, p.row_bytes) : Walk(x, agent, first, hop, bytes);
   };
   Walk wh = held(p.h, sb), wy = held(p.y, ab), wg = held(p.gate, ab), wu(p.du, agent, first, hop, ab), wo(p.dh_out, agent, first, hop, sb);
-  const auto bring = [&](int64_t row, int stage) {
-    if (row < p.t) {
-      const uint32_t to = mine32 + stage * p.stage_bytes;
+  const int rows = first < p.t ? (int)((p.t - 1 - first) / hop) + 1 : 0, ring_bytes = p.stages * stage_bytes;
+  int fill = 0, left = rows;   // the place that is filled next, the rows that are not on their way
+  const float *stats = p.stats + 2 * (agent * p.t + first);
+  const auto bring = [&]() {
+    if (--left >= 0) {
+      const uint32_t to = mine32 + fill;
+      if ((threadIdx.x & 31) == 0) copy_8(to + off_s + rank / 32 * 8, stats);   // each warp its own
       X::copy(to, wh.at, held_s, d, rank);
       if (y) X::copy(to + off_y, wy.at, held_a, d, rank);
       if (gated) X::copy(to + off_g, wg.at, held_a, d, rank);
@@ -445,9 +461,12 @@ __global__ void __launch_bounds__(G * groups_of(G), resident_grad(G, PASSES)) bl
     wg.at += wg.hop;
     wu.at += wu.hop;
     wo.at += wo.hop;
+    stats += 2 * hop;
+    fill += stage_bytes;
+    if (fill == ring_bytes) fill = 0;
     copies_end();
   };
-  for (int i = 0; i + 1 < p.stages; ++i) bring(first + i * hop, i);
+  for (int i = 0; i + 1 < p.stages; ++i) bring();
   const float scale = p.scale ? load(p.scale, p.weights_type, agent * p.scale_stride) : 1.f, over_d = 1.f / (float)p.d;
   Pairs8 wq[PASSES], wp[PASSES];   // scale w_post, w_pre
   Pairs8 sum_pre[PASSES], sum_post[PASSES];
@@ -465,20 +484,17 @@ __global__ void __launch_bounds__(G * groups_of(G), resident_grad(G, PASSES)) bl
   uint8_t *dh = static_cast<uint8_t *>(p.dh.at) + place(p.dh, agent, first) * sb, *dy = static_cast<uint8_t *>(p.dy.at) + place(p.dy, agent, first) * ab;
   uint8_t *da = static_cast<uint8_t *>(p.dgate.at) + place(p.dgate, agent, first) * ab;
   const int64_t hop_h = hop * p.dh.row_stride * sb, hop_y = hop * p.dy.row_stride * ab, hop_a = hop * p.dgate.row_stride * ab;
-  const float2 *stats = reinterpret_cast<const float2 *>(p.stats) + agent * p.t;
-  float2 st = first < p.t ? stats[first] : make_float2(0.f, 0.f);
-  int stage = 0, turn = 0;
-  for (int64_t row = first; row < p.t; row += hop) {
-    if (p.stages > 1) bring(row + (p.stages - 1) * hop, stage == 0 ? p.stages - 1 : stage - 1);
-    else bring(row, 0);
-    const float2 now = st;   // the next row's are on their way
-    if (row + hop < p.t) st = stats[row + hop];
-    const Val<2> rho = all<2>(now.x), r = all<2>(now.y);
+  int from = 0, turn = 0;
+  for (int i = 0; i < rows; ++i) {
+    bring();
     copies_but(p.stages - 1);
     if (WORDS || G == 32) __syncwarp();   // (lanes copy for one another)
     else __syncthreads();
-    const uint8_t *at = mine + stage * p.stage_bytes;
-    stage = stage + 1 == p.stages ? 0 : stage + 1;
+    const uint8_t *at = mine + from;
+    from += stage_bytes;
+    if (from == ring_bytes) from = 0;
+    const float2 now = *reinterpret_cast<const float2 *>(at + off_s + rank / 32 * 8);
+    const Val<2> rho = all<2>(now.x), r = all<2>(now.y);
     Pairs8 hn[PASSES], t[PASSES], yn[PASSES], g[PASSES], slope[PASSES];
     Val<2> a{0.f, 0.f}, b{0.f, 0.f}, c{0.f, 0.f};
 #pragma unroll
@@ -524,10 +540,9 @@ __global__ void __launch_bounds__(G * groups_of(G), resident_grad(G, PASSES)) bl
 #pragma unroll
       for (int k = 0; k < 4; ++k) b = fma(q.v[k], t[j].v[k], b);
     }
-    float s[3] = {a.x + a.y, b.x + b.y, c.x + c.y};
-    group_sums<G, 3>(s, sums, turn);
+    const float3 s = group_sums<G>(make_float3(a.x + a.y, b.x + b.y, c.x + c.y), sums, turn);
     turn ^= 1;
-    const float rm = u ? now.y * s[0] * over_d : 0.f, my = (s[1] - rm * s[2]) * over_d;
+    const float rm = u ? now.y * s.x * over_d : 0.f, my = (s.y - rm * s.z) * over_d;
 #pragma unroll
     for (int j = 0; j < PASSES; ++j) {
       if (u) {
@@ -601,7 +616,7 @@ __global__ void __launch_bounds__(G * groups_of(G), resident_grad(G, PASSES)) bl
     }
   }
   if (p.dscale) {
-    const float s = group_sum<G>(dot, sums, turn);
+    const float s = group_sum<G>(dot, sums, turn);   // (the other place than the last row's)
     if (rank == 0) p.scale_parts[q * kGroups + group] = s;
   }
 }
@@ -642,7 +657,7 @@ template <int G, int PASSES, bool WORDS, int TS, int TA, bool KEPT, int PARTS> c
   p.room[2] = p.gate.at ? X::room(p.d, KEPT ? kKept : p.act_type) : 0;
   p.room[3] = p.w_pre ? X::room(p.d, p.act_type) : 0;
   p.room[4] = p.dh_out.at ? X::room(p.d, p.stream_type) : 0;
-  p.stage_bytes = p.room[0] + p.room[1] + p.room[2] + p.room[3] + p.room[4];
+  p.stage_bytes = p.room[0] + p.room[1] + p.room[2] + p.room[3] + p.room[4] + stats_room(G);
   p.stages = (int32_t)std::max<int64_t>(1, std::min<int64_t>(4, (int64_t)(200 << 10) / (resident_grad(G, PASSES) * kGroups * p.stage_bytes)));
   const int64_t bytes = std::max((int64_t)p.stages * p.stage_bytes * kGroups, kGroups > 1 ? kGroups * 8 * p.d : 0);
   if (bytes > kMostShared) return cudaErrorInvalidConfiguration;

@@ -6,8 +6,8 @@ namespace ceca {
 
 constexpr int kBlock8 = 32;
 
-__host__ __device__ inline int64_t blocks8(int64_t d) { return (d + kBlock8 - 1) / kBlock8; }
-__host__ __device__ inline int64_t kept_row_bytes(int64_t d) { return (d + blocks8(d) + 15) / 16 * 16; }
+__host__ __device__ constexpr int64_t blocks8(int64_t d) { return (d + kBlock8 - 1) / kBlock8; }
+__host__ __device__ constexpr int64_t kept_row_bytes(int64_t d) { return (d + blocks8(d) + 15) / 16 * 16; }
 
 #ifdef __CUDACC__
 // The exponent byte of a block whose largest magnitude has these bits (the sign taken off; a NaN is above all): 255 for one that
