@@ -193,8 +193,9 @@ __global__ void __launch_bounds__(kThreads) wide_grad_kernel(const BlockArgs p) 
 }
 
 // The parts of the weights' gradients, in the order of the rows.
-__global__ void __launch_bounds__(kThreads) finish_kernel(const BlockArgs p) {
-  __shared__ float halves[2][kWarps][32];
+constexpr int kJoiners = 32;   // warps: as many parts are on their way at a time, and more by unrolling
+__global__ void __launch_bounds__(32 * kJoiners) finish_kernel(const BlockArgs p) {
+  __shared__ float halves[2][kJoiners][32];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int64_t agent = blockIdx.y, c = (int64_t)blockIdx.x * 32 + lane;
   const float scale = p.scale ? load(p.scale, p.weights_type, agent * p.scale_stride) : 1.f;
@@ -202,7 +203,7 @@ __global__ void __launch_bounds__(kThreads) finish_kernel(const BlockArgs p) {
   after_first();
   if (c < p.d)
 #pragma unroll 8
-    for (int q = warp; q < p.part_count; q += kWarps) {
+    for (int q = warp; q < p.part_count; q += kJoiners) {
       const float *part = p.parts + ((agent * p.part_count + q) * 2) * p.d + c;
       a += part[0];
       b += part[p.d];
@@ -217,7 +218,7 @@ __global__ void __launch_bounds__(kThreads) finish_kernel(const BlockArgs p) {
   if (warp < 2 && c < p.d) {
     float s = 0.f;
 #pragma unroll
-    for (int i = 0; i < kWarps; ++i) s += halves[warp][i][lane];
+    for (int i = 0; i < kJoiners; ++i) s += halves[warp][i][lane];
     if (warp == 0 && p.dw_pre) put(p.dw_pre, agent * p.dw_pre_stride + c, s);
     if (warp == 1 && p.dw_post) put(p.dw_post, agent * p.dw_post_stride + c, scale * s);
   }
@@ -273,7 +274,7 @@ int64_t block_grad_parts(int64_t n, int64_t t, int64_t d) {
 }
 
 cudaError_t finish_block_grad(const BlockArgs &p, cudaStream_t s) {
-  return launch_after(finish_kernel, p, dim3((unsigned)ceil_div(p.d, 32), (unsigned)p.n), kThreads, 0, s);
+  return launch_after(finish_kernel, p, dim3((unsigned)ceil_div(p.d, 32), (unsigned)p.n), 32 * kJoiners, 0, s);
 }
 
 }  // namespace ceca

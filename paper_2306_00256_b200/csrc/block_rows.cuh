@@ -39,45 +39,76 @@ __device__ __forceinline__ void copies_but(int behind) {   // waits for all grou
   }
 }
 
-// The channels of a thread of a group of G: with WORDS 8 neighbours (channel 8 (rank + G j) on, in 16-byte words), else every G-th one.
-// They are computed on in pairs.  PASSES: eights a thread.
-template <int G, int PASSES, bool WORDS> struct Lay {
-  static constexpr int kPairs = 4 * PASSES;
-  __device__ static int channel(int rank, int j, int e) { return WORDS ? 8 * (rank + G * j) + e : rank + G * (8 * j + e); }
-};
+// The channels of a thread of a group of G, eight in each of its passes: V = 8: eight neighbours, a 16-byte word of bf16; V = 4: twice four, words of fp32;
+// V = 1: every G-th one, for rows on any boundary.  They are computed on in pairs.
+template <int G, int V> __device__ __forceinline__ int channel(int rank, int j, int e) {
+  return V == 8 ? 8 * (rank + G * j) + e : V == 4 ? 4 * (rank + G * (2 * j + e / 4)) + e % 4 : rank + G * (8 * j + e);
+}
 struct Pairs8 {
   Val<2> v[4];
 };
+// bytes `from` and from + 1 of w, two whole numbers: (x + 128) + 2^23, less 2^23 + 128
+__device__ __forceinline__ Val<2> whole_numbers(uint32_t w, int from) {
+  w ^= 0x80808080u;
+  const Val<2> v = {__uint_as_float(__byte_perm(w, 0x4b000000u, 0x7650u | from)), __uint_as_float(__byte_perm(w, 0x4b000000u, 0x7650u | (from + 1)))};
+  return add(v, all<2>(-8388736.f));
+}
+// four of them, of x: rounded to the nearest in the low bits of a sum with 1.5 2^23
+__device__ __forceinline__ uint32_t hold_four(Val<2> x, Val<2> y, Val<2> by) {
+  const auto low = [](float v) { return __float_as_uint(fminf(fmaxf(v, -127.f), 127.f) + 12582912.f); };
+  x = mul(x, by);
+  y = mul(y, by);
+  return __byte_perm(__byte_perm(low(x.x), low(x.y), 0x0040), __byte_perm(low(y.x), low(y.y), 0x0040), 0x5410);
+}
+__device__ __forceinline__ uint32_t greatest(uint32_t top, Val<2> x) { return max(top, max(magnitude(x.x), magnitude(x.y))); }
+__device__ __forceinline__ uint32_t pack_bf16(Val<2> x) {
+  const __nv_bfloat162 h = __floats2bfloat162_rn(x.x, x.y);
+  return *reinterpret_cast<const uint32_t *>(&h);
+}
+__device__ __forceinline__ Val<2> unpack_bf16(uint32_t x) { return {__uint_as_float(x << 16), __uint_as_float(x & 0xffff0000u)}; }
 
-// A place in shared memory for a row of a tensor, or for a kept row, and its copy and reading.  With WORDS each warp copies what it will
-// read; else the group copies the 16-byte words that the row touches (of the first and last one the bytes inside the row count), and
-// must meet between copying and reading.
-template <int G, int PASSES, bool WORDS> struct Place {
-  using L = Lay<G, PASSES, WORDS>;
+// A place in shared memory for a row of a tensor, or for a kept row, and its copy and reading.  V = 8 and 4: each warp copies what it will read, in
+// whole sectors.  V = 1: the group copies the 16-byte words that the row touches (of the first and last one the bytes inside the row
+// count), and must meet between copying and reading.
+template <int G, int PASSES, int V> struct Place {
+  static constexpr int kEights = G * PASSES;
   // types: DSGD_F32, DSGD_BF16, kKept
   __host__ __device__ static constexpr int room(int64_t d, int32_t type) {
-    if (type == kKept) return WORDS ? 12 * G * PASSES : (int)kept_row_bytes(d);
-    return WORDS ? 16 * G * PASSES * (type == DSGD_BF16 ? 1 : 2) : (int)((d * (type == DSGD_BF16 ? 2 : 4) + 47) / 16 * 16);
+    if (V == 1) return type == kKept ? (int)kept_row_bytes(d) : (int)((d * (type == DSGD_BF16 ? 2 : 4) + 47) / 16 * 16);
+    return type == kKept ? (V == 8 ? 12 : 9) * kEights : (type == DSGD_BF16 ? 16 : 32) * kEights;
   }
   __device__ static void copy(uint32_t to, const uint8_t *from, int32_t type, int d, int rank) {
-    if (WORDS) {
+    const int lane = rank & 31;
+    if (V == 8) {   // bf16, or kept: its exponents' words behind the whole numbers, one for each thread
 #pragma unroll
       for (int j = 0; j < PASSES; ++j) {
         const int at = rank + G * j;
         if (8 * at >= d) continue;
         if (type == kKept) {
           copy_8(to + 8 * at, from + 8 * at);
-          copy_4(to + 8 * G * PASSES + 4 * at, from + ((d + at / 4) & ~3));
-        } else if (type == DSGD_BF16) {
+          copy_4(to + 8 * kEights + 4 * at, from + ((d + at / 4) & ~3));
+        } else {
           copy_16(to + 16 * at, from + 16 * at);
-        } else if ((at ^ 1) * 8 >= d) {   // (the last one, alone)
-          copy_16(to + 16 * at, from + 32 * at);
-          copy_16(to + 16 * (G * PASSES + (at ^ 1)), from + 32 * at + 16);
-        } else {   // two lanes copy each one's 32 bytes together, so that every copy touches whole sectors
-          const int odd = at & 1, even = at ^ odd;
-          copy_16(to + 16 * (odd * G * PASSES + (even ^ odd)), from + 32 * even + 16 * odd);
-          copy_16(to + 16 * (odd * G * PASSES + ((even + 1) ^ odd)), from + 32 * even + 32 + 16 * odd);
         }
+      }
+    } else if (V == 4) {   // as it lies in memory; a warp's channels of a half pass are 128 neighbours
+      const int c0 = 4 * (rank - lane);
+      if (type == DSGD_F32) {
+#pragma unroll
+        for (int k = 0; k < 2 * PASSES; ++k) {
+          const int c = c0 + 4 * (G * k + lane);
+          if (c < d) copy_16(to + 4 * c, from + 4 * c);
+        }
+      } else if (type == DSGD_BF16) {
+#pragma unroll
+        for (int j = 0; j < PASSES; ++j) {
+          const int c = c0 + 4 * G * (2 * j + lane / 16) + 8 * (lane & 15);
+          if (c < d) copy_16(to + 2 * c, from + 2 * c);
+        }
+      } else {
+        const int c = c0 + 4 * G * (lane / 8) + 16 * (lane & 7), e = c0 / kBlock8 + G / 8 * lane;   // (the last copy may take exponents with it)
+        if (lane < 16 * PASSES && c < d) copy_16(to + c, from + c);
+        if (lane < 2 * PASSES && e * kBlock8 < d) copy_4(to + d + e, from + d + e);
       }
     } else {
       const int pad = (int)(reinterpret_cast<uintptr_t>(from) & 15), end = pad + (type == kKept ? (int)kept_row_bytes(d) : d * (type == DSGD_BF16 ? 2 : 4));
@@ -87,37 +118,46 @@ template <int G, int PASSES, bool WORDS> struct Place {
   }
   // the eight channels of pass j; zeros outside the row
   __device__ static Pairs8 read(const uint8_t *place, int pad, int32_t type, int d, int rank, int j) {
-    Pairs8 r;
-    if (WORDS) {
+    Pairs8 r{};
+    if (V == 8) {
       const int at = rank + G * j;
-      if (8 * at >= d) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) r.v[i] = {0.f, 0.f};
-      } else if (type == kKept) {
+      if (8 * at >= d) return r;
+      if (type == kKept) {
         const uint2 q = reinterpret_cast<const uint2 *>(place)[at];
-        const uint32_t e = reinterpret_cast<const uint32_t *>(place + 8 * G * PASSES)[at] >> 8 * ((d + at / 4) & 3) & 255u;
+        const uint32_t e = reinterpret_cast<const uint32_t *>(place + 8 * kEights)[at] >> 8 * ((d + at / 4) & 3) & 255u;
         const Val<2> step = all<2>(step8(e));
 #pragma unroll
-        for (int i = 0; i < 4; ++i) r.v[i] = mul(bytes8(i < 2 ? q.x : q.y, 2 * (i & 1)), step);
-      } else if (type == DSGD_BF16) {
+        for (int i = 0; i < 4; ++i) r.v[i] = mul(whole_numbers(i < 2 ? q.x : q.y, 2 * (i & 1)), step);
+      } else {
         const uint4 w = reinterpret_cast<const uint4 *>(place)[at];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const uint32_t x = (&w.x)[i];
-          r.v[i] = {__uint_as_float(x << 16), __uint_as_float(x & 0xffff0000u)};
+        for (int i = 0; i < 4; ++i) r.v[i] = unpack_bf16((&w.x)[i]);
+      }
+    } else if (V == 4) {
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        const int at = rank + G * (2 * j + k);
+        if (4 * at >= d) continue;
+        if (type == kKept) {
+          const uint32_t q = reinterpret_cast<const uint32_t *>(place)[at];
+          const Val<2> step = all<2>(step8(place[d + at / 8]));
+          r.v[2 * k] = mul(whole_numbers(q, 0), step);
+          r.v[2 * k + 1] = mul(whole_numbers(q, 2), step);
+        } else if (type == DSGD_BF16) {
+          const uint2 w = reinterpret_cast<const uint2 *>(place)[at];
+          r.v[2 * k] = unpack_bf16(w.x);
+          r.v[2 * k + 1] = unpack_bf16(w.y);
+        } else {
+          const float4 a = reinterpret_cast<const float4 *>(place)[at];
+          r.v[2 * k] = {a.x, a.y};
+          r.v[2 * k + 1] = {a.z, a.w};
         }
-      } else {
-        const float4 a = reinterpret_cast<const float4 *>(place)[at], b = reinterpret_cast<const float4 *>(place)[G * PASSES + (at ^ 1)];
-        r.v[0] = {a.x, a.y};
-        r.v[1] = {a.z, a.w};
-        r.v[2] = {b.x, b.y};
-        r.v[3] = {b.z, b.w};
       }
     } else {
       place += pad;
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        const int c = L::channel(rank, j, e);
+        const int c = channel<G, V>(rank, j, e);
         float x = 0.f;
         if (c < d) {
           if (type == kKept) x = (float)(int8_t)place[c] * step8(place[d + c / kBlock8]);
@@ -128,51 +168,24 @@ template <int G, int PASSES, bool WORDS> struct Place {
     }
     return r;
   }
-  // bytes `from` and from + 1 of w, two whole numbers
-  __device__ static Val<2> bytes8(uint32_t w, int from) {
-    w ^= 0x80808080u;   // (x + 128) + 2^23, less 2^23 + 128
-    const Val<2> v = {__uint_as_float(__byte_perm(w, 0x4b000000u, 0x7650u | from)), __uint_as_float(__byte_perm(w, 0x4b000000u, 0x7650u | (from + 1)))};
-    return add(v, all<2>(-8388736.f));
-  }
   // writes eight channels of a row
   __device__ static void write(void *row, int32_t type, const Pairs8 &x, int d, int rank, int j) {
-    if (WORDS) {
+    if (V == 8) {
       const int at = rank + G * j;
-      if (type == DSGD_F32) {   // two lanes write each one's 32 bytes together
-        const bool odd = at & 1, alone = 8 * (at ^ 1) >= d;
-        float4 a = make_float4(x.v[0].x, x.v[0].y, x.v[1].x, x.v[1].y), b = make_float4(x.v[2].x, x.v[2].y, x.v[3].x, x.v[3].y);
-        const float4 give = odd ? a : b;
-        float4 got;
-        got.x = __shfl_xor_sync(0xffffffffu, give.x, 1);
-        got.y = __shfl_xor_sync(0xffffffffu, give.y, 1);
-        got.z = __shfl_xor_sync(0xffffffffu, give.z, 1);
-        got.w = __shfl_xor_sync(0xffffffffu, give.w, 1);
-        if (8 * at >= d) return;
-        float4 *to = static_cast<float4 *>(row) + 2 * at;
-        if (alone) {
-          to[0] = a;
-          to[1] = b;
-        } else {
-          (odd ? a : b) = got;
-          to[odd ? -1 : 0] = a;   // the second half of the even lane's, or the first of its own
-          to[odd ? 1 : 2] = b;
-        }
-        return;
-      }
-      if (8 * at >= d) return;
-      if (type == DSGD_BF16) {
-        uint4 w;
+      if (8 * at < d) static_cast<uint4 *>(row)[at] = make_uint4(pack_bf16(x.v[0]), pack_bf16(x.v[1]), pack_bf16(x.v[2]), pack_bf16(x.v[3]));
+    } else if (V == 4) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const __nv_bfloat162 h = __floats2bfloat162_rn(x.v[i].x, x.v[i].y);
-          (&w.x)[i] = *reinterpret_cast<const uint32_t *>(&h);
-        }
-        static_cast<uint4 *>(row)[at] = w;
+      for (int k = 0; k < 2; ++k) {
+        const int at = rank + G * (2 * j + k);
+        if (4 * at >= d) continue;
+        const Val<2> a = x.v[2 * k], b = x.v[2 * k + 1];
+        if (type == DSGD_BF16) static_cast<uint2 *>(row)[at] = make_uint2(pack_bf16(a), pack_bf16(b));
+        else static_cast<float4 *>(row)[at] = make_float4(a.x, a.y, b.x, b.y);
       }
     } else {
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        const int c = L::channel(rank, j, e);
+        const int c = channel<G, V>(rank, j, e);
         if (c < d) store(row, type, c, e & 1 ? x.v[e / 2].y : x.v[e / 2].x);
       }
     }
@@ -185,34 +198,36 @@ template <int G, int PASSES, bool WORDS> struct Place {
     if (rank < to - from) row[from + rank] = 0;
   }
   __device__ static void keep(uint8_t *row, const Pairs8 &x, int d, int rank, int j) {
-    if (WORDS) {
+    if (V == 8) {
       const int at = rank + G * j;
       uint32_t top = 0;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) top = max(top, max(magnitude(x.v[i].x), magnitude(x.v[i].y)));
+      for (int i = 0; i < 4; ++i) top = greatest(top, x.v[i]);
       top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
       top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
       if (8 * at >= d) return;
       const uint32_t e = exponent8(top);
       const Val<2> by = all<2>(scale8(e));
-      uint32_t b[8];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const Val<2> v = mul(x.v[i], by);
-        // rounded to the nearest whole number in the low bits of a sum with 1.5 2^23 (a NaN times 0 becomes 0 first: fmaxf drops it, to -127, so it is asked for)
-        b[2 * i] = __float_as_uint(fminf(fmaxf(v.x, -127.f), 127.f) + 12582912.f);
-        b[2 * i + 1] = __float_as_uint(fminf(fmaxf(v.y, -127.f), 127.f) + 12582912.f);
-      }
-      uint2 q;
-      q.x = __byte_perm(__byte_perm(b[0], b[1], 0x0040), __byte_perm(b[2], b[3], 0x0040), 0x5410);
-      q.y = __byte_perm(__byte_perm(b[4], b[5], 0x0040), __byte_perm(b[6], b[7], 0x0040), 0x5410);
+      uint2 q = make_uint2(hold_four(x.v[0], x.v[1], by), hold_four(x.v[2], x.v[3], by));
       if (e == 255u) q = make_uint2(0, 0);
       reinterpret_cast<uint2 *>(row)[at] = q;
       if (at % 4 == 0) row[d + at / 4] = (uint8_t)e;
+    } else if (V == 4) {
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        const int at = rank + G * (2 * j + k);
+        uint32_t top = greatest(greatest(0, x.v[2 * k]), x.v[2 * k + 1]);
+#pragma unroll
+        for (int o = 1; o < 8; o *= 2) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
+        if (4 * at >= d) continue;
+        const uint32_t e = exponent8(top);
+        reinterpret_cast<uint32_t *>(row)[at] = e == 255u ? 0 : hold_four(x.v[2 * k], x.v[2 * k + 1], all<2>(scale8(e)));
+        if (at % 8 == 0) row[d + at / 8] = (uint8_t)e;
+      }
     } else {
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        const int c = L::channel(rank, j, e);
+        const int c = channel<G, V>(rank, j, e);
         const float v = e & 1 ? x.v[e / 2].y : x.v[e / 2].x;
         const uint32_t b = exponent8(__reduce_max_sync(0xffffffffu, magnitude(v)));
         if (c < d) {
@@ -281,6 +296,22 @@ struct Walk {
   __device__ void next() { low += low_hop; }
 };
 
+// A thread's weights, times a number; zeros outside the row and where there are none.
+template <int G, int PASSES, int V>
+__device__ __forceinline__ void weights(Pairs8 *w, const void *from, int32_t type, int64_t at, float by, int d, int rank) {
+  const auto fill = [&](auto *values) {
+#pragma unroll
+    for (int j = 0; j < PASSES; ++j)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const int c = channel<G, V>(rank, j, e);
+        (e & 1 ? w[j].v[e / 2].y : w[j].v[e / 2].x) = values && c < d ? by * widen(values[c]) : 0.f;
+      }
+  };
+  if (type == DSGD_BF16) fill(from ? static_cast<const bf16 *>(from) + at : nullptr);
+  else fill(from ? static_cast<const float *>(from) + at : nullptr);
+}
+
 // Each warp's copy of a row's two statistics, in words of 16 bytes.
 __host__ __device__ constexpr int stats_room(int group) { return group == 32 ? 16 : group / 4; }
 
@@ -289,10 +320,9 @@ __host__ __device__ constexpr int stats_room(int group) { return group == 32 ? 1
   const int32_t ta = TA == kAnyType ? p.act_type : TA;                       \
   const int sb = ts == DSGD_BF16 ? 2 : 4, ab = ta == DSGD_BF16 ? 2 : 4
 
-template <int G, int PASSES, bool WORDS, int TS, int TA, int PARTS>
+template <int G, int PASSES, int V, int TS, int TA, int PARTS>
 __global__ void __launch_bounds__(G * groups_of(G), resident_block(G, PASSES)) block_kernel(const __grid_constant__ BlockArgs p) {
-  using X = Place<G, PASSES, WORDS>;
-  using L = Lay<G, PASSES, WORDS>;
+  using X = Place<G, PASSES, V>;
   extern __shared__ uint4 ring[];
   __shared__ alignas(16) float sums[2][4 * (G / 32)];
   constexpr int kGroups = groups_of(G);
@@ -302,7 +332,7 @@ __global__ void __launch_bounds__(G * groups_of(G), resident_block(G, PASSES)) b
   constexpr bool kAny = PARTS == kAnyParts;
   const bool y = !kAny || p.y.at != nullptr, gated = kAny ? p.gate.at != nullptr : PARTS != kPlain, u = !kAny || p.w_pre != nullptr, silu = kAny ? p.silu : PARTS == kSilu;
   // a row's places in a stage of the ring, where they can be known by now
-  const auto room = [&](int i, int32_t type, bool there) { return WORDS && !kAny ? there ? X::room(0, type) : 0 : p.room[i]; };
+  const auto room = [&](int i, int32_t type, bool there) { return V > 1 && !kAny ? there ? X::room(0, type) : 0 : p.room[i]; };
   const int off_y = room(0, ts, true), off_g = off_y + room(1, ta, y), stage_bytes = off_g + room(2, ta, gated);
   uint8_t *mine = reinterpret_cast<uint8_t *>(ring) + (size_t)group * p.stages * stage_bytes;
   const uint32_t mine32 = smem_u32(mine);
@@ -326,14 +356,8 @@ __global__ void __launch_bounds__(G * groups_of(G), resident_block(G, PASSES)) b
   for (int i = 0; i + 1 < p.stages; ++i) bring();
   const float scale = p.scale ? load(p.scale, p.weights_type, agent * p.scale_stride) : 1.f, over_d = 1.f / (float)p.d;
   Pairs8 wq[PASSES], wp[PASSES];   // scale w_post, w_pre
-#pragma unroll
-  for (int j = 0; j < PASSES; ++j)
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const int c = L::channel(rank, j, e);
-      (e & 1 ? wq[j].v[e / 2].y : wq[j].v[e / 2].x) = y && c < d ? scale * load(p.w_post, p.weights_type, agent * p.w_post_stride + c) : 0.f;
-      (e & 1 ? wp[j].v[e / 2].y : wp[j].v[e / 2].x) = u && c < d ? load(p.w_pre, p.weights_type, agent * p.w_pre_stride + c) : 0.f;
-    }
+  weights<G, PASSES, V>(wq, y ? p.w_post : nullptr, p.weights_type, agent * p.w_post_stride, scale, d, rank);
+  weights<G, PASSES, V>(wp, u ? p.w_pre : nullptr, p.weights_type, agent * p.w_pre_stride, 1.f, d, rank);
   const auto norm = [&](const Pairs8 *a, int turn) {
     const auto squares = [&](float unit) {
       Pairs8 s{};
@@ -359,7 +383,7 @@ __global__ void __launch_bounds__(G * groups_of(G), resident_block(G, PASSES)) b
   for (int i = 0; i < rows; ++i) {
     bring();
     copies_but(p.stages - 1);
-    if (WORDS || G == 32) __syncwarp();   // (lanes copy for one another)
+    if (V > 1 || G == 32) __syncwarp();   // (lanes copy for one another)
     else __syncthreads();
     const uint8_t *at = mine + from;
     from += stage_bytes;
@@ -413,16 +437,15 @@ __global__ void __launch_bounds__(G * groups_of(G), resident_block(G, PASSES)) b
     wh.next();
     wy.next();
     wg.next();
-    if (G > 32 && (!WORDS || !y || !u)) __syncthreads();   // the place is written again only when everybody has read it, and a sum's when everybody has it
+    if (G > 32 && (V == 1 || !y || !u)) __syncthreads();   // the place is written again only when everybody has read it, and a sum's when everybody has it
     else __syncwarp();
   }
   copies_but(0);
 }
 
-template <int G, int PASSES, bool WORDS, int TS, int TA, bool KEPT, int PARTS>
+template <int G, int PASSES, int V, int TS, int TA, bool KEPT, int PARTS>
 __global__ void __launch_bounds__(G * groups_of(G), resident_grad(G, PASSES)) block_grad_kernel(const __grid_constant__ BlockArgs p) {
-  using X = Place<G, PASSES, WORDS>;
-  using L = Lay<G, PASSES, WORDS>;
+  using X = Place<G, PASSES, V>;
   extern __shared__ uint4 ring[];
   __shared__ alignas(16) float sums[2][4 * (G / 32)];
   constexpr int kGroups = groups_of(G);
@@ -434,7 +457,7 @@ __global__ void __launch_bounds__(G * groups_of(G), resident_grad(G, PASSES)) bl
   constexpr bool kAny = PARTS == kAnyParts;
   const bool y = !kAny || p.y.at != nullptr, gated = kAny ? p.gate.at != nullptr : PARTS != kPlain, u = !kAny || p.w_pre != nullptr, silu = kAny ? p.silu : PARTS == kSilu;
   const bool past = !kAny || p.dh_out.at != nullptr;
-  const auto room = [&](int i, int32_t type, bool there) { return WORDS && !kAny ? there ? X::room(0, type) : 0 : p.room[i]; };
+  const auto room = [&](int i, int32_t type, bool there) { return V > 1 && !kAny ? there ? X::room(0, type) : 0 : p.room[i]; };
   const int off_y = room(0, held_s, true), off_g = off_y + room(1, held_a, y), off_u = off_g + room(2, held_a, gated), off_p = off_u + room(3, ta, u),
             off_s = off_p + room(4, ts, past), stage_bytes = off_s + stats_room(G);
   uint8_t *mine = reinterpret_cast<uint8_t *>(ring) + (size_t)group * p.stages * stage_bytes;
@@ -470,17 +493,12 @@ __global__ void __launch_bounds__(G * groups_of(G), resident_grad(G, PASSES)) bl
   const float scale = p.scale ? load(p.scale, p.weights_type, agent * p.scale_stride) : 1.f, over_d = 1.f / (float)p.d;
   Pairs8 wq[PASSES], wp[PASSES];   // scale w_post, w_pre
   Pairs8 sum_pre[PASSES], sum_post[PASSES];
+  weights<G, PASSES, V>(wq, y ? p.w_post : nullptr, p.weights_type, agent * p.w_post_stride, scale, d, rank);
+  weights<G, PASSES, V>(wp, u ? p.w_pre : nullptr, p.weights_type, agent * p.w_pre_stride, 1.f, d, rank);
 #pragma unroll
-  for (int j = 0; j < PASSES; ++j) {
+  for (int j = 0; j < PASSES; ++j)
 #pragma unroll
     for (int k = 0; k < 4; ++k) sum_pre[j].v[k] = sum_post[j].v[k] = {0.f, 0.f};
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const int c = L::channel(rank, j, e);
-      (e & 1 ? wq[j].v[e / 2].y : wq[j].v[e / 2].x) = y && c < d ? scale * load(p.w_post, p.weights_type, agent * p.w_post_stride + c) : 0.f;
-      (e & 1 ? wp[j].v[e / 2].y : wp[j].v[e / 2].x) = u && c < d ? load(p.w_pre, p.weights_type, agent * p.w_pre_stride + c) : 0.f;
-    }
-  }
   uint8_t *dh = static_cast<uint8_t *>(p.dh.at) + place(p.dh, agent, first) * sb, *dy = static_cast<uint8_t *>(p.dy.at) + place(p.dy, agent, first) * ab;
   uint8_t *da = static_cast<uint8_t *>(p.dgate.at) + place(p.dgate, agent, first) * ab;
   const int64_t hop_h = hop * p.dh.row_stride * sb, hop_y = hop * p.dy.row_stride * ab, hop_a = hop * p.dgate.row_stride * ab;
@@ -488,7 +506,7 @@ __global__ void __launch_bounds__(G * groups_of(G), resident_grad(G, PASSES)) bl
   for (int i = 0; i < rows; ++i) {
     bring();
     copies_but(p.stages - 1);
-    if (WORDS || G == 32) __syncwarp();   // (lanes copy for one another)
+    if (V > 1 || G == 32) __syncwarp();   // (lanes copy for one another)
     else __syncthreads();
     const uint8_t *at = mine + from;
     from += stage_bytes;
@@ -586,7 +604,7 @@ __global__ void __launch_bounds__(G * groups_of(G), resident_grad(G, PASSES)) bl
   for (int j = 0; j < PASSES; ++j)
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      const int c = L::channel(rank, j, e);
+      const int c = channel<G, V>(rank, j, e);
       const float x = e & 1 ? sum_pre[j].v[e / 2].y : sum_pre[j].v[e / 2].x, z = e & 1 ? sum_post[j].v[e / 2].y : sum_post[j].v[e / 2].x;
       if (c >= d) continue;
       if (y) dot = fmaf(load(p.w_post, p.weights_type, agent * p.w_post_stride + c), z, dot);
@@ -602,7 +620,7 @@ __global__ void __launch_bounds__(G * groups_of(G), resident_grad(G, PASSES)) bl
     for (int j = 0; j < PASSES; ++j)
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        const int c = L::channel(rank, j, e);
+        const int c = channel<G, V>(rank, j, e);
         if (c >= d) continue;
         all_of[(2 * group) * d + c] = e & 1 ? sum_pre[j].v[e / 2].y : sum_pre[j].v[e / 2].x;
         all_of[(2 * group + 1) * d + c] = e & 1 ? sum_post[j].v[e / 2].y : sum_post[j].v[e / 2].x;
@@ -625,10 +643,10 @@ __global__ void __launch_bounds__(G * groups_of(G), resident_grad(G, PASSES)) bl
 
 constexpr int kMostShared = 220 << 10;
 
-template <int G, int PASSES, bool WORDS, int TS, int TA, int PARTS> cudaError_t launch_block(BlockArgs p, cudaStream_t s) {
+template <int G, int PASSES, int V, int TS, int TA, int PARTS> cudaError_t launch_block(BlockArgs p, cudaStream_t s) {
   static std::atomic<uint64_t> done{0};
-  using X = Place<G, PASSES, WORDS>;
-  auto kernel = block_kernel<G, PASSES, WORDS, TS, TA, PARTS>;
+  using X = Place<G, PASSES, V>;
+  auto kernel = block_kernel<G, PASSES, V, TS, TA, PARTS>;
   constexpr int kGroups = groups_of(G), kThreads = G * kGroups;
   const cudaError_t e = set_max_shared_once(reinterpret_cast<const void *>(kernel), kMostShared, &done);
   if (e != cudaSuccess) return e;
@@ -645,10 +663,10 @@ template <int G, int PASSES, bool WORDS, int TS, int TA, int PARTS> cudaError_t 
   return cudaGetLastError();
 }
 
-template <int G, int PASSES, bool WORDS, int TS, int TA, bool KEPT, int PARTS> cudaError_t launch_block_grad(BlockArgs p, cudaStream_t s) {
+template <int G, int PASSES, int V, int TS, int TA, bool KEPT, int PARTS> cudaError_t launch_block_grad(BlockArgs p, cudaStream_t s) {
   static std::atomic<uint64_t> done{0};
-  using X = Place<G, PASSES, WORDS>;
-  auto kernel = block_grad_kernel<G, PASSES, WORDS, TS, TA, KEPT, PARTS>;
+  using X = Place<G, PASSES, V>;
+  auto kernel = block_grad_kernel<G, PASSES, V, TS, TA, KEPT, PARTS>;
   constexpr int kGroups = groups_of(G), kThreads = G * kGroups;
   cudaError_t e = set_max_shared_once(reinterpret_cast<const void *>(kernel), kMostShared, &done);
   if (e != cudaSuccess) return e;
@@ -670,15 +688,15 @@ template <int G, int PASSES, bool WORDS, int TS, int TA, bool KEPT, int PARTS> c
   return e == cudaSuccess ? finish_block_grad(p, s) : e;
 }
 
-template <bool WORDS, int TS, int TA> cudaError_t launch_rows(const BlockArgs &p, bool grad, cudaStream_t s) {
+template <int V, int TS, int TA> cudaError_t launch_rows(const BlockArgs &p, bool grad, cudaStream_t s) {
   const auto with = [&](auto widest, auto parts) {
     constexpr Shape f = shape_of(decltype(widest)::value), g = grad_shape_of(decltype(widest)::value);
     constexpr int PARTS = decltype(parts)::value;
-    if (!grad) return launch_block<f.group, f.passes, WORDS, TS, TA, PARTS>(p, s);
-    return p.kept ? launch_block_grad<g.group, g.passes, WORDS, TS, TA, true, PARTS>(p, s) : launch_block_grad<g.group, g.passes, WORDS, TS, TA, false, PARTS>(p, s);
+    if (!grad) return launch_block<f.group, f.passes, V, TS, TA, PARTS>(p, s);
+    return p.kept ? launch_block_grad<g.group, g.passes, V, TS, TA, true, PARTS>(p, s) : launch_block_grad<g.group, g.passes, V, TS, TA, false, PARTS>(p, s);
   };
   const auto by = [&](auto widest) {
-    if constexpr (WORDS) {
+    if constexpr (V > 1) {
       if (p.y.at && p.w_pre && (!grad || p.dh_out.at)) {
         if (!p.gate.at) return with(widest, std::integral_constant<int, kPlain>());
         return p.silu ? with(widest, std::integral_constant<int, kSilu>()) : with(widest, std::integral_constant<int, kSigmoid>());

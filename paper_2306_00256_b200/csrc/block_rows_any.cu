@@ -3,6 +3,6 @@
 
 namespace ceca {
 
-cudaError_t block_rows_any(const BlockArgs &p, bool grad, cudaStream_t s) { return launch_rows<false, kAnyType, kAnyType>(p, grad, s); }
+cudaError_t block_rows_any(const BlockArgs &p, bool grad, cudaStream_t s) { return launch_rows<1, kAnyType, kAnyType>(p, grad, s); }
 
 }  // namespace ceca

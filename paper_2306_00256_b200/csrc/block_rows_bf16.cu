@@ -3,6 +3,6 @@
 
 namespace ceca {
 
-cudaError_t block_rows_bf16(const BlockArgs &p, bool grad, cudaStream_t s) { return launch_rows<true, DSGD_BF16, DSGD_BF16>(p, grad, s); }
+cudaError_t block_rows_bf16(const BlockArgs &p, bool grad, cudaStream_t s) { return launch_rows<8, DSGD_BF16, DSGD_BF16>(p, grad, s); }
 
 }  // namespace ceca

@@ -3,6 +3,6 @@
 
 namespace ceca {
 
-cudaError_t block_rows_mixed(const BlockArgs &p, bool grad, cudaStream_t s) { return launch_rows<true, DSGD_F32, DSGD_BF16>(p, grad, s); }
+cudaError_t block_rows_mixed(const BlockArgs &p, bool grad, cudaStream_t s) { return launch_rows<4, DSGD_F32, DSGD_BF16>(p, grad, s); }
 
 }  // namespace ceca
