@@ -257,9 +257,10 @@ cudaError_t rows(const BlockArgs &p, bool grad, cudaStream_t s) {
   for (const dsgd_rows_t *x : {&p.h, &p.y, &p.gate}) words = words && (p.kept || on_words(*x, x == &p.h ? p.stream_type : p.act_type));
   for (const dsgd_rows_t *x : {&p.h_out, &p.dh_out, &p.dh}) words = words && on_words(*x, p.stream_type);
   for (const dsgd_rows_t *x : {&p.u, &p.du, &p.dy, &p.dgate}) words = words && on_words(*x, p.act_type);
-  if (words && p.stream_type == DSGD_BF16 && p.act_type == DSGD_BF16) return block_rows_bf16(p, grad, s);
-  if (words && p.stream_type == DSGD_F32) return p.act_type == DSGD_F32 ? block_rows_f32(p, grad, s) : block_rows_mixed(p, grad, s);
-  return block_rows_any(p, grad, s);
+  if (p.stream_type == DSGD_F32 && p.act_type == DSGD_F32) return words ? block_rows_f32(p, grad, s) : block_odd_rows_f32(p, grad, s);
+  if (p.stream_type == DSGD_F32) return words ? block_rows_mixed(p, grad, s) : block_odd_rows_mixed(p, grad, s);
+  if (p.act_type == DSGD_BF16) return words ? block_rows_bf16(p, grad, s) : block_odd_rows_bf16(p, grad, s);
+  return block_odd_rows_any(p, grad, s);
 }
 
 ceca_status_t status(cudaError_t e) { return e == cudaSuccess ? CECA_OK : CECA_ERR_CUDA; }

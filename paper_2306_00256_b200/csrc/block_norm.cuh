@@ -33,11 +33,7 @@ struct Shape {
   int group, passes;   // threads of a group, eights of channels a thread
 };
 __host__ __device__ constexpr Shape shape_of(int64_t d) {
-#ifdef ALT1
-  return d <= 256 ? Shape{32, 1} : d <= 512 ? Shape{64, 1} : d <= 1024 ? Shape{128, 1} : d <= 2048 ? Shape{256, 1} : d <= 4096 ? Shape{512, 1} : Shape{512, 2};
-#else
   return d <= 256 ? Shape{32, 1} : d <= 512 ? Shape{32, 2} : d <= 1024 ? Shape{64, 2} : d <= 2048 ? Shape{128, 2} : d <= 4096 ? Shape{256, 2} : Shape{512, 2};
-#endif
 }
 __host__ __device__ constexpr Shape grad_shape_of(int64_t d) {
   return d <= 256 ? Shape{32, 1} : d <= 512 ? Shape{64, 1} : d <= 1024 ? Shape{128, 1} : d <= 2048 ? Shape{256, 1} : d <= 4096 ? Shape{512, 1} : Shape{512, 2};
@@ -45,10 +41,7 @@ __host__ __device__ constexpr Shape grad_shape_of(int64_t d) {
 // Groups of a CTA: rows that one warp holds share one.
 __host__ __device__ constexpr int groups_of(int group) { return group == 32 ? 4 : 1; }
 // CTAs an SM that the kernels are compiled for.
-#ifndef FR1
-#define FR1 768
-#endif
-__host__ __device__ constexpr int resident_block(int group, int passes) { return (passes == 2 ? 512 : FR1) / (group * groups_of(group)); }
+__host__ __device__ constexpr int resident_block(int group, int passes) { return (passes == 2 ? 512 : 768) / (group * groups_of(group)); }
 __host__ __device__ constexpr int resident_grad(int group, int passes) { return group == 32 ? 4 : passes == 2 ? (group == 512 ? 1 : 384 / group) : 512 / group; }
 // Whether a tensor's rows all start on 16-byte boundaries.
 inline bool on_words(const dsgd_rows_t &x, int32_t type) {
@@ -57,12 +50,15 @@ inline bool on_words(const dsgd_rows_t &x, int32_t type) {
 }
 int64_t block_grad_parts(int64_t n, int64_t t, int64_t d);           // block_norm.cu: of the sums over rows, per agent
 cudaError_t finish_block_grad(const BlockArgs &p, cudaStream_t s);   // block_norm.cu: joins them
-// The kernels for rows in registers (block_rows.cuh), one translation unit for each pair of types of the stream and of the activations, with all rows on
-// 16-byte boundaries, and one for the rest.
+// The kernels for rows in registers (block_rows.cuh), one translation unit for each pair of types of the stream and of the activations (mixed: fp32 and
+// bf16), for rows that all start on 16-byte boundaries and for others.
 cudaError_t block_rows_f32(const BlockArgs &p, bool grad, cudaStream_t s);
 cudaError_t block_rows_bf16(const BlockArgs &p, bool grad, cudaStream_t s);
-cudaError_t block_rows_mixed(const BlockArgs &p, bool grad, cudaStream_t s);   // fp32 and bf16
-cudaError_t block_rows_any(const BlockArgs &p, bool grad, cudaStream_t s);
+cudaError_t block_rows_mixed(const BlockArgs &p, bool grad, cudaStream_t s);
+cudaError_t block_odd_rows_f32(const BlockArgs &p, bool grad, cudaStream_t s);
+cudaError_t block_odd_rows_bf16(const BlockArgs &p, bool grad, cudaStream_t s);
+cudaError_t block_odd_rows_mixed(const BlockArgs &p, bool grad, cudaStream_t s);
+cudaError_t block_odd_rows_any(const BlockArgs &p, bool grad, cudaStream_t s);   // any types
 
 #ifdef __CUDACC__
 __device__ __forceinline__ float load(const void *p, int32_t type, int64_t i) {

@@ -696,7 +696,7 @@ template <int V, int TS, int TA> cudaError_t launch_rows(const BlockArgs &p, boo
     return p.kept ? launch_block_grad<g.group, g.passes, V, TS, TA, true, PARTS>(p, s) : launch_block_grad<g.group, g.passes, V, TS, TA, false, PARTS>(p, s);
   };
   const auto by = [&](auto widest) {
-    if constexpr (V > 1) {
+    if constexpr (TS != kAnyType) {
       if (p.y.at && p.w_pre && (!grad || p.dh_out.at)) {
         if (!p.gate.at) return with(widest, std::integral_constant<int, kPlain>());
         return p.silu ? with(widest, std::integral_constant<int, kSilu>()) : with(widest, std::integral_constant<int, kSigmoid>());

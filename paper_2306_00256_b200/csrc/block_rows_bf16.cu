@@ -1,4 +1,4 @@
-// Block norms with rows in registers: bf16 throughout.
+// Block norms with rows in registers: bf16 throughout, rows on 16-byte boundaries.
 #include "block_rows.cuh"
 
 namespace ceca {

@@ -1,4 +1,4 @@
-// Block norms with rows in registers: fp32 throughout.
+// Block norms with rows in registers: fp32 throughout, rows on 16-byte boundaries.
 #include "block_rows.cuh"
 
 namespace ceca {

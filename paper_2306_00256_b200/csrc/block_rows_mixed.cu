@@ -1,4 +1,4 @@
-// Block norms with rows in registers: an fp32 stream and bf16 activations.
+// Block norms with rows in registers: an fp32 stream and bf16 activations, rows on 16-byte boundaries.
 #include "block_rows.cuh"
 
 namespace ceca {
