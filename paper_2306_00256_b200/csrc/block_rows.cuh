@@ -180,15 +180,17 @@ template <int G, int PASSES, int V> struct Place {
   __device__ static void keep(uint8_t *row, const Pairs8 &x, int d, int rank, int j) {
     if (V == 8) {
       const int at = rank + G * j;
-      uint32_t top = 0;
+      float most = 0.f;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) top = greatest(top, x.v[i]);
+      for (int i = 0; i < 4; ++i) most = greatest(most, x.v[i]);
+      uint32_t top = __float_as_uint(most);
       top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
       top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
       if (8 * at >= d) return;
       const uint32_t e = exponent8(top);
       const Val<2> by = all<2>(scale8(e));
-      uint2 q = make_uint2(hold_four(x.v[0], x.v[1], by), hold_four(x.v[2], x.v[3], by));
+      const bool cut = cut8(top);
+      uint2 q = make_uint2(hold_four(x.v[0], x.v[1], by, cut), hold_four(x.v[2], x.v[3], by, cut));
       if (e == 255u) q = make_uint2(0, 0);
       reinterpret_cast<uint2 *>(row)[at] = q;
       if (at % 4 == 0) row[d + at / 4] = (uint8_t)e;
@@ -196,12 +198,12 @@ template <int G, int PASSES, int V> struct Place {
 #pragma unroll
       for (int k = 0; k < 2; ++k) {
         const int at = rank + G * (2 * j + k);
-        uint32_t top = greatest(greatest(0, x.v[2 * k]), x.v[2 * k + 1]);
+        uint32_t top = __float_as_uint(greatest(greatest(0.f, x.v[2 * k]), x.v[2 * k + 1]));
 #pragma unroll
         for (int o = 1; o < 8; o *= 2) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
         if (4 * at >= d) continue;
         const uint32_t e = exponent8(top);
-        reinterpret_cast<uint32_t *>(row)[at] = e == 255u ? 0 : hold_four(x.v[2 * k], x.v[2 * k + 1], all<2>(scale8(e)));
+        reinterpret_cast<uint32_t *>(row)[at] = e == 255u ? 0 : hold_four(x.v[2 * k], x.v[2 * k + 1], all<2>(scale8(e)), cut8(top));
         if (at % 8 == 0) row[d + at / 8] = (uint8_t)e;
       }
     } else {

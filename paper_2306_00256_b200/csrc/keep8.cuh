@@ -26,14 +26,26 @@ __device__ __forceinline__ Val<2> whole_numbers(uint32_t w, int from) {
   const Val<2> v = {__uint_as_float(__byte_perm(w, 0x4b000000u, 0x7650u | from)), __uint_as_float(__byte_perm(w, 0x4b000000u, 0x7650u | (from + 1)))};
   return add(v, all<2>(-8388736.f));
 }
-// four of them, of x: rounded to the nearest in the low bits of a sum with 1.5 2^23
-__device__ __forceinline__ uint32_t hold_four(Val<2> x, Val<2> y, Val<2> by) {
-  const auto low = [](float v) { return __float_as_uint(fminf(fmaxf(v, -127.f), 127.f) + 12582912.f); };
+// four of them, of x: rounded to the nearest in the low bits of a sum with 1.5 2^23.  `cut`: some are rounded to 128, which becomes 127.
+__device__ __forceinline__ uint32_t hold_four(Val<2> x, Val<2> y, Val<2> by, bool cut) {
   x = mul(x, by);
   y = mul(y, by);
-  return __byte_perm(__byte_perm(low(x.x), low(x.y), 0x0040), __byte_perm(low(y.x), low(y.y), 0x0040), 0x5410);
+  if (cut) {
+    const auto within = [](float v) { return fminf(fmaxf(v, -127.f), 127.f); };
+    x = {within(x.x), within(x.y)};
+    y = {within(y.x), within(y.y)};
+  }
+  x = add(x, all<2>(12582912.f));
+  y = add(y, all<2>(12582912.f));
+  return __byte_perm(__byte_perm(__float_as_uint(x.x), __float_as_uint(x.y), 0x0040), __byte_perm(__float_as_uint(y.x), __float_as_uint(y.y), 0x0040), 0x5410);
 }
-__device__ __forceinline__ uint32_t greatest(uint32_t top, Val<2> x) { return max(top, max(magnitude(x.x), magnitude(x.y))); }
+// Whether the largest of a block, of these bits, is held as more than 127: mantissas from 127.5 / 128 on.
+__device__ __forceinline__ bool cut8(uint32_t top) { return (top & 0x7fffffu) >= 0x7f0000u; }
+// The larger magnitude, as a number; a NaN if there is one.
+__device__ __forceinline__ float greatest(float top, Val<2> x) {
+  asm("{\n\t.reg .f32 a, b;\n\tabs.f32 a, %1;\n\tabs.f32 b, %2;\n\tmax.NaN.f32 %0, %0, a;\n\tmax.NaN.f32 %0, %0, b;\n\t}" : "+f"(top) : "f"(x.x), "f"(x.y));
+  return top;
+}
 __device__ __forceinline__ uint32_t pack_bf16(Val<2> x) {
   const __nv_bfloat162 h = __floats2bfloat162_rn(x.x, x.y);
   return *reinterpret_cast<const uint32_t *>(&h);
