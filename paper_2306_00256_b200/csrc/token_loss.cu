@@ -33,9 +33,10 @@ struct TokenArgs {
   int64_t r, v, ldz, lddz, pairs;
   float scale, temperature, low, high, kl, beta, smoothing;   // scale = log2(e) / T
   int32_t idx64, bounds64, average, what;
-  RowOut *rows;        // workspace
-  float *row_logp;     // preference
-  double *slopes;      // of each sequence
+  int32_t parts, per;   // of a row, and vectors of each
+  RowOut *rows;         // workspace, r of each; NULL without a gradient
+  float2 *sums;         // r x parts
+  float *row_logp, *row_slopes;   // of the preference loss, the second with a gradient
 };
 
 __device__ __forceinline__ int64_t index_of(const void *p, int32_t wide, int64_t i) {
@@ -79,90 +80,166 @@ __device__ __forceinline__ RowOut row_out(const TokenArgs &p, const RowSum &s, c
   return {s.k, s.rest == 0.f ? 0.f : own / s.rest, own, s.far ? 1 : 0};
 }
 
-constexpr int kThreads = 256, kWarps = kThreads / 32;
+constexpr int kWarps = 4, kThreads = 32 * kWarps;
+// Warps work on their own: on a part of a row of up to 16 vectors a lane, whose loads are all under way at a time.
+constexpr int kVectors = 16, kPart = 32 * kVectors;
 
-__device__ __forceinline__ float cta_max(float x, float *part) {
-  x = warp_max(x);
-  __syncthreads();
-  if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = x;
-  __syncthreads();
-  x = part[0];
-#pragma unroll
-  for (int i = 1; i < kWarps; ++i) x = fmaxf(x, part[i]);
-  return x;
-}
-__device__ __forceinline__ float cta_sum(float x, float *part) {
-  x = warp_sum(x);
-  __syncthreads();
-  if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = x;
-  __syncthreads();
-  x = 0.f;
-#pragma unroll
-  for (int i = 0; i < kWarps; ++i) x += part[i];
-  return x;
-}
-
-// A CTA reads a row twice: its maximum, its sum.
-template <typename TZ> __global__ void __launch_bounds__(kThreads) sum_kernel(const TokenArgs p) {
-  __shared__ float part[kWarps];
-  for (int64_t i = blockIdx.x; i < p.r; i += gridDim.x) {
-    const int64_t tok = index_of(p.tokens, p.idx64, i);
-    const float w = p.what == kPolicy && p.weight ? p.weight[i] : 1.f;
-    const bool live = tok >= 0 && tok < p.v && w != 0.f;
-    if (!live) {
-      if (threadIdx.x == 0) {
-        if (p.what == kLogprob || (p.what == kPolicy && p.logp)) p.logp[i] = 0.f;
-        if (p.what == kPolicy) p.loss[i] = 0.f;
-        if (p.what == kPreference) p.row_logp[i] = 0.f;
-        if (p.rows) p.rows[i] = {0.f, 0.f, 0.f, 0};
-      }
-      continue;
-    }
-    const TZ *z = static_cast<const TZ *>(p.z) + i * p.ldz;
-    float m = -INFINITY;
-    for (int64_t c = threadIdx.x; c < p.v; c += kThreads)
-      if (c != tok) m = fmaxf(m, widen(z[c]));
-    m = cta_max(m, part);
-    RowSum s;
-    s.far = !(fabsf(frame_of(m, p.scale)) < kFar);
-    s.k = s.far ? m == -INFINITY ? widen(z[tok]) : m : frame_of(m, p.scale);
-    const auto exponent = [&](float x) { return s.far ? (x - s.k) * p.scale : fmaf(x, p.scale, -s.k); };
-    float sum = 0.f;
-    for (int64_t c = threadIdx.x; c < p.v; c += kThreads)
-      if (c != tok) sum += m == -INFINITY ? (widen(z[c]) == -INFINITY ? 0.f : NAN) : ex2(exponent(widen(z[c])));
-    s.rest = cta_sum(sum, part);
-    const float own = widen(z[tok]);
-    s.y = own == -INFINITY ? own : own == INFINITY ? NAN : exponent(own);
-    if (threadIdx.x) continue;
-    const Odds o = odds_of(s);
-    if (p.what == kLogprob) p.logp[i] = o.logp;
-    if (p.what == kPolicy) {
-      const float2 l = policy(p, i, w, o.logp);
-      p.loss[i] = l.x;
-      if (p.logp) p.logp[i] = o.logp;
-      if (p.rows) p.rows[i] = row_out(p, s, o, l.y);
-    }
-    if (p.what == kPreference) {
-      p.row_logp[i] = o.logp;
-      if (p.rows) p.rows[i] = row_out(p, s, o, 1.f);   // the sequence's slope comes later
+// The part of a row that a warp takes, in slots: slot s is element s - pad, so that vectors of N slots lie on 16-byte boundaries.  Whole vectors are
+// [w0, w1); what the row has before and after them in this part goes one to a lane (`edge`, a slot, or -1).
+template <typename T> struct WarpPart {
+  static constexpr int N = Vec<T>::N;
+  int pad, w0, w1, edge;
+  __device__ __forceinline__ WarpPart(const T *row, int64_t v, int part, int per) {
+    pad = (int)((reinterpret_cast<uintptr_t>(row) & 15) / sizeof(T));
+    const uint32_t slots = (uint32_t)v + pad;
+    const int vectors = (int)((slots + N - 1) / N), v0 = min(vectors, part * per), v1 = min(vectors, v0 + per), lane = threadIdx.x & 31;
+    w0 = v0 + (v0 == 0 && pad > 0);
+    w1 = max(w0, min(v1, (int)(slots / N)));
+    edge = -1;
+    if (lane < N) {
+      if (v0 == 0 && v1 > 0 && pad > 0 && lane >= pad && lane < slots) edge = lane;
+    } else if (lane < 2 * N) {
+      const uint32_t s = (uint32_t)w1 * N + lane - N;
+      if (v1 == vectors && v1 > v0 && s < slots && s < (uint32_t)v1 * N) edge = (int)s;
     }
   }
+};
+
+// Whether a row is looked at: it has a token, and a weight.
+__device__ __forceinline__ bool is_live(const TokenArgs &p, int64_t i, int64_t tok, float &w) {
+  w = p.what == kPolicy && p.weight ? p.weight[i] : 1.f;
+  return tok >= 0 && tok < p.v && w != 0.f;
+}
+
+// Sums of 2^(z c - k) over the parts of rows without their tokens, each in the frame of its own maximum.
+template <typename TZ> __global__ void __launch_bounds__(kThreads) sum_kernel(const TokenArgs p) {
+  constexpr int N = Vec<TZ>::N;
+  const int lane = threadIdx.x & 31;
+  const int64_t task = (int64_t)blockIdx.x * kWarps + (threadIdx.x >> 5), i = task / p.parts;
+  if (i < p.r) {
+    const int64_t tok = index_of(p.tokens, p.idx64, i);
+    float w;
+    if (is_live(p, i, tok, w)) {
+      const TZ *z = static_cast<const TZ *>(p.z) + i * p.ldz;
+      const WarpPart<TZ> part(z, p.v, (int)(task - i * p.parts), p.per);
+      const uint4 *from = reinterpret_cast<const uint4 *>(z - part.pad) + part.w0 + lane;
+      const int count = part.w1 - part.w0 - lane;   // of this lane's vectors, every 32nd
+      Vec<TZ> a[kVectors];
+#pragma unroll
+      for (int u = 0; u < kVectors; ++u) {
+        a[u] = all_least<TZ>();
+        if (32 * u < count) a[u].w = __ldcs(from + 32 * u);
+      }
+      const int64_t slot = tok + part.pad;
+      float edge = part.edge >= 0 && part.edge != slot ? widen(z[part.edge - part.pad]) : -INFINITY;
+      const int64_t at = slot / N - part.w0 - lane;   // the token's vector, as this lane counts
+      if (at >= 0 && at < count && at % 32 == 0) {
+#pragma unroll
+        for (int u = 0; u < kVectors; ++u)
+          if (at == 32 * u) strike(a[u], 1u << (slot % N));
+      }
+      // the frame of the warp: masked ones alone have a low one
+      const float k = warp_max(fmaxf(frame_of(fmaxf(edge, top_of<kVectors>(a)), p.scale), -kFar));
+      const Val<2> shift = all<2>(-k), by = all<2>(p.scale);
+      Val<2> sum{ex2(fmaf(edge, p.scale, -k)), 0.f};
+#pragma unroll
+      for (int u = 0; u < kVectors; ++u) {
+        if (32 * u >= count) break;
+#pragma unroll
+        for (int e = 0; e < Vec<TZ>::P; ++e) {
+          Val<2> y = fma(pair(a[u], e), by, shift);
+          y.x = ex2(y.x);
+          y.y = ex2(y.y);
+          sum = add(sum, y);
+        }
+      }
+      const float total = warp_sum(sum.x + sum.y);
+      if (lane == 0) p.sums[task] = make_float2(k, total);
+    }
+  }
+  follow_early();
+}
+
+// A warp joins a row's parts: its token's log-probability, the loss, and what the gradient needs.
+template <typename TZ> __global__ void __launch_bounds__(kThreads) join_kernel(const TokenArgs p) {
+  const int lane = threadIdx.x & 31;
+  const int64_t i = (int64_t)blockIdx.x * kWarps + (threadIdx.x >> 5);
+  const bool in = i < p.r;
+  const int64_t tok = in ? index_of(p.tokens, p.idx64, i) : -1;
+  float w = 0.f;
+  const bool live = in && is_live(p, i, tok, w);
+  const TZ *z = static_cast<const TZ *>(p.z) + i * p.ldz;
+  const float own = live ? widen(z[tok]) : 0.f;
+  after_first();
+  if (live) {
+    RowSum s;
+    s.k = -INFINITY;
+    for (int q = lane; q < p.parts; q += 32) s.k = fmaxf(s.k, p.sums[i * p.parts + q].x);
+    s.k = warp_max(s.k);
+    float sum = 0.f;
+    for (int q = lane; q < p.parts; q += 32) {
+      const float2 a = p.sums[i * p.parts + q];
+      sum += a.y * ex2(a.x - s.k);
+    }
+    s.rest = warp_sum(sum);
+    s.far = !(fabsf(s.k) < kFar && s.rest < INFINITY);
+    if (s.far) {   // exponents beyond +-kFar, infinities or NaN: once more, element by element
+      float m = -INFINITY;
+      for (int64_t c = lane; c < p.v; c += 32)
+        if (c != tok) m = fmaxf(m, widen(z[c]));
+      m = warp_max(m);
+      s.k = m == -INFINITY ? own : m;
+      sum = 0.f;
+      for (int64_t c = lane; c < p.v; c += 32) {
+        const float x = widen(z[c]);
+        if (c != tok) sum += m == -INFINITY ? (x == -INFINITY ? 0.f : NAN) : ex2((x - s.k) * p.scale);
+      }
+      s.rest = warp_sum(sum);
+    }
+    s.y = own == -INFINITY ? own : own == INFINITY ? NAN : s.far ? (own - s.k) * p.scale : fmaf(own, p.scale, -s.k);
+    const Odds o = odds_of(s);
+    if (lane == 0) {
+      if (p.what == kLogprob) p.logp[i] = o.logp;
+      if (p.what == kPolicy) {
+        const float2 l = policy(p, i, w, o.logp);
+        p.loss[i] = l.x;
+        if (p.logp) p.logp[i] = o.logp;
+        if (p.rows) p.rows[i] = row_out(p, s, o, l.y);
+      }
+      if (p.what == kPreference) {
+        p.row_logp[i] = o.logp;
+        if (p.rows) p.rows[i] = row_out(p, s, o, 1.f);   // the sequence's slope comes later
+      }
+    }
+  } else if (in && lane == 0) {
+    if (p.what == kLogprob || (p.what == kPolicy && p.logp)) p.logp[i] = 0.f;
+    if (p.what == kPolicy) p.loss[i] = 0.f;
+    if (p.what == kPreference) p.row_logp[i] = 0.f;
+    if (p.rows) p.rows[i] = {0.f, 0.f, 0.f, 0};
+  }
+  if (in && lane == 0 && p.row_slopes) p.row_slopes[i] = 0.f;   // of rows outside all sequences
+  follow_early();
 }
 
 __device__ __forceinline__ int64_t bound(const TokenArgs &p, int64_t j) { return min(max(index_of(p.bounds, p.bounds64, j), (int64_t)0), p.r); }
 
-// A CTA takes a pair: its sequences' sums in 64 bits, the loss, and each one's slope.
-__global__ void __launch_bounds__(kThreads) pair_kernel(const TokenArgs p) {
-  __shared__ double sums[2][kWarps];
-  __shared__ int64_t counts[2][kWarps];
+constexpr int kPairThreads = 512, kPairWarps = kPairThreads / 32;
+
+// A CTA takes a pair: its sequences' sums in 64 bits, the loss, and the slope of each of its rows.
+__global__ void __launch_bounds__(kPairThreads) pair_kernel(const TokenArgs p) {
+  __shared__ double sums[2][kPairWarps];
+  __shared__ int64_t counts[2][kPairWarps];
+  __shared__ float slopes[2];
   const int warp = threadIdx.x >> 5;
+  after_first();
   for (int64_t q = blockIdx.x; q < p.pairs; q += gridDim.x) {
     const float w = p.weight ? p.weight[q] : 1.f;
+    const int64_t cut[3] = {bound(p, 2 * q), bound(p, 2 * q + 1), bound(p, 2 * q + 2)};
     __syncthreads();
     for (int k = 0; k < 2; ++k) {
       double s = 0.;
       int64_t n = 0;
-      for (int64_t i = bound(p, 2 * q + k) + threadIdx.x; i < bound(p, 2 * q + k + 1); i += kThreads) {
+      for (int64_t i = cut[k] + threadIdx.x; i < cut[k + 1]; i += kPairThreads) {
         const int64_t tok = index_of(p.tokens, p.idx64, i);
         s += (double)p.row_logp[i];
         n += tok >= 0 && tok < p.v;
@@ -178,86 +255,127 @@ __global__ void __launch_bounds__(kThreads) pair_kernel(const TokenArgs p) {
       }
     }
     __syncthreads();
-    if (threadIdx.x) continue;
-    double l[2], by[2];
-    for (int k = 0; k < 2; ++k) {
-      int64_t n = 0;
-      l[k] = 0.;
-      for (int i = 0; i < kWarps; ++i) {
-        l[k] += sums[k][i];
-        n += counts[k][i];
+    if (threadIdx.x == 0) {
+      double l[2], by[2];
+      for (int k = 0; k < 2; ++k) {
+        int64_t n = 0;
+        l[k] = 0.;
+        for (int i = 0; i < kPairWarps; ++i) {
+          l[k] += sums[k][i];
+          n += counts[k][i];
+        }
+        by[k] = p.average ? 1. / (double)max(n, (int64_t)1) : 1.;
+        l[k] *= by[k];
+        if (p.logp) p.logp[2 * q + k] = (float)l[k];
+        if (p.ref_logp) l[k] -= (double)p.ref_logp[2 * q + k];
       }
-      by[k] = p.average ? 1. / (double)max(n, (int64_t)1) : 1.;
-      l[k] *= by[k];
-      if (p.logp) p.logp[2 * q + k] = (float)l[k];
-      if (p.ref_logp) l[k] -= (double)p.ref_logp[2 * q + k];
-    }
-    const double m = (double)p.beta * (l[0] - l[1]), e = exp(-fabs(m)), small = e / (1. + e);
-    const double up = log1p(e) + fmax(-m, 0.), down = log1p(e) + fmax(m, 0.);   // -log sigmoid(m), -log sigmoid(-m)
-    const double at_minus = m >= 0. ? small : 1. - small, at = m >= 0. ? 1. - small : small;   // sigmoid(-m), sigmoid(m)
-    const double eps = (double)p.smoothing;
-    if (p.loss) p.loss[q] = w == 0.f ? 0.f : (float)((double)w * ((1. - eps) * up + (eps > 0. ? eps * down : 0.)));
-    if (p.slopes) {
+      const double m = (double)p.beta * (l[0] - l[1]), e = exp(-fabs(m)), small = e / (1. + e);
+      const double up = log1p(e) + fmax(-m, 0.), down = log1p(e) + fmax(m, 0.);                          // -log sigmoid(m), -log sigmoid(-m)
+      const double at_minus = m >= 0. ? small : 1. / (1. + e), at = m >= 0. ? 1. / (1. + e) : small;     // sigmoid(-m), sigmoid(m)
+      const double eps = (double)p.smoothing;
+      if (p.loss) p.loss[q] = w == 0.f ? 0.f : (float)((double)w * ((1. - eps) * up + (eps > 0. ? eps * down : 0.)));
       const double slope = w == 0.f ? 0. : (double)w * (double)p.beta * (eps * at - (1. - eps) * at_minus);
-      p.slopes[2 * q] = slope * by[0];
-      p.slopes[2 * q + 1] = -slope * by[1];
+      slopes[0] = (float)(slope * by[0]);
+      slopes[1] = (float)(-slope * by[1]);
     }
+    if (!p.row_slopes) continue;
+    __syncthreads();
+    for (int k = 0; k < 2; ++k)
+      for (int64_t i = cut[k] + threadIdx.x; i < cut[k + 1]; i += kPairThreads) p.row_slopes[i] = slopes[k];
   }
+  follow_early();
 }
 
-// The sequence that a row lies in, or -1.
-__device__ __forceinline__ int64_t sequence_of(const TokenArgs &p, int64_t i) {
-  if (p.pairs == 0) return -1;
-  int64_t lo = 0, hi = 2 * p.pairs + 1;   // the first bound above i
-  while (lo < hi) {
-    const int64_t mid = (lo + hi) / 2;
-    if (index_of(p.bounds, p.bounds64, mid) > i) hi = mid;
-    else lo = mid + 1;
-  }
-  return lo == 2 * p.pairs + 1 ? -1 : lo - 1;
-}
-
+// A warp writes a part of a row's gradient.
 template <typename TZ> __global__ void __launch_bounds__(kThreads) turn_kernel(const TokenArgs p) {
-  for (int64_t i = blockIdx.x; i < p.r; i += gridDim.x) {
-    RowOut o = p.rows[i];
-    if (p.what == kPreference) {
-      const int64_t j = sequence_of(p, i);
-      const float slope = j < 0 ? 0.f : (float)p.slopes[j];
-      o.factor = slope == 0.f ? 0.f : o.factor * slope;
-      o.own = slope == 0.f ? 0.f : o.own * slope;
-    }
-    const int64_t tok = index_of(p.tokens, p.idx64, i);
-    const TZ *z = static_cast<const TZ *>(p.z) + i * p.ldz;
-    TZ *dz = static_cast<TZ *>(p.dz) + i * p.lddz;
-    for (int64_t c = threadIdx.x; c < p.v; c += kThreads) {
-      float g = 0.f;
-      if (c == tok) g = o.own;
-      else if (o.factor != 0.f) {
-        const float x = widen(z[c]);
-        g = -o.factor * ex2(o.far ? (x - o.k) * p.scale : fmaf(x, p.scale, -o.k));
+  constexpr int N = Vec<TZ>::N;
+  const int lane = threadIdx.x & 31;
+  const int64_t task = (int64_t)blockIdx.x * kWarps + (threadIdx.x >> 5), i = task / p.parts;
+  if (i >= p.r) return;
+  const int64_t tok = index_of(p.tokens, p.idx64, i);
+  const TZ *z = static_cast<const TZ *>(p.z) + i * p.ldz;
+  TZ *dz = static_cast<TZ *>(p.dz) + i * p.lddz;
+  const WarpPart<TZ> part(z, p.v, (int)(task - i * p.parts), p.per);
+  const bool together = ((reinterpret_cast<uintptr_t>(z) ^ reinterpret_cast<uintptr_t>(dz)) & 15) == 0;
+  after_first();
+  RowOut o = p.rows[i];
+  if (p.row_slopes) {
+    const float slope = p.row_slopes[i];
+    o.factor = slope == 0.f ? 0.f : o.factor * slope;
+    o.own = slope == 0.f ? 0.f : o.own * slope;
+  }
+  const bool still = o.factor == 0.f;   // (not for a NaN)
+  const int64_t slot = tok >= 0 && tok < p.v ? tok + part.pad : -1;
+  const auto turned = [&](float x) { return still ? 0.f : -o.factor * ex2(o.far ? (x - o.k) * p.scale : fmaf(x, p.scale, -o.k)); };
+  const auto element = [&](int64_t s) { narrow(dz + s - part.pad, s == slot ? o.own : turned(still ? 0.f : widen(z[s - part.pad]))); };
+  if (together && !o.far) {
+    const uint4 *from = reinterpret_cast<const uint4 *>(z - part.pad) + part.w0 + lane;
+    uint4 *to = reinterpret_cast<uint4 *>(dz - part.pad) + part.w0 + lane;
+    const int count = part.w1 - part.w0 - lane;
+    const Val<2> shift = all<2>(-o.k), by = all<2>(p.scale), factor = all<2>(-o.factor);
+    const int64_t at = slot / N - part.w0 - lane;
+    constexpr int kBatch = 8;
+#pragma unroll
+    for (int h = 0; h < kVectors; h += kBatch) {
+      Vec<TZ> a[kBatch];
+#pragma unroll
+      for (int u = 0; u < kBatch; ++u)
+        if (!still && 32 * (h + u) < count) a[u].w = __ldcs(from + 32 * (h + u));
+#pragma unroll
+      for (int u = 0; u < kBatch; ++u) {
+        if (32 * (h + u) >= count) break;
+        if (still) {
+          a[u].w = make_uint4(0, 0, 0, 0);
+        } else {
+#pragma unroll
+          for (int e = 0; e < Vec<TZ>::P; ++e) {
+            Val<2> y = fma(pair(a[u], e), by, shift);
+            y.x = ex2(y.x);
+            y.y = ex2(y.y);
+            set_pair(a[u], e, mul(y, factor));
+          }
+        }
+        __stcs(to + 32 * (h + u), a[u].w);
       }
-      narrow(dz + c, g);
     }
+    if (part.edge >= 0) element(part.edge);
+    __syncwarp();
+    if (slot >= 0 && at >= 0 && at < count && at % 32 == 0) narrow(dz + tok, o.own);   // by the lane that wrote over it
+  } else {
+    for (int64_t s = (int64_t)part.w0 * N + lane; s < (int64_t)part.w1 * N; s += 32) element(s);
+    if (part.edge >= 0) element(part.edge);
   }
 }
 
 constexpr int64_t kMost = ((int64_t)1 << 31) - 1024;
-bool sizes_ok(int64_t r, int64_t v) { return r >= 0 && r < ((int64_t)1 << 28) && v >= 1 && v < kMost; }
+bool sizes_ok(int64_t r, int64_t v) { return r >= 0 && r < ((int64_t)1 << 28) && v >= 1 && v < kMost && r * ceil_div(v, 4 * kPart) < kMost; }
 
 bool common_ok(int64_t r, int64_t v, int64_t ldz, int64_t lddz, int32_t logits_type, int32_t index_type, float temperature) {
   return sizes_ok(r, v) && ldz >= v && lddz >= v && is_type(logits_type) && is_index(index_type) && temperature > 0.f && std::isfinite(temperature);
 }
 
-TokenArgs common(const void *z, const void *tokens, void *dz, int64_t r, int64_t v, int64_t ldz, int64_t lddz, int32_t index_type, float temperature,
-                 void *workspace) {
+int64_t parts_of(int64_t v, int32_t logits_type) {
+  const int64_t n = 16 / type_bytes(logits_type);
+  return ceil_div(ceil_div(v + n - 1, n), kPart);
+}
+
+TokenArgs common(int32_t what, const void *z, const void *tokens, void *dz, int64_t r, int64_t v, int64_t ldz, int64_t lddz, int32_t logits_type,
+                 int32_t index_type, float temperature, void *workspace) {
   TokenArgs p{};
+  p.what = what;
   p.z = z; p.tokens = tokens; p.dz = dz;
   p.r = r; p.v = v; p.ldz = ldz; p.lddz = lddz;
   p.scale = (float)(1.4426950408889634 / (double)temperature);
   p.temperature = temperature;
   p.idx64 = index_type == DSGD_I64;
-  p.rows = dz ? static_cast<RowOut *>(workspace) : nullptr;
-  p.slopes = reinterpret_cast<double *>(static_cast<RowOut *>(workspace) + r);
+  const int64_t n = 16 / type_bytes(logits_type), vectors = ceil_div(v + n - 1, n);   // of the row on the least fortunate boundary
+  p.parts = (int32_t)parts_of(v, logits_type);
+  p.per = (int32_t)ceil_div(vectors, p.parts);
+  RowOut *rows = static_cast<RowOut *>(workspace);
+  p.rows = dz ? rows : nullptr;
+  p.sums = reinterpret_cast<float2 *>(rows + r);
+  p.row_logp = reinterpret_cast<float *>(p.sums + r * p.parts);
+  p.row_slopes = what == kPreference && dz ? p.row_logp + r : nullptr;
   return p;
 }
 
@@ -265,19 +383,22 @@ bool workspace_ok(const void *workspace, size_t bytes, int64_t r, int64_t v, int
   return workspace && bytes >= dsgd_token_workspace_bytes(r, v, pairs) && !(reinterpret_cast<uintptr_t>(workspace) & 15);
 }
 
-ceca_status_t run(const TokenArgs &p, int32_t logits_type, cudaStream_t s) {
-  const bool wide = logits_type == DSGD_F32;
-  const unsigned grid = (unsigned)std::min<int64_t>(p.r, (int64_t)sm_count() * 8);
+template <typename TZ> cudaError_t run(const TokenArgs &p, cudaStream_t s) {
+  cudaError_t e = cudaSuccess;
+  const unsigned parts = (unsigned)ceil_div(p.r * p.parts, kWarps);
   if (p.r > 0) {
-    if (wide) sum_kernel<float><<<grid, kThreads, 0, s>>>(p);
-    else sum_kernel<bf16><<<grid, kThreads, 0, s>>>(p);
+    sum_kernel<TZ><<<parts, kThreads, 0, s>>>(p);
+    e = cudaGetLastError();
+    if (e == cudaSuccess) e = launch_after(join_kernel<TZ>, p, dim3((unsigned)ceil_div(p.r, kWarps)), kThreads, 0, s);
   }
-  if (p.what == kPreference && p.pairs > 0) pair_kernel<<<(unsigned)std::min<int64_t>(p.pairs, 1024), kThreads, 0, s>>>(p);
-  if (p.dz && p.r > 0) {
-    if (wide) turn_kernel<float><<<grid, kThreads, 0, s>>>(p);
-    else turn_kernel<bf16><<<grid, kThreads, 0, s>>>(p);
-  }
-  return cudaGetLastError() == cudaSuccess ? CECA_OK : CECA_ERR_CUDA;
+  if (e == cudaSuccess && p.what == kPreference && p.pairs > 0) e = launch_after(pair_kernel, p, dim3((unsigned)std::min<int64_t>(p.pairs, 1 << 20)), kPairThreads, 0, s);
+  if (e == cudaSuccess && p.dz && p.r > 0) e = launch_after(turn_kernel<TZ>, p, dim3(parts), kThreads, 0, s);
+  return e;
+}
+
+ceca_status_t run(const TokenArgs &p, int32_t logits_type, void *stream) {
+  const cudaStream_t s = static_cast<cudaStream_t>(stream);
+  return (logits_type == DSGD_F32 ? run<float>(p, s) : run<bf16>(p, s)) == cudaSuccess ? CECA_OK : CECA_ERR_CUDA;
 }
 
 ceca_status_t policy_call(const void *z, const void *tokens, const float *old_logp, const float *advantage, const float *ref_logp, const float *weight,
@@ -291,11 +412,10 @@ ceca_status_t policy_call(const void *z, const void *tokens, const float *old_lo
   if (!z || !tokens || !old_logp || !advantage || !loss) return CECA_ERR_INVALID_ARG;
   if (dz == z && lddz != ldz) return CECA_ERR_UNSUPPORTED;
   if (!workspace_ok(workspace, workspace_bytes, r, v, 0)) return CECA_ERR_WORKSPACE;
-  TokenArgs p = common(z, tokens, dz, r, v, ldz, lddz, index_type, temperature, workspace);
-  p.what = kPolicy;
+  TokenArgs p = common(kPolicy, z, tokens, dz, r, v, ldz, lddz, logits_type, index_type, temperature, workspace);
   p.old_logp = old_logp; p.advantage = advantage; p.ref_logp = ref_logp; p.weight = weight; p.loss = loss; p.logp = logp;
   p.low = 1.f - clip_low; p.high = 1.f + clip_high; p.kl = kl;
-  return run(p, logits_type, static_cast<cudaStream_t>(stream));
+  return run(p, logits_type, stream);
 }
 
 ceca_status_t preference_call(const void *z, const void *tokens, const void *bounds, const float *ref_logp, const float *weight, float *loss,
@@ -309,13 +429,11 @@ ceca_status_t preference_call(const void *z, const void *tokens, const void *bou
   if (r == 0 && pairs == 0) return CECA_OK;
   if (dz == z && dz && lddz != ldz) return CECA_ERR_UNSUPPORTED;
   if (!workspace_ok(workspace, workspace_bytes, r, v, pairs)) return CECA_ERR_WORKSPACE;
-  TokenArgs p = common(z, tokens, dz, r, v, ldz, lddz, index_type, temperature, workspace);
-  p.what = kPreference;
-  p.row_logp = reinterpret_cast<float *>(p.slopes + 2 * pairs);
+  TokenArgs p = common(kPreference, z, tokens, dz, r, v, ldz, lddz, logits_type, index_type, temperature, workspace);
   p.bounds = bounds; p.bounds64 = bounds_type == DSGD_I64;
   p.ref_logp = ref_logp; p.weight = weight; p.loss = loss; p.logp = logp; p.pairs = pairs;
   p.beta = beta; p.smoothing = smoothing; p.average = average != 0;
-  return run(p, logits_type, static_cast<cudaStream_t>(stream));
+  return run(p, logits_type, stream);
 }
 
 }  // namespace
@@ -325,7 +443,7 @@ using namespace ceca;
 
 extern "C" size_t dsgd_token_workspace_bytes(int64_t r, int64_t v, int64_t pairs) {
   if (!sizes_ok(r, v) || pairs < 0 || pairs >= ((int64_t)1 << 27)) return 0;
-  return (sizeof(RowOut) + sizeof(float)) * (size_t)r + 2 * sizeof(double) * (size_t)pairs;
+  return (size_t)r * (sizeof(RowOut) + sizeof(float2) * (size_t)parts_of(v, DSGD_F32) + 2 * sizeof(float)) + 16;
 }
 
 extern "C" ceca_status_t dsgd_token_logprob(const void *z, const void *tokens, float *logp, int64_t r, int64_t v, int64_t ldz, int32_t logits_type,
@@ -334,10 +452,9 @@ extern "C" ceca_status_t dsgd_token_logprob(const void *z, const void *tokens, f
   if (r == 0) return CECA_OK;
   if (!z || !tokens || !logp) return CECA_ERR_INVALID_ARG;
   if (!workspace_ok(workspace, workspace_bytes, r, v, 0)) return CECA_ERR_WORKSPACE;
-  TokenArgs p = common(z, tokens, nullptr, r, v, ldz, v, index_type, temperature, workspace);
-  p.what = kLogprob;
+  TokenArgs p = common(kLogprob, z, tokens, nullptr, r, v, ldz, v, logits_type, index_type, temperature, workspace);
   p.logp = logp;
-  return run(p, logits_type, static_cast<cudaStream_t>(stream));
+  return run(p, logits_type, stream);
 }
 
 extern "C" ceca_status_t dsgd_policy_loss(const void *z, const void *tokens, const float *old_logp, const float *advantage, const float *ref_logp,
