@@ -4,6 +4,7 @@
 //
 // A row is summed without its token: with R = sum of 2^(z c - k) over the others and y the token's exponent in that frame, 1 - q = R / (R + 2^y)
 // and l = -log(1 + R / 2^y) keep their digits where the model is sure, and the others' share of the gradient is (c / T) (1 - q) / R each.
+#include <cooperative_groups.h>
 #include <cuda_runtime.h>
 
 #include <algorithm>
@@ -34,6 +35,7 @@ struct TokenArgs {
   float scale, temperature, low, high, kl, beta, smoothing;   // scale = log2(e) / T
   int32_t idx64, bounds64, average, what;
   int32_t parts, per;   // of a row, and vectors of each
+  int32_t ranks;        // CTAs that hold a row
   RowOut *rows;         // workspace, r of each; NULL without a gradient
   float2 *sums;         // r x parts
   float *row_logp, *row_slopes;   // of the preference loss, the second with a gradient
@@ -83,6 +85,7 @@ __device__ __forceinline__ RowOut row_out(const TokenArgs &p, const RowSum &s, c
 constexpr int kWarps = 4, kThreads = 32 * kWarps;
 // Warps work on their own: on a part of a row of up to 16 vectors a lane, whose loads are all under way at a time.
 constexpr int kVectors = 16, kPart = 32 * kVectors;
+constexpr int kMostRanks = 8;   // CTAs of a cluster
 
 // The part of a row that a warp takes, in slots: slot s is element s - pad, so that vectors of N slots lie on 16-byte boundaries.  Whole vectors are
 // [w0, w1); what the row has before and after them in this part goes one to a lane (`edge`, a slot, or -1).
@@ -160,6 +163,48 @@ template <typename TZ> __global__ void __launch_bounds__(kThreads) sum_kernel(co
   follow_early();
 }
 
+// The sums of a far row, by a warp, element by element.
+template <typename TZ> __device__ __noinline__ void far_sums(const TokenArgs &p, const TZ *z, int64_t tok, float own, RowSum &s) {
+  const int lane = threadIdx.x & 31;
+  float m = -INFINITY, sum = 0.f;
+  for (int64_t c = lane; c < p.v; c += 32)
+    if (c != tok) m = fmaxf(m, widen(z[c]));
+  m = warp_max(m);
+  s.k = m == -INFINITY ? own : m;
+  for (int64_t c = lane; c < p.v; c += 32) {
+    const float x = widen(z[c]);
+    if (c != tok) sum += m == -INFINITY ? (x == -INFINITY ? 0.f : NAN) : ex2((x - s.k) * p.scale);
+  }
+  s.rest = warp_sum(sum);
+}
+// The token's exponent in the frame of the others.
+__device__ __forceinline__ float own_exponent(const TokenArgs &p, const RowSum &s, float own) {
+  return own == -INFINITY ? own : own == INFINITY ? NAN : s.far ? (own - s.k) * p.scale : fmaf(own, p.scale, -s.k);
+}
+// What is written of a row besides its gradient, by one thread; and what the gradient needs.
+__device__ __forceinline__ RowOut finish_row(const TokenArgs &p, int64_t i, const RowSum &s, float w, bool writes) {
+  const Odds o = odds_of(s);
+  RowOut out = row_out(p, s, o, 1.f);   // of the preference loss: the sequence's slope comes later
+  if (p.what == kLogprob && writes) p.logp[i] = o.logp;
+  if (p.what == kPolicy) {
+    const float2 l = policy(p, i, w, o.logp);
+    out = row_out(p, s, o, l.y);
+    if (writes) p.loss[i] = l.x;
+    if (writes && p.logp) p.logp[i] = o.logp;
+  }
+  if (p.what == kPreference && writes) p.row_logp[i] = o.logp;
+  if (p.rows && writes) p.rows[i] = out;
+  if (p.row_slopes && writes) p.row_slopes[i] = 0.f;   // of rows outside all sequences
+  return out;
+}
+__device__ __forceinline__ void finish_dead_row(const TokenArgs &p, int64_t i) {
+  if (p.what == kLogprob || (p.what == kPolicy && p.logp)) p.logp[i] = 0.f;
+  if (p.what == kPolicy) p.loss[i] = 0.f;
+  if (p.what == kPreference) p.row_logp[i] = 0.f;
+  if (p.rows) p.rows[i] = {0.f, 0.f, 0.f, 0};
+  if (p.row_slopes) p.row_slopes[i] = 0.f;
+}
+
 // A warp joins a row's parts: its token's log-probability, the loss, and what the gradient needs.
 template <typename TZ> __global__ void __launch_bounds__(kThreads) join_kernel(const TokenArgs p) {
   const int lane = threadIdx.x & 31;
@@ -183,42 +228,162 @@ template <typename TZ> __global__ void __launch_bounds__(kThreads) join_kernel(c
     }
     s.rest = warp_sum(sum);
     s.far = !(fabsf(s.k) < kFar && s.rest < INFINITY);
-    if (s.far) {   // exponents beyond +-kFar, infinities or NaN: once more, element by element
-      float m = -INFINITY;
-      for (int64_t c = lane; c < p.v; c += 32)
-        if (c != tok) m = fmaxf(m, widen(z[c]));
-      m = warp_max(m);
-      s.k = m == -INFINITY ? own : m;
-      sum = 0.f;
-      for (int64_t c = lane; c < p.v; c += 32) {
-        const float x = widen(z[c]);
-        if (c != tok) sum += m == -INFINITY ? (x == -INFINITY ? 0.f : NAN) : ex2((x - s.k) * p.scale);
-      }
-      s.rest = warp_sum(sum);
-    }
-    s.y = own == -INFINITY ? own : own == INFINITY ? NAN : s.far ? (own - s.k) * p.scale : fmaf(own, p.scale, -s.k);
-    const Odds o = odds_of(s);
-    if (lane == 0) {
-      if (p.what == kLogprob) p.logp[i] = o.logp;
-      if (p.what == kPolicy) {
-        const float2 l = policy(p, i, w, o.logp);
-        p.loss[i] = l.x;
-        if (p.logp) p.logp[i] = o.logp;
-        if (p.rows) p.rows[i] = row_out(p, s, o, l.y);
-      }
-      if (p.what == kPreference) {
-        p.row_logp[i] = o.logp;
-        if (p.rows) p.rows[i] = row_out(p, s, o, 1.f);   // the sequence's slope comes later
-      }
-    }
+    if (s.far) far_sums(p, z, tok, own, s);   // exponents beyond +-kFar, infinities or NaN
+    s.y = own_exponent(p, s, own);
+    finish_row(p, i, s, w, lane == 0);
   } else if (in && lane == 0) {
-    if (p.what == kLogprob || (p.what == kPolicy && p.logp)) p.logp[i] = 0.f;
-    if (p.what == kPolicy) p.loss[i] = 0.f;
-    if (p.what == kPreference) p.row_logp[i] = 0.f;
-    if (p.rows) p.rows[i] = {0.f, 0.f, 0.f, 0};
+    finish_dead_row(p, i);
   }
-  if (in && lane == 0 && p.row_slopes) p.row_slopes[i] = 0.f;   // of rows outside all sequences
   follow_early();
+}
+
+// ---------------------------------------------------------------------------------------------- rows held in registers
+// A warp, a CTA, or a cluster of CTAs reads a row once: its vectors stay in the threads' registers, 16 each, from the sum to the gradient.  The warps' sums meet
+// in one exchange.  THREADS 32: each of a CTA's warps has a row of its own.
+
+template <typename TZ, int THREADS, bool CLUSTER> __global__ void __launch_bounds__(THREADS == 32 ? kThreads : THREADS, THREADS == 256 ? 2 : 5) hold_kernel(const __grid_constant__ TokenArgs p) {
+  constexpr int N = Vec<TZ>::N, W = THREADS / 32, kShares = W * (CLUSTER ? kMostRanks : 1);
+  __shared__ float2 share[kShares];
+  const int lane = threadIdx.x & 31, warp = THREADS == 32 ? 0 : threadIdx.x >> 5, tid = THREADS == 32 ? lane : threadIdx.x;
+  const int ranks = CLUSTER ? p.ranks : 1;
+  const int64_t i = THREADS == 32 ? (int64_t)blockIdx.x * kWarps + (threadIdx.x >> 5) : CLUSTER ? blockIdx.x / ranks : blockIdx.x;
+  const int rank = CLUSTER ? (int)(blockIdx.x - i * ranks) : 0;
+  if (CLUSTER) cluster_arrive(false);   // every CTA of the cluster runs before anybody writes into its shared memory
+  if (THREADS == 32 && i >= p.r) return;
+  const int64_t tok = index_of(p.tokens, p.idx64, i);
+  const TZ *z = static_cast<const TZ *>(p.z) + i * p.ldz;
+  TZ *dz = p.dz && p.what == kPolicy ? static_cast<TZ *>(p.dz) + i * p.lddz : nullptr;
+  // whole vectors of the row, [v0, v0 + count) this CTA's; what lies before and behind them goes to the first and last CTA, an element a thread
+  const int pad = (int)((reinterpret_cast<uintptr_t>(z) & 15) / sizeof(TZ)), begin = pad > 0, end = (int)(((uint32_t)p.v + pad) / N), per = (max(end - begin, 0) + ranks - 1) / ranks;
+  const int v0 = begin + min(rank * per, max(end - begin, 0)), left = max(0, min(per, end - v0)), count = left - tid;
+  int64_t edge = -1;
+  if (rank == 0 && pad > 0 && tid < N && tid >= pad && tid < p.v + pad) edge = tid - pad;
+  if (rank == ranks - 1 && tid >= N && tid < 2 * N && end >= begin) {
+    const int64_t c = (int64_t)end * N + tid - N - pad;
+    if (c < p.v) edge = c;
+  }
+  const bool together = ((reinterpret_cast<uintptr_t>(z) ^ reinterpret_cast<uintptr_t>(dz)) & 15) == 0;
+  const uint4 *from = reinterpret_cast<const uint4 *>(z - pad) + v0 + tid;
+  uint4 *to = reinterpret_cast<uint4 *>(dz - pad) + v0 + tid;   // used where z and dz lie together
+  const int64_t c0 = (int64_t)v0 * N - pad, c1 = c0 + (int64_t)left * N;   // the elements of the CTA's whole vectors
+  float w;
+  if (!is_live(p, i, tok, w)) {
+    if (CLUSTER) cluster_wait();
+    if (tid == 0 && rank == 0) finish_dead_row(p, i);
+    if (!dz) return;
+    if (together)
+      for (int j = 0; j < count; j += THREADS) __stcs(to + j, make_uint4(0, 0, 0, 0));
+    else
+      for (int64_t c = c0 + tid; c < c1; c += THREADS) narrow(dz + c, 0.f);
+    if (edge >= 0) narrow(dz + edge, 0.f);
+    return;
+  }
+  Vec<TZ> a[kVectors];
+#pragma unroll
+  for (int u = 0; u < kVectors; ++u) {
+    a[u] = all_least<TZ>();
+    if (THREADS * u < count) a[u].w = __ldcs(from + THREADS * u);
+  }
+  const float own = widen(z[tok]), e = edge >= 0 && edge != tok ? widen(z[edge]) : -INFINITY;
+  const int64_t slot = tok + pad, at = slot / N - v0 - tid;   // the token's vector, as this thread counts
+  const bool mine = at >= 0 && at < count && at % THREADS == 0;
+  if (mine) {
+#pragma unroll
+    for (int u = 0; u < kVectors; ++u)
+      if (at == THREADS * u) strike(a[u], 1u << (slot % N));
+  }
+  RowSum s;
+  const float k = warp_max(fmaxf(frame_of(fmaxf(e, top_of<kVectors>(a)), p.scale), -kFar));
+  {
+    const Val<2> shift = all<2>(-k), by = all<2>(p.scale);
+    Val<2> sum{ex2(fmaf(e, p.scale, -k)), 0.f};
+#pragma unroll
+    for (int u = 0; u < kVectors; ++u) {
+      if (THREADS * u >= count) break;
+#pragma unroll
+      for (int q = 0; q < Vec<TZ>::P; ++q) {
+        Val<2> y = fma(pair(a[u], q), by, shift);
+        y.x = ex2(y.x);
+        y.y = ex2(y.y);
+        sum = add(sum, y);
+      }
+    }
+    s.k = k;
+    s.rest = warp_sum(sum.x + sum.y);
+  }
+  if (CLUSTER) {
+    cluster_wait();
+    if (lane < ranks) *cooperative_groups::this_cluster().map_shared_rank(share + rank * W + warp, lane) = make_float2(s.k, s.rest);
+    cluster_arrive(true);
+    cluster_wait();
+  } else if (W > 1) {
+    if (lane == 0) share[warp] = make_float2(s.k, s.rest);
+    __syncthreads();
+  }
+  if (W > 1) {   // a share a lane (of 64 two), in one order for all
+    float2 q[(kShares + 31) / 32];
+#pragma unroll
+    for (int j = 0; j < (kShares + 31) / 32; ++j) {
+      q[j] = lane + 32 * j < W * ranks ? share[lane + 32 * j] : make_float2(-INFINITY, 0.f);
+      s.k = j == 0 ? q[j].x : fmaxf(s.k, q[j].x);
+    }
+    s.k = warp_max(s.k);
+    float sum = 0.f;
+#pragma unroll
+    for (int j = 0; j < (kShares + 31) / 32; ++j)
+      if (lane + 32 * j < W * ranks) sum += q[j].y * ex2(q[j].x - s.k);
+    s.rest = warp_sum(sum);
+  }
+  s.far = !(fabsf(s.k) < kFar && s.rest < INFINITY);   // the same for all
+  if (s.far) {
+    far_sums(p, z, tok, own, s);
+    if (CLUSTER) {   // (dz may be z)
+      cluster_arrive(false);
+      cluster_wait();
+    } else if (W > 1) {
+      __syncthreads();
+    }
+  }
+  s.y = own_exponent(p, s, own);
+  const RowOut o = finish_row(p, i, s, w, tid == 0 && rank == 0);
+  if (!dz) return;
+  const bool still = o.factor == 0.f;   // (not for a NaN)
+  const auto turned = [&](float x) { return still ? 0.f : -o.factor * ex2(s.far ? (x - o.k) * p.scale : fmaf(x, p.scale, -o.k)); };
+  if (together && !s.far) {
+    const Val<2> shift = all<2>(-o.k), by = all<2>(p.scale), factor = all<2>(-o.factor);
+#pragma unroll
+    for (int u = 0; u < kVectors; ++u) {
+      if (THREADS * u >= count) break;
+      if (still) {
+        a[u].w = make_uint4(0, 0, 0, 0);
+      } else {
+#pragma unroll
+        for (int q = 0; q < Vec<TZ>::P; ++q) {
+          Val<2> y = fma(pair(a[u], q), by, shift);
+          y.x = ex2(y.x);
+          y.y = ex2(y.y);
+          set_pair(a[u], q, mul(y, factor));
+        }
+      }
+      __stcs(to + THREADS * u, a[u].w);
+    }
+    if (mine) narrow(dz + tok, o.own);   // by the thread that wrote over it
+  } else {
+    for (int64_t c = c0 + tid; c < c1; c += THREADS) narrow(dz + c, c == tok ? o.own : turned(still ? 0.f : widen(z[c])));
+  }
+  if (edge >= 0) narrow(dz + edge, edge == tok ? o.own : turned(e));
+}
+
+template <typename TZ, int THREADS, bool CLUSTER> cudaError_t launch_hold(const TokenArgs &p, cudaStream_t s) {
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3((unsigned)(THREADS == 32 ? ceil_div(p.r, kWarps) : p.r * p.ranks));
+  cfg.blockDim = dim3(THREADS == 32 ? kThreads : THREADS);
+  cfg.stream = s;
+  cudaLaunchAttribute at{};
+  at.id = cudaLaunchAttributeClusterDimension;
+  at.val.clusterDim = {(unsigned)p.ranks, 1, 1};
+  if (CLUSTER) { cfg.attrs = &at; cfg.numAttrs = 1; }
+  return cudaLaunchKernelEx(&cfg, hold_kernel<TZ, THREADS, CLUSTER>, p);
 }
 
 __device__ __forceinline__ int64_t bound(const TokenArgs &p, int64_t j) { return min(max(index_of(p.bounds, p.bounds64, j), (int64_t)0), p.r); }
@@ -383,16 +548,32 @@ bool workspace_ok(const void *workspace, size_t bytes, int64_t r, int64_t v, int
   return workspace && bytes >= dsgd_token_workspace_bytes(r, v, pairs) && !(reinterpret_cast<uintptr_t>(workspace) & 15);
 }
 
-template <typename TZ> cudaError_t run(const TokenArgs &p, cudaStream_t s) {
+// Which form a call takes: a row that 128 threads hold is read once whatever is wanted of it, a longer one where its gradient follows from
+// its own sum, as long as a cluster holds it.
+template <typename TZ> cudaError_t run(TokenArgs p, cudaStream_t s) {
   cudaError_t e = cudaSuccess;
   const unsigned parts = (unsigned)ceil_div(p.r * p.parts, kWarps);
-  if (p.r > 0) {
+  const int64_t whole = p.v / Vec<TZ>::N;
+  p.ranks = 1;
+  while (p.ranks < kMostRanks && whole > (int64_t)kThreads * kVectors * p.ranks) p.ranks *= 2;
+  const bool turns = p.dz && p.what == kPolicy && whole <= (int64_t)256 * kVectors * kMostRanks;
+  if (turns) p.rows = nullptr;
+  if (p.r == 0) {
+  } else if (whole <= kPart) {
+    e = launch_hold<TZ, 32, false>(p, s);
+  } else if (whole <= kThreads * kVectors) {
+    e = launch_hold<TZ, kThreads, false>(p, s);
+  } else if (turns && whole <= (int64_t)kThreads * kVectors * kMostRanks) {
+    e = launch_hold<TZ, kThreads, true>(p, s);
+  } else if (turns) {
+    e = launch_hold<TZ, 256, true>(p, s);
+  } else {
     sum_kernel<TZ><<<parts, kThreads, 0, s>>>(p);
     e = cudaGetLastError();
     if (e == cudaSuccess) e = launch_after(join_kernel<TZ>, p, dim3((unsigned)ceil_div(p.r, kWarps)), kThreads, 0, s);
   }
   if (e == cudaSuccess && p.what == kPreference && p.pairs > 0) e = launch_after(pair_kernel, p, dim3((unsigned)std::min<int64_t>(p.pairs, 1 << 20)), kPairThreads, 0, s);
-  if (e == cudaSuccess && p.dz && p.r > 0) e = launch_after(turn_kernel<TZ>, p, dim3(parts), kThreads, 0, s);
+  if (e == cudaSuccess && p.dz && p.r > 0 && !turns) e = launch_after(turn_kernel<TZ>, p, dim3(parts), kThreads, 0, s);
   return e;
 }
 
