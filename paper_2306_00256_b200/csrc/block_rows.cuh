@@ -55,18 +55,18 @@ template <int G, int PASSES, int V> struct Place {
   // types: DSGD_F32, DSGD_BF16, kKept
   __host__ __device__ static constexpr int room(int64_t d, int32_t type) {
     if (V == 1) return type == kKept ? (int)kept_row_bytes(d) : (int)((d * (type == DSGD_BF16 ? 2 : 4) + 47) / 16 * 16);
-    return type == kKept ? (V == 8 ? 12 : 9) * kEights : (type == DSGD_BF16 ? 16 : 32) * kEights;
+    return type == kKept ? 9 * kEights : (type == DSGD_BF16 ? 16 : 32) * kEights;
   }
   __device__ static void copy(uint32_t to, const uint8_t *from, int32_t type, int d, int rank) {
     const int lane = rank & 31;
-    if (V == 8) {   // bf16, or kept: its exponents' words behind the whole numbers, one for each thread
+    if (V == 8) {   // bf16, or kept: its exponents behind the whole numbers
 #pragma unroll
       for (int j = 0; j < PASSES; ++j) {
         const int at = rank + G * j;
         if (8 * at >= d) continue;
         if (type == kKept) {
           copy_8(to + 8 * at, from + 8 * at);
-          copy_4(to + 8 * kEights + 4 * at, from + ((d + at / 4) & ~3));
+          if (at % 16 == 0) copy_4(to + 8 * kEights + at / 4, from + d + at / 4);   // (a word of exponents: d is a multiple of 8)
         } else {
           copy_16(to + 16 * at, from + 16 * at);
         }
@@ -104,8 +104,7 @@ template <int G, int PASSES, int V> struct Place {
       if (8 * at >= d) return r;
       if (type == kKept) {
         const uint2 q = reinterpret_cast<const uint2 *>(place)[at];
-        const uint32_t e = reinterpret_cast<const uint32_t *>(place + 8 * kEights)[at] >> 8 * ((d + at / 4) & 3) & 255u;
-        const Val<2> step = all<2>(step8(e));
+        const Val<2> step = all<2>(step8(place[8 * kEights + at / 4]));
 #pragma unroll
         for (int i = 0; i < 4; ++i) r.v[i] = mul(whole_numbers(i < 2 ? q.x : q.y, 2 * (i & 1)), step);
       } else {
