@@ -238,18 +238,151 @@ template <typename TZ> __global__ void __launch_bounds__(kThreads) join_kernel(c
 }
 
 // ---------------------------------------------------------------------------------------------- rows held in registers
-// A warp, a CTA, or a cluster of CTAs reads a row once: its vectors stay in the threads' registers, 16 each, from the sum to the gradient.  The warps' sums meet
-// in one exchange.  THREADS 32: each of a CTA's warps has a row of its own.
+// Rows are read once: their vectors stay in the threads' registers, 16 each, from the sum to the gradient.
 
-template <typename TZ, int THREADS, bool CLUSTER> __global__ void __launch_bounds__(THREADS == 32 ? kThreads : THREADS, THREADS == 256 ? 2 : 5) hold_kernel(const __grid_constant__ TokenArgs p) {
+// Of short rows a warp holds ROWS, 16 / ROWS vectors of each a lane.  What is computed of a row but once, lane j does for row j (modulo ROWS): that
+// costs as much as all the exponentials of 500 logits.
+template <typename TZ, int ROWS> __global__ void __launch_bounds__(kThreads, 5) short_kernel(const __grid_constant__ TokenArgs p) {
+  constexpr int N = Vec<TZ>::N, V = kVectors / ROWS;
+  const int lane = threadIdx.x & 31, j0 = lane % ROWS;
+  const int64_t first = ((int64_t)blockIdx.x * kWarps + (threadIdx.x >> 5)) * ROWS, i = first + j0;   // this lane's row
+  if (first >= p.r) return;
+  const bool in = i < p.r;
+  const int64_t tok = in ? index_of(p.tokens, p.idx64, i) : -1;
+  float w = 0.f;
+  const bool live = in && is_live(p, i, tok, w);
+  const TZ *z = static_cast<const TZ *>(p.z) + first * p.ldz;
+  TZ *dz = p.dz && p.what == kPolicy ? static_cast<TZ *>(p.dz) + first * p.lddz : nullptr;
+  const float own = live ? widen(z[j0 * p.ldz + tok]) : 0.f;
+  const uint32_t lives = __ballot_sync(0xffffffffu, live);
+  // of row j: whole vectors [begin, end), the element before or behind them that is this lane's, or -1
+  const auto pad_of = [&](int j) { return (int)(((uint32_t)reinterpret_cast<uintptr_t>(z) + (uint32_t)j * (uint32_t)p.ldz * (uint32_t)sizeof(TZ) & 15) / sizeof(TZ)); };
+  const auto end_of = [&](int pad) { return (int)(((uint32_t)p.v + pad) / N); };
+  const auto edge_of = [&](int pad) {
+    const int end = end_of(pad);
+    if (lane < N) return pad > 0 && lane >= pad && lane < p.v + pad ? lane - pad : -1;
+    const int c = end * N + lane - N - pad;
+    return lane < 2 * N && end >= (pad > 0) && c < p.v ? c : -1;
+  };
+  Vec<TZ> a[ROWS][V];
+  float edges[ROWS];
+#pragma unroll
+  for (int j = 0; j < ROWS; ++j) {
+    const int pad = pad_of(j), begin = pad > 0, count = end_of(pad) - begin - lane;
+    const uint4 *from = reinterpret_cast<const uint4 *>(z + j * p.ldz - pad) + begin + lane;
+    const bool there = lives >> j & 1;
+#pragma unroll
+    for (int u = 0; u < V; ++u) {
+      a[j][u] = all_least<TZ>();
+      if (there && 32 * u < count) a[j][u].w = __ldcs(from + 32 * u);
+    }
+    const int edge = edge_of(pad);
+    edges[j] = there && edge >= 0 ? widen(z[j * p.ldz + edge]) : -INFINITY;
+  }
+  RowSum s;
+  s.k = s.rest = 0.f;
+#pragma unroll
+  for (int j = 0; j < ROWS; ++j) {
+    const int pad = pad_of(j), begin = pad > 0, count = end_of(pad) - begin - lane;
+    const int t = __shfl_sync(0xffffffffu, (int)tok, j);   // (of a live row it is below 2^31)
+    if (!(lives >> j & 1)) continue;
+    const int slot = t + pad, at = slot / N - begin - lane;   // the token's vector, as this lane counts
+    if (at >= 0 && at < count && at % 32 == 0) {
+#pragma unroll
+      for (int u = 0; u < V; ++u)
+        if (at == 32 * u) strike(a[j][u], 1u << (slot % N));
+    }
+    if (edge_of(pad) == t) edges[j] = -INFINITY;
+    const float k = warp_max(fmaxf(frame_of(fmaxf(edges[j], top_of<V>(a[j])), p.scale), -kFar));
+    const Val<2> shift = all<2>(-k), by = all<2>(p.scale);
+    Val<2> sum{ex2(fmaf(edges[j], p.scale, -k)), 0.f};
+#pragma unroll
+    for (int u = 0; u < V; ++u) {
+      if (32 * u >= count) break;
+#pragma unroll
+      for (int q = 0; q < Vec<TZ>::P; ++q) {
+        Val<2> y = fma(pair(a[j][u], q), by, shift);
+        y.x = ex2(y.x);
+        y.y = ex2(y.y);
+        sum = add(sum, y);
+      }
+    }
+    const float rest = warp_sum(sum.x + sum.y);
+    if (j0 == j) {
+      s.k = k;
+      s.rest = rest;
+    }
+  }
+  s.far = live && !(fabsf(s.k) < kFar && s.rest < INFINITY);
+  const uint32_t fars = __ballot_sync(0xffffffffu, s.far);
+#pragma unroll 1
+  for (int j = 0; j < ROWS; ++j)
+    if (fars >> j & 1) {
+      RowSum f{};
+      far_sums(p, z + j * p.ldz, __shfl_sync(0xffffffffu, tok, j), __shfl_sync(0xffffffffu, own, j), f);
+      if (j0 == j) {
+        s.k = f.k;
+        s.rest = f.rest;
+      }
+    }
+  RowOut o{0.f, 0.f, 0.f, 0};
+  if (live) {
+    s.y = own_exponent(p, s, own);
+    o = finish_row(p, i, s, w, lane < ROWS);
+  } else if (in && lane < ROWS) {
+    finish_dead_row(p, i);
+  }
+  if (!dz) return;
+#pragma unroll
+  for (int j = 0; j < ROWS; ++j) {
+    if (first + j >= p.r) break;
+    const float k = __shfl_sync(0xffffffffu, o.k, j), by_all = __shfl_sync(0xffffffffu, o.factor, j), at_token = __shfl_sync(0xffffffffu, o.own, j);
+    const int t = (lives >> j & 1) ? __shfl_sync(0xffffffffu, (int)tok, j) : -1;
+    const bool far = fars >> j & 1, still = by_all == 0.f;   // (not for a NaN)
+    const TZ *row = z + j * p.ldz;
+    TZ *drow = dz + j * p.lddz;
+    const int pad = pad_of(j), begin = pad > 0, end = end_of(pad), count = end - begin - lane, edge = edge_of(pad);
+    const auto turned = [&](float x) { return still ? 0.f : -by_all * ex2(far ? (x - k) * p.scale : fmaf(x, p.scale, -k)); };
+    if (((reinterpret_cast<uintptr_t>(row) ^ reinterpret_cast<uintptr_t>(drow)) & 15) == 0 && !far) {
+      uint4 *to = reinterpret_cast<uint4 *>(drow - pad) + begin + lane;
+      const Val<2> shift = all<2>(-k), by = all<2>(p.scale), factor = all<2>(-by_all);
+#pragma unroll
+      for (int u = 0; u < V; ++u) {
+        if (32 * u >= count) break;
+        if (still) {
+          a[j][u].w = make_uint4(0, 0, 0, 0);
+        } else {
+#pragma unroll
+          for (int q = 0; q < Vec<TZ>::P; ++q) {
+            Val<2> y = fma(pair(a[j][u], q), by, shift);
+            y.x = ex2(y.x);
+            y.y = ex2(y.y);
+            set_pair(a[j][u], q, mul(y, factor));
+          }
+        }
+        __stcs(to + 32 * u, a[j][u].w);
+      }
+      if (t >= 0) {   // by the lane that wrote over it
+        const int at = (t + pad) / N - begin - lane;
+        if (at >= 0 && at < count && at % 32 == 0) narrow(drow + t, at_token);
+      }
+    } else {
+      for (int c = begin * N - pad + lane; c < end * N - pad; c += 32) narrow(drow + c, c == t ? at_token : turned(still ? 0.f : widen(row[c])));
+    }
+    if (edge >= 0) narrow(drow + edge, edge == t ? at_token : turned(edges[j]));
+  }
+}
+
+// A CTA or a cluster of CTAs holds a longer row.  The warps' sums meet in one exchange.
+
+template <typename TZ, int THREADS, bool CLUSTER> __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 2 : 5) hold_kernel(const __grid_constant__ TokenArgs p) {
   constexpr int N = Vec<TZ>::N, W = THREADS / 32, kShares = W * (CLUSTER ? kMostRanks : 1);
   __shared__ float2 share[kShares];
-  const int lane = threadIdx.x & 31, warp = THREADS == 32 ? 0 : threadIdx.x >> 5, tid = THREADS == 32 ? lane : threadIdx.x;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int ranks = CLUSTER ? p.ranks : 1;
-  const int64_t i = THREADS == 32 ? (int64_t)blockIdx.x * kWarps + (threadIdx.x >> 5) : CLUSTER ? blockIdx.x / ranks : blockIdx.x;
+  const int64_t i = CLUSTER ? blockIdx.x / ranks : blockIdx.x;
   const int rank = CLUSTER ? (int)(blockIdx.x - i * ranks) : 0;
   if (CLUSTER) cluster_arrive(false);   // every CTA of the cluster runs before anybody writes into its shared memory
-  if (THREADS == 32 && i >= p.r) return;
   const int64_t tok = index_of(p.tokens, p.idx64, i);
   const TZ *z = static_cast<const TZ *>(p.z) + i * p.ldz;
   TZ *dz = p.dz && p.what == kPolicy ? static_cast<TZ *>(p.dz) + i * p.lddz : nullptr;
@@ -316,11 +449,11 @@ template <typename TZ, int THREADS, bool CLUSTER> __global__ void __launch_bound
     if (lane < ranks) *cooperative_groups::this_cluster().map_shared_rank(share + rank * W + warp, lane) = make_float2(s.k, s.rest);
     cluster_arrive(true);
     cluster_wait();
-  } else if (W > 1) {
+  } else {
     if (lane == 0) share[warp] = make_float2(s.k, s.rest);
     __syncthreads();
   }
-  if (W > 1) {   // a share a lane (of 64 two), in one order for all
+  {   // a share a lane (of 64 two), in one order for all
     float2 q[(kShares + 31) / 32];
 #pragma unroll
     for (int j = 0; j < (kShares + 31) / 32; ++j) {
@@ -340,7 +473,7 @@ template <typename TZ, int THREADS, bool CLUSTER> __global__ void __launch_bound
     if (CLUSTER) {   // (dz may be z)
       cluster_arrive(false);
       cluster_wait();
-    } else if (W > 1) {
+    } else {
       __syncthreads();
     }
   }
@@ -376,14 +509,18 @@ template <typename TZ, int THREADS, bool CLUSTER> __global__ void __launch_bound
 
 template <typename TZ, int THREADS, bool CLUSTER> cudaError_t launch_hold(const TokenArgs &p, cudaStream_t s) {
   cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3((unsigned)(THREADS == 32 ? ceil_div(p.r, kWarps) : p.r * p.ranks));
-  cfg.blockDim = dim3(THREADS == 32 ? kThreads : THREADS);
+  cfg.gridDim = dim3((unsigned)(p.r * p.ranks));
+  cfg.blockDim = dim3(THREADS);
   cfg.stream = s;
   cudaLaunchAttribute at{};
   at.id = cudaLaunchAttributeClusterDimension;
   at.val.clusterDim = {(unsigned)p.ranks, 1, 1};
   if (CLUSTER) { cfg.attrs = &at; cfg.numAttrs = 1; }
   return cudaLaunchKernelEx(&cfg, hold_kernel<TZ, THREADS, CLUSTER>, p);
+}
+template <typename TZ, int ROWS> cudaError_t launch_short(const TokenArgs &p, cudaStream_t s) {
+  short_kernel<TZ, ROWS><<<(unsigned)ceil_div(p.r, kWarps * ROWS), kThreads, 0, s>>>(p);
+  return cudaGetLastError();
 }
 
 __device__ __forceinline__ int64_t bound(const TokenArgs &p, int64_t j) { return min(max(index_of(p.bounds, p.bounds64, j), (int64_t)0), p.r); }
@@ -559,8 +696,9 @@ template <typename TZ> cudaError_t run(TokenArgs p, cudaStream_t s) {
   const bool turns = p.dz && p.what == kPolicy && whole <= (int64_t)256 * kVectors * kMostRanks;
   if (turns) p.rows = nullptr;
   if (p.r == 0) {
-  } else if (whole <= kPart) {
-    e = launch_hold<TZ, 32, false>(p, s);
+  } else if (whole <= kPart) {   // several rows a warp where there are enough of them to keep all SMs at work
+    const bool many = p.r >= 32 * (int64_t)sm_count();
+    e = many && whole <= kPart / 4 ? launch_short<TZ, 4>(p, s) : many && whole <= kPart / 2 ? launch_short<TZ, 2>(p, s) : launch_short<TZ, 1>(p, s);
   } else if (whole <= kThreads * kVectors) {
     e = launch_hold<TZ, kThreads, false>(p, s);
   } else if (turns && whole <= (int64_t)kThreads * kVectors * kMostRanks) {

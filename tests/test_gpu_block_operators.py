@@ -424,6 +424,39 @@ def test_policy_loss_and_gradient(r, v, dtype, it, temperature, kl):
     _close(ceca.dsgd_policy_loss(z, tok, old, adv, **kw), want["loss"], "loss alone")
 
 
+@pytest.mark.parametrize("r,v,ld", [(4800, 60, 60), (4801, 203, 203), (4739, 500, 504), (4736, 2040, 2040), (4740, 900, 901), (5001, 13, 13)])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_losses_of_many_short_rows(r, v, ld, dtype):
+    src, tok, old, adv, ref, w = _policy_inputs(r, v, dtype, 1.0, 41)
+    for row, x in ((9, NAN), (10, INF), (11, -INF), (3000, 2.0**100)):   # rows that take the slow way, beside others
+        src[row, ::2] = x
+    z, _ = _inside((r, v), (ld, 1), 0, dtype)
+    z.copy_(src)
+    out, buf = _inside((r, v), (ld, 1), 0, dtype)
+    kw = dict(ref_logp=ref, weight=w, kl=0.1, clip_high=0.3)
+    loss, dz = ceca.dsgd_policy_grad(z, tok, old, adv, dz=out, **kw)
+    want = blocks.policy(_np(src), _np(tok), _np(old), _np(adv), _np(ref), _np(w), high=0.3, kl=np.float64(np.float32(0.1)), bf16=dtype == BF16)
+    fine = np.isfinite(want["loss"][0])
+    for i in (9, 10, 11, 3000):   # (the ratio was made for other logits)
+        fine[i] = False
+    ok = torch.from_numpy(fine).to(DEV)
+    _close(loss[ok], tuple(x[fine] for x in want["loss"]), "loss")
+    _close(dz[ok], tuple(x[fine] for x in want["dz"]), "dz")
+    assert _untouched(out, buf)
+    _close(ceca.dsgd_token_logprob(z, tok), blocks.token_logprob(_np(src), _np(tok)), "logp")
+    bounds = [0, r // 3, r // 2, r // 2 + 1, r - 5]
+    tok2 = tok.clone()
+    tok2[[9, 10, 11, 1]] = -1
+    got = ceca.dsgd_preference_grad(z, tok2, torch.tensor(bounds, device=DEV), average=True)
+    want = blocks.preference(_np(src), _np(tok2), bounds, average=True, bf16=dtype == BF16, beta=np.float64(np.float32(0.1)))
+    for g, k in zip(got, ("loss", "logp", "dz")):
+        _close(g, want[k], k)
+    same = z.clone() if ld == v else None
+    if same is not None:
+        l2, d2 = ceca.dsgd_policy_grad(same, tok, old, adv, dz=same, **kw)
+        assert torch.equal(l2.nan_to_num(), loss.nan_to_num()) and torch.equal(d2.nan_to_num(), dz.nan_to_num())
+
+
 PAIRS = [  # r, v, bounds
     (2, 5, [0, 1, 2]), (40, 33, [0, 7, 7, 20, 38]), (300, 501, [3, 100, 180, 180, 290]), (64, 4099, [0, 30, 64]), (12, 50001, [0, 5, 12]),
     (700, 2050, [0, 100, 230, 300, 460, 600, 690]), (9, 7, [0, 0, 0, 4, 9]), (30, 32000, [0, 10, 29]),
