@@ -600,7 +600,7 @@ template <typename TZ> __global__ void __launch_bounds__(kThreads) turn_kernel(c
   const WarpPart<TZ> part(z, p.v, (int)(task - i * p.parts), p.per);
   const bool together = ((reinterpret_cast<uintptr_t>(z) ^ reinterpret_cast<uintptr_t>(dz)) & 15) == 0;
   after_first();
-  RowOut o = p.rows[i];
+  RowOut o = p.rows ? p.rows[i] : RowOut{};
   if (p.row_slopes) {
     const float slope = p.row_slopes[i];
     o.factor = slope == 0.f ? 0.f : o.factor * slope;
@@ -682,11 +682,13 @@ TokenArgs common(int32_t what, const void *z, const void *tokens, void *dz, int6
 }
 
 bool workspace_ok(const void *workspace, size_t bytes, int64_t r, int64_t v, int64_t pairs) {
-  return workspace && bytes >= dsgd_token_workspace_bytes(r, v, pairs) && !(reinterpret_cast<uintptr_t>(workspace) & 15);
+  const size_t need = dsgd_token_workspace_bytes(r, v, pairs);
+  return need == 0 || (workspace && bytes >= need && !(reinterpret_cast<uintptr_t>(workspace) & 15));
 }
 
 // Which form a call takes: a row that 128 threads hold is read once whatever is wanted of it, a longer one where its gradient follows from
-// its own sum, as long as a cluster holds it.
+// its own sum, as long as a cluster holds it, or where there are so few that one launch instead of two is what counts (256 rows of 32000
+// bf16: 7.6 us in two, 6.1 in one).  Other rows are streamed.
 template <typename TZ> cudaError_t run(TokenArgs p, cudaStream_t s) {
   cudaError_t e = cudaSuccess;
   const unsigned parts = (unsigned)ceil_div(p.r * p.parts, kWarps);
@@ -695,13 +697,13 @@ template <typename TZ> cudaError_t run(TokenArgs p, cudaStream_t s) {
   while (p.ranks < kMostRanks && whole > (int64_t)kThreads * kVectors * p.ranks) p.ranks *= 2;
   const bool turns = p.dz && p.what == kPolicy && whole <= (int64_t)256 * kVectors * kMostRanks;
   if (turns) p.rows = nullptr;
-  if (p.r == 0) {
+  if (p.r == 0 || (p.what == kPreference && p.pairs == 0)) {
   } else if (whole <= kPart) {   // several rows a warp where there are enough of them to keep all SMs at work
     const bool many = p.r >= 32 * (int64_t)sm_count();
     e = many && whole <= kPart / 4 ? launch_short<TZ, 4>(p, s) : many && whole <= kPart / 2 ? launch_short<TZ, 2>(p, s) : launch_short<TZ, 1>(p, s);
   } else if (whole <= kThreads * kVectors) {
     e = launch_hold<TZ, kThreads, false>(p, s);
-  } else if (turns && whole <= (int64_t)kThreads * kVectors * kMostRanks) {
+  } else if ((turns || p.r * p.ranks <= 5 * (int64_t)sm_count()) && whole <= (int64_t)kThreads * kVectors * kMostRanks) {
     e = launch_hold<TZ, kThreads, true>(p, s);
   } else if (turns) {
     e = launch_hold<TZ, 256, true>(p, s);
@@ -752,6 +754,10 @@ ceca_status_t preference_call(const void *z, const void *tokens, const void *bou
   p.bounds = bounds; p.bounds64 = bounds_type == DSGD_I64;
   p.ref_logp = ref_logp; p.weight = weight; p.loss = loss; p.logp = logp; p.pairs = pairs;
   p.beta = beta; p.smoothing = smoothing; p.average = average != 0;
+  if (pairs == 0) {   // a gradient of 0, for which nothing is summed
+    p.rows = nullptr;
+    p.row_slopes = nullptr;
+  }
   return run(p, logits_type, stream);
 }
 
@@ -761,7 +767,7 @@ ceca_status_t preference_call(const void *z, const void *tokens, const void *bou
 using namespace ceca;
 
 extern "C" size_t dsgd_token_workspace_bytes(int64_t r, int64_t v, int64_t pairs) {
-  if (!sizes_ok(r, v) || pairs < 0 || pairs >= ((int64_t)1 << 27)) return 0;
+  if (!sizes_ok(r, v) || pairs < 0 || pairs >= ((int64_t)1 << 27) || (pairs == 0 && v <= 4 * kThreads * kVectors)) return 0;   // (rows of so many are held)
   return (size_t)r * (sizeof(RowOut) + sizeof(float2) * (size_t)parts_of(v, DSGD_F32) + 2 * sizeof(float)) + 16;
 }
 

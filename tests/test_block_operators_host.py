@@ -218,15 +218,17 @@ def test_gradients_refuse_outputs_that_are_missing_or_crossed(name, args):
 
 
 def test_losses_refuse_a_workspace_that_does_not_do():
-    size = ceca.dsgd_token_workspace_bytes(2, 8, 1)
-    less = ceca.dsgd_token_workspace_bytes(2, 8)
-    assert size >= less
+    assert ceca.dsgd_token_workspace_bytes(2, 8) == 0 < ceca.dsgd_token_workspace_bytes(2, 8, 1)
+    size = ceca.dsgd_token_workspace_bytes(2, 9000, 1)
+    assert size >= ceca.dsgd_token_workspace_bytes(2, 9000) > 0
     for ws, have in ((None, 0), (ODD, size)):
         for name, args in (("dsgd_token_logprob", LOGP), ("dsgd_policy_loss", PLOSS), ("dsgd_policy_grad", PGRAD), ("dsgd_preference_loss", QLOSS),
                            ("dsgd_preference_grad", QGRAD)):
-            assert _call(name, args, ws=ws, size=have) == WORKSPACE
-    assert _call("dsgd_preference_grad", QGRAD, size=size - 1) == WORKSPACE
-    for bad in ((-1, 8, 0), (2, 0, 0), (2, 8, -1), (1 << 28, 8, 0)):
+            wide = dict(v=9000, ldz=9000) | (dict(lddz=9000) if "lddz" in args else {})
+            assert _call(name, args, ws=ws, size=have, **wide) == WORKSPACE
+    assert _call("dsgd_preference_loss", QLOSS, v=9000, ldz=9000, size=size - 1) == WORKSPACE
+    assert _call("dsgd_preference_loss", QLOSS, ws=None) == WORKSPACE
+    for bad in ((-1, 8, 0), (2, 0, 0), (2, 8, -1), (1 << 28, 8, 0), (1 << 27, 1 << 20, 0)):
         assert ceca.dsgd_token_workspace_bytes(*bad) == 0
 
 
