@@ -5,6 +5,10 @@
 //
 // Forward: two sums over the group a row, y^2 and h_out^2.  Gradient, with q = s g w_post yn (what the block added), f = w_pre du and t = dh_out + r f:
 // the three sums A = hn f, B = q t, C = q hn at once, then m = A / d, dh = t - r m hn and mean(yn e) = (B - r m C) / d.
+//
+// Bytes and instructions bound these kernels together: some 30 instructions a channel forward, 50 in the gradient.  Of the measured copy rate they reach
+// (8 x 4096 x 2048, silu gates) 0.82 forward and 0.90 in the gradient in bf16, 0.85 and 0.82 with an fp32 stream, 0.82 and 0.69 where 8 bits are written
+// and read; rows of 771 fp32 channels 0.81 and 0.75, of 2047 bf16 channels, read and written one by one, 0.58 and 0.44.
 #pragma once
 #include <cuda_runtime.h>
 
@@ -47,6 +51,7 @@ template <int G, int V> __device__ __forceinline__ int channel(int rank, int j, 
 struct Pairs8 {
   Val<2> v[4];
 };
+
 // A place in shared memory for a row of a tensor, or for a kept row, and its copy and reading.  V = 8 and 4: each warp copies what it will read, in
 // whole sectors.  V = 1: the group copies the 16-byte words that the row touches (of the first and last one the bytes inside the row
 // count), and must meet between copying and reading.
@@ -263,7 +268,6 @@ __device__ __forceinline__ float total(const Pairs8 &a) {
   return s.x + s.y;
 }
 
-
 // A tensor's rows that a group takes: the next one to copy, and where one lies.
 struct Walk {
   const uint8_t *at;
@@ -425,7 +429,7 @@ __global__ void __launch_bounds__(G * groups_of(G), resident_block(G, PASSES)) b
 }
 
 template <int G, int PASSES, int V, int TS, int TA, bool KEPT, int PARTS>
-__global__ void __launch_bounds__(G * groups_of(G), resident_grad(G, PASSES)) block_grad_kernel(const __grid_constant__ BlockArgs p) {
+__global__ void __launch_bounds__(G * groups_of(G), resident_grad(G)) block_grad_kernel(const __grid_constant__ BlockArgs p) {
   using X = Place<G, PASSES, V>;
   extern __shared__ uint4 ring[];
   __shared__ alignas(16) float sums[2][4 * (G / 32)];
@@ -657,7 +661,7 @@ template <int G, int PASSES, int V, int TS, int TA, bool KEPT, int PARTS> cudaEr
   p.room[3] = p.w_pre ? X::room(p.d, p.act_type) : 0;
   p.room[4] = p.dh_out.at ? X::room(p.d, p.stream_type) : 0;
   p.stage_bytes = p.room[0] + p.room[1] + p.room[2] + p.room[3] + p.room[4] + stats_room(G);
-  p.stages = (int32_t)std::max<int64_t>(1, std::min<int64_t>(4, (int64_t)(200 << 10) / (resident_grad(G, PASSES) * kGroups * p.stage_bytes)));
+  p.stages = (int32_t)std::max<int64_t>(1, std::min<int64_t>(4, (int64_t)(200 << 10) / (resident_grad(G) * kGroups * p.stage_bytes)));
   const int64_t bytes = std::max((int64_t)p.stages * p.stage_bytes * kGroups, kGroups > 1 ? kGroups * 8 * p.d : 0);
   if (bytes > kMostShared) return cudaErrorInvalidConfiguration;
   p.part_count = (int32_t)block_grad_parts(p.n, p.t, p.d);
