@@ -190,10 +190,10 @@ template <int G, int PASSES, int V> struct Place {
       uint32_t top = __float_as_uint(most);
       top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
       top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+      const bool cut = __any_sync(0xffffffffu, cut8(top));   // of one warp in thirty: a branch, not a choice for each
       if (8 * at >= d) return;
       const uint32_t e = exponent8(top);
       const Val<2> by = all<2>(scale8(e));
-      const bool cut = cut8(top);
       uint2 q = make_uint2(hold_four(x.v[0], x.v[1], by, cut), hold_four(x.v[2], x.v[3], by, cut));
       if (e == 255u) q = make_uint2(0, 0);
       reinterpret_cast<uint2 *>(row)[at] = q;
@@ -205,9 +205,10 @@ template <int G, int PASSES, int V> struct Place {
         uint32_t top = __float_as_uint(greatest(greatest(0.f, x.v[2 * k]), x.v[2 * k + 1]));
 #pragma unroll
         for (int o = 1; o < 8; o *= 2) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
+        const bool cut = __any_sync(0xffffffffu, cut8(top));
         if (4 * at >= d) continue;
         const uint32_t e = exponent8(top);
-        reinterpret_cast<uint32_t *>(row)[at] = e == 255u ? 0 : hold_four(x.v[2 * k], x.v[2 * k + 1], all<2>(scale8(e)), cut8(top));
+        reinterpret_cast<uint32_t *>(row)[at] = e == 255u ? 0 : hold_four(x.v[2 * k], x.v[2 * k + 1], all<2>(scale8(e)), cut);
         if (at % 8 == 0) row[d + at / 8] = (uint8_t)e;
       }
     } else {

@@ -4,7 +4,8 @@
 // in a row and goes from row to row, so that nothing is divided on the way.  Keeping, the lanes that share a block of 32 channels find its largest
 // magnitude by exchange; where x does not start on a 16-byte boundary a lane shifts its channels out of two words.  Bringing back, a lane takes the
 // 16-byte words of x, and shifts the whole numbers.
-// 8 x 8192 x 2048 bf16: kept in 87 us, brought back in 75 (0.71 and 0.82 of the measured copy rate).
+// 8 x 8192 x 2048 bf16: kept in 80 us, brought back in 71 (0.77 and 0.88 of the measured copy rate); 2047
+// channels, shifted: 133 and 101.
 #include <cuda_runtime.h>
 
 #include <algorithm>
@@ -16,23 +17,34 @@
 namespace ceca {
 namespace {
 
-// Few rows at a time and many more CTAs than run at once: that way some read while others write, and the last ones end together.  (8 x 8192 x 2048 bf16: 87 us
-// kept, 75 brought back; with 4 rows, or one CTA for each place on an SM, 90 to 105 and 80 to 110.)
-constexpr int kThreads = 256, kDeep = 2, kWaves = 64;
+// Few rows at a time and many more CTAs than run at once: that way some read while others write, and the last ones end together.  (8 x 8192 x 2048 bf16: 80 us
+// kept, 71 brought back; with 4 rows at a time, or one CTA for each place on an SM, 10 to 30 us more.)
+constexpr int kThreads = 256, kDeep = 2, kWaves = 48;
 
 struct KeepArgs {
   dsgd_rows_t x;
   uint8_t *kept;
-  int64_t t, rows, row_bytes, hop, rounds;   // a thread takes kDeep neighbouring rows of every kDeep hop, so many times
-  int32_t d, blocks, per_row, flat;          // vectors of a row; flat: the rows lie at equal distances throughout
+  int64_t t, rows, row_bytes, hop, step_x, step_kept;   // a thread takes kDeep neighbouring rows of every kDeep hop, so many times
+  int32_t rounds, d, blocks, per_row, flat;          // vectors of a row; flat: the rows lie at equal distances throughout
 };
 
-template <typename T> __device__ __forceinline__ T *row_of(const KeepArgs &p, int64_t row) {
-  T *x = static_cast<T *>(p.x.at);
-  if (p.flat) return x + row * p.x.row_stride;
-  const int64_t agent = row / p.t;
-  return x + agent * p.x.agent_stride + (row - agent * p.t) * p.x.row_stride;
-}
+// The rows that a thread takes: row 0 to kDeep - 1 from `row` on, then kDeep hop further.
+template <typename T> struct Rows {
+  int64_t row;
+  T *x;            // of rows at equal distances
+  uint8_t *kept;
+  __device__ __forceinline__ Rows(const KeepArgs &p, uint32_t first) : row((int64_t)first * kDeep), x(static_cast<T *>(p.x.at) + row * p.x.row_stride), kept(p.kept + row * p.row_bytes) {}
+  __device__ __forceinline__ T *at(const KeepArgs &p, int u) const {
+    if (p.flat) return x + u * p.x.row_stride;
+    const int64_t agent = (row + u) / p.t;
+    return static_cast<T *>(p.x.at) + agent * p.x.agent_stride + (row + u - agent * p.t) * p.x.row_stride;
+  }
+  __device__ __forceinline__ void next(const KeepArgs &p) {
+    row += p.hop * kDeep;
+    x += p.step_x;
+    kept += p.step_kept;
+  }
+};
 
 // N values of 16 bytes, in pairs.
 template <int N> struct Values {
@@ -42,6 +54,16 @@ __device__ __forceinline__ Values<4> widened(uint4 a, const float *) { return {{
 __device__ __forceinline__ Values<8> widened(uint4 a, const bf16 *) { return {{unpack_bf16(a.x), unpack_bf16(a.y), unpack_bf16(a.z), unpack_bf16(a.w)}}; }
 __device__ __forceinline__ uint4 narrowed(const Values<4> &a) { return make_uint4(__float_as_uint(a.v[0].x), __float_as_uint(a.v[0].y), __float_as_uint(a.v[1].x), __float_as_uint(a.v[1].y)); }
 __device__ __forceinline__ uint4 narrowed(const Values<8> &a) { return make_uint4(pack_bf16(a.v[0]), pack_bf16(a.v[1]), pack_bf16(a.v[2]), pack_bf16(a.v[3])); }
+
+// The bits of the largest magnitude of 16 bytes of values (two bf16 at a time).
+__device__ __forceinline__ uint32_t top_of(uint4 a, const float *) {
+  const uint32_t m = 0x7fffffffu;
+  return max(max(a.x & m, a.y & m), max(a.z & m, a.w & m));
+}
+__device__ __forceinline__ uint32_t top_of(uint4 a, const bf16 *) {
+  const uint32_t m = 0x7fff7fffu, t = __vmaxu2(__vmaxu2(a.x & m, a.y & m), __vmaxu2(a.z & m, a.w & m));
+  return max(t << 16, t & 0xffff0000u);
+}
 
 // 16 bytes from any boundary on, of a row that ends at `end` (what lies behind is anything).
 template <bool WORDS> __device__ __forceinline__ uint4 take(const void *at, const void *end) {
@@ -62,41 +84,40 @@ template <bool WORDS> __device__ __forceinline__ uint4 take(const void *at, cons
 
 template <typename T, bool WORDS> __global__ void __launch_bounds__(kThreads, 6) keep_kernel(const __grid_constant__ KeepArgs p) {
   constexpr int N = 16 / sizeof(T);
-  const int64_t id = (int64_t)blockIdx.x * kThreads + threadIdx.x, first = id / p.per_row;
+  const uint32_t id = blockIdx.x * kThreads + threadIdx.x, first = id / (uint32_t)p.per_row;
   const int c = N * (int)(id - first * p.per_row);
-  const bool here = first < p.hop && c < p.d;
-  for (int64_t i = 0; i < p.rounds; ++i) {   // the same for all, who exchange
-    const int64_t row = (first + i * p.hop) * kDeep;
+  const bool taken = first < p.hop, here = taken && c < p.d;
+  Rows<const T> at(p, first);
+  for (int i = 0; i < p.rounds; ++i, at.next(p)) {   // the same for all, who exchange
     uint4 a[kDeep];
 #pragma unroll
     for (int u = 0; u < kDeep; ++u) {
       a[u] = make_uint4(0, 0, 0, 0);
-      if (!here || row + u >= p.rows) continue;
-      const T *x = row_of<const T>(p, row + u);
+      if (!here || at.row + u >= p.rows) continue;
+      const T *x = at.at(p, u);
       a[u] = take<WORDS>(x + c, x + p.d);
     }
 #pragma unroll
     for (int u = 0; u < kDeep; ++u) {
-      Values<N> v = widened(a[u], static_cast<const T *>(nullptr));
-      if (!WORDS && c + N > p.d) {   // the row's last ones
+      if (!WORDS && c + N > p.d) {   // what lies behind the row's last ones
+        uint8_t *bytes = reinterpret_cast<uint8_t *>(&a[u]);
 #pragma unroll
-        for (int k = 0; k < N; ++k)
-          if (c + k >= p.d) (k & 1 ? v.v[k / 2].y : v.v[k / 2].x) = 0.f;
+        for (int k = 0; k < 16; ++k)
+          if (c + k / (int)sizeof(T) >= p.d) bytes[k] = 0;
       }
-      float most = 0.f;
-#pragma unroll
-      for (int k = 0; k < N / 2; ++k) most = greatest(most, v.v[k]);
-      uint32_t top = __float_as_uint(most);
+      const Values<N> v = widened(a[u], static_cast<const T *>(nullptr));
+      uint32_t top = top_of(a[u], static_cast<const T *>(nullptr));
 #pragma unroll
       for (int o = 1; o < kBlock8 / N; o *= 2) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
-      if (first >= p.hop || row + u >= p.rows) continue;
-      uint8_t *to = p.kept + (row + u) * p.row_bytes;
+      const bool cut = __any_sync(0xffffffffu, cut8(top));   // of one warp in thirty: a branch, not a choice for each
+      if (!taken || at.row + u >= p.rows) continue;
+      uint8_t *to = at.kept + u * p.row_bytes;
       const uint32_t e = exponent8(top);
       if (c < p.d) {
         const Val<2> by = all<2>(scale8(e));
         uint32_t q[2];
 #pragma unroll
-        for (int k = 0; k < N / 4; ++k) q[k] = e == 255u ? 0 : hold_four(v.v[2 * k], v.v[2 * k + 1], by, cut8(top));
+        for (int k = 0; k < N / 4; ++k) q[k] = e == 255u ? 0 : hold_four(v.v[2 * k], v.v[2 * k + 1], by, cut);
         if (!WORDS && c + N > p.d) {
           for (int k = 0; c + k < p.d; ++k) to[c + k] = (uint8_t)(q[k / 4] >> 8 * (k & 3));
         } else if (N == 8) {
@@ -116,20 +137,20 @@ template <typename T, bool WORDS> __global__ void __launch_bounds__(kThreads, 6)
 
 template <typename T, bool WORDS> __global__ void __launch_bounds__(kThreads, 6) bring_kernel(const __grid_constant__ KeepArgs p) {
   constexpr int N = 16 / sizeof(T);
-  const int64_t id = (int64_t)blockIdx.x * kThreads + threadIdx.x, first = id / p.per_row;
+  const uint32_t id = blockIdx.x * kThreads + threadIdx.x, first = id / (uint32_t)p.per_row;
   if (first >= p.hop) return;
   const int slot = N * (int)(id - first * p.per_row);
-  for (int64_t i = 0; i < p.rounds; ++i) {
-    const int64_t row = (first + i * p.hop) * kDeep;
+  Rows<T> rows(p, first);
+  for (int i = 0; i < p.rounds; ++i, rows.next(p)) {
     T *x[kDeep];
     int c[kDeep];
     uint32_t w[kDeep][3], e[kDeep];
 #pragma unroll
     for (int u = 0; u < kDeep; ++u) {
       c[u] = p.d;
-      if (row + u >= p.rows) continue;
-      const uint8_t *from = p.kept + (row + u) * p.row_bytes;
-      x[u] = row_of<T>(p, row + u);
+      if (rows.row + u >= p.rows) continue;
+      const uint8_t *from = rows.kept + u * p.row_bytes;
+      x[u] = rows.at(p, u);
       c[u] = WORDS ? slot : slot - (int)((reinterpret_cast<uintptr_t>(x[u]) & 15) / sizeof(T));
       if (c[u] >= p.d) continue;
       if (WORDS) {
@@ -188,7 +209,9 @@ template <typename T, bool WORDS> cudaError_t launch(const dsgd_rows_t &x, void 
   const int64_t per_row = !back ? p.blocks * (kBlock8 / N) : WORDS ? d / N : ceil_div(d + N - 1, N);
   p.per_row = (int32_t)per_row;
   p.hop = std::max<int64_t>(1, std::min(ceil_div(p.rows, kDeep), (int64_t)sm_count() * kWaves * kThreads / per_row));
-  p.rounds = ceil_div(p.rows, p.hop * kDeep);
+  p.step_x = p.hop * kDeep * x.row_stride;
+  p.step_kept = p.hop * kDeep * p.row_bytes;
+  p.rounds = (int32_t)ceil_div(p.rows, p.hop * kDeep);
   const int64_t grid = ceil_div(p.hop * per_row, kThreads);
   if (back) bring_kernel<T, WORDS><<<(unsigned)grid, kThreads, 0, s>>>(p);
   else keep_kernel<T, WORDS><<<(unsigned)grid, kThreads, 0, s>>>(p);

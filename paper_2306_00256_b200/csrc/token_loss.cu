@@ -4,6 +4,17 @@
 //
 // A row is summed without its token: with R = sum of 2^(z c - k) over the others and y the token's exponent in that frame, 1 - q = R / (R + 2^y)
 // and l = -log(1 + R / 2^y) keep their digits where the model is sure, and the others' share of the gradient is (c / T) (1 - q) / R each.
+//
+// Memory bounds it, and how often a row is read.  Where the derivative follows from the row's own sum (the policy's) it is read once, and stays in registers
+// between the sum and the gradient: several short rows a warp, 32 KB a CTA, up to 256 KB (512 KB with larger CTAs) a cluster of eight.  The preference's
+// derivative waits for the rows of two whole sequences: rows are summed in a stream of 8 KB parts, a warp each, joined, the pairs' losses taken, and
+// all are read again (from L2 no faster: the writes are what takes the time there).  The four launches begin early, each waiting for the one before.
+//
+// 2047 rows of 50001 fp32 logits: log-probabilities 64 us (0.98 of the measured copy rate), policy gradient 162 (0.77).  8192 x 128000 bf16: 299 us (all of it),
+// 816 (0.78: exponentials, 51 % of the special function units, and the exchange between eight CTAs take turns with memory).  16384 x 32000 bf16 policy gradient
+// 387 us (0.83), preference gradient 490 (0.98 for the three passes that it takes, 0.65 for two).
+// Tried for the policy's rows and slower: clusters that stay and fetch their next row to shared memory meanwhile (907 us), 256 threads of 8 vectors each
+// (915), 6 or 4 CTAs an SM instead of 5 (889, 884), and loops without a question for each vector (886).
 #include <cooperative_groups.h>
 #include <cuda_runtime.h>
 
