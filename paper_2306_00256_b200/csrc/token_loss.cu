@@ -11,7 +11,7 @@
 // all are read again (from L2 no faster: the writes are what takes the time there).  The four launches begin early, each waiting for the one before.
 //
 // 2047 rows of 50001 fp32 logits: log-probabilities 64 us (0.98 of the measured copy rate), policy gradient 162 (0.77).  8192 x 128000 bf16: 299 us (all of it),
-// 816 (0.78: exponentials, 51 % of the special function units, and the exchange between eight CTAs take turns with memory).  16384 x 32000 bf16 policy gradient
+// 816 (0.78: exponentials, 51 % of the special function units, and the exchange between eight CTAs take turns with memory).  16384 x 32000 bf16: policy gradient
 // 387 us (0.83), preference gradient 490 (0.98 for the three passes that it takes, 0.65 for two).
 // Tried for the policy's rows and slower: clusters that stay and fetch their next row to shared memory meanwhile (907 us), 256 threads of 8 vectors each
 // (915), 6 or 4 CTAs an SM instead of 5 (889, 884), and loops without a question for each vector (886).
