@@ -93,6 +93,17 @@ __device__ __forceinline__ RowOut row_out(const TokenArgs &p, const RowSum &s, c
   return {s.k, s.rest == 0.f ? 0.f : own / s.rest, own, s.far ? 1 : 0};
 }
 
+// Over a low temperature, or a large weight, a share below 2^-126 is a gradient that is not: where the factor is above 1 the frame is lowered by
+// its binades, and the factor by what that is.  A far row's exponents get them added, `lift`.
+__device__ __forceinline__ float lifted(RowOut &o) {
+  if (!(fabsf(o.factor) >= 2.f)) return 0.f;
+  const float lift = fminf((float)((int)(__float_as_uint(o.factor) >> 23 & 255u) - 127), 64.f);
+  const float low = o.far ? -lift : o.k - lift, by = o.far ? -lift : low - o.k;   // (as it is rounded)
+  if (!o.far) o.k = low;
+  o.factor *= exp2f(by);
+  return o.far ? lift : 0.f;
+}
+
 constexpr int kWarps = 4, kThreads = 32 * kWarps;
 // Warps work on their own: on a part of a row of up to 16 vectors a lane, whose loads are all under way at a time.
 constexpr int kVectors = 16, kPart = 32 * kVectors;
@@ -344,16 +355,17 @@ template <typename TZ, int ROWS> __global__ void __launch_bounds__(kThreads, 5) 
     finish_dead_row(p, i);
   }
   if (!dz) return;
+  const float my_lift = lifted(o);
 #pragma unroll
   for (int j = 0; j < ROWS; ++j) {
     if (first + j >= p.r) break;
-    const float k = __shfl_sync(0xffffffffu, o.k, j), by_all = __shfl_sync(0xffffffffu, o.factor, j), at_token = __shfl_sync(0xffffffffu, o.own, j);
+    const float lift = __shfl_sync(0xffffffffu, my_lift, j), k = __shfl_sync(0xffffffffu, o.k, j), by_all = __shfl_sync(0xffffffffu, o.factor, j), at_token = __shfl_sync(0xffffffffu, o.own, j);
     const int t = (lives >> j & 1) ? __shfl_sync(0xffffffffu, (int)tok, j) : -1;
     const bool far = fars >> j & 1, still = by_all == 0.f;   // (not for a NaN)
     const TZ *row = z + j * p.ldz;
     TZ *drow = dz + j * p.lddz;
     const int pad = pad_of(j), begin = pad > 0, end = end_of(pad), count = end - begin - lane, edge = edge_of(pad);
-    const auto turned = [&](float x) { return still ? 0.f : -by_all * ex2(far ? (x - k) * p.scale : fmaf(x, p.scale, -k)); };
+    const auto turned = [&](float x) { return still ? 0.f : -by_all * ex2(far ? fmaf(x - k, p.scale, lift) : fmaf(x, p.scale, -k)); };
     if (((reinterpret_cast<uintptr_t>(row) ^ reinterpret_cast<uintptr_t>(drow)) & 15) == 0 && !far) {
       uint4 *to = reinterpret_cast<uint4 *>(drow - pad) + begin + lane;
       const Val<2> shift = all<2>(-k), by = all<2>(p.scale), factor = all<2>(-by_all);
@@ -489,10 +501,11 @@ template <typename TZ, int THREADS, bool CLUSTER> __global__ void __launch_bound
     }
   }
   s.y = own_exponent(p, s, own);
-  const RowOut o = finish_row(p, i, s, w, tid == 0 && rank == 0);
+  RowOut o = finish_row(p, i, s, w, tid == 0 && rank == 0);
   if (!dz) return;
   const bool still = o.factor == 0.f;   // (not for a NaN)
-  const auto turned = [&](float x) { return still ? 0.f : -o.factor * ex2(s.far ? (x - o.k) * p.scale : fmaf(x, p.scale, -o.k)); };
+  const float lift = lifted(o);
+  const auto turned = [&](float x) { return still ? 0.f : -o.factor * ex2(s.far ? fmaf(x - o.k, p.scale, lift) : fmaf(x, p.scale, -o.k)); };
   if (together && !s.far) {
     const Val<2> shift = all<2>(-o.k), by = all<2>(p.scale), factor = all<2>(-o.factor);
 #pragma unroll
@@ -618,8 +631,9 @@ template <typename TZ> __global__ void __launch_bounds__(kThreads) turn_kernel(c
     o.own = slope == 0.f ? 0.f : o.own * slope;
   }
   const bool still = o.factor == 0.f;   // (not for a NaN)
+  const float lift = lifted(o);
   const int64_t slot = tok >= 0 && tok < p.v ? tok + part.pad : -1;
-  const auto turned = [&](float x) { return still ? 0.f : -o.factor * ex2(o.far ? (x - o.k) * p.scale : fmaf(x, p.scale, -o.k)); };
+  const auto turned = [&](float x) { return still ? 0.f : -o.factor * ex2(o.far ? fmaf(x - o.k, p.scale, lift) : fmaf(x, p.scale, -o.k)); };
   const auto element = [&](int64_t s) { narrow(dz + s - part.pad, s == slot ? o.own : turned(still ? 0.f : widen(z[s - part.pad]))); };
   if (together && !o.far) {
     const uint4 *from = reinterpret_cast<const uint4 *>(z - part.pad) + part.w0 + lane;

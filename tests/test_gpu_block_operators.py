@@ -694,3 +694,125 @@ def test_calls_on_two_streams_at_once(whole):
     torch.cuda.synchronize()
     for g in got:
         assert all(torch.equal(x, y) for x, y in zip(g, want))
+
+
+# ------------------------------------------------------------------------------------------------ edges
+
+
+def test_offsets_past_32_bits_in_rows():
+    # 2.2e9 channels: the last rows are those of a small call on the same rows
+    t, d, last = 530001, 4104, 5
+    g = torch.Generator(DEV).manual_seed(1)
+
+    def big(seed):
+        x = torch.empty((1, t, d), dtype=BF16, device=DEV)
+        x[:, :1000].normal_(generator=g)
+        x[:, 1000:530000].view(529, 1000, d).copy_(x[:, :1000].expand(529, 1000, d))
+        x[:, -last:].normal_(generator=g)
+        return x
+
+    h, y, a = (big(i) for i in range(3))
+    w, s = _randn((1, d), F32, 5, 1.0, 0.1), _randn((1,), F32, 6)
+    ho, u, stats, kept = ceca.dsgd_block_norm(h, y, w, w, gate=a, scale=s, save=True, keep8=True)
+    end = [x[:, -last:].contiguous() for x in (h, y, a)]
+    small = ceca.dsgd_block_norm(end[0], end[1], w, w, gate=end[2], scale=s, save=True, keep8=True)
+    assert torch.equal(ho[:, -last:], small[0]) and torch.equal(u[:, -last:], small[1]) and torch.equal(stats[:, -last:], small[2])
+    assert all(torch.equal(x[:, -last:], z) for x, z in zip(kept, small[3]))
+    du, dho = a, y
+    for src, few in (((h, y, a), end), (kept, small[3])):
+        got = ceca.dsgd_block_norm_grad(src[0], src[1], w, w, stats, du, dho, gate=src[2], scale=s)
+        want = ceca.dsgd_block_norm_grad(few[0], few[1], w, w, small[2], end[2], end[1], gate=few[2], scale=s)
+        assert all(torch.equal(x[:, -last:], z) for x, z in zip(got[:3], want[:3]))
+        del got
+    k = ceca.dsgd_keep8(u)
+    assert torch.equal(k[:, -last:], ceca.dsgd_keep8(small[1]))
+    assert torch.equal(ceca.dsgd_bring8(k, d, BF16)[:, -last:], ceca.dsgd_bring8(k[:, -last:].contiguous(), d, BF16))
+
+
+def test_offsets_past_32_bits_in_logits():
+    r, v, last = 16700, 131073, 6
+    z = torch.empty((r, v), dtype=BF16, device=DEV)
+    z[:200].normal_(generator=torch.Generator(DEV).manual_seed(2))
+    for i in range(200, r, 200):
+        z[i:i + 200].copy_(z[:min(200, r - i)])
+    z[-last:].normal_(generator=torch.Generator(DEV).manual_seed(3))
+    tok = torch.randint(0, v, (r,), generator=_gen(4)).to(DEV)
+    adv, old = _randn((r,), F32, 5), torch.full((r,), -11.0, device=DEV)
+    end, few = z[-last:].clone(), tok[-last:].clone()
+    assert torch.equal(ceca.dsgd_policy_grad(z, tok, old, adv)[1][-last:], ceca.dsgd_policy_grad(end, few, old[-last:].clone(), adv[-last:].clone())[1])
+    want = blocks.token_logprob(_np(end), _np(few))
+    _close(ceca.dsgd_token_logprob(z, tok)[-last:], want, "logp")
+    b = torch.tensor([0, r - last, r - last + 2, r - 3, r], device=DEV)
+    dz = ceca.dsgd_preference_grad(z, tok, b, average=True)[2]
+    small = blocks.preference(_np(end), _np(few), [0, 0, 2, 3, 6], average=True, bf16=True, beta=np.float64(np.float32(0.1)))
+    _close(dz[-4:], tuple(x[-4:] for x in small["dz"]), "dz")   # the second pair
+
+
+@pytest.mark.parametrize("temperature", [1e-3, 0.05, 30.0, 1e4])
+@pytest.mark.parametrize("v", [300, 20000])
+def test_losses_at_other_temperatures(temperature, v):
+    r, temp = 30, np.float64(np.float32(temperature))
+    z, tok = _logits(r, v, F32, 51)
+    z *= min(1.0, temperature * 10)   # (what a policy at that temperature has learnt)
+    lp = torch.from_numpy(blocks.token_logprob(_np(z), _np(tok), temp)[0])
+    old, adv = (lp - 0.1).float().to(DEV), _randn((r,), F32, 52)
+    loss, dz = ceca.dsgd_policy_grad(z, tok, old, adv, temperature=temperature)
+    want = blocks.policy(_np(z), _np(tok), _np(old), _np(adv), temperature=temp)
+    _close(loss, want["loss"], "loss")
+    _close(dz, want["dz"], "dz")
+    got = ceca.dsgd_preference_grad(z, tok, torch.tensor([0, 11, 30], device=DEV), temperature=temperature)
+    want = blocks.preference(_np(z), _np(tok), [0, 11, 30], temperature=temp, beta=np.float64(np.float32(0.1)))
+    for g, k in zip(got, ("loss", "logp", "dz")):
+        _close(g, want[k], k)
+
+
+def test_many_agents_of_few_rows():
+    n, t, d = 3000, 2, 40
+    b = Block(n, t, d, (F32, F32, F32), 61)
+    h, u, stats, kept = b.run(1, save=True, keep8=True)
+    want = b.want(1, 1e-6)
+    _close(h, want["h"], "h_out")
+    _close(u, want["u"], "u")
+    _check_grad(b.grad(1, kept, stats), b.want_grad(1, stats, kept=True), b.types)
+
+
+def test_block_norm_outputs_over_other_inputs():
+    # u over the gate, dy over the gate, dgate over y: each element is read before it is written
+    for d in (96, 99, 9000):
+        b = Block(2, 13, d, (BF16, BF16, F32), 71)
+        h, u, stats, _ = b.run(0, save=True)
+        g = b.gate.clone()
+        ho, uo, _, _ = ceca.dsgd_block_norm(b.h, b.y, b.w_pre, b.w_post, gate=g, scale=b.scale, u=g)
+        assert uo is g and torch.equal(ho, h) and torch.equal(g, u)
+        want = b.grad(0, (b.h, b.y, b.gate), stats)
+        y, g = b.y.clone(), b.gate.clone()
+        got = ceca.dsgd_block_norm_grad(b.h, y, b.w_pre, b.w_post, stats, b.du, b.dh_out, gate=g, scale=b.scale, dy=g, dgate=y)
+        assert all(torch.equal(x, z) for x, z in zip(got, want))
+
+
+def test_one_tensor_in_several_places():
+    # h, y and the gate may be one tensor, as inputs
+    x = _randn((2, 9, 128), F32, 81)
+    w = _randn((2, 128), F32, 82)
+    got = ceca.dsgd_block_norm(x, x, w, w, gate=x, save=True)
+    want = ceca.dsgd_block_norm(x.clone(), x.clone(), w, w, gate=x.clone(), save=True)
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
+def test_a_given_workspace_is_kept_to():
+    b = Block(2, 50, 200, (F32, F32, F32), 91)
+    _, _, stats, _ = b.run(0, save=True)
+    size = ceca.dsgd_block_norm_workspace_bytes(2, 50, 200)
+    ws = torch.full((size + 256,), 7, dtype=torch.uint8, device=DEV)
+    want = b.grad(0, (b.h, b.y, b.gate), stats)
+    got = b.grad(0, (b.h, b.y, b.gate), stats, workspace=ws[:size])
+    assert all(torch.equal(x, z) for x, z in zip(got, want)) and (ws[size:] == 7).all()
+    z, tok = _logits(900, 33000, BF16, 92)
+    size = ceca.dsgd_token_workspace_bytes(900, 33000, 2)
+    ws = torch.full((size + 256,), 7, dtype=torch.uint8, device=DEV)
+    bounds = torch.tensor([0, 100, 300, 301, 880], device=DEV)
+    want = ceca.dsgd_preference_grad(z, tok, bounds)
+    got = ceca.dsgd_preference_grad(z, tok, bounds, workspace=ws[:size])
+    assert all(torch.equal(x, y) for x, y in zip(got, want)) and (ws[size:] == 7).all()
+    size = ceca.dsgd_token_workspace_bytes(900, 33000)
+    assert torch.equal(ceca.dsgd_token_logprob(z, tok, workspace=ws[:size]), ceca.dsgd_token_logprob(z, tok))
