@@ -446,7 +446,7 @@ __global__ void __launch_bounds__(G * groups_of(G), resident_grad(G)) block_grad
   const auto room = [&](int i, int32_t type, bool there) { return V > 1 && !kAny ? there ? X::room(0, type) : 0 : p.room[i]; };
   const int off_y = room(0, held_s, true), off_g = off_y + room(1, held_a, y), off_u = off_g + room(2, held_a, gated), off_p = off_u + room(3, ta, u),
             off_s = off_p + room(4, ts, past), stage_bytes = off_s + stats_room(G);
-  uint8_t *mine = reinterpret_cast<uint8_t *>(ring) + (size_t)group * p.stages * stage_bytes;
+  uint8_t *mine = reinterpret_cast<uint8_t *>(ring) + (size_t)group * (p.stages * stage_bytes + aside_grad(G, PASSES));
   const uint32_t mine32 = smem_u32(mine);
   const auto held = [&](const dsgd_rows_t &x, int bytes) {
     return KEPT ? Walk(x, agent * p.t + first, hop, p.row_bytes) : Walk(x, agent, first, hop, bytes);
@@ -477,10 +477,25 @@ __global__ void __launch_bounds__(G * groups_of(G), resident_grad(G)) block_grad
   };
   for (int i = 0; i + 1 < p.stages; ++i) bring();
   const float scale = p.scale ? load(p.scale, p.weights_type, agent * p.scale_stride) : 1.f, over_d = 1.f / (float)p.d;
-  Pairs8 wq[PASSES], wp[PASSES];   // scale w_post, w_pre
-  Pairs8 sum_pre[PASSES], sum_post[PASSES];
+  // scale w_post and w_pre, in registers or aside
+  Pairs8 wq[PASSES], wp[PASSES];
+  float4 *aside = reinterpret_cast<float4 *>(mine + ring_bytes) + rank;
   weights<G, PASSES, V>(wq, y ? p.w_post : nullptr, p.weights_type, agent * p.w_post_stride, scale, d, rank);
   weights<G, PASSES, V>(wp, u ? p.w_pre : nullptr, p.weights_type, agent * p.w_pre_stride, 1.f, d, rank);
+  const auto put_aside = [&](const Pairs8 &w, int at) {
+    aside[2 * at * G] = make_float4(w.v[0].x, w.v[0].y, w.v[1].x, w.v[1].y);
+    aside[(2 * at + 1) * G] = make_float4(w.v[2].x, w.v[2].y, w.v[3].x, w.v[3].y);
+  };
+  const auto from_aside = [&](Pairs8 &w, int at) {
+    if (!aside_grad(G, PASSES)) return;
+    const float4 a = aside[2 * at * G], b = aside[(2 * at + 1) * G];
+    w = {{{a.x, a.y}, {a.z, a.w}, {b.x, b.y}, {b.z, b.w}}};
+  };
+  if (aside_grad(G, PASSES)) {
+    put_aside(wq[0], 0);
+    put_aside(wp[0], 1);
+  }
+  Pairs8 sum_pre[PASSES], sum_post[PASSES];
 #pragma unroll
   for (int j = 0; j < PASSES; ++j)
 #pragma unroll
@@ -501,6 +516,8 @@ __global__ void __launch_bounds__(G * groups_of(G), resident_grad(G)) block_grad
     const Val<2> rho = all<2>(now.x), r = all<2>(now.y);
     Pairs8 hn[PASSES], t[PASSES], yn[PASSES], g[PASSES], slope[PASSES];
     Val<2> a{0.f, 0.f}, b{0.f, 0.f}, c{0.f, 0.f};
+    from_aside(wq[0], 0);
+    from_aside(wp[0], 1);
 #pragma unroll
     for (int j = 0; j < PASSES; ++j) {
       Pairs8 q{};
@@ -546,6 +563,7 @@ __global__ void __launch_bounds__(G * groups_of(G), resident_grad(G)) block_grad
     }
     const float3 s = group_sums<G>(make_float3(a.x + a.y, b.x + b.y, c.x + c.y), sums, turn);
     turn ^= 1;
+    from_aside(wq[0], 0);
     const float rm = u ? now.y * s.x * over_d : 0.f, my = (s.y - rm * s.z) * over_d;
 #pragma unroll
     for (int j = 0; j < PASSES; ++j) {
@@ -656,14 +674,15 @@ template <int G, int PASSES, int V, int TS, int TA, bool KEPT, int PARTS> cudaEr
   constexpr int kGroups = groups_of(G), kThreads = G * kGroups;
   cudaError_t e = set_max_shared_once(reinterpret_cast<const void *>(kernel), kMostShared, &done);
   if (e != cudaSuccess) return e;
+  constexpr int64_t aside = kGroups * aside_grad(G, PASSES);
   p.room[0] = X::room(p.d, KEPT ? kKept : p.stream_type);
   p.room[1] = p.y.at ? X::room(p.d, KEPT ? kKept : p.act_type) : 0;
   p.room[2] = p.gate.at ? X::room(p.d, KEPT ? kKept : p.act_type) : 0;
   p.room[3] = p.w_pre ? X::room(p.d, p.act_type) : 0;
   p.room[4] = p.dh_out.at ? X::room(p.d, p.stream_type) : 0;
   p.stage_bytes = p.room[0] + p.room[1] + p.room[2] + p.room[3] + p.room[4] + stats_room(G);
-  p.stages = (int32_t)std::max<int64_t>(1, std::min<int64_t>(4, (int64_t)(200 << 10) / (resident_grad(G) * kGroups * p.stage_bytes)));
-  const int64_t bytes = std::max((int64_t)p.stages * p.stage_bytes * kGroups, kGroups > 1 ? kGroups * 8 * p.d : 0);
+  p.stages = (int32_t)std::max<int64_t>(1, std::min<int64_t>(4, ((int64_t)(200 << 10) / resident_grad(G) - aside) / (kGroups * p.stage_bytes)));
+  const int64_t bytes = std::max((int64_t)p.stages * p.stage_bytes * kGroups + aside, kGroups > 1 ? kGroups * 8 * p.d : 0);
   if (bytes > kMostShared) return cudaErrorInvalidConfiguration;
   p.part_count = (int32_t)block_grad_parts(p.n, p.t, p.d);
   p.scale_count = p.part_count * kGroups;
