@@ -174,54 +174,60 @@ template <int G, int PASSES, int V> struct Place {
       }
     }
   }
-  // keeps a row in 8 bits; whole warps call it
-  __device__ static void keep(uint8_t *row, const Pairs8 *x, int d, int rank) {
+  // Keeps a row in 8 bits; whole warps call it.  x: the thread's channels; with V = 1 it takes eight neighbours from the row's place instead, so that it
+  // writes them together and asks three lanes, not all, for their largest.
+  __device__ static void keep(uint8_t *row, const Pairs8 *x, const uint8_t *place, int pad, int32_t type, int d, int rank) {
 #pragma unroll
-    for (int j = 0; j < PASSES; ++j) keep(row, x[j], d, rank, j);
+    for (int j = 0; j < PASSES; ++j) {
+      if (V == 4) {
+        keep_fours(row, x[j], d, rank, j);
+      } else if (V == 8) {
+        keep_eight(row, x[j], d, rank + G * j);
+      } else {
+        const int c = 8 * (rank + G * j);
+        Pairs8 r{};
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          if (c + e >= d) continue;
+          const float v = type == DSGD_BF16 ? widen(reinterpret_cast<const bf16 *>(place + pad)[c + e]) : reinterpret_cast<const float *>(place + pad)[c + e];
+          (e & 1 ? r.v[e / 2].y : r.v[e / 2].x) = v;
+        }
+        keep_eight(row, r, d, rank + G * j);
+      }
+    }
     const int from = d + (int)blocks8(d), to = (int)kept_row_bytes(d);   // the bytes behind the exponents
     if (rank < to - from) row[from + rank] = 0;
   }
-  __device__ static void keep(uint8_t *row, const Pairs8 &x, int d, int rank, int j) {
-    if (V == 8) {
-      const int at = rank + G * j;
-      float most = 0.f;
+  __device__ static void keep_eight(uint8_t *row, const Pairs8 &x, int d, int at) {
+    float most = 0.f;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) most = greatest(most, x.v[i]);
-      uint32_t top = __float_as_uint(most);
-      top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
-      top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
-      const bool cut = __any_sync(0xffffffffu, cut8(top));   // of one warp in thirty: a branch, not a choice for each
-      if (8 * at >= d) return;
+    for (int i = 0; i < 4; ++i) most = greatest(most, x.v[i]);
+    uint32_t top = __float_as_uint(most);
+    top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+    top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+    const bool cut = __any_sync(0xffffffffu, cut8(top));   // of one warp in thirty: a branch, not a choice for each
+    if (8 * at >= d) return;
+    const uint32_t e = exponent8(top);
+    const Val<2> by = all<2>(scale8(e));
+    uint2 q = make_uint2(hold_four(x.v[0], x.v[1], by, cut), hold_four(x.v[2], x.v[3], by, cut));
+    if (e == 255u) q = make_uint2(0, 0);
+    if (V == 8 || 8 * at + 8 <= d) reinterpret_cast<uint2 *>(row)[at] = q;
+    else
+      for (int c = 8 * at; c < d; ++c) row[c] = (uint8_t)((c & 4 ? q.y : q.x) >> 8 * (c & 3));
+    if (at % 4 == 0) row[d + at / 4] = (uint8_t)e;
+  }
+  __device__ static void keep_fours(uint8_t *row, const Pairs8 &x, int d, int rank, int j) {
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      const int at = rank + G * (2 * j + k);
+      uint32_t top = __float_as_uint(greatest(greatest(0.f, x.v[2 * k]), x.v[2 * k + 1]));
+#pragma unroll
+      for (int o = 1; o < 8; o *= 2) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
+      const bool cut = __any_sync(0xffffffffu, cut8(top));
+      if (4 * at >= d) continue;
       const uint32_t e = exponent8(top);
-      const Val<2> by = all<2>(scale8(e));
-      uint2 q = make_uint2(hold_four(x.v[0], x.v[1], by, cut), hold_four(x.v[2], x.v[3], by, cut));
-      if (e == 255u) q = make_uint2(0, 0);
-      reinterpret_cast<uint2 *>(row)[at] = q;
-      if (at % 4 == 0) row[d + at / 4] = (uint8_t)e;
-    } else if (V == 4) {
-#pragma unroll
-      for (int k = 0; k < 2; ++k) {
-        const int at = rank + G * (2 * j + k);
-        uint32_t top = __float_as_uint(greatest(greatest(0.f, x.v[2 * k]), x.v[2 * k + 1]));
-#pragma unroll
-        for (int o = 1; o < 8; o *= 2) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
-        const bool cut = __any_sync(0xffffffffu, cut8(top));
-        if (4 * at >= d) continue;
-        const uint32_t e = exponent8(top);
-        reinterpret_cast<uint32_t *>(row)[at] = e == 255u ? 0 : hold_four(x.v[2 * k], x.v[2 * k + 1], all<2>(scale8(e)), cut);
-        if (at % 8 == 0) row[d + at / 8] = (uint8_t)e;
-      }
-    } else {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const int c = channel<G, V>(rank, j, e);
-        const float v = e & 1 ? x.v[e / 2].y : x.v[e / 2].x;
-        const uint32_t b = exponent8(__reduce_max_sync(0xffffffffu, magnitude(v)));
-        if (c < d) {
-          row[c] = (uint8_t)(int8_t)hold8(v, scale8(b));
-          if (c % kBlock8 == 0) row[d + c / kBlock8] = (uint8_t)b;
-        }
-      }
+      reinterpret_cast<uint32_t *>(row)[at] = e == 255u ? 0 : hold_four(x.v[2 * k], x.v[2 * k + 1], all<2>(scale8(e)), cut);
+      if (at % 8 == 0) row[d + at / 8] = (uint8_t)e;
     }
   }
 };
@@ -378,18 +384,18 @@ __global__ void __launch_bounds__(G * groups_of(G), resident_block(G, PASSES)) b
     float rho = 0.f;
 #pragma unroll
     for (int j = 0; j < PASSES; ++j) h[j] = X::read(at, wh.pad(), ts, d, rank, j);
-    if (p.h8) X::keep(p.h8 + kept_at, h, d, rank);
+    if (p.h8) X::keep(p.h8 + kept_at, h, at, wh.pad(), ts, d, rank);
     if (y) {
       Pairs8 a[PASSES];
 #pragma unroll
       for (int j = 0; j < PASSES; ++j) a[j] = X::read(at + off_y, wy.pad(), ta, d, rank, j);
       rho = norm(a, 0);
-      if (p.y8) X::keep(p.y8 + kept_at, a, d, rank);
+      if (p.y8) X::keep(p.y8 + kept_at, a, at + off_y, wy.pad(), ta, d, rank);
       if (gated) {
         Pairs8 g[PASSES];
 #pragma unroll
         for (int j = 0; j < PASSES; ++j) g[j] = X::read(at + off_g, wg.pad(), ta, d, rank, j);
-        if (p.gate8) X::keep(p.gate8 + kept_at, g, d, rank);
+        if (p.gate8) X::keep(p.gate8 + kept_at, g, at + off_g, wg.pad(), ta, d, rank);
 #pragma unroll
         for (int j = 0; j < PASSES; ++j)
 #pragma unroll
