@@ -194,17 +194,18 @@ __global__ void __launch_bounds__(kThreads) wide_grad_kernel(const BlockArgs p) 
 }
 
 // The parts of the weights' gradients, in the order of the rows.
-constexpr int kJoiners = 32;   // warps: as many parts are on their way at a time, and more by unrolling
+constexpr int kJoiners = 32;   // warps at most: as many parts are on their way at a time, and more by unrolling
+int joiners_of(int64_t parts) { return parts <= 8 ? 4 : parts <= 32 ? 8 : kJoiners; }
 __global__ void __launch_bounds__(32 * kJoiners) finish_kernel(const BlockArgs p) {
   __shared__ float halves[2][kJoiners][32];
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, joiners = blockDim.x >> 5;
   const int64_t agent = blockIdx.y, c = (int64_t)blockIdx.x * 32 + lane;
   const float scale = p.scale ? load(p.scale, p.weights_type, agent * p.scale_stride) : 1.f;
   float a = 0.f, b = 0.f;
   after_first();
   if (c < p.d)
 #pragma unroll 8
-    for (int q = warp; q < p.part_count; q += kJoiners) {
+    for (int q = warp; q < p.part_count; q += joiners) {
       const float *part = p.parts + ((agent * p.part_count + q) * 2) * p.d + c;
       a += part[0];
       b += part[p.d];
@@ -218,8 +219,8 @@ __global__ void __launch_bounds__(32 * kJoiners) finish_kernel(const BlockArgs p
   };
   if (warp < 2 && c < p.d) {
     float s = 0.f;
-#pragma unroll
-    for (int i = 0; i < kJoiners; ++i) s += halves[warp][i][lane];
+#pragma unroll 4
+    for (int i = 0; i < joiners; ++i) s += halves[warp][i][lane];
     if (warp == 0 && p.dw_pre) put(p.dw_pre, agent * p.dw_pre_stride + c, s);
     if (warp == 1 && p.dw_post) put(p.dw_post, agent * p.dw_post_stride + c, scale * s);
   }
@@ -268,15 +269,17 @@ ceca_status_t status(cudaError_t e) { return e == cudaSuccess ? CECA_OK : CECA_E
 
 }  // namespace
 
-// At least four rows a group: a part costs as much as two rows in memory.  Parts are counted by 148 SMs, not by the device's: the workspace's size is
-// asked for without one.
+// At least four rows a group where there are many (a part costs as much as two rows in memory), one where there are few: 16 rows of 2048 bf16 channels
+// take 7.1 us so, 10.3 with four a group, and 256 rows 10.9 with four, 12.6 with one.  Parts are counted by 148 SMs, not by the device's: the workspace's
+// size is asked for without one.
 int64_t block_grad_parts(int64_t n, int64_t t, int64_t d) {
   const Shape z = grad_shape_of(d);
-  return std::max<int64_t>(1, std::min(148 * (int64_t)resident_grad(z.group) / n, ceil_div(t, 4 * groups_of(z.group))));
+  const int64_t groups = groups_of(z.group), few = std::min<int64_t>(ceil_div(t, groups), 32);
+  return std::max<int64_t>(1, std::min(148 * (int64_t)resident_grad(z.group) / n, std::max(few, ceil_div(t, 4 * groups))));
 }
 
 cudaError_t finish_block_grad(const BlockArgs &p, cudaStream_t s) {
-  return launch_after(finish_kernel, p, dim3((unsigned)ceil_div(p.d, 32), (unsigned)p.n), 32 * kJoiners, 0, s);
+  return launch_after(finish_kernel, p, dim3((unsigned)ceil_div(p.d, 32), (unsigned)p.n), 32 * joiners_of(p.part_count), 0, s);
 }
 
 }  // namespace ceca
