@@ -91,7 +91,10 @@ __global__ void __launch_bounds__(kThreads) wide_kernel(const BlockArgs p) {
       }
       return cta_sum(s);
     };
-    const auto norm = [&](auto value) { return inverse_rms(squares(value, 1.f), 1.f / (float)p.d, p.eps, [&](float unit) { return squares(value, unit); }); };
+    const auto norm = [&](auto value) {
+      const float sum = squares(value, 1.f);
+      return sum == INFINITY ? inverse_rms_beyond(squares(value, kLess), 1.f / (float)p.d) : inverse_rms(sum, 1.f / (float)p.d, p.eps);
+    };
     const float rho = p.y.at ? norm([&](int64_t c) { return x.y_at(c); }) : 0.f;
     const float r = p.w_pre ? norm([&](int64_t c) { return x.out(c, rho); }) : 0.f;
     if (threadIdx.x == 0 && p.stats) {

@@ -34,13 +34,13 @@ struct Shape {
   int group, passes;   // threads of a group, eights of channels a thread
 };
 __host__ __device__ constexpr Shape shape_of(int64_t d) {
-  return d <= 256 ? Shape{32, 1} : d <= 512 ? Shape{32, 2} : d <= 1024 ? Shape{64, 2} : d <= 2048 ? Shape{128, 2} : d <= 4096 ? Shape{256, 2} : Shape{512, 2};
+  return d <= 64 ? Shape{8, 1} : d <= 128 ? Shape{16, 1} : d <= 256 ? Shape{32, 1} : d <= 512 ? Shape{32, 2} : d <= 1024 ? Shape{64, 2} : d <= 2048 ? Shape{128, 2} : d <= 4096 ? Shape{256, 2} : Shape{512, 2};
 }
 __host__ __device__ constexpr Shape grad_shape_of(int64_t d) {
-  return d <= 256 ? Shape{32, 1} : d <= 512 ? Shape{64, 1} : d <= 1024 ? Shape{128, 1} : d <= 2048 ? Shape{256, 1} : d <= 4096 ? Shape{512, 1} : Shape{512, 2};
+  return d <= 64 ? Shape{8, 1} : d <= 128 ? Shape{16, 1} : d <= 256 ? Shape{32, 1} : d <= 512 ? Shape{64, 1} : d <= 1024 ? Shape{128, 1} : d <= 2048 ? Shape{256, 1} : d <= 4096 ? Shape{512, 1} : Shape{512, 2};
 }
-// Groups of a CTA: rows that one warp holds share one.
-__host__ __device__ constexpr int groups_of(int group) { return group == 32 ? 4 : 1; }
+// Groups of a CTA: rows that one warp, or a part of one, holds share one.
+__host__ __device__ constexpr int groups_of(int group) { return group <= 32 ? 128 / group : 1; }
 // CTAs an SM that the kernels are compiled for: 512 threads of 128 registers (forward, with 8 channels each, 768 of 80).
 __host__ __device__ constexpr int resident_block(int group, int passes) { return (passes == 2 ? 512 : 768) / (group * groups_of(group)); }
 __host__ __device__ constexpr int resident_grad(int group) { return 512 / (group * groups_of(group)); }
@@ -91,11 +91,10 @@ __device__ __forceinline__ Gates gates_of(Val<2> a, bool silu) {
   return {sig, slope};
 }
 
-// 1 / sqrt(sum / d + eps) of a sum of squares; one that overflowed is taken again by `again`, of the values times 2^-100.
-template <typename Again> __device__ __forceinline__ float inverse_rms(float sum, float over_d, float eps, Again again) {
-  if (sum == INFINITY) return 0x1p-100f / sqrtf(again(0x1p-100f) * over_d);   // (eps is nothing beside it)
-  return rsqrtf(fmaf(sum, over_d, eps));
-}
+// 1 / sqrt(sum / d + eps) of a sum of squares, and of one that overflowed and was taken again of the values times kLess (eps is nothing beside it).
+constexpr float kLess = 0x1p-100f;
+__device__ __forceinline__ float inverse_rms(float sum, float over_d, float eps) { return rsqrtf(fmaf(sum, over_d, eps)); }
+__device__ __forceinline__ float inverse_rms_beyond(float sum, float over_d) { return kLess / sqrtf(sum * over_d); }
 #endif
 
 }  // namespace ceca

@@ -60,10 +60,11 @@ template <int G, int PASSES, int V> struct Place {
   // types: DSGD_F32, DSGD_BF16, kKept
   __host__ __device__ static constexpr int room(int64_t d, int32_t type) {
     if (V == 1) return type == kKept ? (int)kept_row_bytes(d) : (int)((d * (type == DSGD_BF16 ? 2 : 4) + 47) / 16 * 16);
-    return type == kKept ? 9 * kEights : (type == DSGD_BF16 ? 16 : 32) * kEights;
+    return type == kKept ? (9 * kEights + 31) / 16 * 16 : (type == DSGD_BF16 ? 16 : 32) * kEights;
   }
   __device__ static void copy(uint32_t to, const uint8_t *from, int32_t type, int d, int rank) {
-    const int lane = rank & 31;
+    constexpr int kLanes = G < 32 ? G : 32;   // that copy together
+    const int lane = rank % kLanes;
     if (V == 8) {   // bf16, or kept: its exponents behind the whole numbers
 #pragma unroll
       for (int j = 0; j < PASSES; ++j) {
@@ -87,13 +88,13 @@ template <int G, int PASSES, int V> struct Place {
       } else if (type == DSGD_BF16) {
 #pragma unroll
         for (int j = 0; j < PASSES; ++j) {
-          const int c = c0 + 4 * G * (2 * j + lane / 16) + 8 * (lane & 15);
+          const int c = c0 + 4 * G * (2 * j + lane / (kLanes / 2)) + 8 * (lane % (kLanes / 2));
           if (c < d) copy_16(to + 2 * c, from + 2 * c);
         }
       } else {
-        const int c = c0 + 4 * G * (lane / 8) + 16 * (lane & 7), e = c0 / kBlock8 + G / 8 * lane;   // (the last copy may take exponents with it)
-        if (lane < 16 * PASSES && c < d) copy_16(to + c, from + c);
-        if (lane < 2 * PASSES && e * kBlock8 < d) copy_4(to + d + e, from + d + e);
+        const int c = c0 + 4 * G * (lane / (kLanes / 4)) + 16 * (lane % (kLanes / 4)), e = c0 / kBlock8 + G / 8 * lane;   // (the last copy may take exponents with it)
+        if (lane < kLanes / 2 * PASSES && c < d) copy_16(to + c, from + c);
+        if (lane < (G < 32 ? 1 : 2 * PASSES) && e * kBlock8 < d) copy_4(to + d + e, from + d + e);
       }
     } else {
       const int pad = (int)(reinterpret_cast<uintptr_t>(from) & 15), end = pad + (type == kKept ? (int)kept_row_bytes(d) : d * (type == DSGD_BF16 ? 2 : 4));
@@ -195,8 +196,7 @@ template <int G, int PASSES, int V> struct Place {
         keep_eight(row, r, d, rank + G * j);
       }
     }
-    const int from = d + (int)blocks8(d), to = (int)kept_row_bytes(d);   // the bytes behind the exponents
-    if (rank < to - from) row[from + rank] = 0;
+    for (int c = d + (int)blocks8(d) + rank; c < (int)kept_row_bytes(d); c += G) row[c] = 0;   // the bytes behind the exponents
   }
   __device__ static void keep_eight(uint8_t *row, const Pairs8 &x, int d, int at) {
     float most = 0.f;
@@ -234,11 +234,12 @@ template <int G, int PASSES, int V> struct Place {
 
 // The sum over a group, in one order, the same on all its threads.  `turn` says which of two places is used: consecutive
 // sums take the other one, so that one barrier is enough.
-template <int G> __device__ __forceinline__ float group_sum(float x, float (*place)[4 * (G / 32)], int turn) {
+__host__ __device__ constexpr int warps_of(int group) { return group <= 32 ? 1 : group / 32; }
+template <int G> __device__ __forceinline__ float group_sum(float x, float (*place)[4 * warps_of(G)], int turn) {
+  constexpr int W = warps_of(G);
 #pragma unroll
-  for (int o = 16; o; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
-  if (G == 32) return x;
-  constexpr int W = G / 32;
+  for (int o = (G < 32 ? G : 32) / 2; o; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
+  if (G <= 32) return x;
   const int lane = threadIdx.x & 31;
   if (lane == 0) place[turn][threadIdx.x >> 5] = x;
   __syncthreads();
@@ -248,7 +249,8 @@ template <int G> __device__ __forceinline__ float group_sum(float x, float (*pla
   return x;
 }
 // Three sums at once: lanes first share out the numbers (x to lanes 0 to 7, y to 8 to 15, z to 16 to 23; 24 to 31 have a zero), so that most steps move one.
-template <int G> __device__ __forceinline__ float3 group_sums(float3 v, float (*place)[4 * (G / 32)], int turn) {
+template <int G> __device__ __forceinline__ float3 group_sums(float3 v, float (*place)[4 * warps_of(G)], int turn) {
+  if (G < 32) return make_float3(group_sum<G>(v.x, place, turn), group_sum<G>(v.y, place, turn), group_sum<G>(v.z, place, turn));
   const int lane = threadIdx.x & 31;
   const bool upper = lane & 16, odd = lane & 8;
   const float a = __shfl_xor_sync(0xffffffffu, upper ? v.x : v.z, 16), b = __shfl_xor_sync(0xffffffffu, upper ? v.y : 0.f, 16);
@@ -257,7 +259,7 @@ template <int G> __device__ __forceinline__ float3 group_sums(float3 v, float (*
 #pragma unroll
   for (int o = 4; o; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
   if (G > 32) {
-    constexpr int W = G / 32;
+    constexpr int W = warps_of(G);
     if ((lane & 7) == 0) place[turn][4 * (threadIdx.x >> 5) + lane / 8] = x;
     __syncthreads();
     // lane 8 n + w reads number n of warp w (of 16 warps two), and the warps' are summed as the lanes' were
@@ -305,7 +307,7 @@ __device__ __forceinline__ void weights(Pairs8 *w, const void *from, int32_t typ
 }
 
 // Each warp's copy of a row's two statistics, in words of 16 bytes.
-__host__ __device__ constexpr int stats_room(int group) { return group == 32 ? 16 : group / 4; }
+__host__ __device__ constexpr int stats_room(int group) { return group <= 32 ? 16 : group / 4; }
 
 #define CECA_TYPES                                                           \
   const int32_t ts = TS == kAnyType ? p.stream_type : TS;                    \
@@ -316,10 +318,10 @@ template <int G, int PASSES, int V, int TS, int TA, int PARTS>
 __global__ void __launch_bounds__(G * groups_of(G), resident_block(G, PASSES)) block_kernel(const __grid_constant__ BlockArgs p) {
   using X = Place<G, PASSES, V>;
   extern __shared__ uint4 ring[];
-  __shared__ alignas(16) float sums[2][4 * (G / 32)];
+  __shared__ alignas(16) float sums[2][4 * warps_of(G)];
   constexpr int kGroups = groups_of(G);
   CECA_TYPES;
-  const int rank = G == 32 ? threadIdx.x & 31 : threadIdx.x, group = G == 32 ? threadIdx.x >> 5 : 0, d = (int)p.d;
+  const int rank = threadIdx.x % G, group = threadIdx.x / G, d = (int)p.d;
   const int64_t agent = blockIdx.x / p.part_count, first = (blockIdx.x - agent * p.part_count) * kGroups + group, hop = (int64_t)p.part_count * kGroups;
   constexpr bool kAny = PARTS == kAnyParts;
   const bool y = !kAny || p.y.at != nullptr, gated = kAny ? p.gate.at != nullptr : PARTS != kPlain, u = !kAny || p.w_pre != nullptr, silu = kAny ? p.silu : PARTS == kSilu;
@@ -329,7 +331,9 @@ __global__ void __launch_bounds__(G * groups_of(G), resident_block(G, PASSES)) b
   uint8_t *mine = reinterpret_cast<uint8_t *>(ring) + (size_t)group * p.stages * stage_bytes;
   const uint32_t mine32 = smem_u32(mine);
   Walk wh(p.h, agent, first, hop, sb), wy(p.y, agent, first, hop, ab), wg(p.gate, agent, first, hop, ab);
-  const int rows = first < p.t ? (int)((p.t - 1 - first) / hop) + 1 : 0, ring_bytes = p.stages * stage_bytes;
+  const auto count = [&](int64_t from) { return from < p.t ? (int)((p.t - 1 - from) / hop) + 1 : 0; };
+  // groups that share a warp stay together: for as many rows as the first of them has
+  const int rows = count(first), rounds = G < 32 ? count(first - group % (32 / (G < 32 ? G : 32))) : rows, ring_bytes = p.stages * stage_bytes;
   int fill = 0, left = rows;   // the place that is filled next, the rows that are not on their way
   const auto bring = [&]() {
     if (--left >= 0) {
@@ -362,20 +366,25 @@ __global__ void __launch_bounds__(G * groups_of(G), resident_block(G, PASSES)) b
         }
       return total(s);
     };
-    return inverse_rms(group_sum<G>(squares(1.f), sums, turn), over_d, p.eps, [&](float unit) {
+    const float sum = group_sum<G>(squares(1.f), sums, turn);
+    const bool beyond = sum == INFINITY;   // the same for a group, and, where a warp has several, asked for all of them
+    if (G < 32 ? __any_sync(0xffffffffu, beyond) : beyond) {
       if (G > 32) __syncthreads();
-      return group_sum<G>(squares(unit), sums, turn);
-    });
+      const float less = group_sum<G>(squares(kLess), sums, turn);
+      if (beyond) return inverse_rms_beyond(less, over_d);
+    }
+    return inverse_rms(sum, over_d, p.eps);
   };
   uint8_t *to_h = static_cast<uint8_t *>(p.h_out.at) + place(p.h_out, agent, first) * sb, *to_u = static_cast<uint8_t *>(p.u.at) + place(p.u, agent, first) * ab;
   const int64_t hop_h = hop * p.h_out.row_stride * sb, hop_u = hop * p.u.row_stride * ab;
   int64_t kept_at = (agent * p.t + first) * p.row_bytes;
   float *stats = p.stats ? p.stats + 2 * (agent * p.t + first) : nullptr;
   int from = 0;
-  for (int i = 0; i < rows; ++i) {
+  for (int i = 0; i < rounds; ++i) {
     bring();
+    const int d = G < 32 && i >= rows ? 0 : (int)p.d;   // (a row of nothing)
     copies_but(p.stages - 1);
-    if (V > 1 || G == 32) __syncwarp();   // (lanes copy for one another)
+    if (V > 1 || G <= 32) __syncwarp();   // (lanes copy for one another)
     else __syncthreads();
     const uint8_t *at = mine + from;
     from += stage_bytes;
@@ -420,7 +429,7 @@ __global__ void __launch_bounds__(G * groups_of(G), resident_block(G, PASSES)) b
       }
     }
     if (stats) {
-      if (rank == 0) *reinterpret_cast<float2 *>(stats) = make_float2(rho, r);
+      if (rank == 0 && d) *reinterpret_cast<float2 *>(stats) = make_float2(rho, r);
       stats += 2 * hop;
     }
     to_h += hop_h;
@@ -439,11 +448,11 @@ template <int G, int PASSES, int V, int TS, int TA, bool KEPT, int PARTS>
 __global__ void __launch_bounds__(G * groups_of(G), resident_grad(G)) block_grad_kernel(const __grid_constant__ BlockArgs p) {
   using X = Place<G, PASSES, V>;
   extern __shared__ uint4 ring[];
-  __shared__ alignas(16) float sums[2][4 * (G / 32)];
+  __shared__ alignas(16) float sums[2][4 * warps_of(G)];
   constexpr int kGroups = groups_of(G);
   CECA_TYPES;
   const int32_t held_s = KEPT ? kKept : ts, held_a = KEPT ? kKept : ta;
-  const int rank = G == 32 ? threadIdx.x & 31 : threadIdx.x, group = G == 32 ? threadIdx.x >> 5 : 0, d = (int)p.d;
+  const int rank = threadIdx.x % G, group = threadIdx.x / G, d = (int)p.d;
   const int64_t agent = blockIdx.x / p.part_count, cta = blockIdx.x - agent * p.part_count;
   const int64_t first = cta * kGroups + group, hop = (int64_t)p.part_count * kGroups;
   constexpr bool kAny = PARTS == kAnyParts;
@@ -458,13 +467,15 @@ __global__ void __launch_bounds__(G * groups_of(G), resident_grad(G)) block_grad
     return KEPT ? Walk(x, agent * p.t + first, hop, p.row_bytes) : Walk(x, agent, first, hop, bytes);
   };
   Walk wh = held(p.h, sb), wy = held(p.y, ab), wg = held(p.gate, ab), wu(p.du, agent, first, hop, ab), wo(p.dh_out, agent, first, hop, sb);
-  const int rows = first < p.t ? (int)((p.t - 1 - first) / hop) + 1 : 0, ring_bytes = p.stages * stage_bytes;
+  const auto count = [&](int64_t from) { return from < p.t ? (int)((p.t - 1 - from) / hop) + 1 : 0; };
+  // groups that share a warp stay together: for as many rows as the first of them has
+  const int rows = count(first), rounds = G < 32 ? count(first - group % (32 / (G < 32 ? G : 32))) : rows, ring_bytes = p.stages * stage_bytes;
   int fill = 0, left = rows;   // the place that is filled next, the rows that are not on their way
   const float *stats = p.stats + 2 * (agent * p.t + first);
   const auto bring = [&]() {
     if (--left >= 0) {
       const uint32_t to = mine32 + fill;
-      if ((threadIdx.x & 31) == 0) copy_8(to + off_s + rank / 32 * 8, stats);   // each warp its own
+      if (rank % 32 == 0) copy_8(to + off_s + rank / 32 * 8, stats);   // each warp its own
       X::copy(to, wh.at, held_s, d, rank);
       if (y) X::copy(to + off_y, wy.at, held_a, d, rank);
       if (gated) X::copy(to + off_g, wg.at, held_a, d, rank);
@@ -510,15 +521,16 @@ __global__ void __launch_bounds__(G * groups_of(G), resident_grad(G)) block_grad
   uint8_t *da = static_cast<uint8_t *>(p.dgate.at) + place(p.dgate, agent, first) * ab;
   const int64_t hop_h = hop * p.dh.row_stride * sb, hop_y = hop * p.dy.row_stride * ab, hop_a = hop * p.dgate.row_stride * ab;
   int from = 0, turn = 0;
-  for (int i = 0; i < rows; ++i) {
+  for (int i = 0; i < rounds; ++i) {
     bring();
+    const int d = G < 32 && i >= rows ? 0 : (int)p.d;   // (a row of nothing)
     copies_but(p.stages - 1);
-    if (V > 1 || G == 32) __syncwarp();   // (lanes copy for one another)
+    if (V > 1 || G <= 32) __syncwarp();   // (lanes copy for one another)
     else __syncthreads();
     const uint8_t *at = mine + from;
     from += stage_bytes;
     if (from == ring_bytes) from = 0;
-    const float2 now = *reinterpret_cast<const float2 *>(at + off_s + rank / 32 * 8);
+    const float2 now = d ? *reinterpret_cast<const float2 *>(at + off_s + rank / 32 * 8) : make_float2(0.f, 0.f);
     const Val<2> rho = all<2>(now.x), r = all<2>(now.y);
     Pairs8 hn[PASSES], t[PASSES], yn[PASSES], g[PASSES], slope[PASSES];
     Val<2> a{0.f, 0.f}, b{0.f, 0.f}, c{0.f, 0.f};
@@ -636,7 +648,7 @@ __global__ void __launch_bounds__(G * groups_of(G), resident_grad(G)) block_grad
         all_of[(2 * group + 1) * d + c] = e & 1 ? sum_post[j].v[e / 2].y : sum_post[j].v[e / 2].x;
       }
     __syncthreads();
-    for (int c = threadIdx.x; c < 2 * d; c += 32 * kGroups) {
+    for (int c = threadIdx.x; c < 2 * d; c += G * kGroups) {
       float x = 0.f;
 #pragma unroll
       for (int i = 0; i < kGroups; ++i) x += all_of[2 * i * d + c];
@@ -715,6 +727,8 @@ template <int V, int TS, int TA> cudaError_t launch_rows(const BlockArgs &p, boo
     }
     return with(widest, std::integral_constant<int, kAnyParts>());
   };
+  if (p.d <= 64) return by(std::integral_constant<int, 64>());
+  if (p.d <= 128) return by(std::integral_constant<int, 128>());
   if (p.d <= 256) return by(std::integral_constant<int, 256>());
   if (p.d <= 512) return by(std::integral_constant<int, 512>());
   if (p.d <= 1024) return by(std::integral_constant<int, 1024>());

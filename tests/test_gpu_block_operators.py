@@ -776,6 +776,25 @@ def test_many_agents_of_few_rows():
     _check_grad(b.grad(1, kept, stats), b.want_grad(1, stats, kept=True), b.types)
 
 
+@pytest.mark.parametrize("d", [1, 8, 31, 33, 56, 64, 65, 72, 104, 127, 128])
+@pytest.mark.parametrize("types", TYPES)
+def test_block_norm_of_narrow_rows(d, types):
+    # several rows a warp, of which some have a row less than others; one that overflows beside others that do not
+    n, t = 2, 1000 if d % 3 else 37
+    b = Block(n, t, d, types, 111)
+    if types[1] == F32:
+        b.y[0, 5] *= 1e25
+        b.y[1, t - 1] *= 1e25
+    for keep in (False, True):
+        h, u, stats, kept = b.run(1, save=True, keep8=keep)
+        want = b.want(1, 1e-6)
+        for got, k in ((h, "h"), (u, "u"), (stats, "stats")):
+            _close(got, want[k], k)
+        if keep:
+            assert all(torch.equal(k, ceca.dsgd_keep8(x)) for k, x in zip(kept, (b.h, b.y, b.gate)))
+        _check_grad(b.grad(1, kept if keep else (b.h, b.y, b.gate), stats), b.want_grad(1, stats, kept=keep), types)
+
+
 def test_block_norm_outputs_over_other_inputs():
     # u over the gate, dy over the gate, dgate over y: each element is read before it is written
     for d in (96, 99, 9000):
