@@ -60,7 +60,7 @@ template <int G, int PASSES, int V> struct Place {
   // types: DSGD_F32, DSGD_BF16, kKept
   __host__ __device__ static constexpr int room(int64_t d, int32_t type) {
     if (V == 1) return type == kKept ? (int)kept_row_bytes(d) : (int)((d * (type == DSGD_BF16 ? 2 : 4) + 47) / 16 * 16);
-    return type == kKept ? (9 * kEights + 31) / 16 * 16 : (type == DSGD_BF16 ? 16 : 32) * kEights;
+    return type == kKept ? (9 * kEights + 15) / 16 * 16 : (type == DSGD_BF16 ? 16 : 32) * kEights;
   }
   __device__ static void copy(uint32_t to, const uint8_t *from, int32_t type, int d, int rank) {
     constexpr int kLanes = G < 32 ? G : 32;   // that copy together
@@ -196,7 +196,9 @@ template <int G, int PASSES, int V> struct Place {
         keep_eight(row, r, d, rank + G * j);
       }
     }
-    for (int c = d + (int)blocks8(d) + rank; c < (int)kept_row_bytes(d); c += G) row[c] = 0;   // the bytes behind the exponents
+    const int from = d + (int)blocks8(d), to = (int)kept_row_bytes(d);   // the bytes behind the exponents, fewer than 16
+    if (rank < to - from) row[from + rank] = 0;
+    if (G < 16 && rank + G < to - from) row[from + rank + G] = 0;
   }
   __device__ static void keep_eight(uint8_t *row, const Pairs8 &x, int d, int at) {
     float most = 0.f;
@@ -321,7 +323,7 @@ __global__ void __launch_bounds__(G * groups_of(G), resident_block(G, PASSES)) b
   __shared__ alignas(16) float sums[2][4 * warps_of(G)];
   constexpr int kGroups = groups_of(G);
   CECA_TYPES;
-  const int rank = threadIdx.x % G, group = threadIdx.x / G, d = (int)p.d;
+  const int rank = threadIdx.x % G, group = threadIdx.x / G, width = (int)p.d, d = width;
   const int64_t agent = blockIdx.x / p.part_count, first = (blockIdx.x - agent * p.part_count) * kGroups + group, hop = (int64_t)p.part_count * kGroups;
   constexpr bool kAny = PARTS == kAnyParts;
   const bool y = !kAny || p.y.at != nullptr, gated = kAny ? p.gate.at != nullptr : PARTS != kPlain, u = !kAny || p.w_pre != nullptr, silu = kAny ? p.silu : PARTS == kSilu;
@@ -382,7 +384,7 @@ __global__ void __launch_bounds__(G * groups_of(G), resident_block(G, PASSES)) b
   int from = 0;
   for (int i = 0; i < rounds; ++i) {
     bring();
-    const int d = G < 32 && i >= rows ? 0 : (int)p.d;   // (a row of nothing)
+    const int d = G < 32 && i >= rows ? 0 : width;   // (a row of nothing)
     copies_but(p.stages - 1);
     if (V > 1 || G <= 32) __syncwarp();   // (lanes copy for one another)
     else __syncthreads();
@@ -429,7 +431,7 @@ __global__ void __launch_bounds__(G * groups_of(G), resident_block(G, PASSES)) b
       }
     }
     if (stats) {
-      if (rank == 0 && d) *reinterpret_cast<float2 *>(stats) = make_float2(rho, r);
+      if (rank == 0 && (G >= 32 || d)) *reinterpret_cast<float2 *>(stats) = make_float2(rho, r);
       stats += 2 * hop;
     }
     to_h += hop_h;
@@ -452,7 +454,7 @@ __global__ void __launch_bounds__(G * groups_of(G), resident_grad(G)) block_grad
   constexpr int kGroups = groups_of(G);
   CECA_TYPES;
   const int32_t held_s = KEPT ? kKept : ts, held_a = KEPT ? kKept : ta;
-  const int rank = threadIdx.x % G, group = threadIdx.x / G, d = (int)p.d;
+  const int rank = threadIdx.x % G, group = threadIdx.x / G, width = (int)p.d, d = width;
   const int64_t agent = blockIdx.x / p.part_count, cta = blockIdx.x - agent * p.part_count;
   const int64_t first = cta * kGroups + group, hop = (int64_t)p.part_count * kGroups;
   constexpr bool kAny = PARTS == kAnyParts;
@@ -523,14 +525,14 @@ __global__ void __launch_bounds__(G * groups_of(G), resident_grad(G)) block_grad
   int from = 0, turn = 0;
   for (int i = 0; i < rounds; ++i) {
     bring();
-    const int d = G < 32 && i >= rows ? 0 : (int)p.d;   // (a row of nothing)
+    const int d = G < 32 && i >= rows ? 0 : width;   // (a row of nothing)
     copies_but(p.stages - 1);
     if (V > 1 || G <= 32) __syncwarp();   // (lanes copy for one another)
     else __syncthreads();
     const uint8_t *at = mine + from;
     from += stage_bytes;
     if (from == ring_bytes) from = 0;
-    const float2 now = d ? *reinterpret_cast<const float2 *>(at + off_s + rank / 32 * 8) : make_float2(0.f, 0.f);
+    const float2 now = G >= 32 || d ? *reinterpret_cast<const float2 *>(at + off_s + rank / 32 * 8) : make_float2(0.f, 0.f);
     const Val<2> rho = all<2>(now.x), r = all<2>(now.y);
     Pairs8 hn[PASSES], t[PASSES], yn[PASSES], g[PASSES], slope[PASSES];
     Val<2> a{0.f, 0.f}, b{0.f, 0.f}, c{0.f, 0.f};
