@@ -26,9 +26,9 @@ struct BlockArgs {
   int32_t room[5];              // bytes of a row's place in a stage, by tensor
 };
 
-// Rows of up to kWidest channels are held in registers by a group of threads, 8 or 16 channels each.  Of the same work, what a row costs besides
+// Rows of up to kWidest channels are held in registers by a group of threads (a part of a warp, a warp, or a CTA), 8 or 16 channels each.  Of the same work, what a row costs besides
 // (its sums, its addresses) is less with 16, as long as registers last: forward they do (8 x 4096 x 2048 bf16 125 us, 144 with 8 channels a thread), and
-// the gradient has twice as much to hold (181 us with 8 channels, 216 with 16).  kWidest is what 512 threads hold.
+// the gradient has twice as much to hold (180 us with 8 channels, 216 with 16).  kWidest is what 512 threads hold.
 constexpr int64_t kWidest = 8192;
 struct Shape {
   int group, passes;   // threads of a group, eights of channels a thread
@@ -44,8 +44,8 @@ __host__ __device__ constexpr int groups_of(int group) { return group <= 32 ? 12
 // CTAs an SM that the kernels are compiled for: 512 threads of 128 registers (forward, with 8 channels each, 768 of 80).
 __host__ __device__ constexpr int resident_block(int group, int passes) { return (passes == 2 ? 512 : 768) / (group * groups_of(group)); }
 __host__ __device__ constexpr int resident_grad(int group) { return 512 / (group * groups_of(group)); }
-// Bytes of a group's weights that the gradient keeps in shared memory, for the registers' sake (8 x 4096 x 2047 bf16: 298 us, 367 with them in registers; fp32 stream
-// of 2048 channels 256 and 277).  With 16 channels a thread there is no room for them beside the rows.
+// Bytes of a group's weights that the gradient keeps in shared memory, for the registers' sake (8 x 4096 x 2047 bf16: 290 us, 367 with them in registers; fp32 stream
+// of 2048 channels 260 and 277).  With 16 channels a thread there is no room for them beside the rows.
 __host__ __device__ constexpr int aside_grad(int group, int passes) { return passes == 1 ? 64 * group : 0; }
 // Whether a tensor's rows all start on 16-byte boundaries.
 inline bool on_words(const dsgd_rows_t &x, int32_t type) {

@@ -1,14 +1,15 @@
 // Internal: the end of a block and the start of the next, and its gradient, for rows that a group of threads holds in registers.
 //
 // A group takes every so-many-th row of an agent.  The next rows are copied to a ring in shared memory while one is computed on, so that loads are always
-// under way; the weights, and the sums of their gradients, stay in registers.
+// under way; the weights (of the gradient in shared memory), and the sums of their gradients, stay in registers.
 //
 // Forward: two sums over the group a row, y^2 and h_out^2.  Gradient, with q = s g w_post yn (what the block added), f = w_pre du and t = dh_out + r f:
 // the three sums A = hn f, B = q t, C = q hn at once, then m = A / d, dh = t - r m hn and mean(yn e) = (B - r m C) / d.
 //
 // Bytes and instructions bound these kernels together: some 30 instructions a channel forward, 50 in the gradient.  Of the measured copy rate they reach
-// (8 x 4096 x 2048, silu gates) 0.82 forward and 0.90 in the gradient in bf16, 0.85 and 0.82 with an fp32 stream, 0.82 and 0.69 where 8 bits are written
-// and read; rows of 771 fp32 channels 0.81 and 0.75, of 2047 bf16 channels, read and written one by one, 0.58 and 0.44.
+// (8 x 4096 x 2048, silu gates) 0.82 forward and 0.91 in the gradient in bf16, 0.85 and 0.86 with an fp32 stream, 0.84 and 0.70 where 8 bits are written
+// and read; rows of 771 fp32 channels 0.78 and 0.82, of 2047 bf16 channels, read and written one by one, 0.57 and 0.57, of 64 bf16 channels, four rows a
+// warp, 0.79 and 0.77 (0.22 and 0.26 with a warp for each).
 #pragma once
 #include <cuda_runtime.h>
 

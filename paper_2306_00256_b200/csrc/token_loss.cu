@@ -6,13 +6,13 @@
 // and l = -log(1 + R / 2^y) keep their digits where the model is sure, and the others' share of the gradient is (c / T) (1 - q) / R each.
 //
 // Memory bounds it, and how often a row is read.  Where the derivative follows from the row's own sum (the policy's) it is read once, and stays in registers
-// between the sum and the gradient: several short rows a warp, 32 KB a CTA, up to 256 KB (512 KB with larger CTAs) a cluster of eight.  The preference's
+// between the sum and the gradient: several short rows a warp, 16 or 32 KB a CTA, up to 256 KB (512 KB with larger CTAs) a cluster of eight.  The preference's
 // derivative waits for the rows of two whole sequences: rows are summed in a stream of 8 KB parts, a warp each, joined, the pairs' losses taken, and
 // all are read again (from L2 no faster: the writes are what takes the time there).  The four launches begin early, each waiting for the one before.
 //
 // 2047 rows of 50001 fp32 logits: log-probabilities 64 us (0.98 of the measured copy rate), policy gradient 162 (0.77).  8192 x 128000 bf16: 299 us (all of it),
-// 816 (0.78: exponentials, 51 % of the special function units, and the exchange between eight CTAs take turns with memory).  16384 x 32000 bf16: policy gradient
-// 387 us (0.83), preference gradient 490 (0.98 for the three passes that it takes, 0.65 for two).
+// 817 (0.78: exponentials, 51 % of the special function units, and the exchange between eight CTAs take turns with memory).  16384 x 32000 bf16: policy gradient
+// 381 us (0.84), preference gradient 489 (0.98 for the three passes that it takes, 0.65 for two); 8192 x 8192 bf16 51 us (0.80; 62 by CTAs of 128 threads).
 // Tried for the policy's rows and slower: clusters that stay and fetch their next row to shared memory meanwhile (907 us), 256 threads of 8 vectors each
 // (915), 6 or 4 CTAs an SM instead of 5 (889, 884), and loops without a question for each vector (886).
 #include <cooperative_groups.h>
@@ -398,7 +398,7 @@ template <typename TZ, int ROWS> __global__ void __launch_bounds__(kThreads, 5) 
 
 // A CTA or a cluster of CTAs holds a longer row.  The warps' sums meet in one exchange.
 
-template <typename TZ, int THREADS, bool CLUSTER> __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 2 : 5) hold_kernel(const __grid_constant__ TokenArgs p) {
+template <typename TZ, int THREADS, bool CLUSTER> __global__ void __launch_bounds__(THREADS, THREADS == 256 ? 2 : 640 / THREADS) hold_kernel(const __grid_constant__ TokenArgs p) {
   constexpr int N = Vec<TZ>::N, W = THREADS / 32, kShares = W * (CLUSTER ? kMostRanks : 1);
   __shared__ float2 share[kShares];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -726,6 +726,8 @@ template <typename TZ> cudaError_t run(TokenArgs p, cudaStream_t s) {
   } else if (whole <= kPart) {   // several rows a warp where there are enough of them to keep all SMs at work
     const bool many = p.r >= 32 * (int64_t)sm_count();
     e = many && whole <= kPart / 4 ? launch_short<TZ, 4>(p, s) : many && whole <= kPart / 2 ? launch_short<TZ, 2>(p, s) : launch_short<TZ, 1>(p, s);
+  } else if (whole <= 64 * kVectors) {
+    e = launch_hold<TZ, 64, false>(p, s);
   } else if (whole <= kThreads * kVectors) {
     e = launch_hold<TZ, kThreads, false>(p, s);
   } else if ((turns || p.r * p.ranks <= 5 * (int64_t)sm_count()) && whole <= (int64_t)kThreads * kVectors * kMostRanks) {

@@ -371,7 +371,7 @@ def test_block_norm_gradient_against_differences_of_the_library():
 
 # ------------------------------------------------------------------------------------------------ tokens and losses
 
-LOGITS = [(1, 1), (2, 2), (3, 7), (70, 33), (5, 1000), (200, 501), (40, 4099), (3, 50001), (600, 2050), (7, 32000), (2, 200000)]
+LOGITS = [(1, 1), (2, 2), (3, 7), (70, 33), (5, 1000), (200, 501), (40, 4099), (33, 6001), (3, 50001), (600, 2050), (7, 32000), (2, 200000)]
 
 
 def _logits(r, v, dtype, seed, it=torch.int64):
