@@ -440,7 +440,7 @@ int64_t dsgd_kept_row_bytes(int64_t d);
  * are not allowed).  t = 0 does nothing.
  * Errors: CECA_ERR_INVALID_ARG (NULL where data is needed, n or d < 1, n > 65535, t < 0, t or d >= 2^31 - 1024, a row stride below d, a negative
  * stride, eps not positive and finite, neither y nor w_pre, a gate without y, a bad type), CECA_ERR_ALIGNMENT (stats, h8, y8, gate8).
- * Speed: best where d is a multiple of 8 and every row starts on a 16-byte boundary.
+ * Speed: best where d is a multiple of 8, at most 8192, and every row starts on a 16-byte boundary.
  */
 ceca_status_t dsgd_block_norm(dsgd_rows_t h, dsgd_rows_t y, dsgd_rows_t gate, const void *w_pre, const void *w_post, const void *scale,
                               int64_t w_pre_stride, int64_t w_post_stride, int64_t scale_stride, dsgd_rows_t h_out, dsgd_rows_t u,
