@@ -318,7 +318,7 @@ extern "C" ceca_status_t dsgd_block_norm(dsgd_rows_t h, dsgd_rows_t y, dsgd_rows
 
 extern "C" size_t dsgd_block_norm_workspace_bytes(int32_t n, int64_t t, int64_t d) {
   if (!sizes_ok(n, t, d)) return 0;
-  if (d <= kWidest) return (size_t)n * block_grad_parts(n, t, d) * (8 * (size_t)d + 16);
+  if (d <= kWidest) return (4 * (size_t)n * block_grad_parts(n, t, d) * part_floats(d) + 15) / 16 * 16;
   const Sizes z = sizes_of(n, t, d);
   return 8 * (size_t)n * t + 4 * (size_t)n * z.part_count * (2 * (size_t)d + z.column_blocks);
 }

@@ -44,6 +44,8 @@ __host__ __device__ constexpr int groups_of(int group) { return group <= 32 ? 12
 // CTAs an SM that the kernels are compiled for: 512 threads of 128 registers (forward, with 8 channels each, 768 of 80).
 __host__ __device__ constexpr int resident_block(int group, int passes) { return (passes == 2 ? 512 : 768) / (group * groups_of(group)); }
 __host__ __device__ constexpr int resident_grad(int group) { return 512 / (group * groups_of(group)); }
+// Floats of the workspace that a part of the gradient's sums takes: those of both weights by channel, and the scale's, one of each group.
+__host__ __device__ constexpr int64_t part_floats(int64_t d) { return 2 * d + groups_of(grad_shape_of(d).group); }
 // Bytes of a group's weights that the gradient keeps in shared memory, for the registers' sake (8 x 4096 x 2047 bf16: 290 us, 367 with them in registers; fp32 stream
 // of 2048 channels 260 and 277).  With 16 channels a thread there is no room for them beside the rows.
 __host__ __device__ constexpr int aside_grad(int group, int passes) { return passes == 1 ? 64 * group : 0; }

@@ -708,7 +708,7 @@ template <int G, int PASSES, int V, int TS, int TA, bool KEPT, int PARTS> cudaEr
   p.part_count = (int32_t)block_grad_parts(p.n, p.t, p.d);
   p.scale_count = p.part_count * kGroups;
   p.parts = reinterpret_cast<float *>(p.means);   // the workspace
-  p.scale_parts = p.parts + (size_t)p.n * p.part_count * 2 * p.d;
+  p.scale_parts = p.parts + (size_t)p.n * p.part_count * 2 * p.d;   // the rest of part_floats
   kernel<<<(unsigned)(p.n * p.part_count), kThreads, (size_t)bytes, s>>>(p);
   e = cudaGetLastError();
   return e == cudaSuccess ? finish_block_grad(p, s) : e;
