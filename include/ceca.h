@@ -403,7 +403,7 @@ typedef struct {
   int64_t agent_stride, row_stride;
 } dsgd_rows_t;
 
-/* What a gate's values go through: sigmoid(a), or a sigmoid(a). */
+/* What a gate's values go through: sigmoid(a), or a sigmoid(a).  Below a = -87.3 either is 0 (within 2^-119), and at -infinity too. */
 typedef enum { DSGD_GATE_SIGMOID = 0, DSGD_GATE_SILU = 1 } dsgd_gate_t;
 
 /*

@@ -4,7 +4,8 @@ import pytest
 import torch
 
 import paper_2306_00256_b200 as ceca
-from test_gpu_block_operators import DEV, TYPES, Block, _check_grad
+from oracle import blocks
+from test_gpu_block_operators import DEV, INF, NAMES, NAN, TYPES, Block, _check_grad, _close
 
 pytestmark = pytest.mark.gpu
 
@@ -25,3 +26,35 @@ def test_block_norm_gradient_keeps_to_its_workspace(n, t, d, types):
         ws.fill_(255)   # NaNs: nothing is read that was not written
         again = b.grad(1, src, stats, workspace=ws[:size])
         assert (ws[size:] == 255).all() and all(torch.equal(x, y) for x, y in zip(got, again))
+
+
+@pytest.mark.parametrize("d", [40, 256, 771, 2048, 9000])   # every form of the kernels
+@pytest.mark.parametrize("types", TYPES)
+@pytest.mark.parametrize("act", [blocks.SIGMOID, blocks.SILU])
+def test_gates_far_below_zero_are_shut(d, types, act):
+    far = [-86.0, -88.0, -100.0, -1e4, -1e30, -1e38, float(torch.finfo(types[1]).min)]
+    b = Block(1, 4 + len(far), d, types, 131)
+    for i, a in enumerate(far):
+        b.gate[0, 3 + i, i % 2::2] = a
+    # below -87.3 the sigmoid is held at 2^-126: it is off by that at most and silu and its slope by 87.4 times that, below 2^-119;
+    # what they are multiplied with (scale, weight, the normalised y, dh) stays below 2^9 here
+    floor = 2.0 ** -110
+
+    def near(got, pair, name):
+        _close(got, (pair[0], pair[1] + floor), name)
+
+    h, u, stats, kept = b.run(act, save=True, keep8=True)
+    want = b.want(act, 1e-6)
+    near(h, want["h"], "h_out")
+    near(u, want["u"], "u")
+    for src, held in (((b.h, b.y, b.gate), False), (kept, True)):
+        wg = b.want_grad(act, stats, held)
+        for k, g in zip(NAMES, b.grad(act, src, stats)):
+            near(g, wg[k], k)
+    # -infinity is as shut as the lowest value
+    low = b.run(act), b.grad(act, (b.h, b.y, b.gate), stats)
+    b.gate[b.gate < -1e20] = -INF
+    shut = b.run(act), b.grad(act, (b.h, b.y, b.gate), stats)
+    assert all(torch.equal(x, y) for x, y in zip(low[0][:2] + low[1], shut[0][:2] + shut[1]))
+    b.gate[0, 3, 1] = NAN
+    assert torch.isnan(b.run(act)[0][0, 3, 1])
