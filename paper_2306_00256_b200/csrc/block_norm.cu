@@ -203,9 +203,9 @@ __global__ void __launch_bounds__(32 * kJoiners) finish_kernel(const BlockArgs p
   __shared__ float halves[2][kJoiners][32];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, joiners = blockDim.x >> 5;
   const int64_t agent = blockIdx.y, c = (int64_t)blockIdx.x * 32 + lane;
-  const float scale = p.scale ? load(p.scale, p.weights_type, agent * p.scale_stride) : 1.f;
   float a = 0.f, b = 0.f;
-  after_first();
+  after_first();   // (without rows, of the caller's own kernels, which may have written the scale)
+  const float scale = p.part_count == 0 ? 0.f : p.scale ? load(p.scale, p.weights_type, agent * p.scale_stride) : 1.f;
   if (c < p.d)
 #pragma unroll 8
     for (int q = warp; q < p.part_count; q += joiners) {

@@ -5,7 +5,7 @@ import torch
 
 import paper_2306_00256_b200 as ceca
 from oracle import blocks
-from test_gpu_block_operators import DEV, INF, NAMES, NAN, TYPES, Block, _check_grad, _close
+from test_gpu_block_operators import DEV, F32, INF, NAMES, NAN, TYPES, Block, _check_grad, _close, _randn
 
 pytestmark = pytest.mark.gpu
 
@@ -58,3 +58,16 @@ def test_gates_far_below_zero_are_shut(d, types, act):
     assert all(torch.equal(x, y) for x, y in zip(low[0][:2] + low[1], shut[0][:2] + shut[1]))
     b.gate[0, 3, 1] = NAN
     assert torch.isnan(b.run(act)[0][0, 3, 1])
+
+
+@pytest.mark.parametrize("d", [40, 300, 9000])
+@pytest.mark.parametrize("scale", [NAN, INF, 0.5])
+def test_block_norm_gradient_of_no_rows_is_zero_whatever_the_scale(d, scale):
+    b = Block(2, 0, d, (F32, F32, F32), 1)
+    stats = torch.empty((2, 0, 2), device=DEV)
+    b.scale.fill_(scale)   # right before, on the same stream
+    got = b.grad(0, (b.h, b.y, b.gate), stats)
+    assert all((g == 0).all() for g in got[3:])
+    before = {k: _randn(v.shape, F32, 70 + i) for i, (k, v) in enumerate(zip(NAMES[3:], got[3:]))}
+    got = b.grad(0, (b.h, b.y, b.gate), stats, accumulate=True, **{k: v.clone() for k, v in before.items()})
+    assert all(torch.equal(g, before[k]) for k, g in zip(NAMES[3:], got[3:]))
