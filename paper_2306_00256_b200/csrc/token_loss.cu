@@ -626,7 +626,7 @@ template <typename TZ> __global__ void __launch_bounds__(kThreads) turn_kernel(c
   after_first();
   RowOut o = p.rows ? p.rows[i] : RowOut{};
   if (p.row_slopes) {
-    const float slope = p.row_slopes[i];
+    const float slope = tok >= 0 && tok < p.v ? p.row_slopes[i] : 0.f;   // a row without a token stays still whatever its sequence's slope is, a NaN too
     o.factor = slope == 0.f ? 0.f : o.factor * slope;
     o.own = slope == 0.f ? 0.f : o.own * slope;
   }

@@ -1,11 +1,12 @@
 """The operators around a model's blocks and behind its logits at the edges of their range: workspaces to the byte, gates and logits far out, rows
 without a token beside rows of NaN.  Bounds as in oracle/blocks.py."""
+import numpy as np
 import pytest
 import torch
 
 import paper_2306_00256_b200 as ceca
 from oracle import blocks
-from test_gpu_block_operators import DEV, F32, INF, NAMES, NAN, TYPES, Block, _check_grad, _close, _randn
+from test_gpu_block_operators import BF16, DEV, F32, INF, NAMES, NAN, TYPES, Block, _check_grad, _close, _logits, _np, _randn
 
 pytestmark = pytest.mark.gpu
 
@@ -71,3 +72,26 @@ def test_block_norm_gradient_of_no_rows_is_zero_whatever_the_scale(d, scale):
     before = {k: _randn(v.shape, F32, 70 + i) for i, (k, v) in enumerate(zip(NAMES[3:], got[3:]))}
     got = b.grad(0, (b.h, b.y, b.gate), stats, accumulate=True, **{k: v.clone() for k, v in before.items()})
     assert all(torch.equal(g, before[k]) for k, g in zip(NAMES[3:], got[3:]))
+
+
+@pytest.mark.parametrize("v", [7, 1001, 6001, 40000])   # rows held by a warp and by a CTA, rows in parts
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("broken", ["nan", "both masked"])
+def test_preference_rows_without_a_token_stay_still_beside_broken_ones(v, dtype, broken):
+    r, bounds = 900, [0, 6, 12, 400, 900]
+    z, tok = _logits(r, v, dtype, 61)
+    tok[:] = torch.arange(r, device=DEV) % v
+    tok[[0, 1, 7, 450]] = torch.tensor([-1, v, -5, -1], device=DEV)
+    z[1] = NAN
+    z[7, ::2] = INF
+    at = [3] if broken == "nan" else [3, 9]
+    for i in at:
+        z[i, tok[i]] = NAN if broken == "nan" else -INF
+    b = torch.tensor(bounds, device=DEV)
+    for out in (torch.full_like(z, 5), None):
+        loss, logp, dz = ceca.dsgd_preference_grad(z, tok, b, average=out is None, dz=out)
+        assert torch.isnan(loss[0]) and (dz[[0, 1, 7, 450]] == 0).all()
+        assert torch.isnan(dz[2]).all() and torch.isnan(dz[8]).all()
+        rest = blocks.preference(_np(z[12:]), _np(tok[12:]), [0, 388, 888], average=out is None, bf16=dtype == BF16, beta=np.float64(np.float32(0.1)))
+        _close(loss[1:], rest["loss"], "loss")
+        _close(dz[12:], rest["dz"], "dz")
