@@ -599,7 +599,7 @@ __global__ void __launch_bounds__(kPairThreads) pair_kernel(const TokenArgs p) {
       const double up = log1p(e) + fmax(-m, 0.), down = log1p(e) + fmax(m, 0.);                          // -log sigmoid(m), -log sigmoid(-m)
       const double at_minus = m >= 0. ? small : 1. / (1. + e), at = m >= 0. ? 1. / (1. + e) : small;     // sigmoid(-m), sigmoid(m)
       const double eps = (double)p.smoothing;
-      if (p.loss) p.loss[q] = w == 0.f ? 0.f : (float)((double)w * ((1. - eps) * up + (eps > 0. ? eps * down : 0.)));
+      if (p.loss) p.loss[q] = w == 0.f ? 0.f : (float)((double)w * ((eps < 1. ? (1. - eps) * up : 0.) + (eps > 0. ? eps * down : 0.)));   // (either may be infinite)
       const double slope = w == 0.f ? 0. : (double)w * (double)p.beta * (eps * at - (1. - eps) * at_minus);
       slopes[0] = (float)(slope * by[0]);
       slopes[1] = (float)(-slope * by[1]);

@@ -95,3 +95,13 @@ def test_preference_rows_without_a_token_stay_still_beside_broken_ones(v, dtype,
         rest = blocks.preference(_np(z[12:]), _np(tok[12:]), [0, 388, 888], average=out is None, bf16=dtype == BF16, beta=np.float64(np.float32(0.1)))
         _close(loss[1:], rest["loss"], "loss")
         _close(dz[12:], rest["dz"], "dz")
+
+
+@pytest.mark.parametrize("smoothing", [0.0, 1.0])
+@pytest.mark.parametrize("v", [9, 20000])
+def test_preference_of_an_impossible_answer_that_the_smoothing_wants(smoothing, v):
+    z, tok = _logits(8, v, F32, 71)
+    tok[:] = torch.arange(8, device=DEV)
+    z[5 if smoothing == 0 else 1, 5 if smoothing == 0 else 1] = -INF
+    loss, logp, dz = ceca.dsgd_preference_grad(z, tok, torch.tensor([0, 4, 8], device=DEV), smoothing=smoothing)
+    assert loss[0] == 0 and (dz == 0).all()
