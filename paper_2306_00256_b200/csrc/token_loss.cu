@@ -77,8 +77,9 @@ __device__ __forceinline__ Odds odds_of(const RowSum &s) {
 
 // The loss of a row and its derivative by the token's log-probability, both times the weight.
 __device__ __forceinline__ float2 policy(const TokenArgs &p, int64_t i, float w, float l) {
-  const float adv = p.advantage[i], ratio = expf(l - p.old_logp[i]);
-  const float plain = ratio * adv, clipped = fminf(fmaxf(ratio, p.low), p.high) * adv;
+  const float adv = p.advantage[i], past = l - p.old_logp[i], ratio = expf(past);
+  const float plain = adv == 0.f && past < INFINITY ? 0.f : ratio * adv;   // (0 too where a finite ratio is beyond fp32)
+  const float clipped = fminf(fmaxf(ratio, p.low), p.high) * adv;
   const bool free = !(plain > clipped);   // (a NaN goes on)
   float loss = -(free ? plain : clipped), slope = free ? -plain : 0.f;
   if (p.ref_logp && p.kl != 0.f) {

@@ -105,3 +105,18 @@ def test_preference_of_an_impossible_answer_that_the_smoothing_wants(smoothing, 
     z[5 if smoothing == 0 else 1, 5 if smoothing == 0 else 1] = -INF
     loss, logp, dz = ceca.dsgd_preference_grad(z, tok, torch.tensor([0, 4, 8], device=DEV), smoothing=smoothing)
     assert loss[0] == 0 and (dz == 0).all()
+
+
+@pytest.mark.parametrize("v", [9, 3000, 20000, 140000])
+def test_policy_rows_without_an_advantage_whose_ratio_leaves_fp32(v):
+    z, tok = _logits(7, v, F32, 73, torch.int32)
+    old = torch.full((7,), -300.0, device=DEV)
+    adv = torch.tensor([0.0, -0.0, 0.0, 0.0, 0.0, -1.0, 1.0], device=DEV)
+    for kl in (0.0, 0.1):
+        ref = torch.full((7,), -3.0, device=DEV)
+        loss, dz = ceca.dsgd_policy_grad(z, tok, old, adv, ref_logp=ref, kl=kl)
+        want = blocks.policy(_np(z), _np(tok), _np(old), _np(adv), _np(ref), kl=np.float64(np.float32(kl)))
+        rest = [0, 1, 2, 3, 4, 6]   # of row 5 the loss leaves fp32 too
+        _close(loss[rest], tuple(x[rest] for x in want["loss"]), "loss")
+        _close(dz[rest], tuple(x[rest] for x in want["dz"]), "dz")
+        assert loss[5] == INF
