@@ -500,6 +500,7 @@ size_t dsgd_token_workspace_bytes(int64_t r, int64_t v, int64_t pairs);
  * none of its other inputs is looked at.  The gradient is, with c = w_i (-p A where the ratio's own value is the smaller or equal one, else 0, and - kl (exp(x) - 1)):
  *   dz[i, k] = c / T ((k = tokens[i]) - softmax(z[i, :] / T)[k])
  * 1 - softmax at the token is taken from the other entries' sum, so that it keeps its digits where the model is sure.
+ * A NaN or +infinity among the logits of a row that is looked at, or a c that is a NaN, makes all of its dz NaN.
  * old_logp, advantage, ref_logp (may be NULL), weight (may be NULL), loss, logp (may be NULL; 0 in rows without a token or weight): device fp32, r.
  * dz: device, logits_type, row stride lddz >= v; it may be z with the same row stride (another one: CECA_ERR_UNSUPPORTED).
  * Also refused: clip_low not in [0, 1], clip_high or kl negative or not finite.

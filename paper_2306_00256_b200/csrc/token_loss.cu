@@ -91,7 +91,7 @@ __device__ __forceinline__ float2 policy(const TokenArgs &p, int64_t i, float w,
 }
 __device__ __forceinline__ RowOut row_out(const TokenArgs &p, const RowSum &s, const Odds &o, float slope) {
   const float by = slope / p.temperature, own = by * o.other;
-  return {s.k, s.rest == 0.f ? 0.f : own / s.rest, own, s.far ? 1 : 0};
+  return {s.k, s.rest == 0.f ? (own == own ? 0.f : own) : own / s.rest, own, s.far ? 1 : 0};   // (a NaN is one for the whole row)
 }
 
 // Over a low temperature, or a large weight, a share below 2^-126 is a gradient that is not: where the factor is above 1 the frame is lowered by

@@ -120,3 +120,19 @@ def test_policy_rows_without_an_advantage_whose_ratio_leaves_fp32(v):
         _close(loss[rest], tuple(x[rest] for x in want["loss"]), "loss")
         _close(dz[rest], tuple(x[rest] for x in want["dz"]), "dz")
         assert loss[5] == INF
+
+
+@pytest.mark.parametrize("v", [9, 3000, 20000, 140000])
+@pytest.mark.parametrize("own", [NAN, INF])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_a_row_of_nothing_but_a_broken_token(v, own, dtype):
+    z, tok = _logits(6, v, dtype, 75, torch.int32)
+    tok[:] = 5
+    z[3] = -INF
+    z[3, 5] = own
+    f = torch.full((6,), -1.0, device=DEV)
+    loss, dz = ceca.dsgd_policy_grad(z, tok, f, f)
+    assert torch.isnan(loss[3]) and torch.isnan(dz[3]).all()
+    assert torch.isfinite(dz[[0, 1, 2, 4, 5]]).all()
+    loss, _, dz = ceca.dsgd_preference_grad(z, tok, torch.tensor([0, 2, 4], device=DEV))
+    assert torch.isnan(loss[0]) and torch.isnan(dz[:4]).all() and (dz[4:] == 0).all()
