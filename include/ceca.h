@@ -521,7 +521,8 @@ ceca_status_t dsgd_policy_grad(const void *z, const void *tokens, const float *o
  * R = ref_logp (0 when NULL):
  *   loss[p] = w_p ( -(1 - smoothing) log sigmoid(m) - smoothing log sigmoid(-m) ),   w_p = weight[p] (1 when NULL)
  * (smoothing 0 or 1: one term alone, whatever the other is).  L goes to logp[0..2*pairs).  dz is the gradient of the sum of all losses; it is 0 in
- * rows without a token, of pairs of weight 0, and outside all sequences.  Bounds outside [0, r] are taken as the nearest of the two.  L is summed in 64 bits in the order of the rows' numbers.
+ * rows without a token, of pairs of weight 0, and outside all sequences.  Bounds outside [0, r] are taken as the nearest of the two.  L is summed in 64 bits, in an order that
+ * depends on the bounds alone: results are identical from run to run.
  * ref_logp: device fp32, 2*pairs, may be NULL; weight, loss: device fp32, pairs, weight may be NULL; logp: device fp32, 2*pairs, may be NULL;
  * dz as above.  pairs = 0 writes a gradient of 0.
  * Also refused: pairs < 0 or >= 2^27, beta not finite, smoothing not in [0, 1].
