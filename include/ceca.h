@@ -484,7 +484,8 @@ size_t dsgd_block_norm_workspace_bytes(int32_t n, int64_t t, int64_t d);
  * workspace: device, 16-byte aligned, dsgd_token_workspace_bytes(r, v, pairs) bytes (pairs = 0 but for the preference loss; 0, and then NULL will do,
  * for short rows), here and in the losses below.
  * Errors of all five: CECA_ERR_INVALID_ARG (NULL where data is needed, r < 0, r >= 2^28, v < 1, v >= 2^31 - 1024, r v >= 2^42, a row stride below the row,
- * temperature not positive and finite, a bad type, and what each call names), CECA_ERR_WORKSPACE.
+ * temperature not positive and finite, a bad type, and what each call names), CECA_ERR_WORKSPACE, and CECA_ERR_UNSUPPORTED for a loss or logp in the
+ * place of another float input or output than a weight.  But for dz and z no output may overlap an input or another output.
  */
 ceca_status_t dsgd_token_logprob(const void *z, const void *tokens, float *logp, int64_t r, int64_t v, int64_t ldz, int32_t logits_type,
                                  int32_t index_type, float temperature, void *workspace, size_t workspace_bytes, void *stream);
@@ -521,8 +522,8 @@ ceca_status_t dsgd_policy_grad(const void *z, const void *tokens, const float *o
  * R = ref_logp (0 when NULL):
  *   loss[p] = w_p ( -(1 - smoothing) log sigmoid(m) - smoothing log sigmoid(-m) ),   w_p = weight[p] (1 when NULL)
  * (smoothing 0 or 1: one term alone, whatever the other is).  L goes to logp[0..2*pairs).  dz is the gradient of the sum of all losses; it is 0 in
- * rows without a token, of pairs of weight 0, and outside all sequences.  Bounds outside [0, r] are taken as the nearest of the two.  L is summed in 64 bits, in an order that
- * depends on the bounds alone: results are identical from run to run.
+ * rows without a token, of pairs of weight 0, and outside all sequences.  Bounds outside [0, r] are taken as the nearest of the two.  L is summed in
+ * 64 bits, in an order that depends on the bounds alone: results are identical from run to run.
  * ref_logp: device fp32, 2*pairs, may be NULL; weight, loss: device fp32, pairs, weight may be NULL; logp: device fp32, 2*pairs, may be NULL;
  * dz as above.  pairs = 0 writes a gradient of 0.
  * Also refused: pairs < 0 or >= 2^27, beta not finite, smoothing not in [0, 1].

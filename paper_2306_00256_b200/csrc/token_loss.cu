@@ -20,6 +20,7 @@
 
 #include <algorithm>
 #include <cmath>
+#include <initializer_list>
 
 #include "ceca.h"
 #include "logits.cuh"
@@ -712,6 +713,13 @@ bool workspace_ok(const void *workspace, size_t bytes, int64_t r, int64_t v, int
   return need == 0 || (workspace && bytes >= need && !(reinterpret_cast<uintptr_t>(workspace) & 15));
 }
 
+// Whether what is written lies apart from what other threads may still read.
+bool apart(const float *loss, const float *logp, std::initializer_list<const float *> inputs) {
+  for (const float *x : inputs)
+    if (x && (x == loss || x == logp)) return false;
+  return !loss || loss != logp;
+}
+
 // Which form a call takes: a row that 128 threads hold is read once whatever is wanted of it, a longer one where its gradient follows from
 // its own sum, as long as a cluster holds it, or where there are so few that one launch instead of two is what counts (256 rows of 32000
 // bf16: 7.6 us in two, 6.1 in one).  Other rows are streamed.
@@ -761,6 +769,7 @@ ceca_status_t policy_call(const void *z, const void *tokens, const float *old_lo
   if (!z || !tokens || !old_logp || !advantage || !loss) return CECA_ERR_INVALID_ARG;
   if (dz == z && lddz != ldz) return CECA_ERR_UNSUPPORTED;
   if (!workspace_ok(workspace, workspace_bytes, r, v, 0)) return CECA_ERR_WORKSPACE;
+  if (!apart(loss, logp, {old_logp, advantage, ref_logp})) return CECA_ERR_UNSUPPORTED;
   TokenArgs p = common(kPolicy, z, tokens, dz, r, v, ldz, lddz, logits_type, index_type, temperature, workspace);
   p.old_logp = old_logp; p.advantage = advantage; p.ref_logp = ref_logp; p.weight = weight; p.loss = loss; p.logp = logp;
   p.low = 1.f - clip_low; p.high = 1.f + clip_high; p.kl = kl;
@@ -778,6 +787,7 @@ ceca_status_t preference_call(const void *z, const void *tokens, const void *bou
   if (r == 0 && pairs == 0) return CECA_OK;
   if (dz == z && dz && lddz != ldz) return CECA_ERR_UNSUPPORTED;
   if (!workspace_ok(workspace, workspace_bytes, r, v, pairs)) return CECA_ERR_WORKSPACE;
+  if (pairs > 0 && !apart(loss, logp, {ref_logp})) return CECA_ERR_UNSUPPORTED;
   TokenArgs p = common(kPreference, z, tokens, dz, r, v, ldz, lddz, logits_type, index_type, temperature, workspace);
   p.bounds = bounds; p.bounds64 = bounds_type == DSGD_I64;
   p.ref_logp = ref_logp; p.weight = weight; p.loss = loss; p.logp = logp; p.pairs = pairs;

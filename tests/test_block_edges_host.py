@@ -1,4 +1,6 @@
 """The operators around a model's blocks and behind its logits at the edges of their range, without a GPU."""
+import ctypes
+
 import pytest
 
 import paper_2306_00256_b200 as ceca
@@ -17,3 +19,25 @@ def _written(n, t, d):
 @pytest.mark.parametrize("n,t", [(1, 1), (1, 256), (2, 1000), (8, 4096), (4, 32768), (3000, 2), (65535, 1)])
 def test_block_norm_workspace_holds_what_the_gradient_writes(n, t, d):
     assert _written(n, t, d) <= ceca.dsgd_block_norm_workspace_bytes(n, t, d) < _written(n, t, d) + 16 * n
+
+
+def _at(i):   # stands for device memory: every call here is refused before anything is launched
+    return ctypes.c_void_p(4096 * (i + 1))
+
+
+@pytest.mark.parametrize("over", [dict(loss="old"), dict(loss="adv"), dict(loss="ref"), dict(logp="old"), dict(logp="adv"), dict(logp="ref"), dict(logp="loss")])
+def test_policy_loss_refuses_outputs_over_what_is_read(over):
+    args = {k: _at(i) for i, k in enumerate(("z", "tok", "old", "adv", "ref", "w", "loss", "logp"))}
+    args |= {k: args[v] for k, v in over.items()}
+    lib, ws = ceca.library(), _at(20)
+    assert lib.dsgd_policy_loss(*args.values(), 2, 8, 8, 0, 0, 1.0, 0.2, 0.2, 0.1, ws, 1 << 20, None) == 4
+    assert lib.dsgd_policy_grad(*args.values(), _at(30), 2, 8, 8, 8, 0, 0, 1.0, 0.2, 0.2, 0.1, ws, 1 << 20, None) == 4
+
+
+@pytest.mark.parametrize("over", [dict(loss="ref"), dict(logp="ref"), dict(logp="loss")])
+def test_preference_loss_refuses_outputs_over_what_is_read(over):
+    args = {k: _at(i) for i, k in enumerate(("z", "tok", "bounds", "ref", "w", "loss", "logp"))}
+    args |= {k: args[v] for k, v in over.items()}
+    lib, ws = ceca.library(), _at(20)
+    assert lib.dsgd_preference_loss(*args.values(), 1, 2, 8, 8, 0, 0, 0, 1.0, 0.1, 0.0, 0, ws, 1 << 20, None) == 4
+    assert lib.dsgd_preference_grad(*args.values(), _at(30), 1, 2, 8, 8, 8, 0, 0, 0, 1.0, 0.1, 0.0, 0, ws, 1 << 20, None) == 4
