@@ -483,8 +483,8 @@ size_t dsgd_block_norm_workspace_bytes(int32_t n, int64_t t, int64_t d);
  * z: device, logits_type, r x v with row stride ldz >= v; tokens: device, index_type, r; logp: device fp32, r.
  * workspace: device, 16-byte aligned, dsgd_token_workspace_bytes(r, v, pairs) bytes (pairs = 0 but for the preference loss; 0, and then NULL will do,
  * for short rows), here and in the losses below.
- * Errors of all five: CECA_ERR_INVALID_ARG (NULL where data is needed, r < 0, r >= 2^28, v < 1, v >= 2^31 - 1024, r v >= 2^42, a row stride below the row,
- * temperature not positive and finite, a bad type, and what each call names), CECA_ERR_WORKSPACE, and CECA_ERR_UNSUPPORTED for a loss or logp in the
+ * Errors of all five: CECA_ERR_INVALID_ARG (NULL where data is needed, r < 0, r >= 2^28, v < 1, v >= 2^31 - 1024, r ceil(v / 2048) >= 2^31 - 1024, a row
+ * stride below the row, temperature not finite or below 4.3e-39, a bad type, and what each call names), CECA_ERR_WORKSPACE, and CECA_ERR_UNSUPPORTED for a loss or logp in the
  * place of another float input or output than a weight.  But for dz and z no output may overlap an input or another output.
  */
 ceca_status_t dsgd_token_logprob(const void *z, const void *tokens, float *logp, int64_t r, int64_t v, int64_t ldz, int32_t logits_type,

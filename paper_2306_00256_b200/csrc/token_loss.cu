@@ -679,8 +679,10 @@ template <typename TZ> __global__ void __launch_bounds__(kThreads) turn_kernel(c
 constexpr int64_t kMost = ((int64_t)1 << 31) - 1024;
 bool sizes_ok(int64_t r, int64_t v) { return r >= 0 && r < ((int64_t)1 << 28) && v >= 1 && v < kMost && r * ceil_div(v, 4 * kPart) < kMost; }
 
+float scale_of(float temperature) { return (float)(1.4426950408889634 / (double)temperature); }
 bool common_ok(int64_t r, int64_t v, int64_t ldz, int64_t lddz, int32_t logits_type, int32_t index_type, float temperature) {
-  return sizes_ok(r, v) && ldz >= v && lddz >= v && is_type(logits_type) && is_index(index_type) && temperature > 0.f && std::isfinite(temperature);
+  return sizes_ok(r, v) && ldz >= v && lddz >= v && is_type(logits_type) && is_index(index_type) && temperature > 0.f && std::isfinite(temperature) &&
+         std::isfinite(scale_of(temperature));
 }
 
 int64_t parts_of(int64_t v, int32_t logits_type) {
@@ -694,7 +696,7 @@ TokenArgs common(int32_t what, const void *z, const void *tokens, void *dz, int6
   p.what = what;
   p.z = z; p.tokens = tokens; p.dz = dz;
   p.r = r; p.v = v; p.ldz = ldz; p.lddz = lddz;
-  p.scale = (float)(1.4426950408889634 / (double)temperature);
+  p.scale = scale_of(temperature);
   p.temperature = temperature;
   p.idx64 = index_type == DSGD_I64;
   const int64_t n = 16 / type_bytes(logits_type), vectors = ceil_div(v + n - 1, n);   // of the row on the least fortunate boundary

@@ -41,3 +41,14 @@ def test_preference_loss_refuses_outputs_over_what_is_read(over):
     lib, ws = ceca.library(), _at(20)
     assert lib.dsgd_preference_loss(*args.values(), 1, 2, 8, 8, 0, 0, 0, 1.0, 0.1, 0.0, 0, ws, 1 << 20, None) == 4
     assert lib.dsgd_preference_grad(*args.values(), _at(30), 1, 2, 8, 8, 8, 0, 0, 0, 1.0, 0.1, 0.0, 0, ws, 1 << 20, None) == 4
+
+
+@pytest.mark.parametrize("temperature,status", [(1e-39, 1), (1e-45, 1), (4.2e-39, 1), (4.3e-39, 5)])   # (5: of the workspace, which is looked at later)
+def test_losses_refuse_temperatures_whose_reciprocal_leaves_fp32(temperature, status):
+    lib, p, f = ceca.library(), _at(0), [_at(i) for i in range(1, 12)]
+    v = 100000
+    assert lib.dsgd_token_logprob(p, f[0], f[1], 2, v, v, 0, 0, temperature, None, 0, None) == status
+    assert lib.dsgd_policy_loss(p, *f[:7], 2, v, v, 0, 0, temperature, 0.2, 0.2, 0.1, None, 0, None) == status
+    assert lib.dsgd_policy_grad(p, *f[:8], 2, v, v, v, 0, 0, temperature, 0.2, 0.2, 0.1, None, 0, None) == status
+    assert lib.dsgd_preference_loss(p, *f[:6], 1, 2, v, v, 0, 0, 0, temperature, 0.1, 0.0, 0, None, 0, None) == status
+    assert lib.dsgd_preference_grad(p, *f[:7], 1, 2, v, v, v, 0, 0, 0, temperature, 0.1, 0.0, 0, None, 0, None) == status
