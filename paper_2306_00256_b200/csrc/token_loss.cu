@@ -624,17 +624,18 @@ template <typename TZ> __global__ void __launch_bounds__(kThreads) turn_kernel(c
   const TZ *z = static_cast<const TZ *>(p.z) + i * p.ldz;
   TZ *dz = static_cast<TZ *>(p.dz) + i * p.lddz;
   const WarpPart<TZ> part(z, p.v, (int)(task - i * p.parts), p.per);
+  const int64_t slot = tok >= 0 && tok < p.v ? tok + part.pad : -1;
   const bool together = ((reinterpret_cast<uintptr_t>(z) ^ reinterpret_cast<uintptr_t>(dz)) & 15) == 0;
   after_first();
   RowOut o = p.rows ? p.rows[i] : RowOut{};
   if (p.row_slopes) {
-    const float slope = tok >= 0 && tok < p.v ? p.row_slopes[i] : 0.f;   // a row without a token stays still whatever its sequence's slope is, a NaN too
-    o.factor = slope == 0.f ? 0.f : o.factor * slope;
-    o.own = slope == 0.f ? 0.f : o.own * slope;
+    const float slope = p.row_slopes[i];
+    const bool stays = slope == 0.f || slot < 0;   // without a token whatever the sequence's slope is, a NaN too
+    o.factor = stays ? 0.f : o.factor * slope;
+    o.own = stays ? 0.f : o.own * slope;
   }
   const bool still = o.factor == 0.f;   // (not for a NaN)
   const float lift = lifted(o);
-  const int64_t slot = tok >= 0 && tok < p.v ? tok + part.pad : -1;
   const auto turned = [&](float x) { return still ? 0.f : -o.factor * ex2(o.far ? fmaf(x - o.k, p.scale, lift) : fmaf(x, p.scale, -o.k)); };
   const auto element = [&](int64_t s) { narrow(dz + s - part.pad, s == slot ? o.own : turned(still ? 0.f : widen(z[s - part.pad]))); };
   if (together && !o.far) {
