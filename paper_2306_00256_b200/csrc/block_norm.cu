@@ -256,7 +256,8 @@ bool rows_ok(const dsgd_rows_t &x, int64_t d) { return !x.at || (x.row_stride >=
 // (two agents' rows in one place would be written by both)
 bool out_ok(const dsgd_rows_t &x, int32_t n, int64_t d) { return rows_ok(x, d) && (!x.at || n == 1 || x.agent_stride >= d); }
 
-// Rows in registers, by types and alignment.
+// Rows in registers, by types and alignment.  A bf16 stream with fp32 activations, which no model here has, is read and written one by one wherever its rows
+// start (8 x 4096 x 2048, silu: 208 us forward, 733 for the gradient; the other way round, in words, 168 and 261).
 cudaError_t rows(const BlockArgs &p, bool grad, cudaStream_t s) {
   bool words = p.d % 8 == 0;
   for (const dsgd_rows_t *x : {&p.h, &p.y, &p.gate}) words = words && (p.kept || on_words(*x, x == &p.h ? p.stream_type : p.act_type));

@@ -343,7 +343,7 @@ py::tuple block_norm_grad(const Tensor &h, const Maybe &y, const Maybe &w_pre, c
     bg = Block(gate, "gate", shape, act);
   }
   const Block bu(du, "du", shape, act), bo(dh_out, "dh_out", shape, stream_type);
-  const auto strides = [](const Maybe &m, const Block &b) {   // 0 where the gradient is one row, or one number's, for all
+  const auto strides = [](const Maybe &m, const Block &b) {   // 0 where the gradient is one row for all
     return m ? dsgd_rows_t{b.at.at, m->stride(0), m->stride(1)} : b.at;
   };
   int32_t wt = -1;

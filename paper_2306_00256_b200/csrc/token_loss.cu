@@ -10,9 +10,10 @@
 // derivative waits for the rows of two whole sequences: rows are summed in a stream of 8 KB parts, a warp each, joined, the pairs' losses taken, and
 // all are read again (from L2 no faster: the writes are what takes the time there).  The four launches begin early, each waiting for the one before.
 //
-// 2047 rows of 50001 fp32 logits: log-probabilities 64 us (0.98 of the measured copy rate), policy gradient 162 (0.77).  8192 x 128000 bf16: 299 us (all of it),
-// 817 (0.78: exponentials, 51 % of the special function units, and the exchange between eight CTAs take turns with memory).  16384 x 32000 bf16: policy gradient
-// 381 us (0.84), preference gradient 489 (0.98 for the three passes that it takes, 0.65 for two); 8192 x 8192 bf16 51 us (0.80; 62 by CTAs of 128 threads).
+// 2047 rows of 50001 fp32 logits: log-probabilities 64 us (0.98 of the measured copy rate), policy gradient 163 (0.76).  8192 x 128000 bf16: 299 us (all of it),
+// 819 (0.78: no one unit is full, special functions 51 %, issue slots 47 %; load, sum, exchange between eight CTAs and write of a row follow one another).
+// 16384 x 32000 bf16: policy gradient 388 us (0.82), preference gradient 492 (0.97 for the three passes that it takes, 0.65 for two); 8192 x 8192 bf16 54 us
+// (0.76; by CTAs of 128 threads a fifth more).
 // Tried for the policy's rows and slower: clusters that stay and fetch their next row to shared memory meanwhile (907 us), 256 threads of 8 vectors each
 // (915), 6 or 4 CTAs an SM instead of 5 (889, 884), and loops without a question for each vector (886).
 #include <cooperative_groups.h>
